@@ -69,6 +69,27 @@ class AllocResult(ctypes.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class Kv8Cache(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("block_table", ctypes.c_void_p)] + \
+               [(n, _I32) for n in ("num_blocks", "table_rows", "table_stride", "kv_heads", "head_dim")]
+
+
+class Kv8WriteArgs(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n", "rows", "max_len", "q_heads", "n_axes")] + \
+               [("sections", _I32 * 3), ("tab_rows", _I32)] + \
+               [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out")] + \
+               [(n, ctypes.c_int64) for n in ("ldq", "ldk", "ldv", "ldq_out")] + \
+               [(n, ctypes.c_void_p) for n in ("row_start", "pos0", "seq", "axis_pos", "cos_tab", "sin_tab")]
+
+
+class Kv8AttnArgs(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n", "rows", "max_q_len", "max_kv_len", "q_heads", "causal")] + \
+               [("scale", ctypes.c_float)] + [(n, ctypes.c_void_p) for n in ("q", "out")] + \
+               [(n, ctypes.c_int64) for n in ("ldq", "ldo")] + \
+               [(n, ctypes.c_void_p) for n in ("row_start", "kv_len", "seq", "workspace")] + \
+               [("workspace_bytes", ctypes.c_int64)]
+
+
 class EbrlError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{ERRORS.get(code, code)}: {msg}")
@@ -84,6 +105,7 @@ EXPORTED = [
     "ebrl_read_state", "ebrl_generate_weight_host", "ebrl_read_weight", "ebrl_write_weight",
     "ebrl_profile_enable", "ebrl_profile_read", "ebrl_op_gemm", "ebrl_op_gemm_plan",
     "ebrl_op_gemm_noalloc", "ebrl_op_stream_read",
+    "ebrl_op_kv8_write", "ebrl_op_kv8_attn", "ebrl_op_kv8_attn_workspace",
     "ebrl_alloc_solve", "ebrl_alloc_objective", "ebrl_alloc_monitor_create", "ebrl_alloc_monitor_observe",
     "ebrl_alloc_monitor_destroy", "ebrl_alloc_refine",
     "ebrl_sched_create", "ebrl_sched_destroy", "ebrl_sched_dispatch", "ebrl_sched_complete",
@@ -125,6 +147,9 @@ def lib():
         "ebrl_op_gemm_plan": (i32, [i32, i32, i32, i32, i32, i32, vp]),
         "ebrl_op_gemm_noalloc": (i32, [i32, vp, vp, vp, i32, i32, i32, vp]),
         "ebrl_op_stream_read": (i32, [vp, i64, vp, vp]),
+        "ebrl_op_kv8_write": (i32, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8WriteArgs), vp]),
+        "ebrl_op_kv8_attn": (i32, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8AttnArgs), vp]),
+        "ebrl_op_kv8_attn_workspace": (i64, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8AttnArgs)]),
         "ebrl_alloc_solve": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocLimits),
                                    ctypes.POINTER(AllocResult)]),
         "ebrl_alloc_objective": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocResult)]),
@@ -361,6 +386,159 @@ def op_stream_read(buf, out, stream=None) -> None:
     rc = lib().ebrl_op_stream_read(buf.data_ptr(), buf.numel() * buf.element_size(), out.data_ptr(), s)
     if rc != EBRL_OK:
         raise EbrlError(rc, "ebrl_op_stream_read")
+
+
+# ------------------------------------------------------- 8-bit KV cache --
+# include/ebrl_kv8.h.  The cache is three tensors on one GPU: codes, any 8-bit
+# dtype, [num_blocks, 2, kv_heads, 16 * head_dim]; scales, float32
+# [num_blocks, 2, kv_heads]; block_table, int32 [sequences, pages].
+
+KV8_PAGE = 16
+
+
+def kv8_alloc(num_blocks: int, kv_heads: int, head_dim: int, device="cuda"):
+    """(codes, scales) of an empty 8-bit cache, the codes as float8_e4m3fn."""
+    import torch
+    codes = torch.zeros((num_blocks, 2, kv_heads, KV8_PAGE * head_dim), dtype=torch.uint8, device=device)
+    return codes.view(torch.float8_e4m3fn), torch.ones((num_blocks, 2, kv_heads), device=device)
+
+
+def _kv8_bad(what: str):
+    raise EbrlError(-1, f"kv8: {what}")
+
+
+def _kv8_cache(codes, scales, table) -> Kv8Cache:
+    import torch
+    nb, two, hkv, wide = codes.shape if codes.dim() == 4 else (0, 0, 0, 0)
+    if two != 2 or wide % KV8_PAGE or codes.element_size() != 1 or not codes.is_contiguous():
+        _kv8_bad(f"codes {tuple(codes.shape)} {codes.dtype}: contiguous 8-bit [num_blocks, 2, kv_heads, 16 * head_dim]")
+    if scales.shape != (nb, 2, hkv) or scales.dtype != torch.float32 or not scales.is_contiguous():
+        _kv8_bad(f"scales {tuple(scales.shape)} {scales.dtype}: contiguous float32 [num_blocks, 2, kv_heads]")
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+        _kv8_bad(f"block_table {tuple(table.shape)} {table.dtype}: contiguous int32 [sequences, pages]")
+    return Kv8Cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), nb, table.shape[0], table.shape[1], hkv,
+                    wide // KV8_PAGE)
+
+
+def _kv8_rows(name, t, dtype, rows, dev):
+    """Pointer, width and row stride of a [rows, width] tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype != dtype or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1) or t.device != dev:
+        _kv8_bad(f"{name} {tuple(t.shape)} {t.dtype} on {t.device}: [{rows}, width] {dtype} on {dev}, rows contiguous")
+    return t.data_ptr(), t.shape[1], t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+
+
+def _kv8_ints(name, t, n, dev):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != dev:
+        _kv8_bad(f"{name} {tuple(t.shape)} {t.dtype} on {t.device}: {n} contiguous int32 on {dev}")
+    return t.data_ptr()
+
+
+def _kv8_dtype(t) -> int:
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        _kv8_bad(f"rows are bfloat16 or float32, not {t.dtype}")
+    return DTYPE_BF16 if t.dtype == torch.bfloat16 else DTYPE_FP32
+
+
+def _kv8_call(fn, name, cache, args, dev, stream):
+    """The call on `stream` (None: the current one of the tensors' device)."""
+    import torch
+    if dev.type != "cuda":
+        _kv8_bad(f"the cache is on {dev}, not on a GPU")
+    with torch.cuda.device(dev):
+        rc = fn(ctypes.byref(cache), ctypes.byref(args),
+                torch.cuda.current_stream(dev).cuda_stream if stream is None else stream)
+    if rc != EBRL_OK:
+        raise EbrlError(rc, name)
+
+
+def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=None, q_out=None, sections=(),
+                 axis_pos=None, cos=None, sin=None, seq=None, stream=None) -> None:
+    """Rotary positions on q and k and the write of k and v into the cache
+    (ebrl_op_kv8_write).  k, v, q, q_out: [rows, heads * head_dim]; row_start
+    [n + 1], pos0 [n], seq [n]: int32; axis_pos: int32 [rows, axes]; sections:
+    pairs of each axis (empty: no rotation); cos, sin: float32 [positions,
+    head_dim / 2].  `stream`: a raw handle whose order the tensors follow."""
+    import torch
+    c, dev = _kv8_cache(codes, scales, block_table), codes.device
+    n, rows, axes = pos0.numel(), k.shape[0], len(sections)
+    a = Kv8WriteArgs(dtype=_kv8_dtype(k), n=n, rows=rows, max_len=max_len, n_axes=axes)
+    a.k, wk, a.ldk = _kv8_rows("k", k, k.dtype, rows, dev)
+    a.v, wv, a.ldv = _kv8_rows("v", v, k.dtype, rows, dev)
+    hd = c.head_dim
+    if wk != c.kv_heads * hd or wv != wk:
+        _kv8_bad(f"k and v have {wk} and {wv} columns, the cache {c.kv_heads} heads of {hd}")
+    if (q is None) != (q_out is None) or axes > 3 or (axes == 0 and q is not None):
+        _kv8_bad("q and q_out go together, with one to three axes")
+    if q is not None:
+        a.q, wq, a.ldq = _kv8_rows("q", q, k.dtype, rows, dev)
+        a.q_out, wo, a.ldq_out = _kv8_rows("q_out", q_out, k.dtype, rows, dev)
+        if wq % hd or wo != wq:
+            _kv8_bad(f"q and q_out have {wq} and {wo} columns: heads of {hd}")
+        a.q_heads = wq // hd
+    if axes:
+        a.sections[:axes] = list(sections)
+        for t in (cos, sin):
+            if t is None or t.dim() != 2 or t.shape != cos.shape or t.shape[1] != hd // 2 or \
+                    t.dtype != torch.float32 or not t.is_contiguous() or t.device != dev:
+                _kv8_bad(f"cos and sin: contiguous float32 [positions, {hd // 2}] on {dev}")
+        a.tab_rows, a.cos_tab, a.sin_tab = cos.shape[0], cos.data_ptr(), sin.data_ptr()
+        a.axis_pos = _kv8_ints("axis_pos", axis_pos, rows * axes, dev)
+    a.row_start, a.pos0 = _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("pos0", pos0, n, dev)
+    a.seq = _kv8_ints("seq", seq, n, dev)
+    if scales.device != dev or block_table.device != dev:
+        _kv8_bad("codes, scales and block_table are on one device")
+    _kv8_call(lib().ebrl_op_kv8_write, "ebrl_op_kv8_write", c, a, dev, stream)
+
+
+def _kv8_attn_args(c, q, n, max_q_len, max_kv_len) -> Kv8AttnArgs:
+    if q.dim() != 2 or q.shape[1] % c.head_dim:
+        _kv8_bad(f"q {tuple(q.shape)}: [rows, heads * {c.head_dim}]")
+    return Kv8AttnArgs(dtype=_kv8_dtype(q), n=n, rows=q.shape[0], max_q_len=max_q_len, max_kv_len=max_kv_len,
+                       q_heads=q.shape[1] // c.head_dim)
+
+
+def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
+    """A workspace for op_kv8_attn calls with these sizes, on the cache's device, ready for use."""
+    import torch
+    c = Kv8Cache(0, 0, 0, codes.shape[0], block_table.shape[0], block_table.shape[1], codes.shape[2],
+                 codes.shape[3] // KV8_PAGE)
+    a = _kv8_attn_args(c, q, n, max_q_len, max_kv_len)
+    need = lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(a))
+    if need < 0:
+        raise EbrlError(need, "ebrl_op_kv8_attn_workspace")
+    return torch.zeros(need, dtype=torch.uint8, device=codes.device)
+
+
+def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len, max_kv_len, causal=True, scale=None,
+                workspace=None, seq=None, stream=None) -> None:
+    """out = softmax(scale q K^T) V over the 8-bit cache (ebrl_op_kv8_attn).
+    q, out: [rows, heads * head_dim]; row_start [n + 1], kv_len [n], seq [n]:
+    int32; scale None: 1 / sqrt(head_dim).  workspace: from
+    kv8_attn_workspace, one for each chain of calls that may overlap others;
+    None makes one for this call (not with an explicit stream, which torch's
+    allocator does not follow)."""
+    c, dev = _kv8_cache(codes, scales, block_table), codes.device
+    n = kv_len.numel()
+    a = _kv8_attn_args(c, q, n, max_q_len, max_kv_len)
+    a.causal, a.scale = int(bool(causal)), c.head_dim ** -0.5 if scale is None else scale
+    a.q, _, a.ldq = _kv8_rows("q", q, q.dtype, a.rows, dev)
+    a.out, wo, a.ldo = _kv8_rows("out", out, q.dtype, a.rows, dev)
+    if wo != q.shape[1]:
+        _kv8_bad(f"out has {wo} columns, q {q.shape[1]}")
+    a.row_start, a.kv_len = _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("kv_len", kv_len, n, dev)
+    a.seq = _kv8_ints("seq", seq, n, dev)
+    if scales.device != dev or block_table.device != dev or (workspace is not None and workspace.device != dev):
+        _kv8_bad("codes, scales, block_table and workspace are on one device")
+    if workspace is None:
+        if stream is not None:
+            _kv8_bad("a call on an explicit stream needs a workspace")
+        workspace = kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _kv8_call(lib().ebrl_op_kv8_attn, "ebrl_op_kv8_attn", c, a, dev, stream)
 
 
 def create_cu_masked_stream(device: int, mask_words: Sequence[int]) -> int:

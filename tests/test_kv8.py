@@ -1,0 +1,597 @@
+"""The 8-bit KV cache's operators (include/ebrl_kv8.h) against a plain float64
+form: what a write stores, byte for byte, and attention within bounds that
+follow from its arithmetic; the calls that are refused."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_27547_amd import ebrl as E
+from tests import kv8_ref as R
+
+gpu = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+# ------------------------------------------------------------ no GPU needed --
+
+def _attn_args(**kw):
+    a = E.Kv8AttnArgs(dtype=E.DTYPE_BF16, n=2, rows=2, max_q_len=1, max_kv_len=100, q_heads=4, causal=1, scale=0.125,
+                      ldq=256, ldo=256)
+    for f in ("q", "out", "row_start", "kv_len"):
+        setattr(a, f, 4096 * (1 + "q out row_start kv_len".split().index(f)))
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def _cache(**kw):
+    c = E.Kv8Cache(1 << 20, 2 << 20, 3 << 20, 8, 2, 4, 2, 64)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def _attn(c, a):
+    return E.lib().ebrl_op_kv8_attn(ctypes.byref(c), ctypes.byref(a), None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(codes=0), dict(codes=(1 << 20) + 8), dict(scales=0), dict(block_table=0), dict(num_blocks=0), dict(table_rows=0),
+    dict(table_stride=0), dict(table_stride=1 << 27), dict(kv_heads=0), dict(kv_heads=3), dict(head_dim=32),
+    dict(head_dim=96)])
+def test_attn_refuses_cache(bad):
+    assert _attn(_cache(**bad), _attn_args()) == -1
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=2), dict(n=-1), dict(rows=-1), dict(max_q_len=-1), dict(max_kv_len=-1), dict(max_kv_len=(1 << 30) + 1),
+    dict(q_heads=0), dict(q_heads=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+    dict(scale=float("inf")), dict(q=0), dict(out=0), dict(q=4096 + 8), dict(ldq=255), dict(ldq=260), dict(ldo=128),
+    dict(row_start=0), dict(kv_len=0), dict(out=4096), dict(max_kv_len=10000)])   # the last: needs a workspace
+def test_attn_refuses_arguments(bad):
+    assert _attn(_cache(), _attn_args(**bad)) == -1
+
+
+def test_attn_of_nothing_is_ok():
+    for kw in (dict(n=0), dict(rows=0), dict(max_q_len=0)):
+        assert _attn(_cache(), _attn_args(**kw)) == 0
+
+
+def _write_args(**kw):
+    a = E.Kv8WriteArgs(dtype=E.DTYPE_BF16, n=2, rows=4, max_len=3, q_heads=4, n_axes=2, tab_rows=10, ldq=256, ldk=128,
+                       ldv=128, ldq_out=256)
+    a.sections[0], a.sections[1] = 20, 12
+    for i, f in enumerate(("q", "k", "v", "q_out", "row_start", "pos0", "axis_pos", "cos_tab", "sin_tab")):
+        setattr(a, f, 4096 * (1 + i))
+    for k, v in kw.items():
+        if k == "sections":
+            for i, x in enumerate(v):
+                a.sections[i] = x
+        else:
+            setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=7), dict(n=-1), dict(rows=-1), dict(max_len=-1), dict(q_heads=-1), dict(n_axes=4), dict(n_axes=-1),
+    dict(n_axes=0), dict(sections=(20, 13)), dict(sections=(32, 0)), dict(sections=(33, -1)), dict(tab_rows=0),
+    dict(cos_tab=0), dict(sin_tab=4), dict(axis_pos=0), dict(k=0), dict(v=4104), dict(ldk=127), dict(ldv=130),
+    dict(q=0), dict(q_out=0), dict(ldq_out=8), dict(row_start=0), dict(pos0=0), dict(q_out=4096, ldq_out=512)])
+def test_write_refuses_arguments(bad):
+    assert E.lib().ebrl_op_kv8_write(ctypes.byref(_cache()), ctypes.byref(_write_args(**bad)), None) == -1
+
+
+@pytest.mark.parametrize("bad", [dict(codes=0), dict(codes=8), dict(scales=0), dict(block_table=0), dict(head_dim=80),
+                                 dict(num_blocks=-1)])
+def test_write_refuses_cache(bad):
+    assert E.lib().ebrl_op_kv8_write(ctypes.byref(_cache(**bad)), ctypes.byref(_write_args()), None) == -1
+
+
+def test_write_of_nothing_is_ok():
+    for kw in (dict(n=0), dict(rows=0), dict(max_len=0)):
+        assert E.lib().ebrl_op_kv8_write(ctypes.byref(_cache()), ctypes.byref(_write_args(**kw)), None) == 0
+
+
+def test_workspace_sizes():
+    c = _cache(table_stride=10000)
+
+    def need(**kw):
+        return E.lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(_attn_args(**kw)))
+    assert need(max_kv_len=1) == 0 and need(n=0, max_kv_len=100000) == 0
+    assert need(max_kv_len=100000) > 0
+    assert need(q_heads=3) == -1 and need(dtype=5) == -1
+    # enough sequences fill the chip without cutting their keys
+    assert need(n=4096, rows=4096, max_kv_len=4096) == 0
+
+
+def test_binding_refuses():
+    codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
+    table = torch.zeros((1, 4), dtype=torch.int32)
+    k = torch.zeros((1, 128), dtype=torch.bfloat16)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    ok = dict(codes=codes, scales=scales, block_table=table, k=k, v=k, row_start=i32(0, 1), pos0=i32(0), max_len=1)
+
+    def refused(f, **kw):
+        with pytest.raises(E.EbrlError):
+            f(**kw)
+    refused(E.op_kv8_write, **ok)                                             # not on a GPU
+    for bad in (dict(codes=codes.view(torch.uint8)[:, :1]), dict(codes=codes.float()), dict(scales=scales.double()),
+                dict(block_table=table.long()), dict(v=k.float()), dict(k=k[:, :64]), dict(pos0=i32(0).long()),
+                dict(row_start=i32(0)), dict(q=k), dict(k=torch.zeros((1, 128), dtype=torch.float16)),
+                dict(sections=(32,)), dict(sections=(8, 8, 8, 8))):
+        refused(E.op_kv8_write, **{**ok, **bad})
+    at = dict(codes=codes, scales=scales, block_table=table, q=k, out=k.clone(), row_start=i32(0, 1), kv_len=i32(1),
+              max_q_len=1, max_kv_len=1)
+    for bad in (dict(), dict(out=k.float()), dict(q=k[:, :65], out=k[:, :65]), dict(kv_len=i32(1, 1)),
+                dict(q=k.half(), out=k.half()), dict(stream=0), dict(out=k[:, :64])):
+        refused(E.op_kv8_attn, **{**at, **bad})
+
+
+def test_reference_encode_matches_torch():
+    """The test's own e4m3 rounding against torch's, ties and small values among them."""
+    x = np.concatenate([np.linspace(-448, 448, 4001), R.CODE[:127], (R.CODE[:126] + R.CODE[1:127]) / 2,
+                        np.random.default_rng(0).standard_normal(4000) * 2.0 ** -7])
+    x = x.astype(np.float32)
+    t = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(t, R.encode(x))
+
+
+# ------------------------------------------------------------------ the GPU --
+
+def _bits(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+class Pool:
+    """A cache whose sequences hold `lens` tokens of random values, pages in random order."""
+
+    def __init__(self, seed, lens, hkv, hd, room=0, extra=3, spread=1.0):
+        self.rng = np.random.default_rng(seed)
+        self.hkv, self.hd = hkv, hd
+        pages = [(n + room + R.PAGE - 1) // R.PAGE for n in lens]
+        self.nb = sum(pages) + extra
+        order = self.rng.permutation(self.nb).astype(np.int32)
+        self.table = np.full((len(lens), max(pages + [1]) + 1), -1, np.int32)
+        at = 0
+        for i, p in enumerate(pages):
+            self.table[i, :p] = order[at:at + p]
+            at += p
+        # slots that hold no token are NaN codes, and so is what pages without any hold
+        self.codes = np.full((self.nb, 2, hkv, R.PAGE * hd), 0x7F, np.uint8)
+        self.scales = np.full((self.nb, 2, hkv), np.nan, np.float32)
+        for i, n in enumerate(lens):
+            if n:
+                x = self.rng.standard_normal((2, n, hkv, hd)) * np.exp2(self.rng.uniform(-spread, spread, (2, n, 1, 1)))
+                R.write(self.codes, self.scales, self.table[i:i + 1], x[0], x[1], [0, n], [0], n)
+
+    def gpu(self):
+        codes = torch.from_numpy(self.codes.copy()).cuda().view(torch.float8_e4m3fn)
+        return codes, torch.from_numpy(self.scales.copy()).cuda(), torch.from_numpy(self.table).cuda()
+
+
+def _ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32).cuda()
+
+
+def _tables(n, hd):
+    ang = np.arange(n)[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)
+    return np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+
+
+def _rows(rng, rows, heads, hd, dt, pad=0):
+    """(device rows, strided if pad, and their float64 values)"""
+    t = torch.from_numpy(rng.standard_normal((rows, heads * hd + pad))).to(dt).cuda()[:, :heads * hd]
+    return t, t.double().cpu().numpy().reshape(rows, heads, hd)
+
+
+def _same_codes(got, want):
+    """Codes equal; a zero's sign and a NaN's may differ."""
+    g, w = R.CODE[got], R.CODE[want]
+    np.testing.assert_array_equal(g, w)
+
+
+def _check_write(pool, dt, hq, past, new, sections, pad, seed, max_len=None, seq=None, outside=2):
+    rng = np.random.default_rng(seed)
+    hkv, hd = pool.hkv, pool.hd
+    rows = sum(new) + outside
+    start = np.concatenate([[0], np.cumsum(new)])
+    k, k64 = _rows(rng, rows, hkv, hd, dt, pad)
+    v, v64 = _rows(rng, rows, hkv, hd, dt, 2 * pad)
+    q, q64 = _rows(rng, rows, hq, hd, dt, pad)
+    cos, sin = _tables(200, hd)
+    axes = len(sections)
+    axis_pos = rng.integers(0, 200, (rows, axes)).astype(np.int32) if axes > 1 else None
+    codes, scales, table = pool.gpu()
+    q_out = torch.full_like(q, 7.0)
+    mx = max(list(new) + [1]) if max_len is None else max_len
+    E.op_kv8_write(codes, scales, table, k, v, _ints(start), _ints(past), mx, q=q if axes else None,
+                   q_out=q_out if axes else None, sections=sections,
+                   axis_pos=None if axis_pos is None else torch.from_numpy(axis_pos).cuda(),
+                   cos=torch.from_numpy(cos).cuda() if axes else None, sin=torch.from_numpy(sin).cuda() if axes else None,
+                   seq=None if seq is None else _ints(seq))
+    wc, ws = pool.codes.copy(), pool.scales.copy()
+    wq = R.write(wc, ws, pool.table, k64, v64, list(start), list(past), mx, list(sections), axis_pos, cos, sin, seq,
+                 q64 if axes else None)
+    _same_codes(_bits(codes), wc)
+    np.testing.assert_array_equal(scales.cpu().numpy(), ws)
+    if axes:
+        got = q_out.double().cpu().numpy().reshape(wq.shape)
+        out = np.isnan(wq)
+        assert np.all(got[out] == 7.0)
+        half = torch.finfo(dt).eps / 2
+        assert np.all(np.abs(got - wq)[~out] <= half * np.abs(wq[~out]) * (1 + 2.0 ** -20) + 1e-38)
+    return codes, scales
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 4, 64), (6, 2, 128), (8, 8, 128), (5, 1, 64)])
+@pytest.mark.parametrize("past,new", [([0], [1]), ([0, 0], [16, 33]), ([5, 15, 16, 31], [1, 1, 1, 1]),
+                                      ([3, 0, 17, 40], [20, 0, 60, 7])])
+def test_write_one_axis(dtype, hq, hkv, hd, past, new):
+    pool = Pool(1, past, hkv, hd, room=max(new) + 1)
+    _check_write(pool, DT[dtype], hq, past, new, (hd // 2,), 0, 2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd,sections", [(64, ()), (64, (16, 16)), (64, (1, 30, 1)), (128, (32, 16, 16)), (128, (33, 31)),
+                                         (128, (2, 61, 1)), (128, ())])
+def test_write_axes_and_strides(dtype, hd, sections):
+    past, new = [9, 0, 32, 2], [40, 17, 1, 14]
+    pool = Pool(3, past, 3, hd, room=41)
+    _check_write(pool, DT[dtype], 6, past, new, sections, 8, 4)
+
+
+@gpu
+def test_write_many_heads_and_pages():
+    """Enough (page, head) pairs for the waves to take several heads in turn."""
+    past, new = list(range(0, 120, 3)), [50] * 40
+    pool = Pool(5, past, 40, 64, room=51)
+    _check_write(pool, torch.bfloat16, 41, past, new, (20, 12), 0, 6)
+
+
+@gpu
+def test_write_keeps_to_its_bounds():
+    """Row ranges past the rows and max_len are cut, unknown table rows and
+    pages that are none are skipped, positions are cut to the tables."""
+    past = [4, 18, 0, 30]
+    pool = Pool(7, past, 2, 64, room=40)
+    pool.table[1, 2] = pool.nb                    # a page past the pool ...
+    pool.table[3, 2] = -5                         # ... and one before it
+    _check_write(pool, torch.bfloat16, 2, past, [20, 30, 6, 25], (32,), 0, 8, max_len=19)
+    _check_write(pool, torch.bfloat16, 2, past, [20, 30, 6, 25], (32,), 0, 9, seq=[0, -1, 4, 3])
+    # rows that end in the middle of the last sequence, a position past the table's row
+    _check_write(pool, torch.bfloat16, 2, [4, 18, 0, pool.table.shape[1] * 16 - 3], [3, 3, 3, 9], (32,), 0, 10, outside=-4)
+    _check_write(pool, torch.bfloat16, 2, [-1, 1 << 30, 0, 190], [3, 3, 3, 9], (32,), 0, 11)
+
+
+@gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_write_token_by_token_grows_the_scale(hd):
+    """Forty tokens one at a time, sizes over 2^-30 .. 2^30: every step's bytes, and, where the sizes do not
+    underflow, the bytes that one call for all gives."""
+    rng = np.random.default_rng(12)
+    pool = Pool(13, [0], 2, hd, room=48)
+    codes, scales, table = pool.gpu()
+    wc, ws = pool.codes.copy(), pool.scales.copy()
+    size = np.exp2(rng.uniform(-30, 30, 40)) * (np.arange(40) % 7 != 3)
+    x = torch.from_numpy((rng.standard_normal((2, 40, 2 * hd)) * size[:, None])).float().cuda()
+    for j in range(40):
+        k, v = x[0, j:j + 1], x[1, j:j + 1]
+        E.op_kv8_write(codes, scales, table, k, v, _ints([0, 1]), _ints([j]), 1)
+        R.write(wc, ws, pool.table, k.double().cpu().numpy().reshape(1, 2, hd),
+                v.double().cpu().numpy().reshape(1, 2, hd), [0, 1], [j], 1)
+        _same_codes(_bits(codes), wc)
+        np.testing.assert_array_equal(scales.cpu().numpy(), ws)
+
+
+@gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_write_in_parts_is_the_write_at_once(hd):
+    """Values within 2^12 of each other lose nothing when a page's scale grows: any split gives the same values."""
+    rng = np.random.default_rng(14)
+    n = 61
+    x = torch.from_numpy(rng.uniform(0.5, 1.0, (2, n, 3 * hd)) * rng.choice([-1, 1], (2, n, 3 * hd)) *
+                         np.exp2(rng.integers(0, 6, (2, n, 1)))).bfloat16().cuda()
+    whole = Pool(15, [0], 3, hd, room=n).gpu()
+    E.op_kv8_write(*whole, x[0], x[1], _ints([0, n]), _ints([0]), n)
+    for cuts in ([0, 1, n], [0, 7, 8, 30, n], list(range(n + 1))):
+        part = Pool(15, [0], 3, hd, room=n).gpu()
+        for a, b in zip(cuts, cuts[1:]):
+            E.op_kv8_write(*part, x[0, a:b], x[1, a:b], _ints([0, b - a]), _ints([a]), b - a)
+        vw = R.CODE[_bits(whole[0])] * whole[1].cpu().numpy()[..., None]
+        vp = R.CODE[_bits(part[0])] * part[1].cpu().numpy()[..., None]
+        np.testing.assert_array_equal(vw, vp)
+
+
+@gpu
+def test_write_special_values():
+    """NaN, infinities and 2^127 become NaN and leave the scale to the others; zeros, the largest and the least."""
+    hd = 64
+    pool = Pool(16, [0], 1, hd, room=64)
+    x = np.ones((4, hd), np.float32)
+    x[0, 3], x[0, 5], x[0, 9] = np.nan, np.inf, -np.inf
+    x[1, :] = 0
+    x[2, :] = 1e-38
+    x[3, 7], x[3, 8] = 2.0 ** 127, -(2.0 ** 126)
+    for lo, hi in ((0, 1), (1, 2), (2, 3), (3, 4), (0, 4)):
+        codes, scales, table = pool.gpu()
+        wc, ws = pool.codes.copy(), pool.scales.copy()
+        t = torch.from_numpy(x[lo:hi]).cuda()
+        E.op_kv8_write(codes, scales, table, t, t, _ints([0, hi - lo]), _ints([0]), hi - lo)
+        x64 = x[lo:hi].astype(np.float64).reshape(hi - lo, 1, hd)
+        R.write(wc, ws, pool.table, x64, x64, [0, hi - lo], [0], hi - lo)
+        _same_codes(_bits(codes), wc)
+        np.testing.assert_array_equal(scales.cpu().numpy(), ws)
+
+
+@gpu
+def test_write_rotates_in_place():
+    rng = np.random.default_rng(17)
+    pool = Pool(18, [0], 2, 128, room=40)
+    k, _ = _rows(rng, 33, 2, 128, torch.bfloat16)
+    q, _ = _rows(rng, 33, 4, 128, torch.bfloat16)
+    cos, sin = (torch.from_numpy(t).cuda() for t in _tables(64, 128))
+    apart = torch.empty_like(q)
+    for out in (apart, q):
+        E.op_kv8_write(*pool.gpu(), k, k, _ints([0, 33]), _ints([0]), 33, q=q, q_out=out, sections=(64,), cos=cos, sin=sin)
+    assert torch.equal(apart, q)
+
+
+def _check_attn(pool, dt, hq, lens, ql, causal, seed, pad=0, seq=None, outside=2, max_kv=None, scale=None, q_scale=1.0,
+                max_q=None, workspace=None):
+    rng = np.random.default_rng(seed)
+    hd = pool.hd
+    rows = sum(ql) + outside
+    start = np.concatenate([[0], np.cumsum(ql)])
+    q, _ = _rows(rng, rows, hq, hd, dt, pad)
+    q *= q_scale
+    q64 = q.double().cpu().numpy().reshape(rows, hq, hd)
+    codes, scales, table = pool.gpu()
+    out = torch.full((rows, hq * hd + 2 * pad), 7.0, dtype=dt, device="cuda")[:, :hq * hd]
+    mq = max(list(ql) + [1]) if max_q is None else max_q
+    mk = max(list(lens) + [1]) if max_kv is None else max_kv
+    E.op_kv8_attn(codes, scales, table, q, out, _ints(start), _ints(lens), mq, mk, causal=causal, scale=scale,
+                  seq=None if seq is None else _ints(seq), workspace=workspace)
+    want, bound = R.attend(pool.codes, pool.scales, pool.table, q64, list(start), list(lens), mq, mk, causal,
+                           hd ** -0.5 if scale is None else scale, seq, dt == torch.bfloat16)
+    got = out.double().cpu().numpy().reshape(want.shape)
+    _held(got, want, bound)
+    return out
+
+
+def _held(got, want, bound):
+    outside = np.isnan(bound) & ~np.isnan(got)
+    assert np.all(got[outside] == 7.0)          # rows of no sequence (want NaN there too)
+    inside = ~np.isnan(bound)
+    bad = ~(np.abs(got - want) <= bound) & inside
+    assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], want[bad][:5], bound[bad][:5])
+    err = np.linalg.norm((got - want)[inside]) / max(np.linalg.norm(want[inside]), 1e-30)
+    print(f"rel {err:.2e}, largest share of the bound {np.max(np.abs(got - want)[inside] / np.maximum(bound[inside], 1e-30)):.2f}")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 4, 64), (6, 2, 128), (16, 1, 128), (15, 3, 64), (40, 2, 64)])
+def test_attn_decode(dtype, hq, hkv, hd):
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 100, 0, 128, 129, 257, 300]
+    pool = Pool(20, lens, hkv, hd)
+    _check_attn(pool, DT[dtype], hq, lens, [1] * len(lens), True, 21, pad=8)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 4, 64), (6, 2, 128), (8, 1, 64)])
+def test_attn_prompt(dtype, causal, hq, hkv, hd):
+    lens, ql = [1, 17, 70, 5, 40, 0, 33, 64], [1, 17, 50, 9, 0, 3, 2, 64]     # 9 rows on 5 keys: four see none
+    pool = Pool(22, lens, hkv, hd)
+    _check_attn(pool, DT[dtype], hq, lens, ql, causal, 23, pad=8)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ql", [1, 3, 8, 20, 70])
+def test_attn_long_keys_are_cut_and_joined(dtype, ql):
+    lens = [2100, 900, 1]
+    pool = Pool(24, lens, 2, 128)
+    _check_attn(pool, DT[dtype], 4, lens, [ql, ql, 1], True, 25)
+
+
+@gpu
+def test_attn_one_long_sequence():
+    lens = [20011]
+    pool = Pool(26, lens, 1, 64)
+    _check_attn(pool, torch.bfloat16, 2, lens, [1], True, 27)
+    _check_attn(pool, torch.float32, 2, lens, [2], True, 28)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attn_strong_scores(dtype):
+    """Weights on few keys, and sizes that differ by page."""
+    lens = [200, 77]
+    pool = Pool(29, lens, 2, 64, spread=6.0)
+    _check_attn(pool, DT[dtype], 4, lens, [1, 1], True, 30, q_scale=4.0)
+    _check_attn(pool, DT[dtype], 4, lens, [60, 30], True, 31, q_scale=4.0, scale=0.5)
+    _check_attn(pool, DT[dtype], 4, lens, [60, 30], False, 32, scale=1e-6)
+
+
+@gpu
+@pytest.mark.parametrize("ql", [1, 40])
+def test_attn_keeps_to_its_bounds(ql):
+    """Unknown table rows are empty, pages that are none are not seen, row
+    ranges and lengths are cut."""
+    lens = [60, 90, 33, 48]
+    pool = Pool(33, lens, 2, 64)
+    pool.table[1, 2], pool.table[1, 5] = pool.nb, -7
+    pool.table[2, :] = -1
+    n = [ql] * 4
+    _check_attn(pool, torch.bfloat16, 4, lens, n, True, 34)
+    _check_attn(pool, torch.bfloat16, 4, lens, n, False, 35, seq=[3, 4, -1, 0])
+    _check_attn(pool, torch.bfloat16, 4, lens, n, True, 36, max_kv=50, outside=-ql)
+    _check_attn(pool, torch.bfloat16, 4, [60, 90, 10 ** 9, -3], n, True, 37, max_kv=200, max_q=max(1, ql - 3))
+
+
+@gpu
+@pytest.mark.parametrize("ql", [1, 5, 40])
+@pytest.mark.parametrize("hkv", [2, 4])
+def test_attn_nan_counts_only_where_it_is_seen(ql, hkv):
+    """NaN keys and values: rows that see them are NaN (a value's in its dim
+    alone), rows that do not are what they are without."""
+    hd, n = 64, 70
+    rng = np.random.default_rng(38)
+    pool = Pool(39, [n, n], hkv, hd)
+    clean = pool.codes.copy()
+
+    def put(t, dim, value):
+        pg = pool.table[0, t // 16]
+        pool.codes[pg, value, 0, R.order(hd, value)[t % 16, dim]] = 0xFF
+    put(n - 2, 5, 1)          # seen by the last two rows only
+    put(n - 20, 17, 1)
+    put(n - 1, 3, 0)          # the last row is NaN as a whole
+    rows = [ql, ql]
+    start = [0, ql, 2 * ql]
+    q, q64 = _rows(rng, 2 * ql, 4, hd, torch.bfloat16)
+    res = []
+    for c in (clean, pool.codes):
+        out = torch.empty_like(q)
+        E.op_kv8_attn(torch.from_numpy(c).cuda(), torch.from_numpy(pool.scales).cuda(), torch.from_numpy(pool.table).cuda(),
+                      q, out, _ints(start), _ints([n, n]), ql, n)
+        res.append(out.double().cpu().numpy().reshape(2, ql, 4, hd))
+    want = res[0].copy()
+    mine = 4 // hkv
+    for j in range(ql):
+        sees = n - ql + j
+        if sees >= n - 2:
+            want[0, j, :mine, 5] = np.nan
+        if sees >= n - 20:
+            want[0, j, :mine, 17] = np.nan
+        if sees >= n - 1:
+            want[0, j, :mine] = np.nan
+    assert rows and np.array_equal(np.isnan(want), np.isnan(res[1]))
+    np.testing.assert_array_equal(want, res[1])
+
+
+@gpu
+@pytest.mark.parametrize("ql", [1, 33])
+def test_attn_workspace_serves_call_after_call(ql):
+    """One workspace, calls of several shapes that it is large enough for, results the same each time."""
+    lens = [3000, 1200]
+    pool = Pool(40, lens, 2, 64)
+    codes, scales, table = pool.gpu()
+    q = torch.randn((2 * ql, 256), device="cuda").bfloat16()
+    ws = E.kv8_attn_workspace(codes, table, q, 2, ql, 3000)
+    assert ws.numel() > 0
+    first = None
+    for _ in range(3):
+        out = torch.empty_like(q)
+        E.op_kv8_attn(codes, scales, table, q, out, _ints([0, ql, 2 * ql]), _ints(lens), ql, 3000, workspace=ws)
+        first = out if first is None else first
+        assert torch.equal(first, out)
+    fresh = torch.empty_like(q)
+    E.op_kv8_attn(codes, scales, table, q, fresh, _ints([0, ql, 2 * ql]), _ints(lens), ql, 3000)
+    assert torch.equal(first, fresh)
+    with pytest.raises(E.EbrlError):
+        E.op_kv8_attn(codes, scales, table, q, fresh, _ints([0, ql, 2 * ql]), _ints(lens), ql, 3000, workspace=ws[:-16])
+
+
+@gpu
+def test_decode_loop_in_a_graph():
+    """Write and attention of a token in a captured graph, replayed with new
+    rows and lengths beside eager work, against eager calls on another cache;
+    two graphs with a workspace each."""
+    lens, steps, hq, hkv, hd = [50, 700, 15], 5, 4, 2, 128
+    pool = Pool(41, lens, hkv, hd, room=steps)
+    cos, sin = (torch.from_numpy(t).cuda() for t in _tables(800, hd))
+    start = _ints([0, 1, 2, 3])
+    mx = max(lens) + steps
+    x = torch.randn((steps, 3, (hq + 2 * hkv) * hd), device="cuda").bfloat16()
+
+    def step(cache, qkv, q, out, pos, kvl, ws):
+        E.op_kv8_write(*cache, qkv[:, hq * hd:(hq + hkv) * hd], qkv[:, (hq + hkv) * hd:], start, pos, 1,
+                       q=qkv[:, :hq * hd], q_out=q, sections=(hd // 2,), cos=cos, sin=sin)
+        E.op_kv8_attn(*cache, q, out, start, kvl, 1, mx, workspace=ws)
+
+    eager, want = pool.gpu(), []
+    for j in range(steps):
+        q, out = torch.empty((3, hq * hd), device="cuda").bfloat16(), torch.empty((3, hq * hd), device="cuda").bfloat16()
+        step(eager, x[j], q, out, _ints(lens) + j, _ints(lens) + j + 1, None)
+        want.append(out)
+    graphs = []
+    for _ in range(2):
+        s = {"cache": pool.gpu(), "qkv": x[0].clone(), "q": torch.empty_like(want[0]), "out": torch.empty_like(want[0]),
+             "pos": _ints(lens), "kvl": _ints(lens) + 1}
+        s["ws"] = E.kv8_attn_workspace(s["cache"][0], s["cache"][2], s["q"], 3, 1, mx)
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            step(s["cache"], s["qkv"], s["q"], s["out"], s["pos"], s["kvl"], s["ws"])
+        graphs.append((g, s))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for j in range(steps):
+        for (g, s), st in zip(graphs, streams):
+            st.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(st):
+                s["qkv"].copy_(x[j])
+                s["pos"].copy_(_ints(lens) + j)
+                s["kvl"].copy_(_ints(lens) + j + 1)
+                g.replay()
+        torch.cuda.synchronize()
+        for _, s in graphs:
+            assert torch.equal(s["out"], want[j]), j
+    for _, s in graphs:
+        assert np.array_equal(_bits(s["cache"][0]), _bits(eager[0]))
+        np.testing.assert_array_equal(s["cache"][1].cpu().numpy(), eager[1].cpu().numpy())
+
+
+@gpu
+def test_prompt_then_tokens_match_the_definition():
+    """A prompt's rows written and attended to in two parts, then tokens, every output against the float64 form."""
+    hq, hkv, hd, n = 4, 2, 64, 90
+    rng = np.random.default_rng(42)
+    pool = Pool(43, [0, 0], hkv, hd, room=n)
+    cos, sin = _tables(n, hd)
+    dc, ds = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    codes, scales, table = pool.gpu()
+    wc, ws = pool.codes.copy(), pool.scales.copy()
+    for a, b in ((0, 37), (37, 80), (80, 81), (81, 82), (82, 90)):
+        m = b - a
+        q, q64 = _rows(rng, 2 * m, hq, hd, torch.bfloat16)
+        k, k64 = _rows(rng, 2 * m, hkv, hd, torch.bfloat16)
+        v, v64 = _rows(rng, 2 * m, hkv, hd, torch.bfloat16)
+        axis = rng.integers(0, n, (2 * m, 3)).astype(np.int32)
+        start = [0, m, 2 * m]
+        out = torch.empty_like(q)
+        E.op_kv8_write(codes, scales, table, k, v, _ints(start), _ints([a, a]), m, q=q, q_out=q, sections=(12, 10, 10),
+                       axis_pos=torch.from_numpy(axis).cuda(), cos=dc, sin=ds)
+        E.op_kv8_attn(codes, scales, table, q, out, _ints(start), _ints([b, b]), m, n)
+        R.write(wc, ws, pool.table, k64, v64, start, [a, a], m, [12, 10, 10], axis, cos, sin)
+        _same_codes(_bits(codes), wc)
+        qr = q.double().cpu().numpy().reshape(2 * m, hq, hd)
+        want, bound = R.attend(wc, ws, pool.table, qr, start, [b, b], m, n, True, hd ** -0.5)
+        _held(out.double().cpu().numpy().reshape(want.shape), want, bound)
+
+
+@gpu
+def test_calls_on_another_stream():
+    pool = Pool(44, [300, 40], 2, 64)
+    codes, scales, table = pool.gpu()
+    q = torch.randn((2, 256), device="cuda").bfloat16()
+    st, kl = _ints([0, 1, 2]), _ints([300, 40])
+    want = torch.empty_like(q)
+    E.op_kv8_attn(codes, scales, table, q, want, st, kl, 1, 300)
+    s = torch.cuda.Stream()
+    got = torch.empty_like(q)
+    ws = E.kv8_attn_workspace(codes, table, q, 2, 1, 300)
+    torch.cuda.synchronize()
+    E.op_kv8_attn(codes, scales, table, q, got, st, kl, 1, 300, workspace=ws, stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(want, got)
+    with torch.cuda.stream(s):
+        E.op_kv8_attn(codes, scales, table, q, got.zero_(), st, kl, 1, 300)
+    s.synchronize()
+    assert torch.equal(want, got)
