@@ -109,14 +109,13 @@ int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_a
  * that sees no key gets zeros; rows outside every sequence are left as they
  * were.  Scores, the softmax's maximum and sum and the weighted sum are held
  * in 32 bits.  With few rows the keys are cut into parts that run at the same
- * time, joined by the part that finishes last, in the parts' order: the result
- * does not depend on the order they finish in.  The cut follows n, max_q_len,
- * max_kv_len and the heads.
+ * time and are joined in their order by a second launch.  The cut follows n,
+ * max_q_len, max_kv_len and the heads.
  *
- * The workspace has to be zero before its first use; each call leaves it
- * ready for the next.  Calls that may overlap in time (other streams, graphs
- * replayed side by side) need a workspace each.  Returns EBRL_E_INVALID on
- * bad arguments or too small a workspace. */
+ * The workspace holds the parts; what is in it before a call does not matter.
+ * Calls that may overlap in time (other streams, graphs replayed side by side)
+ * need a workspace each.  Returns EBRL_E_INVALID on bad arguments or too small
+ * a workspace. */
 int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, void* stream);
 
 #ifdef __cplusplus

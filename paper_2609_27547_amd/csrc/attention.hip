@@ -30,37 +30,7 @@ namespace ebrl {
 
 // --------------------------------------------------------- bf16 prefill --
 
-typedef __attribute__((address_space(3))) void* attn_lds_ptr_t;
 typedef short attn_v4s __attribute__((ext_vector_type(4)));
-
-// global_load_lds_dwordx4 issued as inline assembly: the compiler neither
-// counts it nor guards LDS reads against it; the kernel waits on vmcnt and
-// synchronises the workgroup itself before reading a filled buffer.
-EBRL_DEV void attn_dma16(const void* g, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 :: "v"(g), "s"(lds_addr) : "memory", "m0");
-}
-
-// Lanes l and l ^ 16, then l and l ^ 32, combined with VALU lane swaps
-// (v_permlane16_swap / v_permlane32_swap hand each lane both values of its
-// pair), instead of LDS-routed swizzles that queue behind the K/V traffic.
-// Both lanes of a pair get the same result (the operations commute).
-EBRL_DEV float attn_max_xor16_32(float v) {
-    const unsigned u = __builtin_bit_cast(unsigned, v);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    v = fmaxf(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
-    const unsigned w = __builtin_bit_cast(unsigned, v);
-    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
-}
-EBRL_DEV float attn_sum_xor16_32(float v) {
-    const unsigned u = __builtin_bit_cast(unsigned, v);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    v = __builtin_bit_cast(float, (unsigned)a[0]) + __builtin_bit_cast(float, (unsigned)a[1]);
-    const unsigned w = __builtin_bit_cast(unsigned, v);
-    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return __builtin_bit_cast(float, (unsigned)b[0]) + __builtin_bit_cast(float, (unsigned)b[1]);
-}
 
 // One KT-key tile (a multiple of 32) of the online-softmax attention for the
 // wave's 16 queries (lane (r, g): query r, keys 16 kt + 4 g + v): scores
@@ -166,13 +136,6 @@ EBRL_DEV void attn_tile_math(const bf16_t* tk, const bf16_t* tv, int k0, int mas
             acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb, acc[dt], 0, 0, 0);
         }
     }
-}
-
-// s_waitcnt on the vector-memory counter only (gfx9 encoding: expcnt and
-// lgkmcnt fields at their maxima).
-template <int N> EBRL_DEV void attn_wait_vmcnt() {
-    static_assert(N >= 0 && N < 64, "vmcnt range");
-    __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | 0xF00 | ((N >> 4) << 14));
 }
 
 // One workgroup per (query tile of ATTN_Q_TILE rows, head): NW waves of 16

@@ -502,7 +502,7 @@ def _kv8_attn_args(c, q, n, max_q_len, max_kv_len) -> Kv8AttnArgs:
 
 
 def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
-    """A workspace for op_kv8_attn calls with these sizes, on the cache's device, ready for use."""
+    """A workspace for op_kv8_attn calls with these sizes, on the cache's device."""
     import torch
     c = Kv8Cache(0, 0, 0, codes.shape[0], block_table.shape[0], block_table.shape[1], codes.shape[2],
                  codes.shape[3] // KV8_PAGE)
@@ -510,7 +510,7 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     need = lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(a))
     if need < 0:
         raise EbrlError(need, "ebrl_op_kv8_attn_workspace")
-    return torch.zeros(need, dtype=torch.uint8, device=codes.device)
+    return torch.empty(need, dtype=torch.uint8, device=codes.device)
 
 
 def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len, max_kv_len, causal=True, scale=None,
