@@ -83,17 +83,29 @@ template <> EBRL_DEV void kv8_load<bf16_t, 8>(const bf16_t* p, float* o) {
         o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-// Eight results of 64 bits, each rounded once.
-EBRL_DEV void kv8_store8(float* p, const double* y) {
-    *reinterpret_cast<float4*>(p) = make_float4((float)y[0], (float)y[1], (float)y[2], (float)y[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4((float)y[4], (float)y[5], (float)y[6], (float)y[7]);
+EBRL_DEV void kv8_store8(float* p, const float* y) {
+    *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(y[4], y[5], y[6], y[7]);
 }
-EBRL_DEV void kv8_store8(bf16_t* p, const double* y) {
+EBRL_DEV void kv8_store8(bf16_t* p, const float* y) {
     bf16x8 o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (__bf16)kv8_odd(y[i]);
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)y[i];
     *reinterpret_cast<bf16x8*>(p) = o;
 }
+
+// N elements as they lie in memory (N * sizeof(T) a multiple of 16 bytes).
+template <typename T, int N> struct Kv8Raw {
+    uint4 w[N * sizeof(T) / 16];
+    EBRL_DEV void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    EBRL_DEV void get(float (&o)[N]) const {
+#pragma unroll
+        for (int q = 0; q < N; q += 8) kv8_load<T, 8>(reinterpret_cast<const T*>(w) + q, o + q);
+    }
+};
 
 struct Kv8WriteKernelArgs {
     ebrl_kv8_cache c;
@@ -103,6 +115,94 @@ struct Kv8WriteKernelArgs {
     int rot_units, v_units;   // waves of a (sequence, page): for the Q and K heads, for the V heads
 };
 
+// The new tokens of one page: slots s0 .. s1 - 1 of `page` (outside the pool:
+// there is none), slot t's row row0 + t.
+struct Kv8Span { int s0, s1, row0, pos0, page; };
+EBRL_DEV bool kv8_span(const Kv8WriteKernelArgs& w, int i, int pg, Kv8Span& s) {
+    const ebrl_kv8_write_args& a = w.a;
+    const int trow = a.seq ? a.seq[i] : i;
+    const int r0 = min(max(a.row_start[i], 0), a.rows);
+    const int len = min(min(a.row_start[i + 1], a.rows) - r0, a.max_len);
+    const int p0 = a.pos0[i];
+    if (trow < 0 || trow >= w.c.table_rows || len <= 0 || p0 < 0 || p0 >= w.c.table_stride * KV8_PAGE) return false;
+    const int at = p0 / KV8_PAGE + pg;
+    if (at >= w.c.table_stride) return false;
+    const int first = at * KV8_PAGE - p0;             // token of slot 0, counted from the first new one
+    s.s0 = max(-first, 0);
+    s.s1 = min(KV8_PAGE, len - first);
+    s.row0 = r0 + first;
+    s.pos0 = at * KV8_PAGE;
+    s.page = w.c.block_table[(size_t)trow * w.c.table_stride + at];
+    return s.s1 > s.s0;
+}
+
+// The table row of a pair's axis.
+EBRL_DEV int kv8_axis_row(int pair, int b1, int b2, int row0, int row1, int row2) {
+    return pair < b1 ? row0 : pair < b2 ? row1 : row2;
+}
+
+// Cosines and sines of N pairs from pair `at` on (multiples of 4) for `row` at
+// cache position `pos`: each from the table row of its axis's position.
+template <int HALF, int N>
+EBRL_DEV void kv8_angles(const ebrl_kv8_write_args& a, int row, int pos, int at, float (&cs)[N], float (&sn)[N]) {
+    const int* ap = a.axis_pos ? a.axis_pos + (size_t)row * a.n_axes : nullptr;
+    const int b1 = a.sections[0], b2 = b1 + (a.n_axes > 1 ? a.sections[1] : 0);
+    const int most = a.tab_rows - 1;
+    const int row0 = min(max(ap ? ap[0] : pos, 0), most), row1 = min(max(a.n_axes > 1 ? ap[1] : 0, 0), most);
+    const int row2 = min(max(a.n_axes > 2 ? ap[2] : 0, 0), most);
+    // four pairs of one axis at a time, unless axes change inside four
+    const bool whole = (b1 & 3) == 0 && (b2 & 3) == 0;
+#pragma unroll
+    for (int q = 0; q < N; q += 4) {
+        if (whole) {
+            const size_t o = (size_t)kv8_axis_row(at + q, b1, b2, row0, row1, row2) * HALF + at + q;
+            kv8_load<float, 4>(a.cos_tab + o, cs + q);
+            kv8_load<float, 4>(a.sin_tab + o, sn + q);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const size_t o = (size_t)kv8_axis_row(at + q + j, b1, b2, row0, row1, row2) * HALF + at + q + j;
+                cs[q + j] = a.cos_tab[o];
+                sn[q + j] = a.sin_tab[o];
+            }
+        }
+    }
+}
+
+// Pairs (x0, x1) turned, in 64 bits (the products are exact, so each result is
+// rounded once there) and rounded to odd, so that the rounding that follows is
+// that of the 64-bit value; `whole`: the results are the 32-bit values.
+template <int N>
+EBRL_DEV void kv8_turn(float (&x0)[N], float (&x1)[N], const float (&cs)[N], const float (&sn)[N], bool whole) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const double c = cs[q], s = sn[q], u = x0[q], v = x1[q];
+        const double y0 = fma(u, c, -(v * s)), y1 = fma(v, c, u * s);
+        x0[q] = whole ? (float)y0 : kv8_odd(y0);
+        x1[q] = whole ? (float)y1 : kv8_odd(y1);
+    }
+}
+
+// Exponent of a group's stored scale.
+EBRL_DEV int kv8_stored_exponent(float scale) {
+    return min(max((int)(__float_as_uint(scale) >> 23 & 255) - 127, KV8_EXP_MIN), KV8_EXP_MAX);
+}
+
+// Largest magnitude that is stored of x; what is not stored becomes NaN.
+template <int N> EBRL_DEV float kv8_amax(float (&x)[N]) {
+    float am = 0.f;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        x[q] = kv8_storable(x[q]);
+        am = fmaxf(am, fabsf(x[q]));   // passes a NaN over
+    }
+    return am;
+}
+
+// A call of several tokens a sequence: a wave takes the new tokens of a page
+// and a run of heads, Q and K heads or V heads.  Bound by bytes.  Four heads a
+// wave in turn share the cosines and sines; one head a wave where there are
+// too few waves to fill the chip.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
 {
@@ -116,21 +216,10 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
     const int unit = id % per_page;
     const unsigned sp = id / per_page;
     const int pg = sp % w.pages, i = sp / w.pages;
-    if (i >= a.n) return;
-
-    // the new tokens of this page: slots s0 .. s1 - 1, rows row0 ..
-    const int trow = a.seq ? a.seq[i] : i;
-    const int r0 = min(max(a.row_start[i], 0), a.rows);
-    const int len = min(min(a.row_start[i + 1], a.rows) - r0, a.max_len);
-    const int p0 = a.pos0[i];
-    if (trow < 0 || trow >= w.c.table_rows || len <= 0 || p0 < 0 || p0 >= w.c.table_stride * KV8_PAGE) return;
-    const int page_at = p0 / KV8_PAGE + pg;
-    if (page_at >= w.c.table_stride) return;
-    const int first = page_at * KV8_PAGE - p0;             // token of slot 0, counted from the first new one
-    const int s0 = max(-first, 0), s1 = min(KV8_PAGE, len - first);
-    if (s1 <= s0) return;
-    const int page = w.c.block_table[(size_t)trow * w.c.table_stride + page_at];
-    const bool there = page >= 0 && page < w.c.num_blocks;
+    Kv8Span s;
+    if (i >= a.n || !kv8_span(w, i, pg, s)) return;
+    const int s0 = s.s0, s1 = s.s1;
+    const bool there = s.page >= 0 && s.page < w.c.num_blocks;
     const int hkv = w.c.kv_heads;
     uint8_t* const codes = (uint8_t*)w.c.codes;
 
@@ -138,87 +227,47 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
         // Q and K heads: lane (t, g) has slot t's pairs PL g .. PL g + PL - 1
         const int t = lane >> 2, g = lane & 3;
         const bool mine = t >= s0 && t < s1;
-        const int row = r0 + first + (mine ? t : s0);
+        const int slot = mine ? t : s0, row = s.row0 + slot;
         float cs[PL], sn[PL];
-        if (a.n_axes) {
-            const int* ap = a.axis_pos ? a.axis_pos + (size_t)row * a.n_axes : nullptr;
-            const int b1 = a.sections[0], b2 = b1 + (a.n_axes > 1 ? a.sections[1] : 0);
-            int pos[3];
-            pos[0] = ap ? ap[0] : p0 + (row - r0);
-            pos[1] = a.n_axes > 1 ? ap[1] : 0;
-            pos[2] = a.n_axes > 2 ? ap[2] : 0;
-            size_t base[3];
-#pragma unroll
-            for (int x = 0; x < 3; ++x) base[x] = (size_t)min(max(pos[x], 0), a.tab_rows - 1) * HALF;
-#pragma unroll
-            for (int q = 0; q < PL; q += 4) {
-                const int at = PL * g + q;
-                auto axis = [&](int pair) { return pair < b1 ? 0 : pair < b2 ? 1 : 2; };
-                if (axis(at) == axis(at + 3)) {
-                    const int x = axis(at);
-                    const size_t o = (x == 0 ? base[0] : x == 1 ? base[1] : base[2]) + at;
-                    kv8_load<float, 4>(a.cos_tab + o, cs + q);
-                    kv8_load<float, 4>(a.sin_tab + o, sn + q);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int x = axis(at + j);
-                        const size_t o = (x == 0 ? base[0] : x == 1 ? base[1] : base[2]) + at + j;
-                        cs[q + j] = a.cos_tab[o];
-                        sn[q + j] = a.sin_tab[o];
-                    }
-                }
-            }
-        }
+        if (a.n_axes) kv8_angles<HALF, PL>(a, row, s.pos0 + slot, PL * g, cs, sn);
         const int h_lo = unit * w.per_wave, h_hi = min(h_lo + w.per_wave, a.q_heads + hkv);
+        auto src = [&](int h) {
+            return (h < a.q_heads ? (const T*)a.q + (size_t)row * a.ldq + h * HD
+                                  : (const T*)a.k + (size_t)row * a.ldk + (h - a.q_heads) * HD) + PL * g;
+        };
+        Kv8Raw<T, PL> r0, r1;
+        r0.load(src(h_lo));
+        r1.load(src(h_lo) + HALF);
         for (int h = h_lo; h < h_hi; ++h) {
             const bool isq = h < a.q_heads;
             const int hh = isq ? h : h - a.q_heads;
-            const T* src = isq ? (const T*)a.q + (size_t)row * a.ldq : (const T*)a.k + (size_t)row * a.ldk;
-            src += hh * HD + PL * g;
             float x0[PL], x1[PL];
-#pragma unroll
-            for (int q = 0; q < PL; q += 8) {
-                kv8_load<T, 8>(src + q, x0 + q);
-                kv8_load<T, 8>(src + HALF + q, x1 + q);
-            }
-            double y0[PL], y1[PL];
-#pragma unroll
-            for (int q = 0; q < PL; ++q) {
-                y0[q] = x0[q];
-                y1[q] = x1[q];
-                if (a.n_axes) {
-                    y0[q] = (double)x0[q] * cs[q] - (double)x1[q] * sn[q];
-                    y1[q] = (double)x1[q] * cs[q] + (double)x0[q] * sn[q];
-                }
-            }
+            r0.get(x0);
+            r1.get(x1);
+            const T* const next = src(min(h + 1, h_hi - 1));   // in flight while this head is worked on
+            r0.load(next);
+            r1.load(next + HALF);
+            if (a.n_axes) kv8_turn<PL>(x0, x1, cs, sn, sizeof(T) == 4 && isq);
             if (isq) {
                 if (mine) {
                     T* dst = (T*)a.q_out + (size_t)row * a.ldq_out + hh * HD + PL * g;
 #pragma unroll
                     for (int q = 0; q < PL; q += 8) {
-                        kv8_store8(dst + q, y0 + q);
-                        kv8_store8(dst + HALF + q, y1 + q);
+                        kv8_store8(dst + q, x0 + q);
+                        kv8_store8(dst + HALF + q, x1 + q);
                     }
                 }
                 continue;
             }
             if (!there) continue;
-            float am = 0.f;
-#pragma unroll
-            for (int q = 0; q < PL; ++q) {
-                x0[q] = kv8_storable(kv8_odd(y0[q]));
-                x1[q] = kv8_storable(kv8_odd(y1[q]));
-                am = fmaxf(am, fmaxf(fabsf(x0[q]), fabsf(x1[q])));   // fmax passes a NaN over
-            }
-            am = wave_max(mine ? am : 0.f);
-            int e = kv8_exponent(am);
-            const size_t grp = ((size_t)page * 2) * hkv + hh;
+            const float am = fmaxf(kv8_amax<PL>(x0), kv8_amax<PL>(x1));
+            int e = kv8_exponent(wave_max(mine ? am : 0.f));
+            const size_t grp = (size_t)s.page * 2 * hkv + hh;
             // lane's codes: pairs' first elements, and second ones HALF dims on
             uint8_t* const dst = codes + grp * (KV8_PAGE * HD) + t * 64 + PL * g;
             constexpr int HI = HD == 128 ? 1024 : 32;
             if (s0 > 0) {
-                const int was = min(max((int)(__float_as_uint(w.c.scales[grp]) >> 23 & 255) - 127, KV8_EXP_MIN), KV8_EXP_MAX);
+                const int was = kv8_stored_exponent(w.c.scales[grp]);
                 if (e > was && t < s0) {
                     const float sh = kv8_pow2(was - e);
 #pragma unroll
@@ -256,58 +305,49 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
         constexpr int NC = HD / 64;
         const int u = unit - w.rot_units;
         const int h_lo = u * w.per_wave, h_hi = min(h_lo + w.per_wave, hkv);
-        unsigned keep = 0;               // bytes of a dword that are not new
+        // bytes of a dword that hold slots before the new ones (their values
+        // stay), and those or slots behind (their bytes stay)
+        unsigned before = 0, keep = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) {
+            if (4 * g + j < s0) before |= 0xffu << (8 * j);
             if (4 * g + j < s0 || 4 * g + j >= s1) keep |= 0xffu << (8 * j);
+        }
         for (int h = h_lo; h < h_hi; ++h) {
-            float x[NC][4][4];
+            float x[4][4 * NC];
             float am = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int t = 4 * g + j;
                 const bool mine = t >= s0 && t < s1;
-                const T* src = (const T*)a.v + (size_t)(r0 + first + (mine ? t : s0)) * a.ldv + h * HD + 4 * l;
+                const T* src = (const T*)a.v + (size_t)(s.row0 + (mine ? t : s0)) * a.ldv + h * HD + 4 * l;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    kv8_load<T, 4>(src + 64 * c, x[c][j]);
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        x[c][j][d] = kv8_storable(x[c][j][d]);
-                        if (mine) am = fmaxf(am, fabsf(x[c][j][d]));
-                    }
-                }
+                for (int c = 0; c < NC; ++c) kv8_load<T, 4>(src + 64 * c, x[j] + 4 * c);
+                const float m = kv8_amax<4 * NC>(x[j]);
+                if (mine) am = fmaxf(am, m);
             }
-            am = wave_max(am);
-            int e = kv8_exponent(am);
-            const size_t grp = ((size_t)page * 2 + 1) * hkv + h;
+            int e = kv8_exponent(wave_max(am));
+            const size_t grp = ((size_t)s.page * 2 + 1) * hkv + h;
             uint4* const dst = reinterpret_cast<uint4*>(codes + grp * (KV8_PAGE * HD)) + lane;
             float sh = 1.f;
             if (s0 > 0) {
-                const int was = min(max((int)(__float_as_uint(w.c.scales[grp]) >> 23 & 255) - 127, KV8_EXP_MIN), KV8_EXP_MAX);
+                const int was = kv8_stored_exponent(w.c.scales[grp]);
                 if (e > was) sh = kv8_pow2(was - e);
                 e = max(e, was);
             }
             const float inv = kv8_pow2(-e);
-            // slots before s0 keep their values, slots behind s1 their bytes
-            unsigned before = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (4 * g + j < s0) before |= 0xffu << (8 * j);
             if (keep != ~0u || (before && sh != 1.f)) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    unsigned o[4], n[4] = {0, 0, 0, 0};
-                    if (keep) {
-                        const uint4 old = dst[64 * c];
-                        n[0] = old.x; n[1] = old.y; n[2] = old.z; n[3] = old.w;
-                    }
+                    uint4 old = make_uint4(0, 0, 0, 0);
+                    if (keep) old = dst[64 * c];
+                    unsigned o[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
-                        const unsigned nw = kv8_pack4(x[c][0][d] * inv, x[c][1][d] * inv, x[c][2][d] * inv, x[c][3][d] * inv);
-                        unsigned od = n[d];
-                        if (sh != 1.f) od = (kv8_shift4(od, sh) & before) | (od & ~before);
-                        o[d] = (od & keep) | (nw & ~keep);
+                        const int q = 4 * c + d;
+                        const unsigned nw = kv8_pack4(x[0][q] * inv, x[1][q] * inv, x[2][q] * inv, x[3][q] * inv);
+                        if (sh != 1.f) o[d] = (kv8_shift4(o[d], sh) & before) | (o[d] & ~before);
+                        o[d] = (o[d] & keep) | (nw & ~keep);
                     }
                     dst[64 * c] = make_uint4(o[0], o[1], o[2], o[3]);
                 }
@@ -317,13 +357,139 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
     }
 }
 
+// Largest over the LPH lanes (4 or 8) that share a head.
+template <int LPH> EBRL_DEV float kv8_head_max(float v) {
+    v = fmaxf(v, dpp_f<DPP_SWAP1>(v));
+    v = fmaxf(v, dpp_f<DPP_SWAP2>(v));
+    return LPH == 8 ? fmaxf(v, dpp_f<DPP_HALF_MIRROR>(v)) : v;
+}
+
+// One token a sequence: a wave takes 64 / LPH heads of a sequence's token,
+// eight pairs (Q, K) or sixteen dims (V) a lane, so that every lane has work.
+// Bound by latency: the chain is lengths, page, scale, codes.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void kv8_write_token_kernel(Kv8WriteKernelArgs w)
+{
+    constexpr int HALF = HD / 2, LPH = HD / 16, HPW = 64 / LPH;
+    const ebrl_kv8_write_args& a = w.a;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per = w.rot_units + w.v_units;
+    const unsigned id = blockIdx.x * 4u + wave;
+    const int unit = id % per, i = id / per;
+    Kv8Span s;
+    if (i >= a.n || !kv8_span(w, i, 0, s)) return;
+    const int t = s.s0, row = s.row0 + t;
+    const bool there = s.page >= 0 && s.page < w.c.num_blocks;
+    const int hkv = w.c.kv_heads;
+    const int j = lane % LPH;
+    if (unit < w.rot_units) {
+        const int h = unit * HPW + lane / LPH, hs = min(h, a.q_heads + hkv - 1);
+        const bool isq = hs < a.q_heads;
+        const int hh = isq ? hs : hs - a.q_heads;
+        const T* src = isq ? (const T*)a.q + (size_t)row * a.ldq : (const T*)a.k + (size_t)row * a.ldk;
+        src += hh * HD + 8 * j;
+        const size_t grp = (size_t)(there ? s.page : 0) * 2 * hkv + hh;
+        const float stored = isq ? 0.f : w.c.scales[grp];
+        float x0[8], x1[8], cs[8], sn[8];
+        kv8_load<T, 8>(src, x0);
+        kv8_load<T, 8>(src + HALF, x1);
+        if (a.n_axes) {
+            kv8_angles<HALF, 8>(a, row, s.pos0 + t, 8 * j, cs, sn);
+            kv8_turn<8>(x0, x1, cs, sn, sizeof(T) == 4 && isq);
+        }
+        if (isq) {
+            T* dst = (T*)a.q_out + (size_t)row * a.ldq_out + hh * HD + 8 * j;
+            kv8_store8(dst, x0);
+            kv8_store8(dst + HALF, x1);
+        }
+        int e = kv8_exponent(kv8_head_max<LPH>(fmaxf(kv8_amax<8>(x0), kv8_amax<8>(x1))));
+        if (isq || !there || h != hs) return;
+        uint8_t* const dst = (uint8_t*)w.c.codes + grp * (KV8_PAGE * HD) + 8 * j;
+        constexpr int HI = HD == 128 ? 1024 : 32;
+        if (t > 0) {
+            const int was = kv8_stored_exponent(stored);
+            if (e > was) {
+                const float sh = kv8_pow2(was - e);
+                for (int b = 0; b < t; ++b)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint2* const at = reinterpret_cast<uint2*>(dst + b * 64 + x * HI);
+                        *at = make_uint2(kv8_shift4(at->x, sh), kv8_shift4(at->y, sh));
+                    }
+            }
+            e = max(e, was);
+        }
+        const float inv = kv8_pow2(-e);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float* const y = x ? x1 : x0;
+            *reinterpret_cast<uint2*>(dst + t * 64 + x * HI) =
+                make_uint2(kv8_pack4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                           kv8_pack4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+        }
+        if (j == 0) w.c.scales[grp] = kv8_pow2(e);
+    } else {
+        const int h = (unit - w.rot_units) * HPW + lane / LPH, hh = min(h, hkv - 1);
+        const T* src = (const T*)a.v + (size_t)row * a.ldv + hh * HD + 16 * j;
+        float x[16];
+        kv8_load<T, 8>(src, x);
+        kv8_load<T, 8>(src + 8, x + 8);
+        const size_t grp = ((size_t)(there ? s.page : 0) * 2 + 1) * hkv + hh;
+        // the lane's 16 dims are 64 bytes of each four slots
+        uint4* const dst = reinterpret_cast<uint4*>((uint8_t*)w.c.codes + grp * (KV8_PAGE * HD) + j / 4 * 1024) + j % 4 * 4;
+        const float stored = w.c.scales[grp];
+        uint4 old[4];
+#pragma unroll
+        for (int x4 = 0; x4 < 4; ++x4) old[x4] = dst[t / 4 * 16 + x4];
+        int e = kv8_exponent(kv8_head_max<LPH>(kv8_amax<16>(x)));
+        if (!there || h != hh) return;
+        float sh = 1.f;
+        if (t > 0) {
+            const int was = kv8_stored_exponent(stored);
+            if (e > was) sh = kv8_pow2(was - e);
+            e = max(e, was);
+        }
+        const float inv = kv8_pow2(-e);
+        if (sh != 1.f)
+            for (int b = 0; b < t / 4; ++b)
+#pragma unroll
+                for (int x4 = 0; x4 < 4; ++x4) {
+                    uint4* const at = dst + b * 16 + x4;
+                    const uint4 o = *at;
+                    *at = make_uint4(kv8_shift4(o.x, sh), kv8_shift4(o.y, sh), kv8_shift4(o.z, sh), kv8_shift4(o.w, sh));
+                }
+        const int bit = 8 * (t & 3);
+        const unsigned before = (1u << bit) - 1, mine = 0xffu << bit;
+#pragma unroll
+        for (int x4 = 0; x4 < 4; ++x4) {
+            unsigned o[4] = {old[x4].x, old[x4].y, old[x4].z, old[x4].w};
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const float v = x[4 * x4 + d] * inv;
+                if (sh != 1.f) o[d] = (kv8_shift4(o[d], sh) & before) | (o[d] & ~before);
+                o[d] = (o[d] & ~mine) | (kv8_pack4(v, v, v, v) & mine);
+            }
+            dst[t / 4 * 16 + x4] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        if (j == 0) w.c.scales[grp] = kv8_pow2(e);
+    }
+}
+
 // ------------------------------------------------------------- attention --
 
 // How a call is cut into workgroups of four waves.
+enum Kv8Kind {
+    KV8_WAVE,     // decode: each wave has a (sequence, KV head)'s rows, up to 16, to itself
+    KV8_GROUP,    // decode: the four waves share the rows and deal the keys
+    KV8_PAIRS,    // prompt: two waves share 16 rows, 32 rows a workgroup
+    KV8_ROWS,     // prompt: 16 rows a wave, 64 a workgroup
+    KV8_TALL      // prompt, bf16: 32 rows a wave, 128 a workgroup
+};
 struct Kv8Plan {
-    bool decode = true;   // the waves share 16 rows and deal the keys, or share the keys and have 32 rows each
-    int tile_rows = 16;   // query rows (token, head of the group) of a workgroup
-    int tiles = 1;        // workgroups that a (sequence, KV head)'s rows take
+    Kv8Kind kind = KV8_GROUP;
+    int tile_rows = 16;   // query rows (token, head of the group) of a workgroup or, KV8_WAVE, a wave
+    int tiles = 1;        // of them, that a (sequence, KV head)'s rows take
     int parts = 1;        // most parts that a tile's keys are cut into
     int part_keys = 0;    // keys of a part
 };
@@ -332,6 +498,7 @@ struct Kv8AttnKernelArgs {
     ebrl_kv8_cache c;
     ebrl_kv8_attn_args a;
     int grp, tiles, tile_rows, parts, part_keys;
+    int join_rows;    // rows of a tile, at most
     float scale_log2;
     float* part_o;    // [unit][part][tile_rows][head_dim], unit = (sequence, KV head, tile)
     float* part_ml;   // [unit][part][tile_rows][2]: maximum and sum
@@ -346,20 +513,24 @@ struct Kv8Tile {
     int end;           // those keys
     const int* table;  // the sequence's pages
 };
+// Sequence i's row of the block table, or -1.
+EBRL_DEV int kv8_table_row(const Kv8AttnKernelArgs& w, int i) {
+    const int row = w.a.seq ? w.a.seq[i] : i;
+    return row < w.c.table_rows ? max(row, -1) : -1;
+}
 EBRL_DEV Kv8Tile kv8_tile(const Kv8AttnKernelArgs& w, int i, int tile) {
     const ebrl_kv8_attn_args& a = w.a;
     Kv8Tile t;
-    const int trow = a.seq ? a.seq[i] : i;
+    const int trow = kv8_table_row(w, i);
     t.r0 = min(max(a.row_start[i], 0), a.rows);
     t.m = min(max(min(a.row_start[i + 1], a.rows) - t.r0, 0), a.max_q_len);
     t.rows = t.m * w.grp;
     t.t0 = tile * w.tile_rows;
-    const bool known = trow >= 0 && trow < w.c.table_rows;
-    t.len = known ? min(max(a.kv_len[i], 0), min(a.max_kv_len, w.c.table_stride * KV8_PAGE)) : 0;
+    t.len = trow >= 0 ? min(max(a.kv_len[i], 0), min(a.max_kv_len, w.c.table_stride * KV8_PAGE)) : 0;
     const int last = (min(t.t0 + w.tile_rows, t.rows) - 1) / w.grp;
     t.end = a.causal ? max(min(t.len, t.len - t.m + last + 1), 0) : t.len;
     t.parts = max(1, (t.end + w.part_keys - 1) / w.part_keys);
-    t.table = w.c.block_table + (size_t)(known ? trow : 0) * w.c.table_stride;
+    t.table = w.c.block_table + (size_t)max(trow, 0) * w.c.table_stride;
     return t;
 }
 
@@ -371,6 +542,9 @@ EBRL_DEV bf16x8 kv8_bf16(unsigned lo, unsigned hi, float sl, float sh) {
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sh, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+
+// Bit 7 of each byte that is a NaN code.
+EBRL_DEV unsigned kv8_nan_bytes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 // A float as NP bf16 terms that add up to it (three hold all 24 bits).
 template <int NP> EBRL_DEV void kv8_split(float x, __bf16* o) {
@@ -403,14 +577,19 @@ template <typename T, int HD, int QT> struct Kv8Rows {
             const T* src = (const T*)w.a.q + (size_t)(t.r0 + tok) * w.a.ldq + h * HD;
 #pragma unroll
             for (int s = 0; s < HD / 32; ++s) {
-                float x[8];
-                kv8_load<T, 8>(src + (s >> 1) * 64 + g * 16 + (s & 1) * 8, x);
+                const T* const at = src + (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+                if constexpr (NP == 1) {
+                    q[qt][0][s] = *reinterpret_cast<const bf16x8*>(at);
+                } else {
+                    float x[8];
+                    kv8_load<T, 8>(at, x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    __bf16 p[NP];
-                    kv8_split<NP>(x[j], p);
+                    for (int j = 0; j < 8; ++j) {
+                        __bf16 p[NP];
+                        kv8_split<NP>(x[j], p);
 #pragma unroll
-                    for (int y = 0; y < NP; ++y) q[qt][y][s][j] = p[y];
+                        for (int y = 0; y < NP; ++y) q[qt][y][s][j] = p[y];
+                    }
                 }
             }
             mx[qt] = -INFINITY;
@@ -426,16 +605,17 @@ template <typename T, int HD, int QT> struct Kv8Rows {
         if (wr0 >= t.rows) end = 0;
     }
 
-    // Two pages (32 keys from k0 on) in the lanes' order: kc, vc their codes,
-    // ks, vs their scales, there: whether each is one.
-    EBRL_DEV void step(uint4 (&kc)[2][NC], uint4 (&vc)[2][NC], const float (&ks)[2], const float (&vs)[2],
-                       const bool (&there)[2], int k0, int len, float scale_log2, int lane)
+    // P pages (an even number; 16 P keys from k0 on) in the lanes' order: kc, vc
+    // their codes, ks, vs their scales, there: whether each is one.
+    template <int P>
+    EBRL_DEV void step(uint4 (&kc)[P][NC], uint4 (&vc)[P][NC], const float (&ks)[P], const float (&vs)[P],
+                       const bool (&there)[P], int k0, int len, float scale_log2, int lane)
     {
         const int g = lane >> 4;
         // S^T = K Q^T
-        f32x4 s[QT][2];
+        f32x4 s[QT][P];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < P; ++t) {
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -454,22 +634,33 @@ template <typename T, int HD, int QT> struct Kv8Rows {
                         s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, q[qt][p][2 * c + 1], s[qt][t], 0, 0, 0);
             }
         }
+        // Codes of V that are NaN where not every row sees every key: a bit
+        // each, pairs of pages apart.
+        uint64_t nan_v[P / 2];
+        bool all_there = true;
+#pragma unroll
+        for (int t = 0; t < P; ++t) {
+            all_there &= there[t];
+            if (t % 2) nan_v[t / 2] = 0;
+        }
         bool nans = false;
-        if (k0 + 32 > all || !there[0] || !there[1]) {
+        if (k0 + 16 * P > all || !all_there) {
             // some row does not see some key.  Slots past the last key may
             // hold anything: their weights are zero, and so have their
             // values to be.
             unsigned bad = 0;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < P; ++t) {
                 const int left = there[t] ? len - (k0 + 16 * t + 4 * g) : 0;
                 const unsigned ok = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    vc[t][c].x &= ok; vc[t][c].y &= ok; vc[t][c].z &= ok; vc[t][c].w &= ok;
-                    const unsigned x[4] = {vc[t][c].x, vc[t][c].y, vc[t][c].z, vc[t][c].w};
+                    unsigned* const x = reinterpret_cast<unsigned*>(&vc[t][c]);
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) bad |= ((x[d] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    for (int d = 0; d < 4; ++d) {
+                        x[d] &= ok;
+                        bad |= kv8_nan_bytes(x[d]);
+                    }
                 }
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt)
@@ -478,6 +669,22 @@ template <typename T, int HD, int QT> struct Kv8Rows {
                         s[qt][t][v] = there[t] && k0 + 16 * t + 4 * g + v < lim[qt] ? s[qt][t][v] : -INFINITY;
             }
             nans = __any(bad != 0);
+            if (nans) {
+                // a NaN counts for the rows that see its key alone: the
+                // product takes it as zero
+#pragma unroll
+                for (int t = 0; t < P; ++t)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        unsigned* const x = reinterpret_cast<unsigned*>(&vc[t][c]);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) {
+                            const unsigned z = kv8_nan_bytes(x[d]) >> 7;
+                            x[d] &= ~(z * 0xffu);
+                            nan_v[t / 2] |= (uint64_t)(z * 0x01020408u >> 24 & 15u) << (4 * ((t % 2 * NC + c) * 4 + d));
+                        }
+                    }
+            }
         }
         // Weights are 2^(x - mx), x = score log2(e) / sqrt(hd).  mx is a whole
         // number that follows the row's maximum: it moves when a weight would
@@ -490,7 +697,7 @@ template <typename T, int HD, int QT> struct Kv8Rows {
         for (int qt = 0; qt < QT; ++qt) {
             tm[qt] = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < P; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) tm[qt] = fmaxf(tm[qt], s[qt][t][v]);
             move |= tm[qt] * scale_log2 > mx[qt] + KV8_SLACK;
@@ -506,32 +713,35 @@ template <typename T, int HD, int QT> struct Kv8Rows {
                 for (int d = 0; d < HD / 16; ++d) acc[qt][d] *= alpha;
             }
         }
-        bf16x8 pb[QT][NP];
+        // O^T += V^T P^T for a pair of pages: row r of product 4 c + d is dim
+        // 64 c + 4 r + d, a lane's eight keys those that its scores are of
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-            const float use = mx[qt] == -INFINITY ? 0.f : mx[qt];
+        for (int u = 0; u < P; u += 2) {
+            bf16x8 pb[QT][NP];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int qt = 0; qt < QT; ++qt) {
+                const float use = mx[qt] == -INFINITY ? 0.f : mx[qt];
+                float ps = 0.f;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float p = fast_exp2(fmaf(s[qt][t][v], scale_log2, -use));
-                    sum[qt] += p;
-                    __bf16 o[NP];
-                    kv8_split<NP>(p, o);
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int y = 0; y < NP; ++y) pb[qt][y][4 * t + v] = o[y];
-                }
-        }
-        // O^T += V^T P^T: row r of product 4 c + d is dim 64 c + 4 r + d, a
-        // lane's eight keys those that its scores are of
+                    for (int v = 0; v < 4; ++v) {
+                        const float p = fast_exp2(fmaf(s[qt][u + t][v], scale_log2, -use));
+                        ps += p;
+                        __bf16 o[NP];
+                        kv8_split<NP>(p, o);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const unsigned x0[4] = {vc[0][c].x, vc[0][c].y, vc[0][c].z, vc[0][c].w};
-            const unsigned x1[4] = {vc[1][c].x, vc[1][c].y, vc[1][c].z, vc[1][c].w};
-            if (!nans) {
+                        for (int y = 0; y < NP; ++y) pb[qt][y][4 * t + v] = o[y];
+                    }
+                sum[qt] += ps;
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const unsigned x0[4] = {vc[u][c].x, vc[u][c].y, vc[u][c].z, vc[u][c].w};
+                const unsigned x1[4] = {vc[u + 1][c].x, vc[u + 1][c].y, vc[u + 1][c].z, vc[u + 1][c].w};
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const bf16x8 va = kv8_bf16(x0[d], x1[d], vs[0], vs[1]);
+                    const bf16x8 va = kv8_bf16(x0[d], x1[d], vs[u], vs[u + 1]);
 #pragma unroll
                     for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
@@ -539,38 +749,33 @@ template <typename T, int HD, int QT> struct Kv8Rows {
                             acc[qt][4 * c + d] =
                                 __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][p], acc[qt][4 * c + d], 0, 0, 0);
                 }
-            } else {
-                // a value is NaN, and not every row sees its key: products
-                // with NaNs taken as zero, then a count of those each row sees
+            }
+        }
+        if (nans) {
+            // how many NaNs of a dim each row sees
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    bf16x8 va = kv8_bf16(x0[d], x1[d], vs[0], vs[1]), isnan;
+            for (int u = 0; u < P; u += 2)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const unsigned b = (j < 4 ? x0[d] : x1[d]) >> (8 * (j & 3)) & 0x7f;
-                        isnan[j] = (__bf16)(b == 0x7f ? 1.f : 0.f);
-                        if (b == 0x7f) va[j] = (__bf16)0.f;
-                    }
+                for (int qt = 0; qt < QT; ++qt) {
+                    int below = lim[qt];
+                    asm volatile("" : "+v"(below));   // keeps what follows in this rare branch
+                    bf16x8 sees;
 #pragma unroll
-                    for (int qt = 0; qt < QT; ++qt) {
-                        bf16x8 sees;
+                    for (int j = 0; j < 8; ++j)
+                        sees[j] = (__bf16)(k0 + 16 * (u + (j >> 2)) + 4 * g + (j & 3) < below ? 1.f : 0.f);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int key = k0 + 16 * (j >> 2) + 4 * g + (j & 3);
-                            sees[j] = (__bf16)(there[j >> 2] && key < lim[qt] ? 1.f : 0.f);
-                        }
+                    for (int x = 0; x < 4 * NC; ++x) {
+                        bf16x8 isnan;
 #pragma unroll
-                        for (int p = NP - 1; p >= 0; --p)
-                            acc[qt][4 * c + d] =
-                                __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][p], acc[qt][4 * c + d], 0, 0, 0);
+                        for (int j = 0; j < 8; ++j)
+                            isnan[j] = (__bf16)((nan_v[u / 2] >> (4 * ((j >> 2) * NC * 4 + x) + (j & 3)) & 1) ? 1.f : 0.f);
                         const f32x4 n =
                             __builtin_amdgcn_mfma_f32_16x16x32_bf16(isnan, sees, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
-                            if (n[v] > 0.f) acc[qt][4 * c + d][v] = __uint_as_float(0x7fc00000u);
+                            if (n[v] > 0.f) acc[qt][x][v] = __uint_as_float(0x7fc00000u);
                     }
                 }
-            }
         }
     }
 };
@@ -582,62 +787,93 @@ EBRL_DEV T* kv8_out(const Kv8AttnKernelArgs& w, const Kv8Tile& t, int kvh, int r
     return (T*)w.a.out + (size_t)(t.r0 + tok) * w.a.ldo + (size_t)(kvh * w.grp + (row - tok * w.grp)) * HD;
 }
 
-// One query row a sequence, or few: the four waves of a workgroup share 16
-// rows and deal the pairs of pages of its part of the keys.  Bound by the
-// bytes of the cache: codes go straight to registers, the next two pages' in
-// flight while two are worked on.
+// A row's state: the result if its keys are in one part, else that part (the
+// `to`-th of the workspace).  Lane group g has dims 64 c + 16 g .. + 15.
 template <typename T, int HD>
+EBRL_DEV void kv8_store(const Kv8AttnKernelArgs& w, const f32x4 (&acc)[HD / 16], float mx, float sum, int parts, T* out,
+                        size_t to, int g)
+{
+    const float inv = parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int d = 64 * c + 16 * g + 4 * v;
+            const f32x4 o = {acc[4 * c][v] * inv, acc[4 * c + 1][v] * inv, acc[4 * c + 2][v] * inv, acc[4 * c + 3][v] * inv};
+            if (parts == 1) st4<T>(out + d, o[0], o[1], o[2], o[3]);
+            else *reinterpret_cast<f32x4*>(w.part_o + to * HD + d) = o;
+        }
+    if (parts > 1 && g == 0) { w.part_ml[2 * to] = mx; w.part_ml[2 * to + 1] = sum; }
+}
+
+// 16 bytes that are read once: marked non-temporal.
+EBRL_DEV uint4 kv8_stream16(const uint8_t* p) {
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+}
+
+// One query row a sequence, or few: KW waves share a (sequence, KV head)'s
+// rows, at most 16, and deal the pairs of pages of a part of the keys.  Bound
+// by the bytes of the cache: codes go straight to registers, and a step's
+// registers are loaded again as soon as it is done, so that each wave keeps
+// 8 to 16 KB in flight (head dim 128).
+template <typename T, int HD, int KW>
 __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 {
     constexpr int NC = HD / 64;
-    __shared__ __attribute__((aligned(16))) float s_o[4][16][HD + 4];
-    __shared__ float s_m[4][16], s_l[4][16];
+    constexpr int STEP = 32 * KW;              // keys that the waves take at a time
+    __shared__ __attribute__((aligned(16))) float s_o[KW > 1 ? KW : 1][KW > 1 ? 16 : 1][KW > 1 ? HD + 4 : 4];
+    __shared__ float s_m[KW][16], s_l[KW][16];
 
     const int hkv = w.c.kv_heads;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
-    unsigned id = blockIdx.x;
-    const int part = id % w.parts;
-    const unsigned unit = id / w.parts;
-    id = unit;
-    const int tile = id % w.tiles;
-    id /= w.tiles;
-    const int kvh = id % hkv, i = id / hkv;
-    const Kv8Tile t = kv8_tile(w, i, tile);
-    if (t.t0 >= t.rows || part >= t.parts) return;
-    const int k_lo = part * w.part_keys, k_hi = min(t.end, k_lo + w.part_keys);
+    const int kw = KW > 1 ? wave : 0;
+    const unsigned units = (unsigned)w.a.n * hkv, id = KW > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
+    const int part = id / units;
+    const unsigned unit = id % units;
+    if (part >= w.parts) return;
+    const int kvh = unit % hkv, i = unit / hkv;
+    // 32 steps of this wave at a time: lane 2 s + t has page t of step s.  The
+    // first pages are asked for before the lengths are known.
+    constexpr int BATCH = 32;
+    const int k_lo = part * w.part_keys;
+    const int p_at = (lane >> 1) * (STEP / KV8_PAGE) + kw * 2 + (lane & 1);
+    const int trow = kv8_table_row(w, i);
+    const int* const table = w.c.block_table + (size_t)max(trow, 0) * w.c.table_stride;
+    int page = k_lo / KV8_PAGE + p_at < w.c.table_stride ? table[k_lo / KV8_PAGE + p_at] : -1;
+    const Kv8Tile t = kv8_tile(w, i, 0);
+    if (t.rows == 0 || part >= t.parts) return;
+    const int k_hi = min(t.end, k_lo + w.part_keys);
 
     const size_t gb = (size_t)KV8_PAGE * HD;   // bytes of a (page, K or V, head) group
     const uint8_t* const codes = (const uint8_t*)w.c.codes + kvh * gb;
     const int k_at = r * 64 + g * 16, v_at = lane * 16;
     Kv8Rows<T, HD, 1> rows;
     const int p_hi = (k_hi + KV8_PAGE - 1) / KV8_PAGE;
-    // 32 steps of this wave at a time: lane 2 s + t has page t of step s
-    constexpr int BATCH = 32;
-    bool first = true;
-    for (int kb = k_lo; kb < k_hi || first; kb += BATCH * 128) {
-        const int at = kb / KV8_PAGE + (lane >> 1) * 8 + wave * 2 + (lane & 1);
-        int page = at < p_hi ? t.table[at] : -1;
-        if (page >= w.c.num_blocks) page = -1;
+    rows.init(w, t, kvh, 0, k_hi, lane);
+    for (int kb = k_lo; kb < k_hi; kb += BATCH * STEP) {
+        const int at = kb / KV8_PAGE + p_at;
+        if (kb > k_lo) page = at < p_hi ? table[at] : -1;
+        if (at >= p_hi || page >= w.c.num_blocks) page = -1;
         float ksv = 1.f, vsv = 1.f;
         if (page >= 0) {
             ksv = w.c.scales[(size_t)page * 2 * hkv + kvh];
             vsv = w.c.scales[((size_t)page * 2 + 1) * hkv + kvh];
         }
-        const int n = (k_hi - kb - wave * 32 + 127) / 128;
+        const int n = (k_hi - kb - kw * 32 + STEP - 1) / STEP;
         const int steps = min(max(n, 0), BATCH);
         auto load = [&](int s, uint4 (&kc)[2][NC], uint4 (&vc)[2][NC]) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                // a page that is none: another's codes, not used
-                const int pg = max(__builtin_amdgcn_readlane(page, 2 * s + x), 0);
+                // a page that is none: page 0's codes, not used
+                const int pg = max(2 * s + x < 64 ? __builtin_amdgcn_readlane(page, 2 * s + x) : 0, 0);
                 const uint8_t* kp = codes + (size_t)pg * 2 * hkv * gb;
                 const uint8_t* vp = kp + (size_t)hkv * gb;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-                    kc[x][c] = *reinterpret_cast<const uint4*>(kp + 1024 * c + k_at);
-                    vc[x][c] = *reinterpret_cast<const uint4*>(vp + 1024 * c + v_at);
+                    kc[x][c] = kv8_stream16(kp + 1024 * c + k_at);
+                    vc[x][c] = kv8_stream16(vp + 1024 * c + v_at);
                 }
             }
         };
@@ -650,73 +886,79 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
                 ks[x] = readlane_f(ksv, 2 * s + x);
                 vs[x] = readlane_f(vsv, 2 * s + x);
             }
-            rows.step(kc, vc, ks, vs, there, kb + s * 128 + wave * 32, t.len, w.scale_log2, lane);
+            rows.step(kc, vc, ks, vs, there, kb + s * STEP + kw * 32, t.len, w.scale_log2, lane);
         };
+        if (steps <= 0) continue;
         uint4 ka[2][NC], va[2][NC], kn[2][NC], vn[2][NC];
-        if (steps > 0) load(0, ka, va);
-        if (first) rows.init(w, t, kvh, t.t0, k_hi, lane);
-        first = false;
+        load(0, ka, va);
+        load(1, kn, vn);
+        asm volatile("" :: "v"(ksv), "v"(vsv));   // waited for here, not on every turn of the loop
+        // the loads are issued on every path, so that the waits leave the
+        // other step's in flight
         for (int s = 0; s < steps; s += 2) {
-            if (s + 1 < steps) load(s + 1, kn, vn);
             work(s, ka, va);
-            if (s + 1 < steps) {
-                if (s + 2 < steps) load(s + 2, ka, va);
-                work(s + 1, kn, vn);
-            }
+            load(s + 2, ka, va);
+            if (s + 1 < steps) work(s + 1, kn, vn);
+            load(s + 3, kn, vn);
         }
     }
     rows.sum[0] = attn_sum_xor16_32(rows.sum[0]);
 
-    // the waves join in their order
+    const size_t to0 = ((size_t)unit * w.parts + part) * 16;
+    if constexpr (KW == 1) {
+        if (r >= t.rows) return;
+        kv8_store<T, HD>(w, rows.acc[0], rows.mx[0], rows.sum[0], t.parts, kv8_out<T, HD>(w, t, kvh, r), to0 + r, g);
+    } else {
+        // the waves join in their order
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const f32x4 o = {rows.acc[0][4 * c][v], rows.acc[0][4 * c + 1][v], rows.acc[0][4 * c + 2][v],
-                             rows.acc[0][4 * c + 3][v]};
-            *reinterpret_cast<f32x4*>(&s_o[wave][r][64 * c + 16 * g + 4 * v]) = o;
-        }
-    if (g == 0) { s_m[wave][r] = rows.mx[0]; s_l[wave][r] = rows.sum[0]; }
-    __syncthreads();
-    const int here = min(16, t.rows - t.t0);
-    for (int x = tid; x < here * (HD / 4); x += 256) {
-        const int row = x / (HD / 4), d = x % (HD / 4) * 4;
-        float M = -INFINITY, L = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            for (int v = 0; v < 4; ++v) {
+                const f32x4 o = {rows.acc[0][4 * c][v], rows.acc[0][4 * c + 1][v], rows.acc[0][4 * c + 2][v],
+                                 rows.acc[0][4 * c + 3][v]};
+                *reinterpret_cast<f32x4*>(&s_o[wave][r][64 * c + 16 * g + 4 * v]) = o;
+            }
+        if (g == 0) { s_m[wave][r] = rows.mx[0]; s_l[wave][r] = rows.sum[0]; }
+        __syncthreads();
+        for (int x = tid; x < t.rows * (HD / 4); x += 256) {
+            const int row = x / (HD / 4), d = x % (HD / 4) * 4;
+            float M = -INFINITY, L = 0.f;
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int y = 0; y < 4; ++y) M = fmaxf(M, s_m[y][row]);
+            for (int y = 0; y < KW; ++y) M = fmaxf(M, s_m[y][row]);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const float my = s_m[y][row];
-            const float wt = my == -INFINITY ? 0.f : fast_exp2(my - M);
-            L += wt * s_l[y][row];
-            o += wt * *reinterpret_cast<const f32x4*>(&s_o[y][row][d]);
-        }
-        if (t.parts == 1) {
-            const float inv = L == 0.f ? 0.f : 1.f / L;
-            st4<T>(kv8_out<T, HD>(w, t, kvh, t.t0 + row) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-        } else {
-            const size_t to = ((size_t)unit * w.parts + part) * 16 + row;
-            *reinterpret_cast<f32x4*>(w.part_o + to * HD + d) = o;
-            if (d == 0) { w.part_ml[2 * to] = M; w.part_ml[2 * to + 1] = L; }
+            for (int y = 0; y < KW; ++y) {
+                const float my = s_m[y][row];
+                const float wt = my == -INFINITY ? 0.f : fast_exp2(my - M);
+                L += wt * s_l[y][row];
+                o += wt * *reinterpret_cast<const f32x4*>(&s_o[y][row][d]);
+            }
+            if (t.parts == 1) {
+                const float inv = L == 0.f ? 0.f : 1.f / L;
+                st4<T>(kv8_out<T, HD>(w, t, kvh, row) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            } else {
+                *reinterpret_cast<f32x4*>(w.part_o + (to0 + row) * HD + d) = o;
+                if (d == 0) { w.part_ml[2 * (to0 + row)] = M; w.part_ml[2 * (to0 + row) + 1] = L; }
+            }
         }
     }
 }
 
-// Many rows: the four waves of a workgroup have 16 QT rows each and share
-// the keys, 64 at a time, through a ring of LDS buffers that DMA fills with
-// raw codes (16 KB a step at head dim 128), in the order in which a lane
-// reads them back: 16 bytes a lane, one after the other.
-template <typename T, int HD, int QT>
+// Many rows: the keys go through two LDS buffers, 64 at a time, that DMA fills
+// with raw codes (16 KB a step at head dim 128) in the order in which a lane
+// reads them back: 16 bytes a lane, one after the other.  A wave has 16 QT rows
+// and takes P pages at a time; with KG 1 the four waves of a workgroup have
+// rows of their own and take all keys, with KG 2 two waves share rows and take
+// 32 keys of each step.
+template <typename T, int HD, int QT, int KG, int P>
 __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 {
     constexpr int NC = HD / 64;
     constexpr int RW = 16 * QT;
-    constexpr int S = 3;                       // ring depth
-    constexpr int SEG = 512;                   // pages whose ids and scales LDS holds
+    constexpr int TR = RW * (4 / KG);
+        constexpr int SEG = 256;                   // pages whose ids and scales LDS holds
     constexpr int GB = KV8_PAGE * HD;
-    constexpr int IPT = 2 * NC;                // DMA instructions of a wave a step: its page's K and V
-    __shared__ __attribute__((aligned(1024))) uint8_t s_kv[S][4][2][GB];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_kv[2][4][2][GB];
     __shared__ __attribute__((aligned(16))) int s_page[SEG];
     __shared__ __attribute__((aligned(16))) float s_ks[SEG], s_vs[SEG];
 
@@ -725,8 +967,8 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     // Workgroups go round-robin to the eight XCDs: a (sequence, KV head) keeps
-    // to one, whose L2 then serves its tiles.  Tiles that see the most keys
-    // start first.
+    // to one, whose L2 then serves its tiles.  Tiles with the most work start
+    // first: causal ones at the end of a sequence, others at its start.
     const unsigned heads = (unsigned)w.a.n * hkv;
     unsigned u, rest;
     if (heads % 8 == 0) {
@@ -737,14 +979,16 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
         u = blockIdx.x % heads;
         rest = blockIdx.x / heads;
     }
-    const int part = rest % w.parts, tile = w.tiles - 1 - (int)(rest / w.parts);
+    const int part = rest % w.parts;
+    const int tile = w.a.causal ? w.tiles - 1 - (int)(rest / w.parts) : rest / w.parts;
     const int kvh = u % hkv, i = u / hkv;
     const unsigned unit = u * w.tiles + tile;
     const Kv8Tile t = kv8_tile(w, i, tile);
     if (t.t0 >= t.rows || part >= t.parts) return;
     const int k_lo = part * w.part_keys, k_hi = min(t.end, k_lo + w.part_keys);
 
-    const int wr0 = t.t0 + wave * RW;
+    const int kg = KG == 1 ? 0 : wave & 1;
+    const int wr0 = t.t0 + wave / KG * RW;
     Kv8Rows<T, HD, QT> rows;
     rows.init(w, t, kvh, wr0, k_hi, lane);
 
@@ -764,7 +1008,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
         }
         __syncthreads();
         auto dma = [&](int it, int buf) {
-            // a page that is none: another's codes, not used
+            // a page that is none: page 0's codes, not used
             const int pg = max(__builtin_amdgcn_readfirstlane(s_page[4 * it + wave]), 0);
             const uint8_t* kp = codes + (size_t)pg * 2 * hkv * GB;
             const uint8_t* vp = kp + (size_t)hkv * GB;
@@ -775,58 +1019,87 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
                 attn_dma16(vp + 1024 * c + v_at, to + GB + 1024 * c);
             }
         };
-        for (int p = 0; p < S - 1 && p < steps; ++p) dma(p, p);
-        int buf = 0;
+        dma(0, 0);
         for (int it = 0; it < steps; ++it) {
+            const int buf = it & 1;
             // this wave's part of step `it` has landed, then every wave's has
             // and every wave is done with the buffer that is filled next
-            if (steps - 1 - it >= 1) attn_wait_vmcnt<IPT>();
-            else attn_wait_vmcnt<0>();
+            attn_wait_vmcnt<0>();
             __syncthreads();
-            if (it + S - 1 < steps) dma(it + S - 1, buf == 0 ? S - 1 : buf - 1);
-            const int k0 = seg + it * 64;
+            if (it + 1 < steps) dma(it + 1, buf ^ 1);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (k0 + 32 * half >= rows.end) break;    // nothing that a row of this wave sees
-                uint4 kc[2][NC], vc[2][NC];
-                float ks[2], vs[2];
-                bool there[2];
+            for (int x = 0; x < 4 / KG; x += P) {
+                const int p0 = kg * (4 / KG) + x, k0 = seg + it * 64 + 16 * p0;
+                if (k0 >= rows.end) break;     // nothing that a row of this wave sees
+                uint4 kc[P][NC], vc[P][NC];
+                float ks[P], vs[P];
+                bool there[P];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int pg = 2 * half + x;
+                for (int y = 0; y < P; ++y) {
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
-                        kc[x][c] = *reinterpret_cast<const uint4*>(&s_kv[buf][pg][0][1024 * c + lane * 16]);
-                        vc[x][c] = *reinterpret_cast<const uint4*>(&s_kv[buf][pg][1][1024 * c + lane * 16]);
+                        kc[y][c] = *reinterpret_cast<const uint4*>(&s_kv[buf][p0 + y][0][1024 * c + lane * 16]);
+                        vc[y][c] = *reinterpret_cast<const uint4*>(&s_kv[buf][p0 + y][1][1024 * c + lane * 16]);
                     }
-                    there[x] = __builtin_amdgcn_readfirstlane(s_page[4 * it + pg]) >= 0;
-                    ks[x] = s_ks[4 * it + pg];
-                    vs[x] = s_vs[4 * it + pg];
+                    there[y] = __builtin_amdgcn_readfirstlane(s_page[4 * it + p0 + y]) >= 0;
+                    ks[y] = s_ks[4 * it + p0 + y];
+                    vs[y] = s_vs[4 * it + p0 + y];
                 }
-                rows.step(kc, vc, ks, vs, there, k0 + 32 * half, t.len, w.scale_log2, lane);
+                rows.step(kc, vc, ks, vs, there, k0, t.len, w.scale_log2, lane);
             }
-            buf = buf == S - 1 ? 0 : buf + 1;
+        }
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) rows.sum[qt] = attn_sum_xor16_32(rows.sum[qt]);
+    if constexpr (KG == 2) {
+        // the second wave of a pair hands its state to the first, in the buffers
+        constexpr int LD = HD + 4;
+        static_assert(TR * (LD + 2) * 4 <= 2 * 4 * 2 * GB, "the states fit the buffers");
+        float* const s_o = reinterpret_cast<float*>(&s_kv[0][0][0][0]);
+        float* const s_ml = s_o + TR * LD;
+        __syncthreads();
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            const int row = wave / 2 * RW + 16 * qt + r;
+            if (kg == 1) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const f32x4 o = {rows.acc[qt][4 * c][v], rows.acc[qt][4 * c + 1][v], rows.acc[qt][4 * c + 2][v],
+                                         rows.acc[qt][4 * c + 3][v]};
+                        *reinterpret_cast<f32x4*>(s_o + row * LD + 64 * c + 16 * g + 4 * v) = o;
+                    }
+                if (g == 0) { s_ml[2 * row] = rows.mx[qt]; s_ml[2 * row + 1] = rows.sum[qt]; }
+            }
+        }
+        __syncthreads();
+        if (kg == 1) return;
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            const int row = wave / 2 * RW + 16 * qt + r;
+            const float m1 = s_ml[2 * row], M = fmaxf(rows.mx[qt], m1);
+            const float w0 = rows.mx[qt] == -INFINITY ? 0.f : fast_exp2(rows.mx[qt] - M);
+            const float w1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
+            rows.mx[qt] = M;
+            rows.sum[qt] = w0 * rows.sum[qt] + w1 * s_ml[2 * row + 1];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(s_o + row * LD + 64 * c + 16 * g + 4 * v);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        rows.acc[qt][4 * c + d][v] = w0 * rows.acc[qt][4 * c + d][v] + w1 * o[d];
+                }
         }
     }
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        const float sum = attn_sum_xor16_32(rows.sum[qt]);
         const int row = wr0 + 16 * qt + r;
         if (row >= t.rows) continue;
-        const float inv = t.parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-        const size_t to = ((size_t)unit * w.parts + part) * (4 * RW) + (row - t.t0);
-        T* const out = kv8_out<T, HD>(w, t, kvh, row);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int d = 64 * c + 16 * g + 4 * v;
-                const f32x4 o = {rows.acc[qt][4 * c][v] * inv, rows.acc[qt][4 * c + 1][v] * inv,
-                                 rows.acc[qt][4 * c + 2][v] * inv, rows.acc[qt][4 * c + 3][v] * inv};
-                if (t.parts == 1) st4<T>(out + d, o[0], o[1], o[2], o[3]);
-                else *reinterpret_cast<f32x4*>(w.part_o + to * HD + d) = o;
-            }
-        if (t.parts > 1 && g == 0) { w.part_ml[2 * to] = rows.mx[qt]; w.part_ml[2 * to + 1] = sum; }
+        kv8_store<T, HD>(w, rows.acc[qt], rows.mx[qt], rows.sum[qt], t.parts, kv8_out<T, HD>(w, t, kvh, row),
+                         ((size_t)unit * w.parts + part) * TR + (row - t.t0), g);
     }
 }
 
@@ -839,7 +1112,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
     __shared__ float s_w[4][KV8_MAX_PARTS];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned per = (w.tile_rows + 3) / 4;
+    const unsigned per = (w.join_rows + 3) / 4;
     const unsigned unit = blockIdx.x / per;
     const int row = (blockIdx.x % per) * 4 + wave;
     unsigned id = unit;
@@ -847,7 +1120,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
     id /= w.tiles;
     const int kvh = id % w.c.kv_heads, i = id / w.c.kv_heads;
     const Kv8Tile t = kv8_tile(w, i, tile);
-    if (t.parts == 1 || row >= w.tile_rows || t.t0 + row >= t.rows) return;
+    if (t.parts == 1 || row >= w.join_rows || t.t0 + row >= t.rows) return;
     const size_t base = (size_t)unit * w.parts * w.tile_rows + row;
     float m = -INFINITY;
     for (int p = lane; p < t.parts; p += 64) m = fmaxf(m, w.part_ml[2 * (base + (size_t)p * w.tile_rows)]);
@@ -879,15 +1152,43 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
 
 static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a) {
     Kv8Plan p;
-    const int64_t rows = (int64_t)a.max_q_len * (a.q_heads / c.kv_heads);
-    p.decode = rows <= 16;
-    p.tile_rows = p.decode ? 16 : a.dtype == EBRL_DTYPE_FP32 ? 64 : 128;
+    const int64_t rows = (int64_t)a.max_q_len * (a.q_heads / c.kv_heads), pairs = (int64_t)a.n * c.kv_heads;
+    auto groups = [&](int tile_rows) { return pairs * ((rows + tile_rows - 1) / tile_rows); };
+    if (rows <= 16) {
+        // A wave of its own for each (sequence, KV head) saves the joining of
+        // four, and pays where keys are few and waves many: 1024 pairs of
+        // 300 keys 20 us against 25, 4096 of 600 99.5 against 104.5; 256 of
+        // 600 16.6 against 15.0, 512 of up to 2048 43 against 31.
+        p.kind = pairs >= 1024 && a.max_kv_len <= 1024 ? KV8_WAVE : KV8_GROUP;
+        p.tile_rows = 16;
+    } else if (a.dtype == EBRL_DTYPE_BF16 && groups(128) >= 512 && a.max_kv_len >= 1024) {
+        // 32 rows a wave halve the conversions of codes, and pay once they
+        // fill the chip twice over and keys are many: 2 x 4 k rows of 32 heads
+        // on 8 k keys 767 us against 909 with 16 rows a wave, 2048 rows on
+        // 8 k keys 249 against 294; 1024 workgroups of 148 rows on 748 keys
+        // 63 against 62, 3072 on 288 keys 81 against 76.
+        p.kind = KV8_TALL;
+        p.tile_rows = 128;
+    } else if (groups(64) >= 512) {
+        p.kind = KV8_ROWS;
+        p.tile_rows = 64;
+    } else {
+        // few workgroups: twice as many of half the rows, two waves sharing
+        // them (600 rows of 32 heads on 600 keys 12.6 us against 15.4; 37
+        // sequences of 148 rows on 730 keys, 888 workgroups of 64 rows, 38 on
+        // both sides; 64 sequences of them 74 against 62)
+        p.kind = KV8_PAIRS;
+        p.tile_rows = 32;
+    }
     p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
-    const int64_t units = (int64_t)a.n * c.kv_heads * p.tiles;
-    const int least = p.decode ? 512 : 512, step = p.decode ? 128 : 64;
-    int64_t want = p.decode ? (1024 + units - 1) / units : 512 / units;
-    want = std::min<int64_t>(std::min<int64_t>(want, KV8_MAX_PARTS), (a.max_kv_len + least - 1) / least);
-    want = std::max<int64_t>(want, 1);
+    // Keys are cut where that brings the workgroups to the 768 that the chip
+    // holds at a time (three a CU), but not below 512 keys a part: three
+    // sequences of 50000 to 131000 keys, 24 pairs, in 32 parts 108 us, in 42
+    // 109, in 96 113; 512 pairs of 4096 keys in one part 87, in two 94.
+    const int64_t units = pairs * p.tiles;
+    int64_t want = p.kind == KV8_WAVE ? 1 : (768 + units / 2 - 1) / units;
+    want = std::max<int64_t>(1, std::min<int64_t>({want, KV8_MAX_PARTS, ((int64_t)a.max_kv_len + 511) / 512}));
+    const int step = p.kind == KV8_GROUP ? 128 : 64;   // keys that a workgroup takes at a time
     const int64_t keys = ((int64_t)a.max_kv_len + want - 1) / want;
     p.part_keys = (int)std::max<int64_t>(step, (keys + step - 1) / step * step);
     p.parts = (int)std::max<int64_t>(1, ((int64_t)a.max_kv_len + p.part_keys - 1) / p.part_keys);
@@ -916,13 +1217,28 @@ static bool kv8_attn_shape_ok(const ebrl_kv8_cache* c, const ebrl_kv8_attn_args*
 }
 
 template <typename T, int HD>
+static void kv8_write_launch(bool token, const Kv8WriteKernelArgs& w, unsigned groups, hipStream_t s) {
+    if (token) hipLaunchKernelGGL((kv8_write_token_kernel<T, HD>), dim3(groups), dim3(256), 0, s, w);
+    else hipLaunchKernelGGL((kv8_write_kernel<T, HD>), dim3(groups), dim3(256), 0, s, w);
+}
+
+template <typename T, int HD>
 static void kv8_attn_launch(const Kv8Plan& p, const Kv8AttnKernelArgs& w, int64_t units, hipStream_t s) {
-    constexpr int QT = sizeof(T) == 4 ? 1 : 2;
     const dim3 grid((unsigned)(units * p.parts)), wg(256);
-    if (p.decode) hipLaunchKernelGGL((kv8_decode_kernel<T, HD>), grid, wg, 0, s, w);
-    else hipLaunchKernelGGL((kv8_prompt_kernel<T, HD, QT>), grid, wg, 0, s, w);
+    switch (p.kind) {
+    case KV8_WAVE:
+        hipLaunchKernelGGL((kv8_decode_kernel<T, HD, 1>), dim3((unsigned)((units + 3) / 4)), wg, 0, s, w);
+        break;
+    case KV8_GROUP: hipLaunchKernelGGL((kv8_decode_kernel<T, HD, 4>), grid, wg, 0, s, w); break;
+    case KV8_PAIRS: hipLaunchKernelGGL((kv8_prompt_kernel<T, HD, 1, 2, 2>), grid, wg, 0, s, w); break;
+    case KV8_ROWS: hipLaunchKernelGGL((kv8_prompt_kernel<T, HD, 1, 1, 2>), grid, wg, 0, s, w); break;
+    case KV8_TALL:
+        if constexpr (sizeof(T) == 2)
+            hipLaunchKernelGGL((kv8_prompt_kernel<T, HD, 2, 1, HD / 32>), grid, wg, 0, s, w);
+        break;
+    }
     if (p.parts > 1)
-        hipLaunchKernelGGL((kv8_join_kernel<T, HD>), dim3((unsigned)(units * ((p.tile_rows + 3) / 4))), wg, 0, s, w);
+        hipLaunchKernelGGL((kv8_join_kernel<T, HD>), dim3((unsigned)(units * ((w.join_rows + 3) / 4))), wg, 0, s, w);
 }
 
 }  // namespace ebrl
@@ -958,22 +1274,26 @@ int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* ar
     Kv8WriteKernelArgs w;
     w.c = *cache;
     w.a = a;
+    const bool token = a.max_len == 1;
     const int64_t len = std::min<int64_t>(a.max_len, a.rows);
-    w.pages = (int)((len + 2 * KV8_PAGE - 2) / KV8_PAGE);
+    w.pages = token ? 1 : (int)((len + 2 * KV8_PAGE - 2) / KV8_PAGE);
     const int64_t sp = (int64_t)a.n * w.pages;
-    w.per_wave = sp * (a.q_heads + 2 * hkv) > 16384 ? 4 : 1;
+    // one head a wave up to some 16 waves a SIMD; from there on, four heads a
+    // wave share their cosines and sines (9 sequences of 3001 to 4095 tokens,
+    // 40 + 8 heads of 128: 182 us with one, 148 with two, 141 with four, 145
+    // with eight; 16 of 600 tokens, 24 + 8 heads: 43, 36.5, 37, 36.5)
+    w.per_wave = token ? 1024 / hd : sp * (a.q_heads + 2 * hkv) > 16384 ? 4 : 1;
     w.rot_units = (a.q_heads + hkv + w.per_wave - 1) / w.per_wave;
     w.v_units = (hkv + w.per_wave - 1) / w.per_wave;
     const int64_t groups = (sp * (w.rot_units + w.v_units) + 3) / 4;
     if (groups > KV8_MAX_GROUPS) return EBRL_E_INVALID;
-    const dim3 grid((unsigned)groups);
     hipStream_t s = (hipStream_t)stream;
     if (esz == 2) {
-        if (hd == 64) hipLaunchKernelGGL((kv8_write_kernel<bf16_t, 64>), grid, dim3(256), 0, s, w);
-        else hipLaunchKernelGGL((kv8_write_kernel<bf16_t, 128>), grid, dim3(256), 0, s, w);
+        if (hd == 64) kv8_write_launch<bf16_t, 64>(token, w, (unsigned)groups, s);
+        else kv8_write_launch<bf16_t, 128>(token, w, (unsigned)groups, s);
     } else {
-        if (hd == 64) hipLaunchKernelGGL((kv8_write_kernel<float, 64>), grid, dim3(256), 0, s, w);
-        else hipLaunchKernelGGL((kv8_write_kernel<float, 128>), grid, dim3(256), 0, s, w);
+        if (hd == 64) kv8_write_launch<float, 64>(token, w, (unsigned)groups, s);
+        else kv8_write_launch<float, 128>(token, w, (unsigned)groups, s);
     }
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
 }
@@ -1009,6 +1329,7 @@ int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args
     w.tile_rows = p.tile_rows;
     w.parts = p.parts;
     w.part_keys = p.part_keys;
+    w.join_rows = (int)std::min<int64_t>(p.tile_rows, (int64_t)a.max_q_len * w.grp);
     w.scale_log2 = a.scale * 1.4426950408889634f;
     w.part_o = (float*)a.workspace;
     w.part_ml = need ? w.part_o + units * p.parts * p.tile_rows * hd : nullptr;

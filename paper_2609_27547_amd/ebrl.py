@@ -403,54 +403,67 @@ def kv8_alloc(num_blocks: int, kv_heads: int, head_dim: int, device="cuda"):
     return codes.view(torch.float8_e4m3fn), torch.ones((num_blocks, 2, kv_heads), device=device)
 
 
-def _kv8_bad(what: str):
-    raise EbrlError(-1, f"kv8: {what}")
+def _kv8_bad(what: str, *tensors):
+    raise EbrlError(-1, "kv8: " + what + "".join(
+        f"; got {None if t is None else (tuple(t.shape), t.stride(), t.dtype, str(t.device))}" for t in tensors))
 
 
-def _kv8_cache(codes, scales, table) -> Kv8Cache:
+def _kv8_cache(codes, scales, table):
+    """The cache as the C struct, and its GPU's index (-1: not on a GPU).  These
+    checks run before every launch, so each property is asked for once."""
     import torch
-    nb, two, hkv, wide = codes.shape if codes.dim() == 4 else (0, 0, 0, 0)
-    if two != 2 or wide % KV8_PAGE or codes.element_size() != 1 or not codes.is_contiguous():
-        _kv8_bad(f"codes {tuple(codes.shape)} {codes.dtype}: contiguous 8-bit [num_blocks, 2, kv_heads, 16 * head_dim]")
-    if scales.shape != (nb, 2, hkv) or scales.dtype != torch.float32 or not scales.is_contiguous():
-        _kv8_bad(f"scales {tuple(scales.shape)} {scales.dtype}: contiguous float32 [num_blocks, 2, kv_heads]")
-    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
-        _kv8_bad(f"block_table {tuple(table.shape)} {table.dtype}: contiguous int32 [sequences, pages]")
-    return Kv8Cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), nb, table.shape[0], table.shape[1], hkv,
-                    wide // KV8_PAGE)
+    shape, dev = codes.shape, codes.get_device()
+    if len(shape) != 4 or shape[1] != 2 or shape[3] % KV8_PAGE or codes.element_size() != 1 or \
+            not codes.is_contiguous():
+        _kv8_bad("codes are contiguous 8-bit [num_blocks, 2, kv_heads, 16 * head_dim]", codes)
+    if scales.shape != shape[:3] or scales.dtype is not torch.float32 or not scales.is_contiguous() or \
+            scales.get_device() != dev:
+        _kv8_bad("scales are contiguous float32 [num_blocks, 2, kv_heads] where the codes are", scales)
+    pages = table.shape
+    if len(pages) != 2 or table.dtype is not torch.int32 or not table.is_contiguous() or table.get_device() != dev:
+        _kv8_bad("block_table is contiguous int32 [sequences, pages] where the codes are", table)
+    return Kv8Cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), shape[0], pages[0], pages[1], shape[2],
+                    shape[3] // KV8_PAGE), dev
 
 
-def _kv8_rows(name, t, dtype, rows, dev):
-    """Pointer, width and row stride of a [rows, width] tensor whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype != dtype or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1) or t.device != dev:
-        _kv8_bad(f"{name} {tuple(t.shape)} {t.dtype} on {t.device}: [{rows}, width] {dtype} on {dev}, rows contiguous")
-    return t.data_ptr(), t.shape[1], t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+def _kv8_rows(name, t, dtype, dev, rows, width):
+    """Pointer and row stride of a [rows, width] tensor whose rows are contiguous."""
+    if t.shape != (rows, width) or t.dtype is not dtype or t.get_device() != dev:
+        _kv8_bad(f"{name} is {dtype} [{rows}, {width}] where the cache is", t)
+    ld, one = t.stride()
+    if one != 1 and width > 1:
+        _kv8_bad(f"{name} has contiguous rows", t)
+    return t.data_ptr(), ld if rows > 1 else max(ld, width)
 
 
 def _kv8_ints(name, t, n, dev):
     import torch
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != dev:
-        _kv8_bad(f"{name} {tuple(t.shape)} {t.dtype} on {t.device}: {n} contiguous int32 on {dev}")
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        _kv8_bad(f"{name} is {n} contiguous int32 where the cache is", t)
     return t.data_ptr()
 
 
-def _kv8_dtype(t) -> int:
+def _kv8_dtype(name, t) -> int:
     import torch
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        _kv8_bad(f"rows are bfloat16 or float32, not {t.dtype}")
-    return DTYPE_BF16 if t.dtype == torch.bfloat16 else DTYPE_FP32
+    dtype = t.dtype
+    if t.dim() != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
+        _kv8_bad(f"{name} is bfloat16 or float32 [rows, heads * head_dim]", t)
+    return DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_FP32
 
 
 def _kv8_call(fn, name, cache, args, dev, stream):
-    """The call on `stream` (None: the current one of the tensors' device)."""
+    """The call on `stream` (None: the current one of the cache's device)."""
     import torch
-    if dev.type != "cuda":
-        _kv8_bad(f"the cache is on {dev}, not on a GPU")
-    with torch.cuda.device(dev):
-        rc = fn(ctypes.byref(cache), ctypes.byref(args),
-                torch.cuda.current_stream(dev).cuda_stream if stream is None else stream)
+    if dev < 0:
+        _kv8_bad("the cache is not on a GPU")
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _kv8_call(fn, name, cache, args, dev, stream)
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    rc = fn(ctypes.byref(cache), ctypes.byref(args), stream)
     if rc != EBRL_OK:
         raise EbrlError(rc, name)
 
@@ -463,42 +476,34 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
     pairs of each axis (empty: no rotation); cos, sin: float32 [positions,
     head_dim / 2].  `stream`: a raw handle whose order the tensors follow."""
     import torch
-    c, dev = _kv8_cache(codes, scales, block_table), codes.device
-    n, rows, axes = pos0.numel(), k.shape[0], len(sections)
-    a = Kv8WriteArgs(dtype=_kv8_dtype(k), n=n, rows=rows, max_len=max_len, n_axes=axes)
-    a.k, wk, a.ldk = _kv8_rows("k", k, k.dtype, rows, dev)
-    a.v, wv, a.ldv = _kv8_rows("v", v, k.dtype, rows, dev)
-    hd = c.head_dim
-    if wk != c.kv_heads * hd or wv != wk:
-        _kv8_bad(f"k and v have {wk} and {wv} columns, the cache {c.kv_heads} heads of {hd}")
+    c, dev = _kv8_cache(codes, scales, block_table)
+    hd, n, axes, dtype = c.head_dim, pos0.numel(), len(sections), _kv8_dtype("k", k)
+    rows, torch_dtype, width = k.shape[0], k.dtype, c.kv_heads * hd
+    k_at, ldk = _kv8_rows("k", k, torch_dtype, dev, rows, width)
+    v_at, ldv = _kv8_rows("v", v, torch_dtype, dev, rows, width)
     if (q is None) != (q_out is None) or axes > 3 or (axes == 0 and q is not None):
-        _kv8_bad("q and q_out go together, with one to three axes")
+        _kv8_bad("q and q_out go together, with one to three axes", q, q_out)
+    q_at = ldq = qo_at = ldqo = q_heads = tab_rows = 0
     if q is not None:
-        a.q, wq, a.ldq = _kv8_rows("q", q, k.dtype, rows, dev)
-        a.q_out, wo, a.ldq_out = _kv8_rows("q_out", q_out, k.dtype, rows, dev)
-        if wq % hd or wo != wq:
-            _kv8_bad(f"q and q_out have {wq} and {wo} columns: heads of {hd}")
-        a.q_heads = wq // hd
+        wide = q.shape[-1]
+        if wide % hd:
+            _kv8_bad(f"q has heads of {hd}", q)
+        q_at, ldq = _kv8_rows("q", q, torch_dtype, dev, rows, wide)
+        qo_at, ldqo = _kv8_rows("q_out", q_out, torch_dtype, dev, rows, wide)
+        q_heads = wide // hd
+    cos_at = sin_at = axis_at = None
     if axes:
-        a.sections[:axes] = list(sections)
+        tab_rows = 0 if cos is None else cos.shape[0]
         for t in (cos, sin):
-            if t is None or t.dim() != 2 or t.shape != cos.shape or t.shape[1] != hd // 2 or \
-                    t.dtype != torch.float32 or not t.is_contiguous() or t.device != dev:
-                _kv8_bad(f"cos and sin: contiguous float32 [positions, {hd // 2}] on {dev}")
-        a.tab_rows, a.cos_tab, a.sin_tab = cos.shape[0], cos.data_ptr(), sin.data_ptr()
-        a.axis_pos = _kv8_ints("axis_pos", axis_pos, rows * axes, dev)
-    a.row_start, a.pos0 = _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("pos0", pos0, n, dev)
-    a.seq = _kv8_ints("seq", seq, n, dev)
-    if scales.device != dev or block_table.device != dev:
-        _kv8_bad("codes, scales and block_table are on one device")
+            if t is None or t.shape != (tab_rows, hd // 2) or t.dtype is not torch.float32 or not t.is_contiguous() or \
+                    t.get_device() != dev:
+                _kv8_bad(f"cos and sin are contiguous float32 [positions, {hd // 2}] where the cache is", cos, sin)
+        cos_at, sin_at = cos.data_ptr(), sin.data_ptr()
+        axis_at = _kv8_ints("axis_pos", axis_pos, rows * axes, dev)
+    a = Kv8WriteArgs(dtype, n, rows, max_len, q_heads, axes, (*sections,), tab_rows, q_at, k_at, v_at, qo_at, ldq, ldk,
+                     ldv, ldqo, _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("pos0", pos0, n, dev),
+                     _kv8_ints("seq", seq, n, dev), axis_at, cos_at, sin_at)
     _kv8_call(lib().ebrl_op_kv8_write, "ebrl_op_kv8_write", c, a, dev, stream)
-
-
-def _kv8_attn_args(c, q, n, max_q_len, max_kv_len) -> Kv8AttnArgs:
-    if q.dim() != 2 or q.shape[1] % c.head_dim:
-        _kv8_bad(f"q {tuple(q.shape)}: [rows, heads * {c.head_dim}]")
-    return Kv8AttnArgs(dtype=_kv8_dtype(q), n=n, rows=q.shape[0], max_q_len=max_q_len, max_kv_len=max_kv_len,
-                       q_heads=q.shape[1] // c.head_dim)
 
 
 def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
@@ -506,7 +511,7 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     import torch
     c = Kv8Cache(0, 0, 0, codes.shape[0], block_table.shape[0], block_table.shape[1], codes.shape[2],
                  codes.shape[3] // KV8_PAGE)
-    a = _kv8_attn_args(c, q, n, max_q_len, max_kv_len)
+    a = Kv8AttnArgs(_kv8_dtype("q", q), n, q.shape[0], max_q_len, max_kv_len, q.shape[-1] // c.head_dim, 1, 1.0)
     need = lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(a))
     if need < 0:
         raise EbrlError(need, "ebrl_op_kv8_attn_workspace")
@@ -521,23 +526,23 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
     kv8_attn_workspace, one for each chain of calls that may overlap others;
     None makes one for this call (not with an explicit stream, which torch's
     allocator does not follow)."""
-    c, dev = _kv8_cache(codes, scales, block_table), codes.device
-    n = kv_len.numel()
-    a = _kv8_attn_args(c, q, n, max_q_len, max_kv_len)
-    a.causal, a.scale = int(bool(causal)), c.head_dim ** -0.5 if scale is None else scale
-    a.q, _, a.ldq = _kv8_rows("q", q, q.dtype, a.rows, dev)
-    a.out, wo, a.ldo = _kv8_rows("out", out, q.dtype, a.rows, dev)
-    if wo != q.shape[1]:
-        _kv8_bad(f"out has {wo} columns, q {q.shape[1]}")
-    a.row_start, a.kv_len = _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("kv_len", kv_len, n, dev)
-    a.seq = _kv8_ints("seq", seq, n, dev)
-    if scales.device != dev or block_table.device != dev or (workspace is not None and workspace.device != dev):
-        _kv8_bad("codes, scales, block_table and workspace are on one device")
+    c, dev = _kv8_cache(codes, scales, block_table)
+    hd, n, dtype = c.head_dim, kv_len.numel(), _kv8_dtype("q", q)
+    rows, wide = q.shape
+    if wide % hd:
+        _kv8_bad(f"q has heads of {hd}", q)
+    q_at, ldq = _kv8_rows("q", q, q.dtype, dev, rows, wide)
+    out_at, ldo = _kv8_rows("out", out, q.dtype, dev, rows, wide)
     if workspace is None:
         if stream is not None:
             _kv8_bad("a call on an explicit stream needs a workspace")
         workspace = kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _kv8_bad("the workspace is contiguous and where the cache is", workspace)
+    a = Kv8AttnArgs(dtype, n, rows, max_q_len, max_kv_len, wide // hd, bool(causal), hd ** -0.5 if scale is None else scale,
+                    q_at, out_at, ldq, ldo, _kv8_ints("row_start", row_start, n + 1, dev),
+                    _kv8_ints("kv_len", kv_len, n, dev), _kv8_ints("seq", seq, n, dev), workspace.data_ptr(),
+                    workspace.nbytes)
     _kv8_call(lib().ebrl_op_kv8_attn, "ebrl_op_kv8_attn", c, a, dev, stream)
 
 

@@ -127,8 +127,10 @@ def gather(codes, scales, table_row, n):
     return K, V, there
 
 
-def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, causal, scale, seq=None, bf16=True):
-    """(out, bound) [rows, hq, hd] float64; rows outside every sequence are NaN in both.
+def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, causal, scale, seq=None, bf16=True,
+           only=None):
+    """(out, bound) [rows, hq, hd] float64; rows outside every sequence are NaN in both.  `only`: the rows to work
+    out; the others get an infinite bound.
 
     The bound, from the arithmetic: a score is a sum of hd (fp32: 3 hd) exact
     products in 32 bits, each addition off by 2^-23 of the sum of the terms'
@@ -147,6 +149,9 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
         n = min(max(kv_len[i], 0), max_kv_len, table.shape[1] * PAGE) if known else 0
         K, V, there = gather(codes, scales, table[tr] if known else None, n)
         for j in range(m):
+            if only is not None and r0 + j not in only:
+                bound[r0 + j] = np.inf
+                continue
             lim = max(0, min(n, n - m + j + 1)) if causal else n
             use = np.flatnonzero(there[:lim])
             for h in range(hq):
