@@ -50,7 +50,7 @@ typedef enum {
     EBRL_E_UNSUPPORTED = -5   /* call not available for this model (e.g. flow on an AR policy) */
 } ebrl_status;
 
-enum { EBRL_DTYPE_FP32 = 0, EBRL_DTYPE_BF16 = 1 };
+enum { EBRL_DTYPE_FP32 = 0, EBRL_DTYPE_BF16 = 1, EBRL_DTYPE_BF16_KV8 = 2 };
 
 /* Policy shape.  The paper names the model families (VLM backbone plus an
  * autoregressive or flow-matching action head, Section 2.1) but no sizes;
@@ -58,7 +58,10 @@ enum { EBRL_DTYPE_FP32 = 0, EBRL_DTYPE_BF16 = 1 };
 typedef struct ebrl_config {
     int32_t dtype;            /* EBRL_DTYPE_FP32: all fp32; EBRL_DTYPE_BF16: bf16
                                  weights, KV and GEMM operands, fp32 accumulate,
-                                 softmax, residual stream, norms and logits */
+                                 softmax, residual stream, norms and logits;
+                                 EBRL_DTYPE_BF16_KV8: the same with the decoder's
+                                 KV cache in 8 bits (ebrl_kv8.h): half the bytes a
+                                 token, no bound of 4096 tokens on a sequence */
     /* vision: n_cams cameras of img x img x 3 float32 pixels, square patches */
     int32_t n_cams, img, patch;
     /* optional ViT encoder before the decoder (0 layers = patch embedding
@@ -73,7 +76,9 @@ typedef struct ebrl_config {
     /* capacity */
     int32_t max_envs;         /* env ids live in [0, max_envs); also max n per call */
     int32_t max_seq;          /* longest prefix T_e accepted by ebrl_prefill */
-    int64_t kv_budget_bytes;  /* KV pool size; 0 = enough for every env at max_seq */
+    int64_t kv_budget_bytes;  /* KV pool size; 0 = enough for every env at max_seq.  An env
+                                 holds the 16-token blocks of its prefix and tail and, in an
+                                 8-bit cache, one more where its prefix ends inside a block */
     double init_std;          /* weight init N(0, init_std^2); presets use 0.02 */
     /* world action model (Section 2.1): the expert also denoises frame_tokens
        latent future-frame tokens of frame_dim channels per env jointly with
@@ -214,7 +219,8 @@ const char* ebrl_last_error(const ebrl_policy* p);
 enum {
     EBRL_STATE_H_LAST_PRE = 0,  /* float32 [d]: env's last prefix row before the final norm */
     EBRL_STATE_H_LAST = 1,      /* float32 [d]: the same row after the final RMSNorm */
-    EBRL_STATE_K = 2,           /* KV dtype [T_e, kv_heads, head_dim]: layer's post-rotary keys */
+    EBRL_STATE_K = 2,           /* KV dtype [T_e, kv_heads, head_dim]: layer's post-rotary keys
+                                   (EBRL_DTYPE_BF16_KV8: the stored values, exact in bf16) */
     EBRL_STATE_V = 3,           /* KV dtype [T_e, kv_heads, head_dim]: layer's values */
     EBRL_STATE_FLOW_V0 = 4,     /* float32 [chunk, adim]: velocity at tau = 1 of the env's
                                    latest flow call */

@@ -53,7 +53,9 @@ struct EnvSlot { int T = 0; std::vector<int> blocks; uint32_t noise_calls = 0; }
 struct ebrl_policy {
     ebrl_config cfg{};
     bool bf16 = true;
+    bool kv8 = false;    // the decoder's KV cache is held in 8 bits
     size_t esz = 2;
+    size_t kv_esz = 2;   // bytes of a cached element
     uint64_t seed = 0;
     int device = 0;
     hipStream_t stream = nullptr;
@@ -86,6 +88,16 @@ struct ebrl_policy {
     std::vector<EnvSlot> envs;
     std::vector<int> bt_host;
     int* bt_dev = nullptr;
+    // 8-bit cache: kv_pool holds every layer's codes, kv8_scales their scales.
+    // The block table has a second row for each env, max_envs + 1 rows on:
+    // the one that decode and denoise calls use, in which the page that the
+    // prefix ends inside is the env's spare page.  A call copies that page
+    // there first, so that writing its own tokens, which may raise the page's
+    // scale, leaves the prefix as it was.
+    float* kv8_scales = nullptr;
+    void* kv8_ws = nullptr;
+    int64_t kv8_ws_bytes = 0;
+    void* QKV = nullptr;      // rows of the QKV projection
     // ViT KV scratch (identity block table)
     void* vit_kv = nullptr;
     int* vit_bt = nullptr;
@@ -320,6 +332,9 @@ struct Placement {
     }
 };
 
+// A stack whose attention reads the decoder's cache, held in 8 bits.
+bool on_kv8(const ebrl_policy* p, const StackDims* s) { return p->kv8 && s != &p->vit; }
+
 Placement placement(const ebrl_policy* p, uint32_t tid) {
     Placement pl;
     const ebrl_config& c = p->cfg;
@@ -352,11 +367,15 @@ Placement placement(const ebrl_policy* p, uint32_t tid) {
     if (l >= (int)layers->size()) return pl;
     const LayerW& w = (*layers)[l];
     const int qn = sd->hq * sd->hd, kn = sd->hkv * sd->hd, qkvn = qn + 2 * kn;
+    // the 8-bit cache's write turns plain heads, the QKV epilogue paired ones
+    const int heads = on_kv8(p, sd) ? 0 : 3;
     switch (slot) {
-    case SLOT_Q: plain(w.qkv, qn, sd->d, sd->d); pl.buf_rows = qkvn; pl.kind = 3; pl.hd = sd->hd; return pl;
-    case SLOT_K: plain(w.qkv, kn, sd->d, sd->d); pl.buf_rows = qkvn; pl.row_off = qn; pl.kind = 3; pl.hd = sd->hd; return pl;
+    case SLOT_Q: plain(w.qkv, qn, sd->d, sd->d); pl.buf_rows = qkvn; pl.kind = heads; pl.hd = sd->hd; return pl;
+    case SLOT_K:
+        plain(w.qkv, kn, sd->d, sd->d); pl.buf_rows = qkvn; pl.row_off = qn; pl.kind = heads; pl.hd = sd->hd;
+        return pl;
     case SLOT_V:
-        plain(w.qkv, kn, sd->d, sd->d); pl.buf_rows = qkvn; pl.row_off = qn + kn; pl.kind = 3; pl.hd = sd->hd;
+        plain(w.qkv, kn, sd->d, sd->d); pl.buf_rows = qkvn; pl.row_off = qn + kn; pl.kind = heads; pl.hd = sd->hd;
         return pl;
     case SLOT_O: plain(w.o, sd->d, qn, qn); return pl;
     case SLOT_GATE: plain(w.gu, sd->mlp, sd->d, sd->d); pl.buf_rows = 2 * sd->mlp; pl.kind = 1; return pl;
@@ -426,7 +445,8 @@ int fill_stack(ebrl_policy* p, uint32_t base, int n) {
 
 int validate(const ebrl_config& c, std::string& why) {
     auto bad = [&](const char* m) { why = m; return EBRL_E_INVALID; };
-    if (c.dtype != EBRL_DTYPE_FP32 && c.dtype != EBRL_DTYPE_BF16) return bad("dtype");
+    if (c.dtype != EBRL_DTYPE_FP32 && c.dtype != EBRL_DTYPE_BF16 && c.dtype != EBRL_DTYPE_BF16_KV8)
+        return bad("dtype");
     if (c.layers < 1 || c.d < 64 || c.d % 64) return bad("decoder width must be a positive multiple of 64");
     if (c.head_dim != 64 && c.head_dim != 128) return bad("head_dim must be 64 or 128");
     if (c.q_heads < 1 || c.kv_heads < 1 || c.q_heads % c.kv_heads) return bad("heads");
@@ -458,7 +478,8 @@ int validate(const ebrl_config& c, std::string& why) {
         const int blocks = (c.max_seq + tail + KV_BLOCK - 1) / KV_BLOCK;
         const int vit_blocks =
             c.n_cams ? (c.n_cams * (c.img / c.patch) * (c.img / c.patch) + KV_BLOCK - 1) / KV_BLOCK : 0;
-        if (c.dtype == EBRL_DTYPE_BF16 && std::max(blocks, vit_blocks) > ATTN_BT_MAX)
+        if ((c.dtype == EBRL_DTYPE_BF16 && blocks > ATTN_BT_MAX) ||
+            (c.dtype != EBRL_DTYPE_FP32 && vit_blocks > ATTN_BT_MAX))
             return bad("sequence too long for the bf16 attention kernels (4096 tokens per sequence)");
     }
     return EBRL_OK;
@@ -478,7 +499,7 @@ int run_gemm(ebrl_policy* p, GemmArgs a, bool split_ok = false) {
     ebrl::gemm(a, p->stream);
     const double flop = 2.0 * a.M * (double)a.N * a.K;
     const double outb = (a.epi == EPI_SWIGLU ? (double)a.M * a.N / 2 : (double)a.M * a.N) *
-                        (a.epi == EPI_SWIGLU || a.epi == EPI_QKV ? p->esz : 4);
+                        (a.epi == EPI_SWIGLU || a.epi == EPI_QKV || a.epi == EPI_ACT ? p->esz : 4);
     prof_end(p, flop, ((double)a.M * a.K + (double)a.N * a.K) * p->esz + outb);
     return EBRL_OK;
 }
@@ -496,6 +517,10 @@ struct BlockCall {
     double attn_flop = 0, attn_bytes = 0;  // algorithmic work of the attention launch
     AttnPrefillArgs pre;
     AttnDecodeArgs dec;
+    // on the 8-bit cache, in place of kv, row_dst, pre and dec
+    ebrl_kv8_cache cache8{};
+    ebrl_kv8_write_args write8{};
+    ebrl_kv8_attn_args attn8{};
 };
 
 // Pre-norms folded into the projection that follows them: the QKV and gate/up
@@ -506,7 +531,7 @@ struct BlockCall {
 bool fold_norm(const ebrl_policy* p, const StackDims& s, int rows, bool decode) {
     const int qkvn = (s.hq + 2 * s.hkv) * s.hd;
     if (!p->bf16) return true;
-    return decode && gemm_row_norm_ok(true, rows, qkvn, s.d, p->ws_floats) &&
+    return decode && !p->kv8 && gemm_row_norm_ok(true, rows, qkvn, s.d, p->ws_floats) &&
            gemm_row_norm_ok(true, rows, 2 * s.mlp, s.d, p->ws_floats);
 }
 
@@ -520,28 +545,44 @@ int run_block(ebrl_policy* p, BlockCall& b) {
         rmsnorm_rows(p->bf16, b.R, s.d, nullptr, p->Xn, s.d, b.rows, s.d, 1e-6f, p->stream);
         prof_end(p, 0, (double)b.rows * s.d * (4 + p->esz));
     }
-    // fused QKV projection: rotary embedding of Q and K and the paged K/V
-    // write happen in the GEMM epilogue
-    RopeKVArgs r;
-    r.q_heads = s.hq;
-    r.Q = p->Qb; r.ldq = qn; r.kv = b.kv; r.row_dst = b.row_dst;
-    r.cos_tab = p->cos_tab; r.sin_tab = p->sin_tab; r.use_rope = b.use_rope;
     GemmArgs g;
-    g.A = normed; g.lda = s.d; g.B = b.w->qkv; g.ldb = s.d; g.M = b.rows; g.N = qkvn; g.K = s.d;
-    g.epi = EPI_QKV; g.rope = &r; g.row_norm = fold;
-    run_gemm(p, g, b.decode);
-    if (b.decode) {
-        b.dec.bf16 = p->bf16; b.dec.Q = p->Qb; b.dec.ldq = qn; b.dec.O = p->Ob; b.dec.ldo = qn;
-        b.dec.q_heads = s.hq; b.dec.kv = b.kv; b.dec.part = p->part; b.dec.counters = p->attn_counters;
-        prof_begin(p, EBRL_K_ATTN_DECODE);
-        attn_decode(b.dec, p->stream);
+    if (on_kv8(p, b.sd)) {
+        // the projection's rows, then their rotary embedding and write into
+        // the cache, then attention over it
+        g.A = p->Xn; g.lda = s.d; g.B = b.w->qkv; g.ldb = s.d; g.M = b.rows; g.N = qkvn; g.K = s.d;
+        g.epi = EPI_ACT; g.C = p->QKV; g.ldc = qkvn;
+        run_gemm(p, g, b.decode);
+        prof_begin(p, EBRL_K_OTHER);
+        int rc = kv8_write(&b.cache8, &b.write8, p->stream);
+        prof_end(p, 0, (double)b.rows * ((qkvn + qn) * p->esz + 2.0 * s.hkv * s.hd));
+        if (rc) return fail(p, rc, "8-bit cache write");
+        prof_begin(p, b.decode ? EBRL_K_ATTN_DECODE : EBRL_K_ATTN_PREFILL);
+        rc = kv8_attn(&b.cache8, &b.attn8, p->cfg.max_envs, p->stream);
         prof_end(p, b.attn_flop, b.attn_bytes);
+        if (rc) return fail(p, rc, "8-bit cache attention");
     } else {
-        b.pre.bf16 = p->bf16; b.pre.Q = p->Qb; b.pre.ldq = qn; b.pre.O = p->Ob; b.pre.ldo = qn;
-        b.pre.q_heads = s.hq; b.pre.kv = b.kv;
-        prof_begin(p, EBRL_K_ATTN_PREFILL);
-        attn_prefill(b.pre, p->stream);
-        prof_end(p, b.attn_flop, b.attn_bytes);
+        // fused QKV projection: rotary embedding of Q and K and the paged K/V
+        // write happen in the GEMM epilogue
+        RopeKVArgs r;
+        r.q_heads = s.hq;
+        r.Q = p->Qb; r.ldq = qn; r.kv = b.kv; r.row_dst = b.row_dst;
+        r.cos_tab = p->cos_tab; r.sin_tab = p->sin_tab; r.use_rope = b.use_rope;
+        g.A = normed; g.lda = s.d; g.B = b.w->qkv; g.ldb = s.d; g.M = b.rows; g.N = qkvn; g.K = s.d;
+        g.epi = EPI_QKV; g.rope = &r; g.row_norm = fold;
+        run_gemm(p, g, b.decode);
+        if (b.decode) {
+            b.dec.bf16 = p->bf16; b.dec.Q = p->Qb; b.dec.ldq = qn; b.dec.O = p->Ob; b.dec.ldo = qn;
+            b.dec.q_heads = s.hq; b.dec.kv = b.kv; b.dec.part = p->part; b.dec.counters = p->attn_counters;
+            prof_begin(p, EBRL_K_ATTN_DECODE);
+            attn_decode(b.dec, p->stream);
+            prof_end(p, b.attn_flop, b.attn_bytes);
+        } else {
+            b.pre.bf16 = p->bf16; b.pre.Q = p->Qb; b.pre.ldq = qn; b.pre.O = p->Ob; b.pre.ldo = qn;
+            b.pre.q_heads = s.hq; b.pre.kv = b.kv;
+            prof_begin(p, EBRL_K_ATTN_PREFILL);
+            attn_prefill(b.pre, p->stream);
+            prof_end(p, b.attn_flop, b.attn_bytes);
+        }
     }
     g = GemmArgs();
     g.A = p->Ob; g.lda = qn; g.B = b.w->o; g.ldb = qn; g.M = b.rows; g.N = s.d; g.K = qn;
@@ -595,9 +636,63 @@ void add_row_dst(const ebrl_policy* p, std::vector<int>& dst, int env, int pos) 
     dst.push_back(p->bt_host[(size_t)env * p->bt_stride + pos / KV_BLOCK]);
 }
 
+// The 8-bit cache of a layer.
+ebrl_kv8_cache dec_kv8(const ebrl_policy* p, int layer) {
+    ebrl_kv8_cache k{};
+    k.codes = (char*)p->kv_pool + (size_t)layer * p->num_blocks * p->block_elems;
+    k.scales = p->kv8_scales + (size_t)layer * p->num_blocks * 2 * p->cfg.kv_heads;
+    k.block_table = p->bt_dev;
+    k.num_blocks = p->num_blocks;
+    k.table_rows = 2 * (p->cfg.max_envs + 1);
+    k.table_stride = p->bt_stride;
+    k.kv_heads = p->cfg.kv_heads;
+    k.head_dim = p->cfg.head_dim;
+    return k;
+}
+
+// What a call on the 8-bit cache gives every block: `rows` rows of n sequences
+// of at most max_len, whose first rows, cache positions, lengths and block-table
+// rows are on the device.  The attention's cut goes by the policy's capacity.
+struct Kv8Call {
+    int n = 0, rows = 0, max_len = 0, max_kv = 0;
+    bool causal = true;
+    const int *start = nullptr, *pos0 = nullptr, *kv_len = nullptr, *seq = nullptr;
+};
+void kv8_block(const ebrl_policy* p, BlockCall& b, int layer, const Kv8Call& r) {
+    const StackDims& s = *b.sd;
+    const int qn = s.hq * s.hd, kn = s.hkv * s.hd, qkvn = qn + 2 * kn;
+    b.cache8 = dec_kv8(p, layer);
+    ebrl_kv8_write_args& w = b.write8;
+    w.dtype = EBRL_DTYPE_BF16; w.n = r.n; w.rows = r.rows; w.max_len = r.max_len; w.q_heads = s.hq;
+    w.n_axes = 1; w.sections[0] = s.hd / 2; w.tab_rows = p->max_pos;
+    w.q = p->QKV; w.k = (const char*)p->QKV + (size_t)qn * p->esz; w.v = (const char*)p->QKV + (size_t)(qn + kn) * p->esz;
+    w.q_out = p->Qb; w.ldq = w.ldk = w.ldv = qkvn; w.ldq_out = qn;
+    w.row_start = r.start; w.pos0 = r.pos0; w.seq = r.seq; w.cos_tab = p->cos_tab; w.sin_tab = p->sin_tab;
+    ebrl_kv8_attn_args& a = b.attn8;
+    a.dtype = EBRL_DTYPE_BF16; a.n = r.n; a.rows = r.rows; a.max_q_len = r.max_len; a.max_kv_len = r.max_kv;
+    a.q_heads = s.hq; a.causal = r.causal; a.scale = 1.0f / sqrtf((float)s.hd);
+    a.q = p->Qb; a.out = p->Ob; a.ldq = a.ldo = qn; a.row_start = r.start; a.kv_len = r.kv_len; a.seq = r.seq;
+    a.workspace = p->kv8_ws; a.workspace_bytes = p->kv8_ws_bytes;
+}
+
+// Block-table row of an env in decode and denoise calls, and the page pair
+// that such a call copies first ({-1, -1}: the prefix ends with a page).
+int kv8_call_row(const ebrl_policy* p, int env) { return p->cfg.max_envs + 1 + env; }
+void add_spare(const ebrl_policy* p, std::vector<int>& pairs, int env) {
+    const int T = p->envs[env].T;
+    const bool inside = env != p->pad_env && T % KV_BLOCK;
+    pairs.push_back(inside ? p->bt_host[(size_t)env * p->bt_stride + T / KV_BLOCK] : -1);
+    pairs.push_back(inside ? p->bt_host[(size_t)kv8_call_row(p, env) * p->bt_stride + T / KV_BLOCK] : -1);
+}
+
+// Blocks that an env with a prefix of T tokens takes.
+int env_blocks(const ebrl_policy* p, int T) {
+    return (T + p->tail + KV_BLOCK - 1) / KV_BLOCK + (p->kv8 && T % KV_BLOCK ? 1 : 0);
+}
+
 PagedKV dec_kv(const ebrl_policy* p, int layer) {
     PagedKV k;
-    k.base = (char*)p->kv_pool + (size_t)layer * p->num_blocks * p->block_elems * p->esz;
+    k.base = (char*)p->kv_pool + (size_t)layer * p->num_blocks * p->block_elems * p->kv_esz;
     k.block_table = p->bt_dev;
     k.bt_stride = p->bt_stride;
     k.kv_heads = p->cfg.kv_heads;
@@ -657,7 +752,7 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
     const bool seeded = !anoise || (F && !fnoise);
     const int rows = n * S, arows = n * c.chunk, frows = n * F;
     std::vector<int> seq_env(env_ids, env_ids + n), q_off(n), q_len(n, S), q_pos0(n), kv_len(n),
-        row_dst, tseq, tq0, calls(n);
+        row_dst, tseq, tq0, calls(n), start, call_row, spare;
     row_dst.reserve((size_t)rows * 2);
     for (int i = 0; i < n; ++i) {
         const int T = p->envs[env_ids[i]].T;
@@ -667,11 +762,18 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
         kv_len[i] = T + S;
         for (int j = 0; j < S; ++j) add_row_dst(p, row_dst, env_ids[i], T + j);
         for (int q0 = 0; q0 < S; q0 += ATTN_Q_TILE) { tseq.push_back(i); tq0.push_back(q0); }
+        if (p->kv8) {
+            start.push_back(i * S);
+            call_row.push_back(kv8_call_row(p, env_ids[i]));
+            add_spare(p, spare, env_ids[i]);
+        }
     }
+    if (p->kv8) start.push_back(rows);
     Meta m;
     const size_t o_env = m.add(seq_env), o_off = m.add(q_off), o_len = m.add(q_len), o_pos0 = m.add(q_pos0),
                  o_kvl = m.add(kv_len), o_dst = m.add(row_dst), o_tseq = m.add(tseq),
-                 o_tq0 = m.add(tq0), o_calls = m.add(calls);
+                 o_tq0 = m.add(tq0), o_calls = m.add(calls), o_start = m.add(start), o_row = m.add(call_row),
+                 o_spare = m.add(spare);
     int* md = nullptr;
     if ((rc = upload_meta(p, m, false, &md))) return rc;
     // caller noise enters and the result leaves through the policy's own
@@ -681,6 +783,7 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
     if (F && fnoise) copy_f32(fnoise, p->flow_f, (size_t)frows * c.frame_dim, p->stream);
     prof_end(p, 0, 0);
     auto body = [&]() -> int {
+        if (p->kv8) kv8_copy_pages(dec_kv8(p, 0), c.layers, reinterpret_cast<const int2*>(md + o_spare), n, p->stream);
         // time-MLP outputs for the fixed tau schedule
         prof_begin(p, EBRL_K_OTHER);
         small_linear(p->bf16, p->temb, c.n_steps, c.exp_d, p->w_t1, c.exp_d, p->tmid, false, p->stream);
@@ -728,8 +831,10 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
                 b.attn_bytes = 2.0 * n * S * p->exp.hq * c.head_dim * p->esz;
                 for (int i = 0; i < n; ++i) {
                     b.attn_flop += 4.0 * c.head_dim * p->exp.hq * (double)S * kv_len[i];
-                    b.attn_bytes += 2.0 * kv_len[i] * p->exp.hkv * c.head_dim * p->esz;
+                    b.attn_bytes += 2.0 * kv_len[i] * p->exp.hkv * c.head_dim * p->kv_esz;
                 }
+                if (p->kv8)
+                    kv8_block(p, b, l, {n, rows, S, c.max_seq + S, false, md + o_start, md + o_pos0, md + o_kvl, md + o_row});
                 int rc2 = run_block(p, b);
                 if (rc2) return rc2;
             }
@@ -831,8 +936,10 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
     ebrl_policy* p = new ebrl_policy();
     p->cfg = *config;
     const ebrl_config& c = p->cfg;
-    p->bf16 = c.dtype == EBRL_DTYPE_BF16;
+    p->bf16 = c.dtype != EBRL_DTYPE_FP32;
+    p->kv8 = c.dtype == EBRL_DTYPE_BF16_KV8;
     p->esz = p->bf16 ? 2 : 4;
+    p->kv_esz = p->kv8 ? 1 : p->esz;
     p->seed = seed;
     if (hipGetDevice(&p->device) != hipSuccess) {
         delete p;
@@ -907,12 +1014,14 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
 
     // ---- paged KV pool
     p->block_elems = (size_t)2 * c.kv_heads * KV_BLOCK * c.head_dim;
-    const size_t block_bytes_all = p->block_elems * p->esz * c.layers;
+    const size_t scale_bytes = p->kv8 ? (size_t)2 * c.kv_heads * sizeof(float) : 0;   // of a block in one layer
+    const size_t block_bytes_all = (p->block_elems * p->kv_esz + scale_bytes) * c.layers;
+    const int env_most = p->bt_stride + (p->kv8 ? 1 : 0);
     int64_t budget = c.kv_budget_bytes;
-    if (budget <= 0) budget = (int64_t)block_bytes_all * p->bt_stride * c.max_envs;
+    if (budget <= 0) budget = (int64_t)block_bytes_all * env_most * c.max_envs;
     const int budget_blocks = (int)(budget / (int64_t)block_bytes_all);
-    if (budget_blocks < p->bt_stride) {
-        fail(p, EBRL_E_INVALID, "kv_budget_bytes holds %d blocks, one env needs %d", budget_blocks, p->bt_stride);
+    if (budget_blocks < env_most) {
+        fail(p, EBRL_E_INVALID, "kv_budget_bytes holds %d blocks, one env needs %d", budget_blocks, env_most);
         return bail(EBRL_E_INVALID);
     }
     // the padding env of decode size classes: a one-token prefix of zeros
@@ -920,21 +1029,28 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
     p->pad_env = c.max_envs;
     const int pad_blocks = (1 + p->tail + KV_BLOCK - 1) / KV_BLOCK;
     p->num_blocks = budget_blocks + pad_blocks;
-    if ((rc = dev_alloc(p, &p->kv_pool, (size_t)p->num_blocks * block_bytes_all))) return bail(rc);
+    const size_t pool_bytes = (size_t)p->num_blocks * p->block_elems * p->kv_esz * c.layers;
+    if ((rc = dev_alloc(p, &p->kv_pool, pool_bytes))) return bail(rc);
+    if (p->kv8) {
+        const size_t scales = (size_t)p->num_blocks * 2 * c.kv_heads * c.layers;
+        if ((rc = dev_alloc_t(p, &p->kv8_scales, scales))) return bail(rc);
+        HIPCHK(p, hipMemset(p->kv8_scales, 0, scales * sizeof(float)));
+    }
     p->free_blocks.resize(budget_blocks);
     for (int b = 0; b < budget_blocks; ++b) p->free_blocks[b] = budget_blocks - 1 - b;
     p->envs.assign(c.max_envs + 1, EnvSlot());
-    p->bt_host.assign((size_t)(c.max_envs + 1) * p->bt_stride, 0);
+    p->bt_host.assign((size_t)(p->kv8 ? 2 : 1) * (c.max_envs + 1) * p->bt_stride, 0);
     {
         EnvSlot& pad = p->envs[p->pad_env];
         pad.T = 1;
         for (int b = 0; b < pad_blocks; ++b) {
             pad.blocks.push_back(budget_blocks + b);
             p->bt_host[(size_t)p->pad_env * p->bt_stride + b] = budget_blocks + b;
+            if (p->kv8) p->bt_host[(size_t)kv8_call_row(p, p->pad_env) * p->bt_stride + b] = budget_blocks + b;
         }
         for (int l = 0; l < c.layers; ++l)
-            HIPCHK(p, hipMemset((char*)dec_kv(p, l).base + (size_t)budget_blocks * p->block_elems * p->esz, 0,
-                                (size_t)pad_blocks * p->block_elems * p->esz));
+            HIPCHK(p, hipMemset((char*)dec_kv(p, l).base + (size_t)budget_blocks * p->block_elems * p->kv_esz, 0,
+                                (size_t)pad_blocks * p->block_elems * p->kv_esz));
     }
     if ((rc = dev_alloc_t(p, &p->bt_dev, p->bt_host.size()))) return bail(rc);
     HIPCHK(p, hipMemcpy(p->bt_dev, p->bt_host.data(), p->bt_host.size() * sizeof(int), hipMemcpyHostToDevice));
@@ -993,6 +1109,7 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
     if ((rc = dev_alloc(p, &p->Xn, R * w_d * p->esz))) return bail(rc);
     if ((rc = dev_alloc(p, &p->Qb, R * w_q * p->esz))) return bail(rc);
     if ((rc = dev_alloc(p, &p->Ob, R * w_q * p->esz))) return bail(rc);
+    if (p->kv8 && (rc = dev_alloc(p, &p->QKV, R * w_qkv * p->esz))) return bail(rc);
     if ((rc = dev_alloc(p, &p->Hb, R * w_mlp * p->esz))) return bail(rc);
     if (c.n_cams && (rc = dev_alloc(p, &p->patches, (size_t)c.max_envs * p->patches_per_env * p->kpad * p->esz)))
         return bail(rc);
@@ -1033,6 +1150,19 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
         if ((rc = dev_alloc_t(p, &p->attn_counters, words))) return bail(rc);
         HIPCHK(p, hipMemset(p->attn_counters, 0, words * 4));
     }
+    if (p->kv8) {
+        // the largest workspace of prefill, decode and denoise calls
+        auto need = [&](const StackDims& s, int n, int max_q, int max_kv) {
+            BlockCall b;
+            b.sd = &s;
+            kv8_block(p, b, 0, {n, n * max_q, max_q, max_kv});
+            p->kv8_ws_bytes = std::max(p->kv8_ws_bytes, kv8_attn_workspace(&b.cache8, &b.attn8, c.max_envs));
+        };
+        need(p->dec, c.max_envs, c.max_seq, c.max_seq);
+        if (c.action_logits) need(p->dec, p->dec_cap, 1, c.max_seq + p->tail);
+        if (c.exp_layers) need(p->exp, c.max_envs, c.chunk + c.frame_tokens, c.max_seq + c.chunk + c.frame_tokens);
+        if ((rc = dev_alloc(p, &p->kv8_ws, (size_t)p->kv8_ws_bytes))) return bail(rc);
+    }
     if (c.exp_layers) {
         const size_t act_rows = (size_t)c.max_envs * c.chunk;
         if ((rc = dev_alloc_t(p, &p->flow_x, act_rows * c.adim))) return bail(rc);
@@ -1048,7 +1178,10 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
                   (size_t)c.max_envs * c.max_seq / 8 + 4096;
     if (c.action_logits)
         p->meta_cap = std::max(p->meta_cap, (size_t)std::min(p->dec_cap, DECODE_MAX_ROWS) *
-                                                    (1 + 3 * (size_t)std::max(c.n_action_tokens - 1, 1)) + 16);
+                                                    (1 + 3 * (size_t)std::max(c.n_action_tokens - 1, 1)) + 16 +
+                                                (p->kv8 ? (size_t)std::min(p->dec_cap, DECODE_MAX_ROWS) *
+                                                                  (4 + (size_t)std::max(c.n_action_tokens - 1, 1)) + 32
+                                                        : 0));
     if ((rc = dev_alloc_t(p, &p->meta_dev, p->meta_cap))) return bail(rc);
     {
         void* hp = nullptr;
@@ -1145,7 +1278,7 @@ int ebrl_prefill(ebrl_policy* p, const ebrl_obs_batch* obs, const int32_t* env_i
     // changes, so a call that fails leaves every existing cache intact
     size_t need = 0, held = 0;
     for (int i = 0; i < n; ++i) {
-        need += (size_t)(T[i] + p->tail + KV_BLOCK - 1) / KV_BLOCK;
+        need += (size_t)env_blocks(p, T[i]);
         held += p->envs[env_ids[i]].blocks.size();
     }
     if (need > p->free_blocks.size() + held)
@@ -1159,12 +1292,17 @@ int ebrl_prefill(ebrl_policy* p, const ebrl_obs_batch* obs, const int32_t* env_i
     for (int i = 0; i < n; ++i) {
         EnvSlot& s = p->envs[env_ids[i]];
         const int nb = (T[i] + p->tail + KV_BLOCK - 1) / KV_BLOCK;
-        for (int b = 0; b < nb; ++b) {
+        for (int b = 0; b < env_blocks(p, T[i]); ++b) {
             s.blocks.push_back(p->free_blocks.back());
             p->free_blocks.pop_back();
         }
         int* row = &p->bt_host[(size_t)env_ids[i] * p->bt_stride];
         for (int b = 0; b < p->bt_stride; ++b) row[b] = b < nb ? s.blocks[b] : 0;
+        if (p->kv8) {
+            int* call = &p->bt_host[(size_t)kv8_call_row(p, env_ids[i]) * p->bt_stride];
+            std::copy(row, row + p->bt_stride, call);
+            if (T[i] % KV_BLOCK) call[T[i] / KV_BLOCK] = s.blocks[nb];
+        }
         s.T = T[i];
     }
     // ---- metadata
@@ -1272,7 +1410,9 @@ int ebrl_prefill(ebrl_policy* p, const ebrl_obs_batch* obs, const int32_t* env_i
         b.pre.n_tiles = (int)tiles.size(); b.pre.causal = true; b.pre.max_kv_len = maxT;
         b.attn_flop = 4.0 * c.head_dim * c.q_heads * causal_pairs;
         // Q read and O written once, every K/V row read once
-        b.attn_bytes = 2.0 * kv_rows * (double)(c.q_heads + c.kv_heads) * c.head_dim * p->esz;
+        b.attn_bytes = 2.0 * kv_rows * (double)(c.q_heads * p->esz + c.kv_heads * p->kv_esz) * c.head_dim;
+        if (p->kv8)
+            kv8_block(p, b, l, {n, M, c.max_seq, c.max_seq, true, md + o_off, md + o_pos0, md + o_len, md + o_env});
         if ((rc = run_block(p, b))) return rc;
     }
     prof_begin(p, EBRL_K_OTHER);
@@ -1311,7 +1451,7 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
     const int nc = n <= 4 ? n : std::min(p->dec_cap, (n + 7) / 8 * 8);
     std::vector<int> seq_env(nc, p->pad_env);
     std::copy(env_ids, env_ids + n, seq_env.begin());
-    std::vector<int> kvlen((size_t)std::max(steps, 1) * nc), row_dst;
+    std::vector<int> kvlen((size_t)std::max(steps, 1) * nc), row_dst, start, pos0, call_row, spare;
     row_dst.reserve((size_t)std::max(steps, 1) * nc * 2);
     for (int k = 1; k <= steps; ++k)
         for (int i = 0; i < nc; ++i) {
@@ -1319,8 +1459,18 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
             kvlen[(size_t)(k - 1) * nc + i] = T + k;
             add_row_dst(p, row_dst, seq_env[i], T + k - 1);
         }
+    if (p->kv8) {
+        start.resize(nc + 1);
+        std::iota(start.begin(), start.end(), 0);
+        for (int len : kvlen) pos0.push_back(len - 1);
+        for (int e : seq_env) {
+            call_row.push_back(kv8_call_row(p, e));
+            add_spare(p, spare, e);
+        }
+    }
     Meta m;
-    const size_t o_env = m.add(seq_env), o_kvl = m.add(kvlen), o_dst = m.add(row_dst);
+    const size_t o_env = m.add(seq_env), o_kvl = m.add(kvlen), o_dst = m.add(row_dst), o_start = m.add(start),
+                 o_pos0 = m.add(pos0), o_row = m.add(call_row), o_spare = m.add(spare);
     int* md = nullptr;
     if ((rc = upload_meta(p, m, false, &md))) return rc;
     // split count of the fp32 attention path: the policy's longest sequence
@@ -1328,6 +1478,8 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
 
     const bool fold = fold_norm(p, p->dec, nc, true);
     auto body = [&]() -> int {
+        if (p->kv8 && steps > 0)
+            kv8_copy_pages(dec_kv8(p, 0), c.layers, reinterpret_cast<const int2*>(md + o_spare), nc, p->stream);
         LogitsArgs la;
         la.bf16 = p->bf16; la.W = p->w_act; la.d = c.d; la.n_bins = c.n_bins; la.n = nc;
         la.tokens = p->dec_tok; la.actions = p->dec_act; la.margins = p->dec_mar; la.ntok = ntok;
@@ -1342,7 +1494,7 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
         for (int k = 1; k <= steps; ++k) {
             double kv_bytes = 0;
             for (int i = 0; i < nc; ++i) kv_bytes += (double)(p->envs[seq_env[i]].T + k);
-            kv_bytes *= 2.0 * c.kv_heads * c.head_dim * p->esz;
+            kv_bytes *= 2.0 * c.kv_heads * c.head_dim * p->kv_esz;
             for (int l = 0; l < c.layers; ++l) {
                 BlockCall b;
                 b.R = p->X; b.rows = nc; b.sd = &p->dec; b.w = &p->L_dec[l]; b.kv = dec_kv(p, l);
@@ -1351,7 +1503,12 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
                 b.dec.seq_env = md + o_env; b.dec.kv_len = md + o_kvl + (size_t)(k - 1) * nc; b.dec.n = nc;
                 b.dec.max_splits = max_splits;
                 b.attn_bytes = kv_bytes;
-                b.attn_flop = kv_bytes / p->esz / (2.0 * c.kv_heads * c.head_dim) * 4.0 * c.q_heads * c.head_dim;
+                b.attn_flop = kv_bytes / p->kv_esz / (2.0 * c.kv_heads * c.head_dim) * 4.0 * c.q_heads * c.head_dim;
+                if (p->kv8) {
+                    const size_t at = (size_t)(k - 1) * nc;
+                    kv8_block(p, b, l, {nc, nc, 1, c.max_seq + p->tail, true, md + o_start, md + o_pos0 + at,
+                                        md + o_kvl + at, md + o_row});
+                }
                 int rc2 = run_block(p, b);
                 if (rc2) return rc2;
             }
@@ -1419,6 +1576,33 @@ int ebrl_read_state(ebrl_policy* p, int32_t what, int32_t env_id, int32_t layer,
         if (s.T <= 0) return fail(p, EBRL_E_STATE, "env %d has no prefix", env_id);
         const size_t row = (size_t)c.kv_heads * c.head_dim * p->esz;
         if (bytes < (int64_t)(row * s.T)) return fail(p, EBRL_E_INVALID, "need %zu bytes", row * s.T);
+        if (p->kv8) {
+            const ebrl_kv8_cache k8 = dec_kv8(p, layer);
+            const size_t gb = (size_t)KV_BLOCK * c.head_dim;
+            std::vector<uint8_t> codes(p->block_elems);
+            std::vector<float> scales(2 * c.kv_heads), x(c.head_dim);
+            for (int t = 0; t < s.T; ++t) {
+                const size_t blk = (size_t)s.blocks[t / KV_BLOCK];
+                if (t % KV_BLOCK == 0) {
+                    HIPCHK(p, hipMemcpy(codes.data(), (char*)k8.codes + blk * p->block_elems, codes.size(),
+                                        hipMemcpyDeviceToHost));
+                    HIPCHK(p, hipMemcpy(scales.data(), k8.scales + blk * scales.size(), scales.size() * sizeof(float),
+                                        hipMemcpyDeviceToHost));
+                }
+                for (int h = 0; h < c.kv_heads; ++h) {
+                    const bool value = what == EBRL_STATE_V;
+                    const size_t grp = (value ? c.kv_heads : 0) + h;
+                    kv8_group_values(codes.data() + grp * gb, scales[grp], value, c.head_dim, t % KV_BLOCK, x.data());
+                    uint16_t* o = (uint16_t*)out + (size_t)t * c.kv_heads * c.head_dim + (size_t)h * c.head_dim;
+                    for (int d = 0; d < c.head_dim; ++d) {   // four significant bits: bf16 holds them
+                        uint32_t u;
+                        memcpy(&u, &x[d], 4);
+                        o[d] = (uint16_t)(u >> 16);
+                    }
+                }
+            }
+            return EBRL_OK;
+        }
         const size_t head_stride = (size_t)KV_BLOCK * c.head_dim * p->esz;
         const char* base = (const char*)dec_kv(p, layer).base;
         for (int b = 0; b * KV_BLOCK < s.T; ++b) {

@@ -5,6 +5,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/ebrl_kv8.h"
 #include "common.h"
 
 namespace ebrl {
@@ -124,6 +125,19 @@ struct AttnDecodeArgs {
     unsigned* counters = nullptr;
 };
 void attn_decode(const AttnDecodeArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------- 8-bit KV cache --
+// The calls of include/ebrl_kv8.h, with their statuses.  plan_n: sequences
+// that the cut into workgroups is made for (the entry points': the call's);
+// the workspace that kv8_attn needs goes by it.
+int kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, hipStream_t s);
+int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n);
+int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n, hipStream_t s);
+// Copies page pairs[i].x to pairs[i].y (device; negative: none) in each of
+// `layers` caches that lie one after the other, `c` the first.
+void kv8_copy_pages(const ebrl_kv8_cache& c, int layers, const int2* pairs, int n, hipStream_t s);
+// Host: the head_dim values of one slot of a (page, K or V, head) group.
+void kv8_group_values(const uint8_t* codes, float scale, bool value, int head_dim, int slot, float* out);
 
 // ----------------------------------------------------------------- misc --
 // Y[row] = rmsnorm(X[src_row]) ; src_row = rows ? rows[i] : i

@@ -1150,9 +1150,11 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
 
 // ------------------------------------------------------- plans, launches --
 
-static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a) {
+// `n`: the sequences that the cut is made for (a policy's calls take its
+// largest batch, so that a sequence's bits do not depend on the call's).
+static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a, int n) {
     Kv8Plan p;
-    const int64_t rows = (int64_t)a.max_q_len * (a.q_heads / c.kv_heads), pairs = (int64_t)a.n * c.kv_heads;
+    const int64_t rows = (int64_t)a.max_q_len * (a.q_heads / c.kv_heads), pairs = (int64_t)n * c.kv_heads;
     auto groups = [&](int tile_rows) { return pairs * ((rows + tile_rows - 1) / tile_rows); };
     if (rows <= 16) {
         // A wave of its own for each (sequence, KV head) saves the joining of
@@ -1241,13 +1243,7 @@ static void kv8_attn_launch(const Kv8Plan& p, const Kv8AttnKernelArgs& w, int64_
         hipLaunchKernelGGL((kv8_join_kernel<T, HD>), dim3((unsigned)(units * ((w.join_rows + 3) / 4))), wg, 0, s, w);
 }
 
-}  // namespace ebrl
-
-using namespace ebrl;
-
-extern "C" {
-
-int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, void* stream) {
+int kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, hipStream_t s) {
     if (!kv8_cache_ok(cache) || !args) return EBRL_E_INVALID;
     const ebrl_kv8_write_args& a = *args;
     const int hd = cache->head_dim, hkv = cache->kv_heads;
@@ -1287,7 +1283,6 @@ int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* ar
     w.v_units = (hkv + w.per_wave - 1) / w.per_wave;
     const int64_t groups = (sp * (w.rot_units + w.v_units) + 3) / 4;
     if (groups > KV8_MAX_GROUPS) return EBRL_E_INVALID;
-    hipStream_t s = (hipStream_t)stream;
     if (esz == 2) {
         if (hd == 64) kv8_write_launch<bf16_t, 64>(token, w, (unsigned)groups, s);
         else kv8_write_launch<bf16_t, 128>(token, w, (unsigned)groups, s);
@@ -1298,16 +1293,16 @@ int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* ar
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
 }
 
-int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args) {
+int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n) {
     if (!kv8_attn_shape_ok(cache, args)) return EBRL_E_INVALID;
     if (args->n == 0 || args->max_q_len == 0) return 0;
-    const Kv8Plan p = kv8_plan(*cache, *args);
+    const Kv8Plan p = kv8_plan(*cache, *args, plan_n);
     if (p.parts == 1) return 0;
     const int64_t units = (int64_t)args->n * cache->kv_heads * p.tiles;
     return units * p.parts * p.tile_rows * (cache->head_dim + 2) * 4;
 }
 
-int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, void* stream) {
+int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n, hipStream_t s) {
     if (!kv8_attn_shape_ok(cache, args) || !(args->scale > 0.f) || !isfinite(args->scale)) return EBRL_E_INVALID;
     const ebrl_kv8_attn_args& a = *args;
     if (a.n == 0 || a.rows == 0 || a.max_q_len == 0) return EBRL_OK;
@@ -1316,9 +1311,9 @@ int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args
     if (!kv8_pointers_ok(cache) || !a.row_start || !a.kv_len || !kv8_rows_ok(a.q, a.ldq, width, esz) ||
         !kv8_rows_ok(a.out, a.ldo, width, esz) || a.q == a.out)
         return EBRL_E_INVALID;
-    const int64_t need = ebrl_op_kv8_attn_workspace(cache, args);
+    const int64_t need = kv8_attn_workspace(cache, args, plan_n);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;
-    const Kv8Plan p = kv8_plan(*cache, a);
+    const Kv8Plan p = kv8_plan(*cache, a, plan_n);
     const int64_t units = (int64_t)a.n * cache->kv_heads * p.tiles;
     if (units * std::max(p.parts, (p.tile_rows + 3) / 4) > KV8_MAX_GROUPS) return EBRL_E_INVALID;
     Kv8AttnKernelArgs w;
@@ -1333,7 +1328,6 @@ int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args
     w.scale_log2 = a.scale * 1.4426950408889634f;
     w.part_o = (float*)a.workspace;
     w.part_ml = need ? w.part_o + units * p.parts * p.tile_rows * hd : nullptr;
-    hipStream_t s = (hipStream_t)stream;
     if (esz == 2) {
         if (hd == 64) kv8_attn_launch<bf16_t, 64>(p, w, units, s);
         else kv8_attn_launch<bf16_t, 128>(p, w, units, s);
@@ -1342,6 +1336,57 @@ int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args
         else kv8_attn_launch<float, 128>(p, w, units, s);
     }
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
+}
+
+// Pages of one layer after another: the codes and scales of page pairs[i].x
+// go to page pairs[i].y (negative: nothing is copied).
+__global__ __launch_bounds__(256) void kv8_copy_kernel(uint8_t* codes, float* scales, int num_blocks, int groups,
+                                                       int group_bytes, const int2* pairs)
+{
+    const int2 p = pairs[blockIdx.x];
+    if (p.x < 0 || p.y < 0 || p.x >= num_blocks || p.y >= num_blocks) return;
+    const size_t layer = (size_t)blockIdx.y * num_blocks;
+    const size_t bytes = (size_t)groups * group_bytes;
+    const uint4* src = reinterpret_cast<const uint4*>(codes + (layer + p.x) * bytes);
+    uint4* dst = reinterpret_cast<uint4*>(codes + (layer + p.y) * bytes);
+    for (size_t i = threadIdx.x; i < bytes / 16; i += 256) dst[i] = src[i];
+    for (int i = threadIdx.x; i < groups; i += 256)
+        scales[(layer + p.y) * groups + i] = scales[(layer + p.x) * groups + i];
+}
+void kv8_copy_pages(const ebrl_kv8_cache& c, int layers, const int2* pairs, int n, hipStream_t s) {
+    if (n <= 0) return;
+    hipLaunchKernelGGL(kv8_copy_kernel, dim3(n, layers), dim3(256), 0, s, (uint8_t*)c.codes, c.scales, c.num_blocks,
+                       2 * c.kv_heads, KV8_PAGE * c.head_dim, pairs);
+}
+
+// Value of an e4m3 code, on the host.
+static float kv8_code_value(unsigned c) {
+    const int e = c >> 3 & 15, m = c & 7;
+    const float v = e == 15 && m == 7 ? NAN : e ? ldexpf(1.f + m / 8.f, e - 7) : ldexpf(m / 8.f, -6);
+    return c & 128 ? -v : v;
+}
+void kv8_group_values(const uint8_t* codes, float scale, bool value, int head_dim, int slot, float* out) {
+    for (int d = 0; d < head_dim; ++d) {
+        const int at = 1024 * (d / 64) + (value ? 256 * (slot / 4) + 16 * (d % 64 / 4) + 4 * (d % 4) + slot % 4
+                                                : 64 * slot + d % 64);
+        out[d] = kv8_code_value(codes[at]) * scale;
+    }
+}
+
+}  // namespace ebrl
+
+extern "C" {
+
+int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, void* stream) {
+    return ebrl::kv8_write(cache, args, (hipStream_t)stream);
+}
+
+int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args) {
+    return args ? ebrl::kv8_attn_workspace(cache, args, args->n) : EBRL_E_INVALID;
+}
+
+int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, void* stream) {
+    return args ? ebrl::kv8_attn(cache, args, args->n, (hipStream_t)stream) : EBRL_E_INVALID;
 }
 
 }  // extern "C"

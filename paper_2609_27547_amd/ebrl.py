@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libebrl.so")
 EBRL_OK = 0
 ERRORS = {-1: "EBRL_E_INVALID", -2: "EBRL_E_OOM", -3: "EBRL_E_HIP", -4: "EBRL_E_STATE",
           -5: "EBRL_E_UNSUPPORTED"}
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_BF16_KV8 = 0, 1, 2
 STATE_H_LAST_PRE, STATE_H_LAST, STATE_K, STATE_V, STATE_FLOW_V0, STATE_PREFIX_LEN, STATE_GRAPHS = range(7)
 K_GEMM, K_GEMM_SKINNY, K_ATTN_PREFILL, K_ATTN_DECODE, K_OTHER = range(5)
 KERNEL_CLASSES = {K_GEMM: "gemm", K_GEMM_SKINNY: "gemm_skinny", K_ATTN_PREFILL: "attn_prefill",
@@ -462,7 +462,9 @@ def _kv8_call(fn, name, cache, args, dev, stream):
         with torch.cuda.device(dev):
             return _kv8_call(fn, name, cache, args, dev, stream)
     if stream is None:
-        stream = torch.cuda.current_stream().cuda_stream
+        # the handle alone: a torch.cuda.Stream object takes 2.7 us to make,
+        # as long as the launch
+        stream = torch._C._cuda_getCurrentRawStream(dev)
     rc = fn(ctypes.byref(cache), ctypes.byref(args), stream)
     if rc != EBRL_OK:
         raise EbrlError(rc, name)
@@ -599,7 +601,7 @@ class Policy:
 
     @property
     def bf16(self) -> bool:
-        return self.cfg.dtype == DTYPE_BF16
+        return self.cfg.dtype != DTYPE_FP32
 
     # calls -----------------------------------------------------------------
     def prefill(self, env_ids, images=None, lang_ids=None, lang_len=None) -> None:

@@ -1,0 +1,232 @@
+"""Policies whose KV cache is held in 8 bits (EBRL_DTYPE_BF16_KV8): against
+the oracle with its K and V rounded as the cache rounds them, and the
+properties that a policy's calls keep.
+
+The bound on a result is that of bf16 policies (tests/parity.py) plus the
+effect that the rounding of K and V has on it in the oracle: the library's K
+and V carry bf16 error before they are rounded, which takes some of them to
+the neighbouring code, so its result lies between none and all of that effect
+away from the rounded oracle's."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+from oracle import model as M
+from tests import kv8_ref as R
+from tests import parity as P
+from tests.test_gpu_parity import TINY_FLOW, TINY_LANG, TINY_VIT, TINY_WAM, _dev, _ebrl_config, _obs
+
+import synth_inputs
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2609_27547_amd import ebrl as E  # noqa: E402
+
+AR = M.Config("kv8ar", bf16=True, n_cams=1, img=64, patch=16, layers=3, d=256, q_heads=6, kv_heads=2, head_dim=128,
+              mlp=512, vocab=200, n_lang=40)
+
+
+def four_bits(x):
+    """e4m3 keeps four significant bits; a page's scale keeps its range."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.round(m * 16) / 16, e)
+
+
+class Rounded(M.Policy):
+    """The oracle with the decoder's (and the expert's) K and V rounded."""
+
+    def block(self, *a, **kw):
+        self._vit = not kw.get("use_rope", True)
+        return super().block(*a, **kw)
+
+    def _r(self, a, point):
+        return four_bits(a) if point == "kv" and not self._vit else a
+
+
+def _policy(o, max_envs, seed=0, **kw):
+    c = _ebrl_config(o, max_envs)
+    c.dtype = E.DTYPE_BF16_KV8
+    return E.Policy(c, seed=seed, **kw)
+
+
+def _rel(a, b):
+    return P.row_rel_err(a, b)
+
+
+@pytest.mark.parametrize("o", [AR, dataclasses.replace(AR, head_dim=64, q_heads=4, kv_heads=4), TINY_VIT],
+                         ids=["grouped", "hd64", "vit"])
+def test_ar_policy_matches_rounded_oracle(o):
+    ids = [2, 0, 4]
+    img, lang = _obs(o, ids, 1001)
+    # prefixes that end inside a page and with one
+    lens = [o.n_lang, max(1, o.n_lang - 8), (-o.n_img_tokens) % 16 or 16]
+    lens = [min(x, o.n_lang) for x in lens]
+    pol = _policy(o, 5)
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang), lang_len=lens)
+    tok, act, _ = pol.decode_actions(ids)
+    torch.cuda.synchronize()
+    tok = tok.cpu().numpy()
+    exact, ref = M.Policy(o, seed=0), Rounded(o, seed=0)
+    for i, e in enumerate(ids):
+        st, se = ref.prefill(img[i], lang[i, :lens[i]]), exact.prefill(img[i], lang[i, :lens[i]])
+        h = pol.read_state(E.STATE_H_LAST_PRE, e)
+        tol = P.TOL_BF16 + _rel(st.h_last_pre, se.h_last_pre)
+        print(f"env {e}: hidden {_rel(h, st.h_last_pre):.2e} (bound {tol:.2e})")
+        assert _rel(h, st.h_last_pre) < tol
+        for what, r in ((E.STATE_K, se.k), (E.STATE_V, se.v)):
+            raw = pol.read_state(what, e, 0)
+            assert not (raw & 0x000F).any()            # four significant bits at most
+            assert _rel(P.bf16_to_f64(raw), r[0]) < 2.0 ** -4 + P.TOL_BF16
+        r, x = ref.decode(st, forced=tok[i, :-1]), exact.decode(se, forced=tok[i, :-1])
+        for k, t in enumerate(tok[i]):
+            lg = r.logits[k]
+            bound = np.sqrt(2.0) * (P.TOL_BF16 + _rel(lg, x.logits[k])) * np.linalg.norm(lg)
+            assert lg[t] >= lg.max() - bound, (e, k)
+    assert np.allclose(act.cpu().numpy(), M.detokenize(tok), atol=1e-6)
+    pol.close()
+
+
+@pytest.mark.parametrize("o", [TINY_FLOW, TINY_WAM], ids=["flow", "wam"])
+@pytest.mark.parametrize("n_lang", [6, 12])             # prefixes of 10 and of 16 tokens
+def test_denoising_matches_rounded_oracle(o, n_lang):
+    o = dataclasses.replace(o, n_lang=n_lang)
+    ids = [0, 2, 3]
+    img, lang = _obs(o, ids, 1004)
+    na = synth_inputs.flow_noise(4, ids, o.chunk, o.adim)
+    nf = synth_inputs.flow_noise(5, ids, o.frame_tokens, o.frame_dim) if o.frame_tokens else None
+    pol = _policy(o, 4)
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang))
+    got = pol.wam_denoise(ids, _dev(nf), _dev(na)) if o.frame_tokens else (pol.flow_denoise(ids, _dev(na)),)
+    torch.cuda.synchronize()
+    exact, ref = M.Policy(o, seed=0), Rounded(o, seed=0)
+    for i, e in enumerate(ids):
+        def run(m):
+            st = m.prefill(img[i], lang[i])
+            return m.wam_denoise(st, nf[i], na[i]) if o.frame_tokens else (m.flow_denoise(st, na[i]),)
+        for g, want, plain in zip(got, run(ref), run(exact)):
+            assert _rel(g[i].cpu().numpy(), want) < P.TOL_BF16 + _rel(want, plain)
+    again = pol.wam_denoise(ids, _dev(nf), _dev(na)) if o.frame_tokens else (pol.flow_denoise(ids, _dev(na)),)
+    alone = pol.wam_denoise([2], _dev(nf[1:2]), _dev(na[1:2])) if o.frame_tokens else \
+        (pol.flow_denoise([2], _dev(na[1:2])),)
+    torch.cuda.synchronize()
+    for g, a, b in zip(got, again, alone):
+        assert torch.equal(g, a) and torch.equal(g[1:2], b)
+    pol.close()
+
+
+def test_decode_leaves_the_prefix_and_does_not_depend_on_the_batch():
+    """Calls again, in other groups, give the same bits, and K, V of the
+    prefix stay as prefill left them though the action tokens' share a page."""
+    o = dataclasses.replace(AR, n_lang=33)
+    ids = list(range(13))
+    img, lang = _obs(o, ids, 1002)
+    lens = [1 + (7 * e) % 33 for e in ids]
+    pol = _policy(o, 13)
+    # action-token embeddings a thousand times the others: their K and V raise the page's scale
+    tid, shape = M.tensor_shapes(o)["E_act"]
+    w = P.bf16_to_f64(pol.read_weight(tid, shape)).astype(np.float32)
+    w[:, :8] *= 1000
+    pol.write_weight(tid, (w.view(np.uint32) >> 16).astype(np.uint16))
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang), lang_len=lens)
+    before = [(pol.read_state(E.STATE_K, e, 1), pol.read_state(E.STATE_V, e, 1)) for e in ids]
+    first = pol.decode_actions(ids)
+    for group in ([5], [3, 12, 0, 7, 9], ids[::-1], [1, 2]):
+        got = pol.decode_actions(group)
+        torch.cuda.synchronize()
+        for a, b in zip(first, got):
+            assert torch.equal(a[group], b)
+    for e in ids:
+        assert np.array_equal(before[e][0], pol.read_state(E.STATE_K, e, 1))
+        assert np.array_equal(before[e][1], pol.read_state(E.STATE_V, e, 1))
+    # prefill alone, and again over an older prefix
+    for e in (4, 11):
+        pol.prefill([e], images=_dev(img[e:e + 1]), lang_ids=_dev(lang[e:e + 1]), lang_len=[lens[e]])
+        assert np.array_equal(before[e][0], pol.read_state(E.STATE_K, e, 1))
+        got = pol.decode_actions([e])
+        torch.cuda.synchronize()
+        for a, b in zip(first, got):
+            assert torch.equal(a[e:e + 1], b)
+    pol.close()
+
+
+def test_budget_holds_nearly_twice_the_environments():
+    o = dataclasses.replace(TINY_LANG, layers=1)
+    fits = {}
+    for dtype in (E.DTYPE_BF16, E.DTYPE_BF16_KV8):
+        c = _ebrl_config(o, 40)
+        c.dtype = dtype
+        c.kv_budget_bytes = 10 * 9 * 2 * 2 * 16 * 64 * 2     # ten environments of nine bf16 blocks
+        pol = E.Policy(c)
+        n = 0
+        lang = _dev(synth_inputs.lang_ids(1, list(range(40)), o.n_lang, o.vocab))
+        while n < 40:
+            try:
+                pol.prefill([n], lang_ids=lang[n:n + 1])
+            except E.EbrlError as ex:
+                assert ex.code == -2
+                break
+            n += 1
+        fits[dtype] = n
+        pol.close()
+    # 130 + 6 tokens: nine blocks, and the 8-bit cache's spare one
+    assert fits[E.DTYPE_BF16] == 10
+    assert fits[E.DTYPE_BF16_KV8] == int(10 * 9 * 4096 * 2 / (10 * (4096 + 16)))
+
+
+def test_prefix_longer_than_the_bf16_kernels_take():
+    o = M.Config("kv8long", bf16=True, n_cams=0, img=32, patch=16, layers=1, d=64, q_heads=2, kv_heads=1, head_dim=64,
+                 mlp=64, vocab=64, n_lang=4503)
+    with pytest.raises(E.EbrlError):
+        E.Policy(_ebrl_config(o, 1))
+    pol = _policy(o, 1)
+    lang = synth_inputs.lang_ids(3, [0], o.n_lang, o.vocab)
+    pol.prefill([0], lang_ids=_dev(lang))
+    tok, _, _ = pol.decode_actions([0])
+    torch.cuda.synchronize()
+    exact, ref = M.Policy(o, seed=0), Rounded(o, seed=0)
+    st, se = ref.prefill(None, lang[0]), exact.prefill(None, lang[0])
+    assert _rel(pol.read_state(E.STATE_H_LAST_PRE, 0), st.h_last_pre) < P.TOL_BF16 + _rel(st.h_last_pre, se.h_last_pre)
+    r = ref.decode(st, forced=tok[0, :-1].cpu().numpy())
+    x = exact.decode(se, forced=tok[0, :-1].cpu().numpy())
+    for k, t in enumerate(tok[0].cpu().numpy()):
+        bound = np.sqrt(2.0) * (P.TOL_BF16 + _rel(r.logits[k], x.logits[k])) * np.linalg.norm(r.logits[k])
+        assert r.logits[k][t] >= r.logits[k].max() - bound
+    pol.close()
+
+
+def test_on_a_cu_masked_stream_and_refusals():
+    """The same bits on a stream with fewer CUs; calls that other policies refuse are refused."""
+    o = AR
+    ids = [0, 1]
+    img, lang = _obs(o, ids, 1003)
+    pol = _policy(o, 2)
+    with pytest.raises(E.EbrlError):
+        pol.decode_actions([0])                        # no prefix yet
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang))
+    first = pol.decode_actions(ids)
+    torch.cuda.synchronize()
+    s = E.create_cu_masked_stream(torch.cuda.current_device(), [0xFFFFFFFF] * 2)
+    pol.bind_stream(s)
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang))
+    got = pol.decode_actions(ids)
+    torch.cuda.synchronize()
+    for a, b in zip(first, got):
+        assert torch.equal(a, b)
+    with pytest.raises(E.EbrlError):
+        pol.flow_denoise(ids)
+    pol.bind_stream(torch.cuda.current_stream().cuda_stream)
+    pol.close()
+    E.destroy_stream(s)
+    c = _ebrl_config(o, 2)
+    c.dtype = 3
+    with pytest.raises(E.EbrlError):
+        E.Policy(c)
+
+
+def test_reference_rounding_is_that_of_the_codes():
+    """four_bits against the codes' own rounding, where a page's scale keeps values normal."""
+    x = np.random.default_rng(0).standard_normal(5000) * 100
+    x = x[(np.abs(x) > 2.0 ** -6) & (np.abs(x) < 448)]
+    assert np.array_equal(four_bits(x), R.CODE[R.encode(x)])
