@@ -21,6 +21,7 @@ namespace ebrl {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int KV8_PAGE = EBRL_KV8_PAGE;
 constexpr int KV8_EXP_MIN = -100, KV8_EXP_MAX = 120;   // 448 * 2^120 > FLT_MAX
@@ -558,10 +559,21 @@ template <int NP> EBRL_DEV void kv8_split(float x, __bf16* o) {
 // The state of a wave's 16 QT query rows.  Lane (r, g) holds query r of each
 // 16: its elements 64 c + 16 g .. + 15, its scores for keys 4 g .. 4 g + 3 of
 // each page, and its results in dims 64 c + 16 g .. + 15.
-template <typename T, int HD, int QT> struct Kv8Rows {
+template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
     static constexpr int NP = sizeof(T) == 4 ? 3 : 1;   // bf16 terms of a query element and of a weight
     static constexpr int NC = HD / 64;
-    bf16x8 q[QT][NP][HD / 32];
+    // MX: K's codes enter the first product as they are, in
+    // v_mfma_scale_f32_16x16x128_f8f6f4 with the page's scale, and q as two
+    // e4m3 terms with scales of their own.  A bf16 element has eight
+    // significant bits and a term four: they are exact down to 2^-13 of the
+    // row's largest element, and off by 2^-21 of that at most below.  The
+    // product takes the same time as the bf16 one, and half the conversions
+    // of codes fall away.  (Head dim 64 would have to put both terms under one
+    // scale, which loses four bits more.)
+    static_assert(!MX || (NP == 1 && HD == 128), "two bf16 terms, one scale each");
+    bf16x8 q[QT][NP][MX ? 1 : HD / 32];
+    i32x8 q8[QT][MX ? 2 : 1];
+    int q8_scale[QT];         // exponent byte of the first term's scale; the second's is 4 less
     f32x4 acc[QT][HD / 16];   // acc[4 c + d][v]: dim 64 c + 16 g + 4 v + d
     float mx[QT], sum[QT];    // log2 of what the weights are relative to; this lane's share of their sum
     int lim[QT];              // keys that the row sees
@@ -575,20 +587,49 @@ template <typename T, int HD, int QT> struct Kv8Rows {
             const int tok = row / w.grp, h = kvh * w.grp + (row - tok * w.grp);
             lim[qt] = w.a.causal ? min(t.len, t.len - t.m + tok + 1) : t.len;
             const T* src = (const T*)w.a.q + (size_t)(t.r0 + tok) * w.a.ldq + h * HD;
+            if constexpr (MX) {
+                float x[2][16];
+                float am = 0.f;
 #pragma unroll
-            for (int s = 0; s < HD / 32; ++s) {
-                const T* const at = src + (s >> 1) * 64 + g * 16 + (s & 1) * 8;
-                if constexpr (NP == 1) {
-                    q[qt][0][s] = *reinterpret_cast<const bf16x8*>(at);
-                } else {
-                    float x[8];
-                    kv8_load<T, 8>(at, x);
+                for (int c = 0; c < 2; ++c) {
+                    kv8_load<T, 8>(src + 64 * c + 16 * g, x[c]);
+                    kv8_load<T, 8>(src + 64 * c + 16 * g + 8, x[c] + 8);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        __bf16 p[NP];
-                        kv8_split<NP>(x[j], p);
+                    for (int j = 0; j < 16; ++j) am = fmaxf(am, fabsf(x[c][j]));
+                }
+                const int e = kv8_exponent(attn_max_xor16_32(am));
+                const float inv = kv8_pow2(-e);
+                q8_scale[qt] = e + 127;
 #pragma unroll
-                        for (int y = 0; y < NP; ++y) q[qt][y][s][j] = p[y];
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        float y[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) y[z] = x[c][j + z] * inv;
+                        const unsigned w0 = kv8_pack4(y[0], y[1], y[2], y[3]);
+                        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w0, false);
+                        const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w0, true);
+                        q8[qt][0][4 * c + j / 4] = (int)w0;
+                        q8[qt][1][4 * c + j / 4] = (int)kv8_pack4((y[0] - lo[0]) * 16.f, (y[1] - lo[1]) * 16.f,
+                                                                  (y[2] - hi[0]) * 16.f, (y[3] - hi[1]) * 16.f);
+                    }
+            } else {
+#pragma unroll
+                for (int s = 0; s < HD / 32; ++s) {
+                    const T* const at = src + (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+                    if constexpr (NP == 1) {
+                        q[qt][0][s] = *reinterpret_cast<const bf16x8*>(at);
+                    } else {
+                        float x[8];
+                        kv8_load<T, 8>(at, x);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            __bf16 p[NP];
+                            kv8_split<NP>(x[j], p);
+#pragma unroll
+                            for (int y = 0; y < NP; ++y) q[qt][y][s][j] = p[y];
+                        }
                     }
                 }
             }
@@ -618,6 +659,18 @@ template <typename T, int HD, int QT> struct Kv8Rows {
         for (int t = 0; t < P; ++t) {
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (MX) {
+                const i32x8 ka = {(int)kc[t][0].x, (int)kc[t][0].y, (int)kc[t][0].z, (int)kc[t][0].w,
+                                  (int)kc[t][NC - 1].x, (int)kc[t][NC - 1].y, (int)kc[t][NC - 1].z, (int)kc[t][NC - 1].w};
+                const int sk = (int)(__float_as_uint(ks[t]) >> 23);
+#pragma unroll
+                for (int p = 1; p >= 0; --p)
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt)
+                        s[qt][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, q8[qt][p], s[qt][t], 0, 0, 0, sk, 0,
+                                                                                    q8_scale[qt] - 4 * p);
+                continue;
+            }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const bf16x8 ka = kv8_bf16(kc[t][c].x, kc[t][c].y, ks[t], ks[t]);
@@ -626,12 +679,12 @@ template <typename T, int HD, int QT> struct Kv8Rows {
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt)
-                        s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, q[qt][p][2 * c], s[qt][t], 0, 0, 0);
+                        s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, q[qt][p][MX ? 0 : 2 * c], s[qt][t], 0, 0, 0);
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt)
-                        s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, q[qt][p][2 * c + 1], s[qt][t], 0, 0, 0);
+                        s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, q[qt][p][MX ? 0 : 2 * c + 1], s[qt][t], 0, 0, 0);
             }
         }
         // Codes of V that are NaN where not every row sees every key: a bit
@@ -849,7 +902,7 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
     const size_t gb = (size_t)KV8_PAGE * HD;   // bytes of a (page, K or V, head) group
     const uint8_t* const codes = (const uint8_t*)w.c.codes + kvh * gb;
     const int k_at = r * 64 + g * 16, v_at = lane * 16;
-    Kv8Rows<T, HD, 1> rows;
+    Kv8Rows<T, HD, 1, false> rows;
     const int p_hi = (k_hi + KV8_PAGE - 1) / KV8_PAGE;
     rows.init(w, t, kvh, 0, k_hi, lane);
     for (int kb = k_lo; kb < k_hi; kb += BATCH * STEP) {
@@ -989,7 +1042,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 
     const int kg = KG == 1 ? 0 : wave & 1;
     const int wr0 = t.t0 + wave / KG * RW;
-    Kv8Rows<T, HD, QT> rows;
+    Kv8Rows<T, HD, QT, sizeof(T) == 2 && HD == 128> rows;
     rows.init(w, t, kvh, wr0, k_hi, lane);
 
     const uint8_t* const codes = (const uint8_t*)w.c.codes + (size_t)kvh * GB;

@@ -134,7 +134,10 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
 
     The bound, from the arithmetic: a score is a sum of hd (fp32: 3 hd) exact
     products in 32 bits, each addition off by 2^-23 of the sum of the terms'
-    magnitudes at most; the exponent's argument is rounded (2^-23 of its size
+    magnitudes at most; bf16 rows may enter it as two e4m3 terms under one
+    power-of-two scale each, the largest element between 224 and 448: exact
+    where the first term is normal (2^-6 and more), else off by half the
+    second's least step, 2^-10 / 16, so by 2^-21 of the largest at most; the exponent's argument is rounded (2^-23 of its size
     and of the score's) and exp2 is good to 2^-22; a weight enters the second
     product rounded to bf16 (2^-8) for bf16 rows, whole for fp32; the two sums
     over keys add 2^-23 a term; the result is rounded to its type."""
@@ -167,7 +170,10 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
                     o = p @ V[use, kh] / l
                     mag = p @ np.abs(V[use, kh]) / l
                     terms = hd * (1 if bf16 else 3)
-                    ds = (terms * 2.0 ** -23 * (np.abs(K[use, kh]) @ np.abs(x)) * scale + np.abs(s) * 2.0 ** -22).max()
+                    ds = terms * 2.0 ** -23 * (np.abs(K[use, kh]) @ np.abs(x)) * scale + np.abs(s) * 2.0 ** -22
+                    if bf16:
+                        ds = ds + 2.0 ** -21 * np.abs(x).max() * np.abs(K[use, kh]).sum(-1) * scale
+                    ds = ds.max()
                     dp = ds + (s.max() - s[p > 0].min() + 1) * 2.0 ** -22 + 2.0 ** -22
                     rel = 2 * dp + 2 * (len(use) * (1 if bf16 else 3) + 8) * 2.0 ** -23 + (2.0 ** -8 if bf16 else 0)
                     out[r0 + j, h] = o

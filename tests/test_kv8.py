@@ -464,6 +464,29 @@ def test_attn_strong_scores(dtype):
     _check_attn(pool, DT[dtype], 4, lens, [1, 1], True, 30, q_scale=4.0)
     _check_attn(pool, DT[dtype], 4, lens, [60, 30], True, 31, q_scale=4.0, scale=0.5)
     _check_attn(pool, DT[dtype], 4, lens, [60, 30], False, 32, scale=1e-6)
+    pool = Pool(69, lens, 2, 128, spread=6.0)
+    _check_attn(pool, DT[dtype], 4, lens, [60, 30], True, 31, q_scale=4.0, scale=0.5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ql", [1, 40])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attn_rows_of_all_sizes(dtype, ql, hd):
+    """Queries whose elements, and whose rows, are powers of two apart; rows of zeros and of the least values."""
+    pool = Pool(67, [90, 41], 2, hd)
+    rng = np.random.default_rng(68)
+    size = np.exp2(rng.integers(-20, 1, (2 * ql, 4 * hd)) + rng.integers(-8, 4, (2 * ql, 1)))
+    size[::7] = 0.0
+    size[3::7] = 1e-37
+    q = torch.from_numpy(rng.standard_normal((2 * ql, 4 * hd)) * size).to(DT[dtype]).cuda()
+    codes, scales, table = pool.gpu()
+    out = torch.empty_like(q)
+    E.op_kv8_attn(codes, scales, table, q, out, _ints([0, ql, 2 * ql]), _ints([90, 41]), ql, 90)
+    q64 = q.double().cpu().numpy().reshape(2 * ql, 4, hd)
+    want, bound = R.attend(pool.codes, pool.scales, pool.table, q64, [0, ql, 2 * ql], [90, 41], ql, 90, True, hd ** -0.5,
+                           bf16=dtype == "bf16")
+    _held(out.double().cpu().numpy().reshape(want.shape), want, bound)
 
 
 @gpu
@@ -485,12 +508,12 @@ def test_attn_keeps_to_its_bounds(ql):
 @gpu
 @pytest.mark.parametrize("copies", [1, 300])
 @pytest.mark.parametrize("ql", [1, 5, 40])
-@pytest.mark.parametrize("hkv", [2, 4])
-def test_attn_nan_counts_only_where_it_is_seen(ql, hkv, copies):
+@pytest.mark.parametrize("hkv,hd", [(2, 64), (4, 64), (2, 128)])
+def test_attn_nan_counts_only_where_it_is_seen(ql, hkv, hd, copies):
     """NaN keys and values: rows that see them are NaN (a value's in its dim
     alone), rows that do not are what they are without.  Copies of the second
     sequence bring the kernels of large batches."""
-    hd, n = 64, 70
+    n = 70
     rng = np.random.default_rng(38)
     pool = Pool(39, [n, n], hkv, hd)
     clean = pool.codes.copy()
