@@ -229,8 +229,6 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
         const int t = lane >> 2, g = lane & 3;
         const bool mine = t >= s0 && t < s1;
         const int slot = mine ? t : s0, row = s.row0 + slot;
-        float cs[PL], sn[PL];
-        if (a.n_axes) kv8_angles<HALF, PL>(a, row, s.pos0 + slot, PL * g, cs, sn);
         const int h_lo = unit * w.per_wave, h_hi = min(h_lo + w.per_wave, a.q_heads + hkv);
         auto src = [&](int h) {
             return (h < a.q_heads ? (const T*)a.q + (size_t)row * a.ldq + h * HD
@@ -239,6 +237,8 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
         Kv8Raw<T, PL> r0, r1;
         r0.load(src(h_lo));
         r1.load(src(h_lo) + HALF);
+        float cs[PL], sn[PL];
+        if (a.n_axes) kv8_angles<HALF, PL>(a, row, s.pos0 + slot, PL * g, cs, sn);
         for (int h = h_lo; h < h_hi; ++h) {
             const bool isq = h < a.q_heads;
             const int hh = isq ? h : h - a.q_heads;
@@ -1157,41 +1157,52 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 }
 
 // Joins the parts of a row's keys, in their order: a wave a row, HD / 4 lanes
-// across it and the others taking further parts.
+// across it and the others taking further parts.  Bound by latency: what it
+// needs of the workspace is asked for before the sequence's lengths, which say
+// how many parts there are, have come.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
 {
-    constexpr int LPR = HD / 4, PG = 64 / LPR;
+    constexpr int LPR = HD / 4, PG = 64 / LPR, AHEAD = 2;
     __shared__ float s_w[4][KV8_MAX_PARTS];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned per = (w.join_rows + 3) / 4;
     const unsigned unit = blockIdx.x / per;
     const int row = (blockIdx.x % per) * 4 + wave;
+    if (row >= w.join_rows) return;
+    const size_t base = (size_t)unit * w.parts * w.tile_rows + row;
+    auto ml = [&](int p) { return *reinterpret_cast<const float2*>(w.part_ml + 2 * (base + (size_t)p * w.tile_rows)); };
+    const int d = lane % LPR * 4, p0 = lane / LPR;
+    auto part = [&](int p) { return *reinterpret_cast<const f32x4*>(w.part_o + (base + (size_t)p * w.tile_rows) * HD + d); };
+    const float2 first = ml(min(lane, w.parts - 1));
+    f32x4 ahead[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) ahead[k] = part(min(p0 + k * PG, w.parts - 1));
     unsigned id = unit;
     const int tile = id % w.tiles;
     id /= w.tiles;
     const int kvh = id % w.c.kv_heads, i = id / w.c.kv_heads;
     const Kv8Tile t = kv8_tile(w, i, tile);
-    if (t.parts == 1 || row >= w.join_rows || t.t0 + row >= t.rows) return;
-    const size_t base = (size_t)unit * w.parts * w.tile_rows + row;
-    float m = -INFINITY;
-    for (int p = lane; p < t.parts; p += 64) m = fmaxf(m, w.part_ml[2 * (base + (size_t)p * w.tile_rows)]);
+    if (t.parts == 1 || t.t0 + row >= t.rows) return;
+    float m = lane < t.parts ? first.x : -INFINITY;
+    for (int p = lane + 64; p < t.parts; p += 64) m = fmaxf(m, ml(p).x);
     const float M = wave_max(m);
     float l = 0.f;
     for (int p = lane; p < t.parts; p += 64) {
-        const float* ml = w.part_ml + 2 * (base + (size_t)p * w.tile_rows);
-        const float wt = ml[0] == -INFINITY ? 0.f : fast_exp2(ml[0] - M);
+        const float2 y = p == lane ? first : ml(p);
+        const float wt = y.x == -INFINITY ? 0.f : fast_exp2(y.x - M);
         s_w[wave][p] = wt;
-        l += wt * ml[1];
+        l += wt * y.y;
     }
     const float L = wave_sum(l);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave's own s_w
-    const int d = lane % LPR * 4;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (p0 + k * PG < t.parts) o += s_w[wave][p0 + k * PG] * ahead[k];
 #pragma unroll 4
-    for (int p = lane / LPR; p < t.parts; p += PG)
-        o += s_w[wave][p] * *reinterpret_cast<const f32x4*>(w.part_o + (base + (size_t)p * w.tile_rows) * HD + d);
+    for (int p = p0 + AHEAD * PG; p < t.parts; p += PG) o += s_w[wave][p] * part(p);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         if (PG == 4) o[v] += swz_xor16_f(o[v]);
