@@ -123,7 +123,7 @@ EBRL_DEV bool kv8_span(const Kv8WriteKernelArgs& w, int i, int pg, Kv8Span& s) {
     const ebrl_kv8_write_args& a = w.a;
     const int trow = a.seq ? a.seq[i] : i;
     const int r0 = min(max(a.row_start[i], 0), a.rows);
-    const int len = min(min(a.row_start[i + 1], a.rows) - r0, a.max_len);
+    const int len = min(min(max(a.row_start[i + 1], 0), a.rows) - r0, a.max_len);
     const int p0 = a.pos0[i];
     if (trow < 0 || trow >= w.c.table_rows || len <= 0 || p0 < 0 || p0 >= w.c.table_stride * KV8_PAGE) return false;
     const int at = p0 / KV8_PAGE + pg;
@@ -524,7 +524,7 @@ EBRL_DEV Kv8Tile kv8_tile(const Kv8AttnKernelArgs& w, int i, int tile) {
     Kv8Tile t;
     const int trow = kv8_table_row(w, i);
     t.r0 = min(max(a.row_start[i], 0), a.rows);
-    t.m = min(max(min(a.row_start[i + 1], a.rows) - t.r0, 0), a.max_q_len);
+    t.m = min(max(min(max(a.row_start[i + 1], 0), a.rows) - t.r0, 0), a.max_q_len);
     t.rows = t.m * w.grp;
     t.t0 = tile * w.tile_rows;
     t.len = trow >= 0 ? min(max(a.kv_len[i], 0), min(a.max_kv_len, w.c.table_stride * KV8_PAGE)) : 0;
@@ -1367,7 +1367,7 @@ int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args
 }
 
 int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n, hipStream_t s) {
-    if (!kv8_attn_shape_ok(cache, args) || !(args->scale > 0.f) || !isfinite(args->scale)) return EBRL_E_INVALID;
+    if (!kv8_attn_shape_ok(cache, args) || !(args->scale > 0.f) || !isfinite(args->scale * 1.4426950408889634f)) return EBRL_E_INVALID;
     const ebrl_kv8_attn_args& a = *args;
     if (a.n == 0 || a.rows == 0 || a.max_q_len == 0) return EBRL_OK;
     const int hd = cache->head_dim, esz = a.dtype == EBRL_DTYPE_FP32 ? 4 : 2;

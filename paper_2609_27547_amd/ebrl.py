@@ -481,6 +481,8 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
     c, dev = _kv8_cache(codes, scales, block_table)
     hd, n, axes, dtype = c.head_dim, pos0.numel(), len(sections), _kv8_dtype("k", k)
     rows, torch_dtype, width = k.shape[0], k.dtype, c.kv_heads * hd
+    if not 0 <= max_len < 1 << 31:
+        _kv8_bad(f"max_len {max_len}")
     k_at, ldk = _kv8_rows("k", k, torch_dtype, dev, rows, width)
     v_at, ldv = _kv8_rows("v", v, torch_dtype, dev, rows, width)
     if (q is None) != (q_out is None) or axes > 3 or (axes == 0 and q is not None):
@@ -508,9 +510,15 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
     _kv8_call(lib().ebrl_op_kv8_write, "ebrl_op_kv8_write", c, a, dev, stream)
 
 
+def _kv8_bounds(max_q_len, max_kv_len):
+    if not 0 <= max_q_len < 1 << 31 or not 0 <= max_kv_len <= 1 << 30:
+        _kv8_bad(f"max_q_len {max_q_len}, max_kv_len {max_kv_len} (at most 2^30)")
+
+
 def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     """A workspace for op_kv8_attn calls with these sizes, on the cache's device."""
     import torch
+    _kv8_bounds(max_q_len, max_kv_len)
     c = Kv8Cache(0, 0, 0, codes.shape[0], block_table.shape[0], block_table.shape[1], codes.shape[2],
                  codes.shape[3] // KV8_PAGE)
     a = Kv8AttnArgs(_kv8_dtype("q", q), n, q.shape[0], max_q_len, max_kv_len, q.shape[-1] // c.head_dim, 1, 1.0)
@@ -533,6 +541,7 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
     rows, wide = q.shape
     if wide % hd:
         _kv8_bad(f"q has heads of {hd}", q)
+    _kv8_bounds(max_q_len, max_kv_len)
     q_at, ldq = _kv8_rows("q", q, q.dtype, dev, rows, wide)
     out_at, ldo = _kv8_rows("out", out, q.dtype, dev, rows, wide)
     if workspace is None:

@@ -174,7 +174,8 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
                     if bf16:
                         ds = ds + 2.0 ** -21 * np.abs(x).max() * np.abs(K[use, kh]).sum(-1) * scale
                     ds = ds.max()
-                    dp = ds + (s.max() - s[p > 0].min() + 1) * 2.0 ** -22 + 2.0 ** -22
+                    low = s[p > 0].min() if (p > 0).any() else np.nan        # NaN among the keys: no bound
+                    dp = ds + (s.max() - low + 1) * 2.0 ** -22 + 2.0 ** -22
                     rel = 2 * dp + 2 * (len(use) * (1 if bf16 else 3) + 8) * 2.0 ** -23 + (2.0 ** -8 if bf16 else 0)
                     out[r0 + j, h] = o
                     bound[r0 + j, h] = mag * rel + np.abs(o) * (2.0 ** -8 if bf16 else 2.0 ** -24) + 2.0 ** -120

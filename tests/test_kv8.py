@@ -48,7 +48,7 @@ def test_attn_refuses_cache(bad):
 @pytest.mark.parametrize("bad", [
     dict(dtype=2), dict(n=-1), dict(rows=-1), dict(max_q_len=-1), dict(max_kv_len=-1), dict(max_kv_len=(1 << 30) + 1),
     dict(q_heads=0), dict(q_heads=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
-    dict(scale=float("inf")), dict(q=0), dict(out=0), dict(q=4096 + 8), dict(ldq=255), dict(ldq=260), dict(ldo=128),
+    dict(scale=float("inf")), dict(scale=3e38), dict(q=0), dict(out=0), dict(q=4096 + 8), dict(ldq=255), dict(ldq=260), dict(ldo=128),
     dict(row_start=0), dict(kv_len=0), dict(out=4096), dict(max_kv_len=10000)])   # the last: needs a workspace
 def test_attn_refuses_arguments(bad):
     assert _attn(_cache(), _attn_args(**bad)) == -1
@@ -120,12 +120,13 @@ def test_binding_refuses():
     for bad in (dict(codes=codes.view(torch.uint8)[:, :1]), dict(codes=codes.float()), dict(scales=scales.double()),
                 dict(block_table=table.long()), dict(v=k.float()), dict(k=k[:, :64]), dict(pos0=i32(0).long()),
                 dict(row_start=i32(0)), dict(q=k), dict(k=torch.zeros((1, 128), dtype=torch.float16)),
-                dict(sections=(32,)), dict(sections=(8, 8, 8, 8))):
+                dict(sections=(32,)), dict(sections=(8, 8, 8, 8)), dict(max_len=-1), dict(max_len=1 << 32)):
         refused(E.op_kv8_write, **{**ok, **bad})
     at = dict(codes=codes, scales=scales, block_table=table, q=k, out=k.clone(), row_start=i32(0, 1), kv_len=i32(1),
               max_q_len=1, max_kv_len=1)
     for bad in (dict(), dict(out=k.float()), dict(q=k[:, :65], out=k[:, :65]), dict(kv_len=i32(1, 1)),
-                dict(q=k.half(), out=k.half()), dict(stream=0), dict(out=k[:, :64])):
+                dict(q=k.half(), out=k.half()), dict(stream=0), dict(out=k[:, :64]), dict(max_kv_len=1 << 32),
+                dict(max_q_len=-1), dict(q=k[0], out=k[0])):
         refused(E.op_kv8_attn, **{**at, **bad})
 
 
@@ -280,6 +281,100 @@ def test_write_keeps_to_its_bounds():
     # rows that end in the middle of the last sequence, a position past the table's row
     _check_write(pool, torch.bfloat16, 2, [4, 18, 0, pool.table.shape[1] * 16 - 3], [3, 3, 3, 9], (32,), 0, 10, outside=-4)
     _check_write(pool, torch.bfloat16, 2, [-1, 1 << 30, 0, 190], [3, 3, 3, 9], (32,), 0, 11)
+
+
+LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+
+
+@gpu
+@pytest.mark.parametrize("max_len", [1, 40])
+def test_write_of_any_numbers(max_len):
+    """Device data that says anything: nothing out of bounds is touched, what is in bounds is written."""
+    rng = np.random.default_rng(70)
+    past = [4, 18, 0, 30, 7, 2]
+    pool = Pool(71, past, 2, 64, room=60)
+    pool.table[4] = [LEAST, MOST, -1, pool.nb, pool.nb - 1, 0][:pool.table.shape[1]] + [0] * max(0, pool.table.shape[1] - 6)
+    n, rows = 9, 50
+    k, k64 = _rows(rng, rows, 2, 64, torch.bfloat16)
+    q, q64 = _rows(rng, rows, 2, 64, torch.bfloat16)
+    axis = rng.choice([LEAST, -1, 0, 3, 199, 200, MOST], (rows, 2)).astype(np.int32)
+    cos, sin = _tables(200, 64)
+    # each sequence's rows are its own: the numbers that are no bounds come between
+    start = [5, 9, LEAST, 3, 17, MOST, 20, -4, 40, 2 ** 30]
+    pos0 = [4, 18, LEAST, 39, MOST, 30, 7, 96, 2]
+    seq = [0, 1, 2, 4, 2, 3, 4, LEAST, 5]
+    codes, scales, table = pool.gpu()
+    q_out = torch.full_like(q, 7.0)
+    E.op_kv8_write(codes, scales, table, k, k, _ints(start), _ints(pos0), max_len, q=q, q_out=q_out, sections=(20, 12),
+                   axis_pos=torch.from_numpy(axis).cuda(), cos=torch.from_numpy(cos).cuda(),
+                   sin=torch.from_numpy(sin).cuda(), seq=_ints(seq))
+    wc, ws = pool.codes.copy(), pool.scales.copy()
+    wq = R.write(wc, ws, pool.table, k64, k64, start, pos0, max_len, [20, 12], axis, cos, sin, seq, q64)
+    _same_codes(_bits(codes), wc)
+    np.testing.assert_array_equal(scales.cpu().numpy(), ws)
+    assert np.array_equal(q_out.double().cpu().numpy().reshape(wq.shape) == 7.0, np.isnan(wq))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("max_q,max_kv", [(1, 100), (3, 64), (40, 100), (40, 1 << 30)])
+def test_attn_of_any_numbers(dtype, max_q, max_kv):
+    rng = np.random.default_rng(72)
+    lens = [40, 70, 100, 33]
+    pool = Pool(73, lens, 2, 64)
+    pool.table[2] = ([LEAST, MOST, pool.table[2, 2], -1, pool.nb, pool.table[2, 5]] + [0] * pool.table.shape[1])[
+        :pool.table.shape[1]]
+    rows = 60
+    start = [5, 9, LEAST, 3, 17, MOST, 20, -4, 40, 2 ** 30]
+    kv_len = [40, 70, LEAST, MOST, -1, 33, 100, 40, 2]
+    seq = [0, 1, 2, 3, 2, 3, 2, LEAST, MOST]
+    q, q64 = _rows(rng, rows, 4, 64, DT[dtype])
+    codes, scales, table = pool.gpu()
+    out = torch.full_like(q, 7.0)
+    # sequences that overlap in their rows write the same rows: those are not looked at
+    E.op_kv8_attn(codes, scales, table, q, out, _ints(start), _ints(kv_len), max_q, max_kv, seq=_ints(seq))
+    got = out.double().cpu().numpy().reshape(q64.shape)
+    count = np.zeros(rows, int)
+    for i in range(9):
+        r0 = min(max(start[i], 0), rows)
+        count[r0:r0 + max(0, min(min(max(start[i + 1], 0), rows) - r0, max_q))] += 1
+    want, bound = R.attend(pool.codes, pool.scales, pool.table, q64, start, kv_len, max_q, max_kv, True, 0.125, seq,
+                           dtype == "bf16")
+    # a page of no tokens holds NaN: rows that see one are NaN
+    bound[count > 1] = np.inf
+    bad = np.isnan(want) & ~np.isnan(bound) | np.isnan(bound) & (count[:, None, None] > 0)
+    assert np.all(got[count == 0] == 7.0)
+    ok = ~bad & (count == 1)[:, None, None] & ~np.isnan(want)
+    assert np.all(np.abs(got - want)[ok] <= bound[ok])
+    assert ok.any()
+
+
+@gpu
+@pytest.mark.parametrize("ql", [1, 40])
+def test_pool_past_four_gib(ql):
+    """Pages whose codes lie past 2^32 bytes, and past 2^31, beside the same sequence in low pages."""
+    hkv, hd, n = 8, 128, 75
+    nb = (1 << 32) // (2 * hkv * 16 * hd) + 64
+    codes = torch.zeros((nb, 2, hkv, 16 * hd), dtype=torch.uint8, device="cuda")
+    scales = torch.ones((nb, 2, hkv), device="cuda")
+    pages = (n + 15) // 16
+    table = torch.tensor([list(range(pages)), list(range(nb - pages, nb)), list(range(nb // 2 + 7, nb // 2 + 7 + pages))],
+                         dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((n, hkv * hd), device="cuda").bfloat16().repeat(3, 1) for _ in range(2))
+    for lo, hi in ((0, 60), (60, 61), (61, n)):            # prompts and a token
+        m = hi - lo
+        rows = torch.cat([torch.arange(lo, hi) + i * n for i in range(3)])
+        E.op_kv8_write(codes, scales, table, k[rows], v[rows], _ints([0, m, 2 * m, 3 * m]), _ints([lo] * 3), m)
+    t = table.long()
+    assert codes[t[0]].any()
+    assert torch.equal(codes[t[0]], codes[t[1]]) and torch.equal(codes[t[0]], codes[t[2]])
+    assert torch.equal(scales[t[0]], scales[t[1]])
+    assert not codes[pages:nb // 2].any()
+    q = torch.randn((ql, 2 * hkv * hd), device="cuda").bfloat16().repeat(3, 1)
+    out = torch.empty_like(q)
+    E.op_kv8_attn(codes, scales, table, q, out, _ints([0, ql, 2 * ql, 3 * ql]), _ints([n] * 3), ql, n)
+    assert torch.equal(out[:ql], out[ql:2 * ql]) and torch.equal(out[:ql], out[2 * ql:])
+    assert out.abs().sum() > 0
 
 
 @gpu
@@ -545,6 +640,30 @@ def test_attn_nan_counts_only_where_it_is_seen(ql, hkv, hd, copies):
             want[0, j, :mine] = np.nan
     assert np.array_equal(np.isnan(want), np.isnan(res[1]))
     np.testing.assert_array_equal(want, res[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ql,copies", [(1, 1), (6, 1), (40, 1), (40, 300), (1, 600)])
+def test_attn_queries_that_are_not_finite(dtype, hd, ql, copies):
+    """A NaN or an infinity in a query row makes that row and head NaN and leaves the others as they are."""
+    pool = Pool(74, [70], 2, hd)
+    n = copies + 1
+    start = [ql * i for i in range(n + 1)]
+    q = torch.randn((n * ql, 4 * hd), device="cuda").to(DT[dtype])
+    codes, scales, table = pool.gpu()
+    res = []
+    for bad in (False, True):
+        if bad:
+            q[0, 3], q[ql - 1, hd + 7], q[-1, 2 * hd + 1] = float("nan"), float("inf"), float("-inf")
+        out = torch.empty_like(q)
+        E.op_kv8_attn(codes, scales, table, q, out, _ints(start), _ints([70] * n), ql, 70, seq=_ints([0] * n))
+        res.append(out.reshape(n * ql, 4, hd))
+    hit = torch.zeros((n * ql, 4), dtype=torch.bool, device="cuda")
+    hit[0, 0] = hit[ql - 1, 1] = hit[-1, 2] = True
+    assert torch.isnan(res[1][hit]).all()
+    assert torch.equal(res[0][~hit], res[1][~hit])
 
 
 @gpu
