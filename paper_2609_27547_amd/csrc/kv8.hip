@@ -201,8 +201,9 @@ template <int N> EBRL_DEV float kv8_amax(float (&x)[N]) {
 }
 
 // A call of several tokens a sequence: a wave takes the new tokens of a page
-// and a run of heads, Q and K heads or V heads.  Bound by bytes.  Four heads a
-// wave in turn share the cosines and sines; one head a wave where there are
+// and a run of heads, Q and K heads or V heads.  Bound by bytes: nine sequences
+// of 3001 to 4095 tokens, 32 Q and 8 + 8 KV heads of 128, take 141 us, 5.0 TB/s,
+// the rate of a copy; 16 of 600 tokens 37 us, 3.7 TB/s.  Four heads a wave in turn share the cosines and sines; one head a wave where there are
 // too few waves to fill the chip.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
@@ -367,7 +368,8 @@ template <int LPH> EBRL_DEV float kv8_head_max(float v) {
 
 // One token a sequence: a wave takes 64 / LPH heads of a sequence's token,
 // eight pairs (Q, K) or sixteen dims (V) a lane, so that every lane has work.
-// Bound by latency: the chain is lengths, page, scale, codes.
+// Bound by latency: the chain is lengths, page, scale, codes (3.3 us for one
+// sequence, 3.6 for 101).
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_write_token_kernel(Kv8WriteKernelArgs w)
 {
@@ -868,7 +870,9 @@ EBRL_DEV uint4 kv8_stream16(const uint8_t* p) {
 // rows, at most 16, and deal the pairs of pages of a part of the keys.  Bound
 // by the bytes of the cache: codes go straight to registers, and a step's
 // registers are loaded again as soon as it is done, so that each wave keeps
-// 8 to 16 KB in flight (head dim 128).
+// 8 to 16 KB in flight (head dim 128).  89 us, 6.0 TB/s, on 61 sequences of 500
+// to 8000 keys (8 KV heads of 128), where a streaming read reaches 7.1; one
+// sequence of 291 keys 6 us, the latency of lengths, pages and codes in turn.
 template <typename T, int HD, int KW>
 __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 {
@@ -1002,7 +1006,10 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 // reads them back: 16 bytes a lane, one after the other.  A wave has 16 QT rows
 // and takes P pages at a time; with KG 1 the four waves of a workgroup have
 // rows of their own and take all keys, with KG 2 two waves share rows and take
-// 32 keys of each step.
+// 32 keys of each step.  Bound by issue: with 32 rows a wave (QT 2, head dim 128,
+// 2 x 4096 rows of 32 heads on 8 k keys) 730 us, 1.10 PFLOP/s; matrix
+// instructions take 42 % of a SIMD's cycles and vector instructions 60 %, and
+// they hardly overlap.  148 rows of 37 sequences on 730 keys 34 us, 480 TFLOP/s.
 template <typename T, int HD, int QT, int KG, int P>
 __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 {
@@ -1159,7 +1166,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 // Joins the parts of a row's keys, in their order: a wave a row, HD / 4 lanes
 // across it and the others taking further parts.  Bound by latency: what it
 // needs of the workspace is asked for before the sequence's lengths, which say
-// how many parts there are, have come.
+// how many parts there are, have come.  5 us for 61 x 8 pairs of two parts.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
 {
@@ -1230,9 +1237,11 @@ static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a, in
     } else if (a.dtype == EBRL_DTYPE_BF16 && groups(128) >= 512 && a.max_kv_len >= 1024) {
         // 32 rows a wave halve the conversions of codes, and pay once they
         // fill the chip twice over and keys are many: 2 x 4 k rows of 32 heads
-        // on 8 k keys 767 us against 909 with 16 rows a wave, 2048 rows on
-        // 8 k keys 249 against 294; 1024 workgroups of 148 rows on 748 keys
-        // 63 against 62, 3072 on 288 keys 81 against 76.
+        // on 8 k keys 726 us against 811 with 16 rows a wave, 2048 rows on
+        // 8 k keys 232 against 258, 4 x 2048 rows on themselves 156 against
+        // 168; as good where 4 x 1024 rows meet 1024 keys (51 against 50) or
+        // 32 x 37 rows 2037 (72 against 71); 128 x 37 rows on 748 keys 118
+        // against 115, 96 x 48 on 288 keys 56 against 48.
         p.kind = KV8_TALL;
         p.tile_rows = 128;
     } else if (groups(64) >= 512) {
@@ -1240,9 +1249,10 @@ static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a, in
         p.tile_rows = 64;
     } else {
         // few workgroups: twice as many of half the rows, two waves sharing
-        // them (600 rows of 32 heads on 600 keys 12.6 us against 15.4; 37
-        // sequences of 148 rows on 730 keys, 888 workgroups of 64 rows, 38 on
-        // both sides; 64 sequences of them 74 against 62)
+        // them (600 rows of 32 heads on 600 keys 17 us against 29, 512 rows
+        // of 4 heads each on 1512 keys 21.5 against 33; 37 sequences of 148
+        // rows on 730 keys, 888 workgroups of 64 rows, 37 against 34; 64
+        // sequences of them 75 against 58)
         p.kind = KV8_PAIRS;
         p.tile_rows = 32;
     }
