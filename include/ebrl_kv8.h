@@ -114,8 +114,9 @@ int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_a
  *
  * The workspace holds the parts; what is in it before a call does not matter.
  * Calls that may overlap in time (other streams, graphs replayed side by side)
- * need a workspace each.  Returns EBRL_E_INVALID on bad arguments or too small
- * a workspace. */
+ * need a workspace each.  Returns EBRL_E_INVALID on bad arguments, too small a
+ * workspace, or where the bounds ask for more than 2^23 workgroups (a tile of
+ * 16 to 128 query rows of a KV head each). */
 int ebrl_op_kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, void* stream);
 
 #ifdef __cplusplus

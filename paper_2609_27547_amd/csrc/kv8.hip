@@ -203,8 +203,9 @@ template <int N> EBRL_DEV float kv8_amax(float (&x)[N]) {
 // A call of several tokens a sequence: a wave takes the new tokens of a page
 // and a run of heads, Q and K heads or V heads.  Bound by bytes: nine sequences
 // of 3001 to 4095 tokens, 32 Q and 8 + 8 KV heads of 128, take 141 us, 5.0 TB/s,
-// the rate of a copy; 16 of 600 tokens 37 us, 3.7 TB/s.  Four heads a wave in turn share the cosines and sines; one head a wave where there are
-// too few waves to fill the chip.
+// the rate of a copy; 16 of 600 tokens 37 us, 3.7 TB/s.  Four heads a wave in
+// turn share the cosines and sines; one head a wave where there are too few
+// waves to fill the chip.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8WriteKernelArgs w)
 {
@@ -1016,7 +1017,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
     constexpr int NC = HD / 64;
     constexpr int RW = 16 * QT;
     constexpr int TR = RW * (4 / KG);
-        constexpr int SEG = 256;                   // pages whose ids and scales LDS holds
+    constexpr int SEG = 256;                   // pages whose ids and scales LDS holds
     constexpr int GB = KV8_PAGE * HD;
     __shared__ __attribute__((aligned(1024))) uint8_t s_kv[2][4][2][GB];
     __shared__ __attribute__((aligned(16))) int s_page[SEG];
@@ -1377,7 +1378,8 @@ int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args
 }
 
 int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n, hipStream_t s) {
-    if (!kv8_attn_shape_ok(cache, args) || !(args->scale > 0.f) || !isfinite(args->scale * 1.4426950408889634f)) return EBRL_E_INVALID;
+    if (!kv8_attn_shape_ok(cache, args) || !(args->scale > 0.f) || !isfinite(args->scale * 1.4426950408889634f))
+        return EBRL_E_INVALID;
     const ebrl_kv8_attn_args& a = *args;
     if (a.n == 0 || a.rows == 0 || a.max_q_len == 0) return EBRL_OK;
     const int hd = cache->head_dim, esz = a.dtype == EBRL_DTYPE_FP32 ? 4 : 2;
@@ -1389,7 +1391,8 @@ int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int pl
     if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;
     const Kv8Plan p = kv8_plan(*cache, a, plan_n);
     const int64_t units = (int64_t)a.n * cache->kv_heads * p.tiles;
-    if (units * std::max(p.parts, (p.tile_rows + 3) / 4) > KV8_MAX_GROUPS) return EBRL_E_INVALID;
+    // (the join's are fewer: there is one only below some 768 units)
+    if (units * p.parts > KV8_MAX_GROUPS) return EBRL_E_INVALID;
     Kv8AttnKernelArgs w;
     w.c = *cache;
     w.a = a;

@@ -585,6 +585,15 @@ def test_attn_rows_of_all_sizes(dtype, ql, hd):
 
 
 @gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_attn_bound_far_above_the_rows(causal):
+    """A bound of 4 M query rows for sequences of 20 and 40: half a million workgroups, most with nothing to do."""
+    lens = [60, 90]
+    pool = Pool(81, lens, 4, 64)
+    _check_attn(pool, torch.bfloat16, 4, lens, [20, 40], causal, 82, max_q=4 << 20)
+
+
+@gpu
 @pytest.mark.parametrize("ql", [1, 40])
 def test_attn_keeps_to_its_bounds(ql):
     """Unknown table rows are empty, pages that are none are not seen, row
