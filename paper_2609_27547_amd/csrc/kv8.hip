@@ -25,6 +25,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int KV8_PAGE = EBRL_KV8_PAGE;
 constexpr int KV8_EXP_MIN = -100, KV8_EXP_MAX = 120;   // 448 * 2^120 > FLT_MAX
+constexpr int KV8_Q_EXP_MIN = -122;   // of a query row's scale: every bf16 number is whole in two terms
 constexpr float KV8_SLACK = 10.f;     // log2 of the largest weight that a softmax keeps
 constexpr int KV8_MAX_PARTS = 256;    // parts that a row's keys are cut into
 
@@ -45,10 +46,10 @@ EBRL_DEV float kv8_odd(double d) {
 EBRL_DEV float kv8_storable(float v) {
     return fabsf(v) < 0x1p127f ? v : __uint_as_float(0x7fc00000u);
 }
-// Least e >= KV8_EXP_MIN with a <= 448 * 2^e = 1.75 * 2^(8 + e); a >= 0, finite.
-EBRL_DEV int kv8_exponent(float a) {
+// Least e >= `least` with a <= 448 * 2^e = 1.75 * 2^(8 + e); a >= 0, finite.
+EBRL_DEV int kv8_exponent(float a, int least = KV8_EXP_MIN) {
     const unsigned u = __float_as_uint(a);
-    return max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), KV8_EXP_MIN);
+    return max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), least);
 }
 EBRL_DEV float kv8_pow2(int e) { return __uint_as_float((unsigned)(max(e, -126) + 127) << 23); }
 EBRL_DEV unsigned kv8_pack4(float a, float b, float c, float d) {
@@ -600,7 +601,8 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) am = fmaxf(am, fabsf(x[c][j]));
                 }
-                const int e = kv8_exponent(attn_max_xor16_32(am));
+                // the terms' scale bytes, e + 127 and 4 less, stay above 0
+                const int e = kv8_exponent(attn_max_xor16_32(am), KV8_Q_EXP_MIN);
                 const float inv = kv8_pow2(-e);
                 q8_scale[qt] = e + 127;
 #pragma unroll

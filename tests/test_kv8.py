@@ -585,12 +585,25 @@ def test_attn_rows_of_all_sizes(dtype, ql, hd):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ql", [1, 40])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("up", [-92, -60, 60, 112])
+def test_attn_sizes_of_keys_and_queries_that_cancel(dtype, ql, hd, up):
+    """Keys 2^up times as large and queries 2^-up: the scores are ordinary."""
+    lens = [90, 41]
+    pool = Pool(83, lens, 2, hd)
+    pool.scales[:, 0] *= 2.0 ** up
+    _check_attn(pool, DT[dtype], 4, lens, [ql, ql], True, 84, q_scale=2.0 ** -up)
+
+
+@gpu
 @pytest.mark.parametrize("causal", [True, False])
 def test_attn_bound_far_above_the_rows(causal):
-    """A bound of 4 M query rows for sequences of 20 and 40: half a million workgroups, most with nothing to do."""
+    """A bound of 6 M query rows for sequences of 20 and 40: 786432 workgroups, most with nothing to do."""
     lens = [60, 90]
     pool = Pool(81, lens, 4, 64)
-    _check_attn(pool, torch.bfloat16, 4, lens, [20, 40], causal, 82, max_q=4 << 20)
+    _check_attn(pool, torch.bfloat16, 4, lens, [20, 40], causal, 82, max_q=6 << 20)
 
 
 @gpu
