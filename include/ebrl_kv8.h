@@ -20,8 +20,9 @@
  *
  * Device-side data that a call cannot check on the host never leads to an
  * access out of bounds: a row of the table outside [0, table_rows) is a
- * sequence of length 0; a page id outside [0, num_blocks), or a token past
- * the table's row, is a token that is not there (not written, not seen); row
+ * sequence of length 0; a page id outside [0, num_blocks) holds no tokens (none
+ * are written there or seen; queries at its positions are still turned); a
+ * sequence ends with the table's row (queries past it are left as well); row
  * ranges are cut to [0, rows] and to the host's max_* bounds; positions are
  * cut to the rotary tables.
  */
@@ -71,8 +72,10 @@ typedef struct ebrl_kv8_write_args {
  * not.  Each result is rounded once, from 64 bits.
  *
  * Tokens pos0[i] .. of each sequence are written; tokens before pos0[i] keep
- * their values and tokens behind the last are left as they were, as are rows
- * of q_out outside every sequence.  A page that holds earlier tokens keeps
+ * their values.  The bytes of slots and pages behind the last token are left as
+ * they were, but a slot behind it in the same page has no value from then on:
+ * the page's scale is that of the tokens up to the last.  Rows of q_out outside
+ * every sequence are left as they were.  A page that holds earlier tokens keeps
  * its scale unless a new token needs a larger one: the earlier tokens' codes
  * are then divided by the power of two that it grew by, which is exact down
  * to 2^-6 of the new scale and rounded below.  Two sequences of a call must
@@ -108,7 +111,8 @@ int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_a
  * does not see do not count, whatever their slots hold, NaN included; a row
  * that sees no key gets zeros; rows outside every sequence are left as they
  * were.  Scores, the softmax's maximum and sum and the weighted sum are held
- * in 32 bits.  With few rows the keys are cut into parts that run at the same
+ * in 32 bits, the sum over weights of up to 2^10: it overflows to infinity only
+ * where the keys' values, times 2^10 and their number, pass the 32-bit range.  With few rows the keys are cut into parts that run at the same
  * time and are joined in their order by a second launch.  The cut follows n,
  * max_q_len, max_kv_len and the heads.
  *

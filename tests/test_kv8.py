@@ -598,6 +598,18 @@ def test_attn_sizes_of_keys_and_queries_that_cancel(dtype, ql, hd, up):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ql", [1, 40])
+@pytest.mark.parametrize("up", [-90, 100])
+def test_attn_values_near_the_ends_of_the_range(dtype, ql, up):
+    """Values 2^up times as large: weights of up to 2^10 over 90 keys leave the sums of 2^100 ones below 2^128."""
+    lens = [90, 41]
+    pool = Pool(85, lens, 2, 128)
+    pool.scales[:, 1] *= 2.0 ** up
+    _check_attn(pool, DT[dtype], 4, lens, [ql, ql], True, 86, scale=1.0)
+
+
+@gpu
 @pytest.mark.parametrize("causal", [True, False])
 def test_attn_bound_far_above_the_rows(causal):
     """A bound of 6 M query rows for sequences of 20 and 40: 786432 workgroups, most with nothing to do."""
