@@ -571,13 +571,18 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
     // e4m3 terms with scales of their own.  A bf16 element has eight
     // significant bits and a term four: they are exact down to 2^-13 of the
     // row's largest element, and off by 2^-21 of that at most below.  The
-    // product takes the same time as the bf16 one, and half the conversions
-    // of codes fall away.  (Head dim 64 would have to put both terms under one
-    // scale, which loses four bits more.)
-    static_assert(!MX || (NP == 1 && HD == 128), "two bf16 terms, one scale each");
+    // products take the same time as the bf16 ones, and half the conversions
+    // of codes fall away.  Head dim 128: a product for each term.  Head dim 64:
+    // one for both.  Of a lane's 32 elements the first 16 are the product's
+    // elements 16 g .. 16 g + 15 and the others 64 more; they hold the first
+    // and the second term of the same dims, K's codes enter twice, and the
+    // scales, which lane g gives for elements 32 g .. 32 g + 31, are the first
+    // term's in lanes 0 and 1 and the second's in lanes 2 and 3.
+    static_assert(!MX || NP == 1, "a bf16 element has two e4m3 terms");
+    static constexpr int QP = MX && HD == 128 ? 2 : 1;  // products for q's terms
     bf16x8 q[QT][NP][MX ? 1 : HD / 32];
-    i32x8 q8[QT][MX ? 2 : 1];
-    int q8_scale[QT];         // exponent byte of the first term's scale; the second's is 4 less
+    i32x8 q8[QT][QP];
+    int q8_scale[QT];         // exponent byte of q8[.][0]'s scale; a second term's is 4 less
     f32x4 acc[QT][HD / 16];   // acc[4 c + d][v]: dim 64 c + 16 g + 4 v + d
     float mx[QT], sum[QT];    // log2 of what the weights are relative to; this lane's share of their sum
     int lim[QT];              // keys that the row sees
@@ -592,10 +597,10 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
             lim[qt] = w.a.causal ? min(t.len, t.len - t.m + tok + 1) : t.len;
             const T* src = (const T*)w.a.q + (size_t)(t.r0 + tok) * w.a.ldq + h * HD;
             if constexpr (MX) {
-                float x[2][16];
+                float x[NC][16];
                 float am = 0.f;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < NC; ++c) {
                     kv8_load<T, 8>(src + 64 * c + 16 * g, x[c]);
                     kv8_load<T, 8>(src + 64 * c + 16 * g + 8, x[c] + 8);
 #pragma unroll
@@ -604,9 +609,9 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                 // the terms' scale bytes, e + 127 and 4 less, stay above 0
                 const int e = kv8_exponent(attn_max_xor16_32(am), KV8_Q_EXP_MIN);
                 const float inv = kv8_pow2(-e);
-                q8_scale[qt] = e + 127;
+                q8_scale[qt] = e + 127 - (QP == 1 && g >= 2 ? 4 : 0);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
                         float y[4];
@@ -615,9 +620,10 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                         const unsigned w0 = kv8_pack4(y[0], y[1], y[2], y[3]);
                         const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w0, false);
                         const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w0, true);
+                        const unsigned w1 = kv8_pack4((y[0] - lo[0]) * 16.f, (y[1] - lo[1]) * 16.f,
+                                                      (y[2] - hi[0]) * 16.f, (y[3] - hi[1]) * 16.f);
                         q8[qt][0][4 * c + j / 4] = (int)w0;
-                        q8[qt][1][4 * c + j / 4] = (int)kv8_pack4((y[0] - lo[0]) * 16.f, (y[1] - lo[1]) * 16.f,
-                                                                  (y[2] - hi[0]) * 16.f, (y[3] - hi[1]) * 16.f);
+                        q8[qt][QP - 1][4 * (QP == 2 ? c : 1) + j / 4] = (int)w1;
                     }
             } else {
 #pragma unroll
@@ -669,7 +675,7 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                                   (int)kc[t][NC - 1].x, (int)kc[t][NC - 1].y, (int)kc[t][NC - 1].z, (int)kc[t][NC - 1].w};
                 const int sk = (int)(__float_as_uint(ks[t]) >> 23);
 #pragma unroll
-                for (int p = 1; p >= 0; --p)
+                for (int p = QP - 1; p >= 0; --p)
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt)
                         s[qt][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, q8[qt][p], s[qt][t], 0, 0, 0, sk, 0,
@@ -1013,8 +1019,13 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 // 2 x 4096 rows of 32 heads on 8 k keys) 730 us, 1.10 PFLOP/s; matrix
 // instructions take 42 % of a SIMD's cycles and vector instructions 60 %, and
 // they hardly overlap.  148 rows of 37 sequences on 730 keys 34 us, 480 TFLOP/s.
+// At head dim 64 K's codes go to the scaled product with 32 rows a wave, held to
+// 128 registers (2048 rows of 32 heads on 8 k keys 172 us against 179; without
+// the bound 167, but 4 x 2048 rows on themselves 93 against 90); with 16 rows
+// preparing q and two registers more cost what it saves (24 prompts of 200 to
+// 424 tokens 20.8 us against 19.1).
 template <typename T, int HD, int QT, int KG, int P>
-__global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
+__global__ __launch_bounds__(256, HD == 64 && QT == 2 ? 4 : 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 {
     constexpr int NC = HD / 64;
     constexpr int RW = 16 * QT;
@@ -1052,7 +1063,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 
     const int kg = KG == 1 ? 0 : wave & 1;
     const int wr0 = t.t0 + wave / KG * RW;
-    Kv8Rows<T, HD, QT, sizeof(T) == 2 && HD == 128> rows;
+    Kv8Rows<T, HD, QT, sizeof(T) == 2 && (HD == 128 || QT == 2)> rows;
     rows.init(w, t, kvh, wr0, k_hi, lane);
 
     const uint8_t* const codes = (const uint8_t*)w.c.codes + (size_t)kvh * GB;

@@ -598,6 +598,18 @@ def test_attn_sizes_of_keys_and_queries_that_cancel(dtype, ql, hd, up):
 
 
 @gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("up", [-92, 0, 112])
+def test_attn_sizes_that_cancel_in_tall_tiles(hd, up):
+    """The same with 32 rows a wave: 260 sequences of 20 rows, all on one sequence's keys."""
+    pool = Pool(87, [90], 2, hd)
+    pool.scales[:, 0] *= 2.0 ** up
+    n = 260
+    _check_attn(pool, torch.bfloat16, 4, [90] * n, [20] * n, True, 88, q_scale=2.0 ** -up, seq=[0] * n, max_kv=1024,
+                only=set(range(40)) | set(range(20 * n - 20, 20 * n)))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("ql", [1, 40])
 @pytest.mark.parametrize("up", [-90, 100])
