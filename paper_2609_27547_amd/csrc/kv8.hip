@@ -1381,13 +1381,14 @@ int kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, hipS
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
 }
 
+static int64_t kv8_plan_bytes(const Kv8Plan& p, const ebrl_kv8_cache& c, int n) {
+    return p.parts == 1 ? 0 : (int64_t)n * c.kv_heads * p.tiles * p.parts * p.tile_rows * (c.head_dim + 2) * 4;
+}
+
 int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n) {
     if (!kv8_attn_shape_ok(cache, args)) return EBRL_E_INVALID;
     if (args->n == 0 || args->max_q_len == 0) return 0;
-    const Kv8Plan p = kv8_plan(*cache, *args, plan_n);
-    if (p.parts == 1) return 0;
-    const int64_t units = (int64_t)args->n * cache->kv_heads * p.tiles;
-    return units * p.parts * p.tile_rows * (cache->head_dim + 2) * 4;
+    return kv8_plan_bytes(kv8_plan(*cache, *args, plan_n), *cache, args->n);
 }
 
 int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n, hipStream_t s) {
@@ -1400,9 +1401,9 @@ int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int pl
     if (!kv8_pointers_ok(cache) || !a.row_start || !a.kv_len || !kv8_rows_ok(a.q, a.ldq, width, esz) ||
         !kv8_rows_ok(a.out, a.ldo, width, esz) || a.q == a.out)
         return EBRL_E_INVALID;
-    const int64_t need = kv8_attn_workspace(cache, args, plan_n);
-    if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;
     const Kv8Plan p = kv8_plan(*cache, a, plan_n);
+    const int64_t need = kv8_plan_bytes(p, *cache, a.n);
+    if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;
     const int64_t units = (int64_t)a.n * cache->kv_heads * p.tiles;
     // (the join's are fewer: there is one only below some 768 units)
     if (units * p.parts > KV8_MAX_GROUPS) return EBRL_E_INVALID;

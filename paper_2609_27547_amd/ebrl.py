@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -147,9 +148,10 @@ def lib():
         "ebrl_op_gemm_plan": (i32, [i32, i32, i32, i32, i32, i32, vp]),
         "ebrl_op_gemm_noalloc": (i32, [i32, vp, vp, vp, i32, i32, i32, vp]),
         "ebrl_op_stream_read": (i32, [vp, i64, vp, vp]),
-        "ebrl_op_kv8_write": (i32, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8WriteArgs), vp]),
-        "ebrl_op_kv8_attn": (i32, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8AttnArgs), vp]),
-        "ebrl_op_kv8_attn_workspace": (i64, [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8AttnArgs)]),
+        # structs by reference, or their bytes
+        "ebrl_op_kv8_write": (i32, [vp, vp, vp]),
+        "ebrl_op_kv8_attn": (i32, [vp, vp, vp]),
+        "ebrl_op_kv8_attn_workspace": (i64, [vp, vp]),
         "ebrl_alloc_solve": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocLimits),
                                    ctypes.POINTER(AllocResult)]),
         "ebrl_alloc_objective": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocResult)]),
@@ -408,22 +410,33 @@ def _kv8_bad(what: str, *tensors):
         f"; got {None if t is None else (tuple(t.shape), t.stride(), t.dtype, str(t.device))}" for t in tensors))
 
 
+# The C structs, packed: these checks and this packing run before every launch
+# and take longer than a small kernel, so each property of a tensor is asked for
+# once and the structs are made from a format (a ctypes.Structure takes twice
+# the time to fill).
+_KV8_CACHE = struct.Struct("3P5i0P")
+_KV8_WRITE = struct.Struct("10i4P4q6P")
+_KV8_ATTN = struct.Struct("7if2P2q4Pq")
+
+
 def _kv8_cache(codes, scales, table):
-    """The cache as the C struct, and its GPU's index (-1: not on a GPU).  These
-    checks run before every launch, so each property is asked for once."""
+    """The packed cache, its KV heads and head dim and its GPU's index (-1: not on a GPU)."""
     import torch
-    shape, dev = codes.shape, codes.get_device()
-    if len(shape) != 4 or shape[1] != 2 or shape[3] % KV8_PAGE or codes.element_size() != 1 or \
-            not codes.is_contiguous():
+    dev = codes.get_device()
+    try:
+        blocks, two, heads, wide = codes.shape
+    except ValueError:
+        two = wide = 0
+    if two != 2 or not wide or wide % KV8_PAGE or codes.element_size() != 1 or not codes.is_contiguous():
         _kv8_bad("codes are contiguous 8-bit [num_blocks, 2, kv_heads, 16 * head_dim]", codes)
-    if scales.shape != shape[:3] or scales.dtype is not torch.float32 or not scales.is_contiguous() or \
+    if scales.shape != (blocks, 2, heads) or scales.dtype is not torch.float32 or not scales.is_contiguous() or \
             scales.get_device() != dev:
         _kv8_bad("scales are contiguous float32 [num_blocks, 2, kv_heads] where the codes are", scales)
     pages = table.shape
     if len(pages) != 2 or table.dtype is not torch.int32 or not table.is_contiguous() or table.get_device() != dev:
         _kv8_bad("block_table is contiguous int32 [sequences, pages] where the codes are", table)
-    return Kv8Cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), shape[0], pages[0], pages[1], shape[2],
-                    shape[3] // KV8_PAGE), dev
+    hd = wide // KV8_PAGE
+    return _KV8_CACHE.pack(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), blocks, *pages, heads, hd), heads, hd, dev
 
 
 def _kv8_rows(name, t, dtype, dev, rows, width):
@@ -436,13 +449,17 @@ def _kv8_rows(name, t, dtype, dev, rows, width):
     return t.data_ptr(), ld if rows > 1 else max(ld, width)
 
 
-def _kv8_ints(name, t, n, dev):
-    import torch
-    if t is None:
-        return None
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
-        _kv8_bad(f"{name} is {n} contiguous int32 where the cache is", t)
-    return t.data_ptr()
+def _kv8_ints(dtype, dev, *named):
+    """Pointers of the (name, tensor or None, elements) given; 0 for None."""
+    at = []
+    for name, t, n in named:
+        if t is None:
+            at.append(0)
+            continue
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+            _kv8_bad(f"{name} is {n} contiguous int32 where the cache is", t)
+        at.append(t.data_ptr())
+    return at
 
 
 def _kv8_dtype(name, t) -> int:
@@ -458,14 +475,14 @@ def _kv8_call(fn, name, cache, args, dev, stream):
     import torch
     if dev < 0:
         _kv8_bad("the cache is not on a GPU")
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return _kv8_call(fn, name, cache, args, dev, stream)
     if stream is None:
         # the handle alone: a torch.cuda.Stream object takes 2.7 us to make,
         # as long as the launch
         stream = torch._C._cuda_getCurrentRawStream(dev)
-    rc = fn(ctypes.byref(cache), ctypes.byref(args), stream)
+    rc = fn(cache, args, stream)
     if rc != EBRL_OK:
         raise EbrlError(rc, name)
 
@@ -478,16 +495,16 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
     pairs of each axis (empty: no rotation); cos, sin: float32 [positions,
     head_dim / 2].  `stream`: a raw handle whose order the tensors follow."""
     import torch
-    c, dev = _kv8_cache(codes, scales, block_table)
-    hd, n, axes, dtype = c.head_dim, pos0.numel(), len(sections), _kv8_dtype("k", k)
-    rows, torch_dtype, width = k.shape[0], k.dtype, c.kv_heads * hd
+    c, heads, hd, dev = _kv8_cache(codes, scales, block_table)
+    n, axes, dtype = pos0.numel(), len(sections), _kv8_dtype("k", k)
+    rows, torch_dtype, width = k.shape[0], k.dtype, heads * hd
     if not 0 <= max_len < 1 << 31:
         _kv8_bad(f"max_len {max_len}")
     k_at, ldk = _kv8_rows("k", k, torch_dtype, dev, rows, width)
     v_at, ldv = _kv8_rows("v", v, torch_dtype, dev, rows, width)
     if (q is None) != (q_out is None) or axes > 3 or (axes == 0 and q is not None):
         _kv8_bad("q and q_out go together, with one to three axes", q, q_out)
-    q_at = ldq = qo_at = ldqo = q_heads = tab_rows = 0
+    q_at = ldq = qo_at = ldqo = q_heads = tab_rows = cos_at = sin_at = 0
     if q is not None:
         wide = q.shape[-1]
         if wide % hd:
@@ -495,7 +512,6 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
         q_at, ldq = _kv8_rows("q", q, torch_dtype, dev, rows, wide)
         qo_at, ldqo = _kv8_rows("q_out", q_out, torch_dtype, dev, rows, wide)
         q_heads = wide // hd
-    cos_at = sin_at = axis_at = None
     if axes:
         tab_rows = 0 if cos is None else cos.shape[0]
         for t in (cos, sin):
@@ -503,10 +519,14 @@ def op_kv8_write(codes, scales, block_table, k, v, row_start, pos0, max_len, q=N
                     t.get_device() != dev:
                 _kv8_bad(f"cos and sin are contiguous float32 [positions, {hd // 2}] where the cache is", cos, sin)
         cos_at, sin_at = cos.data_ptr(), sin.data_ptr()
-        axis_at = _kv8_ints("axis_pos", axis_pos, rows * axes, dev)
-    a = Kv8WriteArgs(dtype, n, rows, max_len, q_heads, axes, (*sections,), tab_rows, q_at, k_at, v_at, qo_at, ldq, ldk,
-                     ldv, ldqo, _kv8_ints("row_start", row_start, n + 1, dev), _kv8_ints("pos0", pos0, n, dev),
-                     _kv8_ints("seq", seq, n, dev), axis_at, cos_at, sin_at)
+    start_at, pos_at, seq_at, axis_at = _kv8_ints(
+        torch.int32, dev, ("row_start", row_start, n + 1), ("pos0", pos0, n), ("seq", seq, n),
+        ("axis_pos", axis_pos if axes else None, rows * axes))
+    try:
+        a = _KV8_WRITE.pack(dtype, n, rows, max_len, q_heads, axes, *sections, *(0, 0, 0)[axes:], tab_rows, q_at, k_at,
+                            v_at, qo_at, ldq, ldk, ldv, ldqo, start_at, pos_at, seq_at, axis_at, cos_at, sin_at)
+    except struct.error as e:
+        raise EbrlError(-1, f"kv8: sections {sections}: {e}") from e
     _kv8_call(lib().ebrl_op_kv8_write, "ebrl_op_kv8_write", c, a, dev, stream)
 
 
@@ -519,10 +539,16 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     """A workspace for op_kv8_attn calls with these sizes, on the cache's device."""
     import torch
     _kv8_bounds(max_q_len, max_kv_len)
-    c = Kv8Cache(0, 0, 0, codes.shape[0], block_table.shape[0], block_table.shape[1], codes.shape[2],
-                 codes.shape[3] // KV8_PAGE)
-    a = Kv8AttnArgs(_kv8_dtype("q", q), n, q.shape[0], max_q_len, max_kv_len, q.shape[-1] // c.head_dim, 1, 1.0)
-    need = lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(a))
+    if codes.dim() != 4 or codes.shape[3] < KV8_PAGE or block_table.dim() != 2:
+        _kv8_bad("codes are [num_blocks, 2, kv_heads, 16 * head_dim], block_table [sequences, pages]", codes, block_table)
+    blocks, _, heads, wide = codes.shape
+    hd = wide // KV8_PAGE
+    c = _KV8_CACHE.pack(0, 0, 0, blocks, *block_table.shape, heads, hd)
+    dtype = _kv8_dtype("q", q)
+    if not 0 <= n < 1 << 31:
+        _kv8_bad(f"n {n}")
+    a = _KV8_ATTN.pack(dtype, n, q.shape[0], max_q_len, max_kv_len, q.shape[1] // hd, 1, 1.0, *(0,) * 9)
+    need = lib().ebrl_op_kv8_attn_workspace(c, a)
     if need < 0:
         raise EbrlError(need, "ebrl_op_kv8_attn_workspace")
     return torch.empty(need, dtype=torch.uint8, device=codes.device)
@@ -536,8 +562,9 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
     kv8_attn_workspace, one for each chain of calls that may overlap others;
     None makes one for this call (not with an explicit stream, which torch's
     allocator does not follow)."""
-    c, dev = _kv8_cache(codes, scales, block_table)
-    hd, n, dtype = c.head_dim, kv_len.numel(), _kv8_dtype("q", q)
+    import torch
+    c, heads, hd, dev = _kv8_cache(codes, scales, block_table)
+    n, dtype = kv_len.numel(), _kv8_dtype("q", q)
     rows, wide = q.shape
     if wide % hd:
         _kv8_bad(f"q has heads of {hd}", q)
@@ -550,10 +577,14 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
         workspace = kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _kv8_bad("the workspace is contiguous and where the cache is", workspace)
-    a = Kv8AttnArgs(dtype, n, rows, max_q_len, max_kv_len, wide // hd, bool(causal), hd ** -0.5 if scale is None else scale,
-                    q_at, out_at, ldq, ldo, _kv8_ints("row_start", row_start, n + 1, dev),
-                    _kv8_ints("kv_len", kv_len, n, dev), _kv8_ints("seq", seq, n, dev), workspace.data_ptr(),
-                    workspace.nbytes)
+    start_at, len_at, seq_at = _kv8_ints(torch.int32, dev, ("row_start", row_start, n + 1), ("kv_len", kv_len, n),
+                                         ("seq", seq, n))
+    try:
+        a = _KV8_ATTN.pack(dtype, n, rows, max_q_len, max_kv_len, wide // hd, 1 if causal else 0,
+                           hd ** -0.5 if scale is None else scale, q_at, out_at, ldq, ldo, start_at, len_at, seq_at,
+                           workspace.data_ptr(), workspace.nbytes)
+    except (struct.error, OverflowError) as e:
+        raise EbrlError(-1, f"kv8: scale {scale}: {e}") from e
     _kv8_call(lib().ebrl_op_kv8_attn, "ebrl_op_kv8_attn", c, a, dev, stream)
 
 

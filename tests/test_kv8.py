@@ -130,6 +130,41 @@ def test_binding_refuses():
         refused(E.op_kv8_attn, **{**at, **bad})
 
 
+def test_binding_refuses_what_the_structs_do_not_hold():
+    codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
+    table = torch.zeros((1, 4), dtype=torch.int32)
+    k = torch.zeros((1, 128), dtype=torch.bfloat16)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    tab = torch.zeros(4, 32)
+    write = dict(codes=codes, scales=scales, block_table=table, k=k, v=k, row_start=i32(0, 1), pos0=i32(0), max_len=1,
+                 cos=tab, sin=tab)
+    for bad in (dict(sections=(1 << 31,)), dict(sections=(31.5,)), dict(codes=codes[:, :, 0]), dict(codes=codes[..., :0])):
+        with pytest.raises(E.EbrlError):
+            E.op_kv8_write(**{**write, **bad})
+    attn = dict(codes=codes, scales=scales, block_table=table, q=k, out=k.clone(), row_start=i32(0, 1), kv_len=i32(1),
+                max_q_len=1, max_kv_len=1, workspace=torch.empty(0, dtype=torch.uint8))
+    for bad in (dict(scale=1e39), dict(codes=codes[..., :0]), dict(block_table=table[0])):
+        with pytest.raises(E.EbrlError):
+            E.op_kv8_attn(**{**attn, **bad})
+    sizes = dict(codes=codes, block_table=table, q=k, n=1, max_q_len=1, max_kv_len=1)
+    assert E.kv8_attn_workspace(**sizes).numel() == 0
+    for bad in (dict(n=-1), dict(n=1 << 31), dict(codes=codes[0]), dict(codes=codes[..., :0]), dict(block_table=table[0]),
+                dict(q=k[0]), dict(max_kv_len=1 << 31)):
+        with pytest.raises(E.EbrlError):
+            E.kv8_attn_workspace(**{**sizes, **bad})
+
+
+def test_packed_structs_are_the_c_structs():
+    for packed, struct in ((E._KV8_CACHE, E.Kv8Cache), (E._KV8_WRITE, E.Kv8WriteArgs), (E._KV8_ATTN, E.Kv8AttnArgs)):
+        values = list(range(1, 1 + len(packed.unpack(bytes(packed.size)))))
+        a = struct.from_buffer_copy(packed.pack(*values))
+        got = []
+        for name, _ in struct._fields_:
+            x = getattr(a, name)
+            got += list(x) if name == "sections" else [x]
+        assert packed.size == ctypes.sizeof(struct) and got == values
+
+
 def test_reference_encode_matches_torch():
     """The test's own e4m3 rounding against torch's, ties and small values among them."""
     x = np.concatenate([np.linspace(-448, 448, 4001), R.CODE[:127], (R.CODE[:126] + R.CODE[1:127]) / 2,
