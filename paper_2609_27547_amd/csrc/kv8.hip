@@ -563,8 +563,16 @@ template <int NP> EBRL_DEV void kv8_split(float x, __bf16* o) {
 // The state of a wave's 16 QT query rows.  Lane (r, g) holds query r of each
 // 16: its elements 64 c + 16 g .. + 15, its scores for keys 4 g .. 4 g + 3 of
 // each page, and its results in dims 64 c + 16 g .. + 15.
-template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
-    static constexpr int NP = sizeof(T) == 4 ? 3 : 1;   // bf16 terms of a query element and of a weight
+template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
+    static constexpr int NP = sizeof(T) == 4 ? 3 : 1;   // bf16 terms of a query element
+    // WP: bf16 terms of a weight.  Three hold all 24 bits (fp32 rows).  Two are
+    // off by 2^-17 at most: decode, whose time is the cache's bytes (61 sequences
+    // 97.4 us, with one term 97.0 to 99.3).  One is off by 2^-8: prompts, which a
+    // second term would slow by a fifth to two fifths.  Their sum is of the
+    // rounded weights, by a product with ones, so that a row's result is a mean
+    // of its keys' values whatever the rounding (a key that outweighs all others
+    // gives its value), and the vector adds fall away (727 us against 737 a long
+    // prompt, 163 against 171 at head dim 64).
     static constexpr int NC = HD / 64;
     // MX: K's codes enter the first product as they are, in
     // v_mfma_scale_f32_16x16x128_f8f6f4 with the page's scale, and q as two
@@ -584,7 +592,8 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
     i32x8 q8[QT][QP];
     int q8_scale[QT];         // exponent byte of q8[.][0]'s scale; a second term's is 4 less
     f32x4 acc[QT][HD / 16];   // acc[4 c + d][v]: dim 64 c + 16 g + 4 v + d
-    float mx[QT], sum[QT];    // log2 of what the weights are relative to; this lane's share of their sum
+    float mx[QT], sum[QT];    // log2 of what the weights are relative to; WP > 1: this lane's share of their sum
+    f32x4 ones[WP == 1 ? QT : 1];   // WP 1: the whole sum, four times
     int lim[QT];              // keys that the row sees
     int all, end;             // keys that every row, that some row of the wave sees
 
@@ -646,6 +655,7 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
             }
             mx[qt] = -INFINITY;
             sum[qt] = 0.f;
+            if constexpr (WP == 1) ones[qt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) acc[qt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -655,6 +665,15 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
             end = min(end, t.len - t.m + (min(wr0 + 16 * QT, t.rows) - 1) / w.grp + 1);
         }
         if (wr0 >= t.rows) end = 0;
+    }
+
+    // After the last step: sum[] is the rows' whole sum.
+    EBRL_DEV void finish() {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            if constexpr (WP == 1) sum[qt] = ones[qt][0];
+            else sum[qt] = attn_sum_xor16_32(sum[qt]);
+        }
     }
 
     // P pages (an even number; 16 P keys from k0 on) in the lanes' order: kc, vc
@@ -772,7 +791,8 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                 const float nm = fmaxf(mx[qt], ceilf(attn_max_xor16_32(tm[qt]) * scale_log2));
                 const float alpha = mx[qt] == nm ? 1.f : ldexpf(1.0f, (int)fmaxf(mx[qt] - nm, -300.f));
                 mx[qt] = nm;
-                sum[qt] *= alpha;
+                if constexpr (WP == 1) ones[qt] *= alpha;
+                else sum[qt] *= alpha;
 #pragma unroll
                 for (int d = 0; d < HD / 16; ++d) acc[qt][d] *= alpha;
             }
@@ -781,7 +801,7 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
         // 64 c + 4 r + d, a lane's eight keys those that its scores are of
 #pragma unroll
         for (int u = 0; u < P; u += 2) {
-            bf16x8 pb[QT][NP];
+            bf16x8 pb[QT][WP];
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
                 const float use = mx[qt] == -INFINITY ? 0.f : mx[qt];
@@ -792,12 +812,18 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                     for (int v = 0; v < 4; ++v) {
                         const float p = fast_exp2(fmaf(s[qt][u + t][v], scale_log2, -use));
                         ps += p;
-                        __bf16 o[NP];
-                        kv8_split<NP>(p, o);
+                        __bf16 o[WP];
+                        kv8_split<WP>(p, o);
 #pragma unroll
-                        for (int y = 0; y < NP; ++y) pb[qt][y][4 * t + v] = o[y];
+                        for (int y = 0; y < WP; ++y) pb[qt][y][4 * t + v] = o[y];
                     }
-                sum[qt] += ps;
+                if constexpr (WP == 1) {
+                    const __bf16 e = (__bf16)1.f;
+                    ones[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16x8{e, e, e, e, e, e, e, e}, pb[qt][0], ones[qt],
+                                                                      0, 0, 0);
+                } else {
+                    sum[qt] += ps;
+                }
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -807,7 +833,7 @@ template <typename T, int HD, int QT, bool MX> struct Kv8Rows {
                 for (int d = 0; d < 4; ++d) {
                     const bf16x8 va = kv8_bf16(x0[d], x1[d], vs[u], vs[u + 1]);
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p)
+                    for (int p = WP - 1; p >= 0; --p)
 #pragma unroll
                         for (int qt = 0; qt < QT; ++qt)
                             acc[qt][4 * c + d] =
@@ -915,7 +941,7 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
     const size_t gb = (size_t)KV8_PAGE * HD;   // bytes of a (page, K or V, head) group
     const uint8_t* const codes = (const uint8_t*)w.c.codes + kvh * gb;
     const int k_at = r * 64 + g * 16, v_at = lane * 16;
-    Kv8Rows<T, HD, 1, false> rows;
+    Kv8Rows<T, HD, 1, false, sizeof(T) == 4 ? 3 : 2> rows;
     const int p_hi = (k_hi + KV8_PAGE - 1) / KV8_PAGE;
     rows.init(w, t, kvh, 0, k_hi, lane);
     for (int kb = k_lo; kb < k_hi; kb += BATCH * STEP) {
@@ -968,7 +994,7 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
             load(s + 3, kn, vn);
         }
     }
-    rows.sum[0] = attn_sum_xor16_32(rows.sum[0]);
+    rows.finish();
 
     const size_t to0 = ((size_t)unit * w.parts + part) * 16;
     if constexpr (KW == 1) {
@@ -1063,7 +1089,7 @@ __global__ __launch_bounds__(256, HD == 64 && QT == 2 ? 4 : 2) void kv8_prompt_k
 
     const int kg = KG == 1 ? 0 : wave & 1;
     const int wr0 = t.t0 + wave / KG * RW;
-    Kv8Rows<T, HD, QT, sizeof(T) == 2 && (HD == 128 || QT == 2)> rows;
+    Kv8Rows<T, HD, QT, sizeof(T) == 2 && (HD == 128 || QT == 2), sizeof(T) == 4 ? 3 : 1> rows;
     rows.init(w, t, kvh, wr0, k_hi, lane);
 
     const uint8_t* const codes = (const uint8_t*)w.c.codes + (size_t)kvh * GB;
@@ -1123,8 +1149,7 @@ __global__ __launch_bounds__(256, HD == 64 && QT == 2 ? 4 : 2) void kv8_prompt_k
             }
         }
     }
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) rows.sum[qt] = attn_sum_xor16_32(rows.sum[qt]);
+    rows.finish();
     if constexpr (KG == 2) {
         // the second wave of a pair hands its state to the first, in the buffers
         constexpr int LD = HD + 4;

@@ -140,7 +140,11 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
     second's least step, 2^-10 / 16, so by 2^-21 of the largest at most; the exponent's argument is rounded (2^-23 of its size
     and of the score's) and exp2 is good to 2^-22; a weight enters the second
     product rounded to bf16 (2^-8) for bf16 rows, whole for fp32; the two sums
-    over keys add 2^-23 a term; the result is rounded to its type."""
+    over keys add 2^-23 a term; the result is rounded to its type.  Where the
+    sum that divides is of the weights as rounded, p (1 + d) with |d| <= 2^-8,
+    the result moves by sum p d (v - o) / sum p (1 + d), so by 2^-8 of the mean
+    |v - o| <= mean |v| + |o|, in place of 2^-8 of the mean |v|, to first order;
+    1 / (1 - 2^-8) of it altogether."""
     rows, hq, hd = q.shape
     hkv = codes.shape[2]
     out, bound = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
@@ -178,5 +182,6 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
                     dp = ds + (s.max() - low + 1) * 2.0 ** -22 + 2.0 ** -22
                     rel = 2 * dp + 2 * (len(use) * (1 if bf16 else 3) + 8) * 2.0 ** -23 + (2.0 ** -8 if bf16 else 0)
                     out[r0 + j, h] = o
-                    bound[r0 + j, h] = mag * rel + np.abs(o) * (2.0 ** -8 if bf16 else 2.0 ** -24) + 2.0 ** -120
+                    sums = np.abs(o) * 2.0 ** -8 + (mag + np.abs(o)) * 2.0 ** -15 if bf16 else 0
+                    bound[r0 + j, h] = mag * rel + sums + np.abs(o) * (2.0 ** -8 if bf16 else 2.0 ** -24) + 2.0 ** -120
     return out, bound
