@@ -1046,7 +1046,6 @@ int ebrl_policy_create(const ebrl_config* config, uint64_t seed, ebrl_policy** o
         for (int b = 0; b < pad_blocks; ++b) {
             pad.blocks.push_back(budget_blocks + b);
             p->bt_host[(size_t)p->pad_env * p->bt_stride + b] = budget_blocks + b;
-            if (p->kv8) p->bt_host[(size_t)kv8_call_row(p, p->pad_env) * p->bt_stride + b] = budget_blocks + b;
         }
         for (int l = 0; l < c.layers; ++l)
             HIPCHK(p, hipMemset((char*)dec_kv(p, l).base + (size_t)budget_blocks * p->block_elems * p->kv_esz, 0,
@@ -1464,7 +1463,9 @@ int ebrl_decode_actions(ebrl_policy* p, const int32_t* env_ids, int32_t n, int32
         std::iota(start.begin(), start.end(), 0);
         for (int len : kvlen) pos0.push_back(len - 1);
         for (int e : seq_env) {
-            call_row.push_back(kv8_call_row(p, e));
+            // rows of the padding env have no table row: they write nothing
+            // (several would share a page) and attend to nothing
+            call_row.push_back(e == p->pad_env ? -1 : kv8_call_row(p, e));
             add_spare(p, spare, e);
         }
     }

@@ -1048,9 +1048,8 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 // At head dim 64 K's codes go to the scaled product with 32 rows a wave, held to
 // 128 registers (2048 rows of 32 heads on 8 k keys 172 us against 179 with
 // conversions; without the bound 167, but 4 x 2048 rows on themselves 93 against
-// 90); with 16 rows
-// preparing q and two registers more cost what it saves (24 prompts of 200 to
-// 424 tokens 20.8 us against 19.1).
+// 90); with 16 rows preparing q and two registers more cost what it saves (24
+// prompts of 200 to 424 tokens 20.8 us against 19.1).
 template <typename T, int HD, int QT, int KG, int P>
 __global__ __launch_bounds__(256, HD == 64 && QT == 2 ? 4 : 2) void kv8_prompt_kernel(Kv8AttnKernelArgs w)
 {
