@@ -112,9 +112,10 @@ int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_a
  * that sees no key gets zeros; rows outside every sequence are left as they
  * were.  Scores, the softmax's maximum and sum and the weighted sum are held
  * in 32 bits; bf16 rows' weights enter the product with V as bf16, in two terms
- * where a KV head has at most 16 rows a sequence.  Weights go up to 2^10: the
- * sum overflows to infinity only where the keys' values, times 2^10 and their
- * number, pass the 32-bit range.  With few rows the keys are cut into parts that
+ * where a KV head has at most 16 rows a sequence.  Weights go up to 2^11: the
+ * sum overflows to infinity only where the keys' values, times 2^11 and their
+ * number, pass the 32-bit range.  Scores, times log2(e), are floats: from 2^24
+ * on they lie whole numbers apart.  With few rows the keys are cut into parts that
  * run at the same time and are joined in their order by a second launch.  The
  * cut follows n, max_q_len, max_kv_len and the heads.
  *

@@ -27,6 +27,7 @@ constexpr int KV8_PAGE = EBRL_KV8_PAGE;
 constexpr int KV8_EXP_MIN = -100, KV8_EXP_MAX = 120;   // 448 * 2^120 > FLT_MAX
 constexpr int KV8_Q_EXP_MIN = -122;   // of a query row's scale: every bf16 number is whole in two terms
 constexpr float KV8_SLACK = 10.f;     // log2 of the largest weight that a softmax keeps
+constexpr float KV8_FAR = 0x1p24f;    // scores from here on are whole numbers, rounded before the maximum is taken off
 constexpr int KV8_MAX_PARTS = 256;    // parts that a row's keys are cut into
 
 // ----------------------------------------------------------------- write --
@@ -560,6 +561,15 @@ template <int NP> EBRL_DEV void kv8_split(float x, __bf16* o) {
     }
 }
 
+// x - m with x = s scale rounded as a float.  The fused form takes the exact
+// product, which from 2^24 on lies further than one from x: where m is the
+// largest x, weights relative to it would be anything.
+EBRL_DEV float kv8_scaled(float s, float scale, float m) {
+#pragma clang fp contract(off)
+    const float x = s * scale;
+    return x - m;
+}
+
 // The state of a wave's 16 QT query rows.  Lane (r, g) holds query r of each
 // 16: its elements 64 c + 16 g .. + 15, its scores for keys 4 g .. 4 g + 3 of
 // each page, and its results in dims 64 c + 16 g .. + 15.
@@ -596,6 +606,7 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
     f32x4 ones[WP == 1 ? QT : 1];   // WP 1: the whole sum, four times
     int lim[QT];              // keys that the row sees
     int all, end;             // keys that every row, that some row of the wave sees
+    bool far;                 // some row's mx is KV8_FAR and more
 
     EBRL_DEV void init(const Kv8AttnKernelArgs& w, const Kv8Tile& t, int kvh, int wr0, int k_hi, int lane) {
         const int r = lane & 15, g = lane >> 4;
@@ -659,6 +670,7 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) acc[qt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        far = false;
         all = end = k_hi;
         if (w.a.causal) {
             all = min(all, t.len - t.m + min(wr0, t.rows - 1) / w.grp + 1);
@@ -771,9 +783,9 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
         }
         // Weights are 2^(x - mx), x = score log2(e) / sqrt(hd).  mx is a whole
         // number that follows the row's maximum: it moves when a weight would
-        // pass 2^KV8_SLACK, and rescaling by a power of two is exact, so
-        // neither the moves nor the cut into steps changes a weight's
-        // rounding to bf16.
+        // pass 2^KV8_SLACK, and rescaling by a power of two is exact, so a
+        // weight's last 32-bit place is all that the moves and the cut into
+        // steps can change.
         bool move = false;
         float tm[QT];
 #pragma unroll
@@ -783,20 +795,38 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
             for (int t = 0; t < P; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) tm[qt] = fmaxf(tm[qt], s[qt][t][v]);
-            move |= tm[qt] * scale_log2 > mx[qt] + KV8_SLACK;
+            move |= kv8_scaled(tm[qt], scale_log2, mx[qt]) > KV8_SLACK;
         }
         if (__any(move)) {
+            far = false;
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
                 const float nm = fmaxf(mx[qt], ceilf(attn_max_xor16_32(tm[qt]) * scale_log2));
                 const float alpha = mx[qt] == nm ? 1.f : ldexpf(1.0f, (int)fmaxf(mx[qt] - nm, -300.f));
                 mx[qt] = nm;
+                far |= fabsf(nm) >= KV8_FAR && nm != -INFINITY;
                 if constexpr (WP == 1) ones[qt] *= alpha;
                 else sum[qt] *= alpha;
 #pragma unroll
                 for (int d = 0; d < HD / 16; ++d) acc[qt][d] *= alpha;
             }
+            far = __any(far);
         }
+        // x - mx, for rows whose mx is far; the others' are what the fused form
+        // below gives, which then takes them as they are
+        if (far) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+                const bool row_far = fabsf(mx[qt]) >= KV8_FAR;
+                const float use = mx[qt] == -INFINITY ? 0.f : mx[qt];
+#pragma unroll
+                for (int t = 0; t < P; ++t)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        s[qt][t][v] = row_far ? kv8_scaled(s[qt][t][v], scale_log2, use) : fmaf(s[qt][t][v], scale_log2, -use);
+            }
+        }
+        const float by = far ? 1.f : scale_log2;
         // O^T += V^T P^T for a pair of pages: row r of product 4 c + d is dim
         // 64 c + 4 r + d, a lane's eight keys those that its scores are of
 #pragma unroll
@@ -804,13 +834,13 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
             bf16x8 pb[QT][WP];
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-                const float use = mx[qt] == -INFINITY ? 0.f : mx[qt];
+                const float use = far || mx[qt] == -INFINITY ? 0.f : mx[qt];
                 float ps = 0.f;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const float p = fast_exp2(fmaf(s[qt][u + t][v], scale_log2, -use));
+                        const float p = fast_exp2(fmaf(s[qt][u + t][v], by, -use));
                         ps += p;
                         __bf16 o[WP];
                         kv8_split<WP>(p, o);

@@ -866,3 +866,53 @@ def test_calls_on_another_stream():
         E.op_kv8_attn(codes, scales, table, q, got.zero_(), st, kl, 1, 300)
     s.synchronize()
     assert torch.equal(want, got)
+
+
+# (sequences, query rows of each, keys, keys of a step's size, bound on the keys): the four ways to cut a call, with
+# 16 rows a wave (of which head dim 128 gives K's codes to the scaled product) and 32, in one part and in several
+LADDERS = {"decode": (1, 1, 60, 1, 60), "decode-wave": (600, 1, 60, 1, 60), "decode-parts": (1, 3, 2100, 40, 2100),
+           "prompt": (1, 40, 60, 1, 60), "prompt-parts": (1, 24, 2100, 40, 2100), "prompt-64": (260, 33, 60, 1, 60),
+           "prompt-128": (260, 20, 60, 1, 1024)}
+
+
+def _ladder(kind, hd, sign, up, dt, causal=True):
+    """Keys in steps, each step's scores above those of the step before by a sixtieth of the largest, queries of one size
+    in all dims: a row's result is the value of the last step that it sees.  Scores in log2 go up to about 2^up (sign 1)
+    or start there (sign -1).  Returns (got, want), [rows, heads, hd]."""
+    n, ql, keys, tie, bound = LADDERS[kind]
+    rng = np.random.default_rng(100 + up)
+    hkv, grp = 2, 2
+    pool = Pool(101, [0], hkv, hd, room=keys)
+    step = np.arange(keys) // tie
+    count = step + 1 if sign > 0 else step[-1] + 1 - step
+    assert count.max() <= hd
+    k = sign * (np.arange(hd) < count[:, None])[:, None, :] * np.ones((1, hkv, 1)) * 2.0 ** (up // 2)
+    v = rng.standard_normal((step[-1] + 1, hkv, hd))[step]
+    R.write(pool.codes, pool.scales, pool.table, k, v, [0, keys], [0], keys)
+    size = rng.uniform(1, 2, (n * ql, hkv * grp, 1)) * 2.0 ** (up - up // 2) / (60 * hd ** -0.5)
+    q = torch.from_numpy((size * np.ones(hd)).reshape(n * ql, -1)).to(dt).cuda()
+    codes, scales, table = pool.gpu()
+    out = torch.full_like(q, 7.0)
+    E.op_kv8_attn(codes, scales, table, q, out, _ints(ql * np.arange(n + 1)), _ints([keys] * n), ql, bound, causal=causal,
+                  seq=_ints([0] * n))
+    _, V, _ = R.gather(pool.codes, pool.scales, pool.table[0], keys)
+    last = keys - ql + np.arange(ql) if causal else np.full(ql, keys - 1)
+    want = np.tile(np.repeat(V[last], grp, axis=1), (n, 1, 1))
+    return out.double().cpu().numpy().reshape(want.shape), want
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kind", list(LADDERS))
+def test_attn_large_scores_give_the_largest_keys_value(kind, hd, dtype):
+    """Scores of 2^20 to 2^100 in log2, of either sign.  A sixtieth of 2^20 is more than any weight's range: one step's
+    value is all of the result, off by the rounding of the weights (one bf16 term: the sum takes them as rounded; two: 2^-17
+    of them; three: 2^-24), of up to 40 sums of them and of the result."""
+    for up in (20, 24, 25, 27, 30, 33, 40, 60, 100):
+        for sign in (1, -1):
+            for causal in (True, False):
+                got, want = _ladder(kind, hd, sign, up, DT[dtype], causal)
+                tol = 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -17 if dtype == "bf16" else 2.0 ** -16
+                bad = ~(np.abs(got - want) <= tol * np.abs(want))
+                assert not bad.any(), (up, sign, causal, got[bad][:4], want[bad][:4])
