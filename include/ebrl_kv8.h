@@ -109,8 +109,9 @@ int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_a
 /* out = softmax(scale q K^T + mask) V over the cache: one query row a
  * sequence (a decode step), a prompt's rows, or any ragged mix.  Keys a row
  * does not see do not count, whatever their slots hold, NaN included; a row
- * that sees no key gets zeros; rows outside every sequence are left as they
- * were.  Scores, the softmax's maximum and sum and the weighted sum are held
+ * that sees no key gets zeros; one whose query is not finite, or whose scores
+ * pass the 32-bit range (the largest upwards, or all downwards), is NaN; rows
+ * outside every sequence are left as they were.  Scores, the softmax's maximum and sum and the weighted sum are held
  * in 32 bits; bf16 rows' weights enter the product with V as bf16, in two terms
  * where a KV head has at most 16 rows a sequence.  Weights go up to 2^11: the
  * sum overflows to infinity only where the keys' values, times 2^11 and their

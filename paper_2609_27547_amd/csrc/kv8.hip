@@ -11,6 +11,8 @@
 //   four significant bits and a power of two, so exact.
 // kv8_decode_kernel, kv8_prompt_kernel: few and many rows; kv8_join_kernel:
 //   parts of a row's keys put together.
+#include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include "../../include/ebrl.h"
@@ -540,6 +542,18 @@ EBRL_DEV Kv8Tile kv8_tile(const Kv8AttnKernelArgs& w, int i, int tile) {
     return t;
 }
 
+// First key of a part of a (sequence, KV head) that is there, or INT_MAX.
+EBRL_DEV int kv8_first_key(const Kv8AttnKernelArgs& w, unsigned pair, int part) {
+    asm volatile("" : "+s"(pair));   // the table's row is worked out again, not kept through the loop over keys
+    const int trow = kv8_table_row(w, pair / w.c.kv_heads);
+    if (trow < 0) return INT_MAX;
+    const int* const table = w.c.block_table + (size_t)trow * w.c.table_stride;
+    const int lo = part * (w.part_keys / KV8_PAGE), hi = min(lo + w.part_keys / KV8_PAGE, w.c.table_stride);
+    for (int p = lo; p < hi; ++p)
+        if (table[p] >= 0 && table[p] < w.c.num_blocks) return p * KV8_PAGE;
+    return INT_MAX;
+}
+
 // Eight codes (two dwords) as bf16, the scales applied.
 EBRL_DEV bf16x8 kv8_bf16(unsigned lo, unsigned hi, float sl, float sh) {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sl, false);
@@ -569,6 +583,9 @@ EBRL_DEV float kv8_scaled(float s, float scale, float m) {
     const float x = s * scale;
     return x - m;
 }
+
+// What a row's weighted sum is multiplied by: 0 where it sees no key.
+EBRL_DEV float kv8_inverse(float mx, float sum) { return mx == -INFINITY ? 0.f : 1.f / sum; }
 
 // The state of a wave's 16 QT query rows.  Lane (r, g) holds query r of each
 // 16: its elements 64 c + 16 g .. + 15, its scores for keys 4 g .. 4 g + 3 of
@@ -679,8 +696,20 @@ template <typename T, int HD, int QT, bool MX, int WP> struct Kv8Rows {
         if (wr0 >= t.rows) end = 0;
     }
 
-    // After the last step: sum[] is the rows' whole sum.
-    EBRL_DEV void finish() {
+    // After the last step: sum[] is the rows' whole sum.  A row that sees keys
+    // of the (sequence, KV head)'s part but whose scores are all -infinity gets
+    // a finite maximum: its result, 0 over a sum of 0, is NaN, and not that of
+    // a row that sees no key.  k_first: the wave's first key.
+    EBRL_DEV void finish(const Kv8AttnKernelArgs& w, unsigned pair, int part, int k_first) {
+        bool none = false;
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) none |= mx[qt] == -INFINITY && k_first < lim[qt];
+        if (__any(none)) {
+            const int first = kv8_first_key(w, pair, part);
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+                if (first < lim[qt]) mx[qt] = fmaxf(mx[qt], -FLT_MAX);
+        }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
             if constexpr (WP == 1) sum[qt] = ones[qt][0];
@@ -913,7 +942,7 @@ template <typename T, int HD>
 EBRL_DEV void kv8_store(const Kv8AttnKernelArgs& w, const f32x4 (&acc)[HD / 16], float mx, float sum, int parts, T* out,
                         size_t to, int g)
 {
-    const float inv = parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = parts > 1 ? 1.f : kv8_inverse(mx, sum);
 #pragma unroll
     for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
@@ -1024,7 +1053,7 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
             load(s + 3, kn, vn);
         }
     }
-    rows.finish();
+    rows.finish(w, unit, part, k_lo + kw * 32);
 
     const size_t to0 = ((size_t)unit * w.parts + part) * 16;
     if constexpr (KW == 1) {
@@ -1056,7 +1085,7 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
                 o += wt * *reinterpret_cast<const f32x4*>(&s_o[y][row][d]);
             }
             if (t.parts == 1) {
-                const float inv = L == 0.f ? 0.f : 1.f / L;
+                const float inv = kv8_inverse(M, L);
                 st4<T>(kv8_out<T, HD>(w, t, kvh, row) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
             } else {
                 *reinterpret_cast<f32x4*>(w.part_o + (to0 + row) * HD + d) = o;
@@ -1179,7 +1208,7 @@ __global__ __launch_bounds__(256, HD == 64 && QT == 2 ? 4 : 2) void kv8_prompt_k
             }
         }
     }
-    rows.finish();
+    rows.finish(w, u, part, k_lo + kg * 32);
     if constexpr (KG == 2) {
         // the second wave of a pair hands its state to the first, in the buffers
         constexpr int LD = HD + 4;
@@ -1284,7 +1313,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnKernelArgs w)
         if (PG == 4) o[v] += swz_xor16_f(o[v]);
         o[v] += __shfl_xor(o[v], 32, 64);
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const float inv = kv8_inverse(M, L);
     if (lane < LPR) st4<T>(kv8_out<T, HD>(w, t, kvh, t.t0 + row) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 

@@ -916,3 +916,40 @@ def test_attn_large_scores_give_the_largest_keys_value(kind, hd, dtype):
                 tol = 2.0 ** -8 + 2.0 ** -16 + 2.0 ** -17 if dtype == "bf16" else 2.0 ** -16
                 bad = ~(np.abs(got - want) <= tol * np.abs(want))
                 assert not bad.any(), (up, sign, causal, got[bad][:4], want[bad][:4])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kind", list(LADDERS))
+def test_attn_scores_that_are_all_minus_infinity(kind, hd, dtype):
+    """A row that sees keys, every score of which is -infinity, is NaN: it is no row that sees none.  One score that is
+    not leaves it that key's value.  Rows that see no key stay zeros; the others hold to the rounding of two weights."""
+    n, ql, keys, _, bound = LADDERS[kind]
+    rng = np.random.default_rng(110)
+    pool = Pool(111, [0], 2, hd, room=keys)
+    k = rng.uniform(1, 2, (keys, 2, hd)) * 2.0 ** 70
+    k[0, :, 7] = 0
+    R.write(pool.codes, pool.scales, pool.table, k, rng.standard_normal((keys, 2, hd)), [0, keys], [0], keys)
+    codes, scales, table = pool.gpu()
+    _, V, _ = R.gather(pool.codes, pool.scales, pool.table[0], keys)
+    q = torch.from_numpy(rng.uniform(1, 2, ((n + 1) * ql, 4 * hd)) * 2.0 ** -76).to(DT[dtype]).cuda()
+    end = n * ql                                  # a last sequence, whose first rows see no key
+    lens = [keys] * n + [max(0, ql - 3)]
+    res = []
+    for bad in (False, True):
+        if bad:
+            q[0, 3] = q[end, 3] = float("-inf")   # head 0
+            q[ql // 2, hd:2 * hd] = -2.0 ** 70    # head 1: finite, every score past the range
+            q[ql - 1, 2 * hd:3 * hd] = 0          # head 2: all but key 0's
+            q[ql - 1, 2 * hd + 7] = -2.0 ** 70
+        out = torch.full_like(q, 7.0)
+        E.op_kv8_attn(codes, scales, table, q, out, _ints(ql * np.arange(n + 2)), _ints(lens), ql, bound,
+                      seq=_ints([0] * (n + 1)))
+        res.append(out.double().cpu().numpy().reshape(-1, 4, hd))
+    want = res[0]
+    assert np.all(want[end:end + min(ql, 3)] == 0)
+    want[0, 0] = want[ql // 2, 1] = np.nan
+    want[ql - 1, 2] = V[0, 1]
+    assert np.array_equal(np.isnan(res[1]), np.isnan(want))
+    assert np.nanmax(np.abs(res[1] - want)) <= 2.0 ** -6 * np.abs(V).max()
