@@ -391,9 +391,9 @@ def op_stream_read(buf, out, stream=None) -> None:
 
 
 # ------------------------------------------------------- 8-bit KV cache --
-# include/ebrl_kv8.h.  The cache is three tensors on one GPU: codes, any 8-bit
-# dtype, [num_blocks, 2, kv_heads, 16 * head_dim]; scales, float32
-# [num_blocks, 2, kv_heads]; block_table, int32 [sequences, pages].
+# include/ebrl_kv8.h.  The cache is three tensors on one GPU: codes, float8_e4m3fn
+# (or their bytes, uint8 or int8), [num_blocks, 2, kv_heads, 16 * head_dim]; scales,
+# float32 [num_blocks, 2, kv_heads]; block_table, int32 [sequences, pages].
 
 KV8_PAGE = 16
 
@@ -419,6 +419,12 @@ _KV8_WRITE = struct.Struct("10i4P4q6P")
 _KV8_ATTN = struct.Struct("7if2P2q4Pq")
 
 
+def _kv8_codes(t) -> bool:
+    import torch
+    dtype = t.dtype
+    return dtype is torch.float8_e4m3fn or dtype is torch.uint8 or dtype is torch.int8
+
+
 def _kv8_cache(codes, scales, table):
     """The packed cache, its KV heads and head dim and its GPU's index (-1: not on a GPU)."""
     import torch
@@ -427,8 +433,8 @@ def _kv8_cache(codes, scales, table):
         blocks, two, heads, wide = codes.shape
     except ValueError:
         two = wide = 0
-    if two != 2 or not wide or wide % KV8_PAGE or codes.element_size() != 1 or not codes.is_contiguous():
-        _kv8_bad("codes are contiguous 8-bit [num_blocks, 2, kv_heads, 16 * head_dim]", codes)
+    if two != 2 or not wide or wide % KV8_PAGE or not _kv8_codes(codes) or not codes.is_contiguous():
+        _kv8_bad("codes are contiguous float8_e4m3fn or bytes [num_blocks, 2, kv_heads, 16 * head_dim]", codes)
     if scales.shape != (blocks, 2, heads) or scales.dtype is not torch.float32 or not scales.is_contiguous() or \
             scales.get_device() != dev:
         _kv8_bad("scales are contiguous float32 [num_blocks, 2, kv_heads] where the codes are", scales)
@@ -539,7 +545,7 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     """A workspace for op_kv8_attn calls with these sizes, on the cache's device."""
     import torch
     _kv8_bounds(max_q_len, max_kv_len)
-    if codes.dim() != 4 or codes.shape[3] < KV8_PAGE or block_table.dim() != 2:
+    if codes.dim() != 4 or codes.shape[3] < KV8_PAGE or not _kv8_codes(codes) or block_table.dim() != 2:
         _kv8_bad("codes are [num_blocks, 2, kv_heads, 16 * head_dim], block_table [sequences, pages]", codes, block_table)
     blocks, _, heads, wide = codes.shape
     hd = wide // KV8_PAGE

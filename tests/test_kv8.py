@@ -953,3 +953,23 @@ def test_attn_scores_that_are_all_minus_infinity(kind, hd, dtype):
     want[ql - 1, 2] = V[0, 1]
     assert np.array_equal(np.isnan(res[1]), np.isnan(want))
     assert np.nanmax(np.abs(res[1] - want)) <= 2.0 ** -6 * np.abs(V).max()
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.bool])
+def test_binding_refuses_codes_of_other_formats(dtype):
+    """Bytes are taken as e4m3 codes; a type that says they are something else is refused."""
+    codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
+    other = codes.view(torch.uint8).view(dtype)
+    table = torch.zeros((1, 4), dtype=torch.int32)
+    k = torch.zeros((1, 128), dtype=torch.bfloat16)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(E.EbrlError, match="codes are"):
+        E.op_kv8_write(other, scales, table, k, k, i32(0, 1), i32(0), 1)
+    with pytest.raises(E.EbrlError, match="codes are"):
+        E.op_kv8_attn(other, scales, table, k, k.clone(), i32(0, 1), i32(1), 1, 1)
+    with pytest.raises(E.EbrlError, match="codes are"):
+        E.kv8_attn_workspace(other, table, k, 1, 1, 1)
+    for raw in (torch.uint8, torch.int8, torch.float8_e4m3fn):
+        with pytest.raises(E.EbrlError, match="not on a GPU"):
+            E.op_kv8_write(codes.view(torch.uint8).view(raw), scales, table, k, k, i32(0, 1), i32(0), 1)
+        assert E.kv8_attn_workspace(codes.view(torch.uint8).view(raw), table, k, 1, 1, 1).numel() == 0
