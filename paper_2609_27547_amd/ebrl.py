@@ -452,7 +452,7 @@ def _kv8_rows(name, t, dtype, dev, rows, width):
     ld, one = t.stride()
     if one != 1 and width > 1:
         _kv8_bad(f"{name} has contiguous rows", t)
-    return t.data_ptr(), ld if rows > 1 else max(ld, width)
+    return t.data_ptr(), ld if rows > 1 else width
 
 
 def _kv8_ints(dtype, dev, *named):

@@ -973,3 +973,15 @@ def test_binding_refuses_codes_of_other_formats(dtype):
         with pytest.raises(E.EbrlError, match="not on a GPU"):
             E.op_kv8_write(codes.view(torch.uint8).view(raw), scales, table, k, k, i32(0, 1), i32(0), 1)
         assert E.kv8_attn_workspace(codes.view(torch.uint8).view(raw), table, k, 1, 1, 1).numel() == 0
+
+
+def test_binding_takes_one_row_of_any_stride():
+    """A single row's stride says nothing: it is not held to the 16 bytes that rows are apart by."""
+    buf = torch.zeros((3, 130), dtype=torch.bfloat16)
+    assert E._kv8_rows("k", buf[:1, :128], torch.bfloat16, -1, 1, 128) == (buf.data_ptr(), 128)
+    assert E._kv8_rows("k", buf[:, :128], torch.bfloat16, -1, 3, 128) == (buf.data_ptr(), 130)
+    codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
+    k = buf[:1, :128]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(E.EbrlError, match="not on a GPU"):
+        E.op_kv8_write(codes, scales, torch.zeros((1, 4), dtype=torch.int32), k, k, i32(0, 1), i32(0), 1)
