@@ -42,7 +42,7 @@ typedef struct ebrl_kv8_cache {
     float* scales;               /* device [num_blocks][2][kv_heads] */
     const int32_t* block_table;  /* device [table_rows][table_stride] page ids */
     int32_t num_blocks, table_rows, table_stride;
-    int32_t kv_heads, head_dim;  /* head_dim 64 or 128 */
+    int32_t kv_heads, head_dim;  /* kv_heads 1 to 2^20, head_dim 64 or 128 */
 } ebrl_kv8_cache;
 
 typedef struct ebrl_kv8_write_args {
@@ -50,7 +50,7 @@ typedef struct ebrl_kv8_write_args {
     int32_t n;                   /* sequences */
     int32_t rows;                /* rows of q, k, v */
     int32_t max_len;             /* most new tokens of a sequence */
-    int32_t q_heads;             /* heads of q; 0: no q */
+    int32_t q_heads;             /* heads of q, at most 2^20; 0: no q */
     int32_t n_axes;              /* rotary axes, 1 to 3; 0: no rotation (then no q) */
     int32_t sections[3];         /* pairs of each axis, >= 1, sum head_dim / 2 */
     int32_t tab_rows;            /* rows of cos_tab, sin_tab */
@@ -88,7 +88,7 @@ typedef struct ebrl_kv8_attn_args {
     int32_t rows;                /* rows of q and out */
     int32_t max_q_len;           /* most query rows of a sequence */
     int32_t max_kv_len;          /* most keys of a sequence, at most 2^30; more are not seen */
-    int32_t q_heads;             /* a multiple of kv_heads: query head h reads KV head h / (q_heads / kv_heads) */
+    int32_t q_heads;             /* a multiple of kv_heads, at most 2^20: query head h reads KV head h / (q_heads / kv_heads) */
     int32_t causal;              /* 0: every row sees all keys; else row j of m sees keys 0 .. kv_len - m + j */
     float scale;                 /* of the scores, > 0 (commonly 1 / sqrt(head_dim)) */
     const void* q;               /* device rows, as in ebrl_kv8_write_args */

@@ -1369,9 +1369,12 @@ static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a, in
     return p;
 }
 
+constexpr int64_t KV8_MAX_GROUPS = 1 << 23;   // workgroups of 256 threads in a launch: under 2^32 threads
+constexpr int KV8_MAX_HEADS = 1 << 20;        // a row's elements are counted in 32 bits
+
 static bool kv8_cache_ok(const ebrl_kv8_cache* c) {
     return c && c->num_blocks >= 1 && c->table_rows >= 1 && c->table_stride >= 1 && c->table_stride < (1 << 27) &&
-           c->kv_heads >= 1 && (c->head_dim == 64 || c->head_dim == 128);
+           c->kv_heads >= 1 && c->kv_heads <= KV8_MAX_HEADS && (c->head_dim == 64 || c->head_dim == 128);
 }
 static bool kv8_pointers_ok(const ebrl_kv8_cache* c) {
     return c->codes && c->scales && c->block_table && (uintptr_t)c->codes % 16 == 0 && (uintptr_t)c->scales % 4 == 0 &&
@@ -1381,14 +1384,18 @@ static bool kv8_pointers_ok(const ebrl_kv8_cache* c) {
 static bool kv8_rows_ok(const void* p, int64_t ld, int64_t width, int esz) {
     return p && (uintptr_t)p % 16 == 0 && ld >= width && ld * esz % 16 == 0 && ld < ((int64_t)1 << 40);
 }
-constexpr int64_t KV8_MAX_GROUPS = 1 << 23;   // workgroups of 256 threads in a launch: under 2^32 threads
 
 static bool kv8_attn_shape_ok(const ebrl_kv8_cache* c, const ebrl_kv8_attn_args* a) {
     return kv8_cache_ok(c) && a && (a->dtype == EBRL_DTYPE_BF16 || a->dtype == EBRL_DTYPE_FP32) && a->n >= 0 &&
            a->rows >= 0 && a->max_q_len >= 0 && a->max_kv_len >= 0 &&
-           a->max_kv_len <= (1 << 30) && a->q_heads >= 1 && a->q_heads % c->kv_heads == 0 &&
+           a->max_kv_len <= (1 << 30) && a->q_heads >= 1 && a->q_heads <= KV8_MAX_HEADS &&
+           a->q_heads % c->kv_heads == 0 &&
            (int64_t)a->max_q_len * (a->q_heads / c->kv_heads) < (1 << 30);
 }
+
+// Whether a cut for n sequences can be counted: a workgroup, at least, for each
+// (sequence, KV head), in 64 bits with their tiles and parts.
+static bool kv8_pairs_ok(const ebrl_kv8_cache& c, int n) { return (int64_t)n * c.kv_heads <= KV8_MAX_GROUPS; }
 
 template <typename T, int HD>
 static void kv8_write_launch(bool token, const Kv8WriteKernelArgs& w, unsigned groups, hipStream_t s) {
@@ -1420,7 +1427,7 @@ int kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, hipS
     const ebrl_kv8_write_args& a = *args;
     const int hd = cache->head_dim, hkv = cache->kv_heads;
     if ((a.dtype != EBRL_DTYPE_BF16 && a.dtype != EBRL_DTYPE_FP32) || a.n < 0 || a.rows < 0 || a.max_len < 0 ||
-        a.q_heads < 0 || a.n_axes < 0 || a.n_axes > 3 || (a.q_heads > 0 && a.n_axes == 0))
+        a.q_heads < 0 || a.q_heads > KV8_MAX_HEADS || a.n_axes < 0 || a.n_axes > 3 || (a.q_heads > 0 && a.n_axes == 0))
         return EBRL_E_INVALID;
     int sum = 0;
     for (int x = 0; x < a.n_axes; ++x) {
@@ -1446,6 +1453,7 @@ int kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, hipS
     const int64_t len = std::min<int64_t>(a.max_len, a.rows);
     w.pages = token ? 1 : (int)((len + 2 * KV8_PAGE - 2) / KV8_PAGE);
     const int64_t sp = (int64_t)a.n * w.pages;
+    if (sp > 4 * KV8_MAX_GROUPS) return EBRL_E_INVALID;   // a wave each, at least
     // one head a wave up to some 16 waves a SIMD; from there on, four heads a
     // wave share their cosines and sines (9 sequences of 3001 to 4095 tokens,
     // 40 + 8 heads of 128: 182 us with one, 148 with two, 141 with four, 145
@@ -1472,6 +1480,7 @@ static int64_t kv8_plan_bytes(const Kv8Plan& p, const ebrl_kv8_cache& c, int n) 
 int64_t kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int plan_n) {
     if (!kv8_attn_shape_ok(cache, args)) return EBRL_E_INVALID;
     if (args->n == 0 || args->max_q_len == 0) return 0;
+    if (!kv8_pairs_ok(*cache, std::max(args->n, plan_n))) return EBRL_E_INVALID;
     return kv8_plan_bytes(kv8_plan(*cache, *args, plan_n), *cache, args->n);
 }
 
@@ -1485,6 +1494,7 @@ int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int pl
     if (!kv8_pointers_ok(cache) || !a.row_start || !a.kv_len || !kv8_rows_ok(a.q, a.ldq, width, esz) ||
         !kv8_rows_ok(a.out, a.ldo, width, esz) || a.q == a.out)
         return EBRL_E_INVALID;
+    if (!kv8_pairs_ok(*cache, std::max(a.n, plan_n))) return EBRL_E_INVALID;
     const Kv8Plan p = kv8_plan(*cache, a, plan_n);
     const int64_t need = kv8_plan_bytes(p, *cache, a.n);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;

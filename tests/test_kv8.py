@@ -985,3 +985,20 @@ def test_binding_takes_one_row_of_any_stride():
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
     with pytest.raises(E.EbrlError, match="not on a GPU"):
         E.op_kv8_write(codes, scales, torch.zeros((1, 4), dtype=torch.int32), k, k, i32(0, 1), i32(0), 1)
+
+
+def test_counts_that_pass_64_bits_are_refused():
+    """Sequences, heads and rows whose number of workgroups wraps round to a few, or to none."""
+    big = dict(ldq=1 << 39, ldo=1 << 39)
+    for heads, n, q in ((1 << 24, 1 << 30, 1 << 16), (1 << 20, (1 << 31) - 1, 1 << 29), (1 << 30, 1 << 30, 128),
+                        (1 << 20, 1 << 22, 1 << 29)):
+        c = _cache(kv_heads=heads)
+        a = _attn_args(n=n, rows=5, max_q_len=q, q_heads=heads, **big)
+        assert _attn(c, a) == -1, (heads, n, q)
+        assert E.lib().ebrl_op_kv8_attn_workspace(ctypes.byref(c), ctypes.byref(a)) == -1, (heads, n, q)
+    wide = dict(ldq=1 << 39, ldk=1 << 39, ldv=1 << 39, ldq_out=1 << 39)
+    top = (1 << 31) - 1
+    for heads, q_heads, n, rows in ((1 << 30, 0, 1 << 30, 1 << 30), (1 << 30, 1 << 30, 1, 16), (2, top, 1, 16),
+                                    (1 << 20, 1 << 20, top, top)):
+        a = _write_args(n=n, rows=rows, max_len=rows, q_heads=q_heads, **wide)
+        assert E.lib().ebrl_op_kv8_write(ctypes.byref(_cache(kv_heads=heads)), ctypes.byref(a), None) == -1, (heads, n)
