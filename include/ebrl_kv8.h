@@ -11,7 +11,9 @@
  * block table: its token t lies in page table[row][t / 16], slot t % 16.
  * Page p has 16 * head_dim e4m3 codes for each of K and V and each KV head,
  * and one scale 2^e for each such group: a value is code * 2^e.  e is the
- * least integer >= -100 with |values| <= 448 * 2^e.  Orders inside a group
+ * least integer >= -100 with |values| <= 448 * 2^e when a page's first token
+ * is written, and grows only while the page keeps earlier tokens, also where a
+ * token that needed it is written over.  Orders inside a group
  * (the ones in which the matrix instructions' lanes take them):
  *   K: byte 1024 (d / 64) + 64 t + d % 64,
  *   V: byte 1024 (d / 64) + 256 (t / 4) + 16 (d % 64 / 4) + 4 (d % 4) + t % 4
@@ -78,7 +80,9 @@ typedef struct ebrl_kv8_write_args {
  * every sequence are left as they were.  A page that holds earlier tokens keeps
  * its scale unless a new token needs a larger one: the earlier tokens' codes
  * are then divided by the power of two that it grew by, which is exact down
- * to 2^-6 of the new scale and rounded below.  Two sequences of a call must
+ * to 2^-6 of the new scale and rounded below.  Writing smaller tokens in the
+ * place of larger ones gives neither the scale nor those roundings back: who
+ * writes the same slots again (a denoiser's steps) copies the page first.  Two sequences of a call must
  * not write the same page.  Returns EBRL_E_INVALID on bad arguments. */
 int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, void* stream);
 

@@ -91,9 +91,10 @@ struct ebrl_policy {
     // 8-bit cache: kv_pool holds every layer's codes, kv8_scales their scales.
     // The block table has a second row for each env, max_envs + 1 rows on:
     // the one that decode and denoise calls use, in which the page that the
-    // prefix ends inside is the env's spare page.  A call copies that page
-    // there first, so that writing its own tokens, which may raise the page's
-    // scale, leaves the prefix as it was.
+    // prefix ends inside is the env's spare page.  A decode call copies that
+    // page there first, a denoise call before each step, so that writing its
+    // own tokens, which may raise the page's scale, leaves the prefix as it
+    // was.
     float* kv8_scales = nullptr;
     void* kv8_ws = nullptr;
     int64_t kv8_ws_bytes = 0;
@@ -783,7 +784,6 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
     if (F && fnoise) copy_f32(fnoise, p->flow_f, (size_t)frows * c.frame_dim, p->stream);
     prof_end(p, 0, 0);
     auto body = [&]() -> int {
-        if (p->kv8) kv8_copy_pages(dec_kv8(p, 0), c.layers, reinterpret_cast<const int2*>(md + o_spare), n, p->stream);
         // time-MLP outputs for the fixed tau schedule
         prof_begin(p, EBRL_K_OTHER);
         small_linear(p->bf16, p->temb, c.n_steps, c.exp_d, p->w_t1, c.exp_d, p->tmid, false, p->stream);
@@ -818,6 +818,10 @@ int denoise(ebrl_policy* p, const int32_t* env_ids, int32_t n, const float* fnoi
         };
         ends(-1, 0);
         for (int k = 0; k < c.n_steps; ++k) {
+            // the prefix's page as prefill left it: a step's tokens may have
+            // raised its scale, which the next step's do not lower
+            if (p->kv8)
+                kv8_copy_pages(dec_kv8(p, 0), c.layers, reinterpret_cast<const int2*>(md + o_spare), n, p->stream);
             for (int l = 0; l < c.exp_layers; ++l) {
                 BlockCall b;
                 b.R = p->X; b.rows = rows; b.sd = &p->exp; b.w = &p->L_exp[l]; b.kv = dec_kv(p, l);

@@ -230,3 +230,55 @@ def test_reference_rounding_is_that_of_the_codes():
     x = np.random.default_rng(0).standard_normal(5000) * 100
     x = x[(np.abs(x) > 2.0 ** -6) & (np.abs(x) < 448)]
     assert np.array_equal(four_bits(x), R.CODE[R.encode(x)])
+
+
+def _first_step_apart(o):
+    """Weights under which the first of two denoising steps has values 2^19 times the second's: the time vector is 2^40 along
+    the first channel at tau = 1 and none at 1/2, no other weight writes that channel, and only the values read it."""
+    p = M.Policy(o, seed=0)
+    w = {name: np.array(p.W(name)) for name in p.shapes if name.startswith("exp.") or name in ("W_ain", "W_aout")}
+    for name, x in w.items():
+        if name == "W_ain" or name.endswith((".o", ".down")):
+            x[0] = 0
+            if name.endswith(".o"):
+                x *= 8                         # attention counts for more of the result
+        elif name.endswith(".v"):
+            x[:, 0] = 2.0 ** 15 * np.sign(x[:, 0])
+        else:
+            x[:, 0] = 0
+    one, half = M.time_embedding(1.0, o.exp_d), M.time_embedding(0.5, o.exp_d)
+    at = int(np.argmax(np.minimum(one, -half)))
+    assert one[at] > 0.25 and half[at] < -0.25
+    w["W_t1"], w["W_t2"] = np.zeros((2, o.exp_d, o.exp_d))
+    w["W_t1"][0, at], w["W_t2"][0, 0] = 512.0, 2.0 ** 32
+    return w
+
+
+def test_denoising_steps_do_not_depend_on_the_steps_before():
+    """The page that a prefix ends inside holds a step's own tokens too: what the first step's large values cost the prefix
+    there is not seen by the second, whose velocity is all of the result (the first's is 2^-20 of it)."""
+    o = dataclasses.replace(TINY_FLOW, n_steps=2)
+    ids = [0, 2, 3]
+    img, lang = _obs(o, ids, 1004)
+    noise = synth_inputs.flow_noise(4, ids, o.chunk, o.adim)
+    w = _first_step_apart(o)
+    pol = _policy(o, 4)
+    for name, x in w.items():
+        bits = np.ascontiguousarray(x, np.float32).view(np.uint32)
+        assert not (bits & 0xFFFF).any()
+        pol.write_weight(M.tensor_shapes(o)[name][0], (bits >> 16).astype(np.uint16))
+    pol.prefill(ids, images=_dev(img), lang_ids=_dev(lang))
+    got = pol.flow_denoise(ids, _dev(noise))
+    torch.cuda.synchronize()
+    exact, ref = M.Policy(o, seed=0, overrides=w), Rounded(o, seed=0, overrides=w)
+    for i in range(len(ids)):
+        def moved(m, lose=0):
+            st = m.prefill(img[i], lang[i])
+            for v in st.v:
+                v[:lose] = 0
+            return 2 * (noise[i] - m.flow_denoise(st, noise[i]))
+        want = moved(ref)
+        tol = P.TOL_BF16 + _rel(want, moved(exact))
+        assert _rel(moved(ref, exact.cfg.prefix_len), want) > 5 * tol     # what a lost prefix would cost
+        assert _rel(2 * (noise[i] - got[i].double().cpu().numpy()), want) < tol
+    pol.close()
