@@ -128,7 +128,7 @@ def gather(codes, scales, table_row, n):
 
 
 def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, causal, scale, seq=None, bf16=True,
-           only=None):
+           only=None, weight_terms=1):
     """(out, bound) [rows, hq, hd] float64; rows outside every sequence are NaN in both.  `only`: the rows to work
     out; the others get an infinite bound.
 
@@ -144,7 +144,10 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
     sum that divides is of the weights as rounded, p (1 + d) with |d| <= 2^-8,
     the result moves by sum p d (v - o) / sum p (1 + d), so by 2^-8 of the mean
     |v - o| <= mean |v| + |o|, in place of 2^-8 of the mean |v|, to first order;
-    1 / (1 - 2^-8) of it altogether."""
+    1 / (1 - 2^-8) of it altogether.  weight_terms 2: bf16 rows' weights in two
+    bf16 terms: what the first leaves of a weight from 2^k to 2^(k+1) is 2^(k-8)
+    at most, and half a step of the second then 2^(k-17); the sum that divides
+    is of the whole weights."""
     rows, hq, hd = q.shape
     hkv = codes.shape[2]
     out, bound = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
@@ -180,8 +183,8 @@ def attend(codes, scales, table, q, row_start, kv_len, max_q_len, max_kv_len, ca
                     ds = ds.max()
                     low = s[p > 0].min() if (p > 0).any() else np.nan        # NaN among the keys: no bound
                     dp = ds + (s.max() - low + 1) * 2.0 ** -22 + 2.0 ** -22
-                    rel = 2 * dp + 2 * (len(use) * (1 if bf16 else 3) + 8) * 2.0 ** -23 + (2.0 ** -8 if bf16 else 0)
+                    rel = 2 * dp + 2 * (len(use) * (1 if bf16 else 3) + 8) * 2.0 ** -23 + (2.0 ** (-8 if weight_terms == 1 else -17) if bf16 else 0)
                     out[r0 + j, h] = o
-                    sums = np.abs(o) * 2.0 ** -8 + (mag + np.abs(o)) * 2.0 ** -15 if bf16 else 0
+                    sums = np.abs(o) * 2.0 ** -8 + (mag + np.abs(o)) * 2.0 ** -15 if bf16 and weight_terms == 1 else 0
                     bound[r0 + j, h] = mag * rel + sums + np.abs(o) * (2.0 ** -8 if bf16 else 2.0 ** -24) + 2.0 ** -120
     return out, bound

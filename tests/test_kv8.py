@@ -1002,3 +1002,107 @@ def test_counts_that_pass_64_bits_are_refused():
                                     (1 << 20, 1 << 20, top, top)):
         a = _write_args(n=n, rows=rows, max_len=rows, q_heads=q_heads, **wide)
         assert E.lib().ebrl_op_kv8_write(ctypes.byref(_cache(kv_heads=heads)), ctypes.byref(a), None) == -1, (heads, n)
+
+
+def _terms(p, n):
+    """Weights as n bf16 terms, added up."""
+    got = np.zeros_like(p)
+    for _ in range(n):
+        got += torch.from_numpy(p - got).bfloat16().double().numpy()
+    return got
+
+
+def _decode_case(seed, lens, hkv, hd, hq):
+    pool = Pool(seed, lens, hkv, hd)
+    q = torch.from_numpy(np.random.default_rng(seed + 1).standard_normal((len(lens), hq * hd))).bfloat16()
+    return pool, q
+
+
+def test_two_term_bound_tells_one_term_from_two():
+    """A decode step whose weights were rounded to one bf16 term would leave the bound that two terms are held to."""
+    lens, hkv, hd, hq = [300, 1000], 2, 64, 4
+    pool, q = _decode_case(120, lens, hkv, hd, hq)
+    q64 = q.double().numpy().reshape(len(lens), hq, hd)
+    want, bound = R.attend(pool.codes, pool.scales, pool.table, q64, [0, 1, 2], lens, 1, 1000, True, hd ** -0.5,
+                           weight_terms=2)
+    for terms, holds in ((1, False), (2, True)):
+        got = np.empty_like(want)
+        for i, n in enumerate(lens):
+            K, V, _ = R.gather(pool.codes, pool.scales, pool.table[i], n)
+            for h in range(hq):
+                s = K[:, h // 2] @ q64[i, h] * hd ** -0.5
+                p = np.exp(s - s.max())
+                got[i, h] = _terms(p, terms) @ V[:, h // 2] / p.sum()
+        got = torch.from_numpy(got).bfloat16().double().numpy()
+        assert bool(np.all(np.abs(got - want) <= bound)) == holds, terms
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv,hd,lens", [(4, 2, 64, [300, 1000, 77]), (6, 2, 128, [300, 1000, 77]), (16, 1, 128, [129]),
+                                            (2, 1, 64, [9001]), (8, 1, 128, [6000, 4000]),
+                                            (20, 10, 64, [(i * 7) % 61 for i in range(103)]),
+                                            (20, 10, 128, [(i * 7) % 61 for i in range(103)])])
+def test_attn_decode_weights_in_two_terms(hq, hkv, hd, lens):
+    pool, q = _decode_case(122, lens, hkv, hd, hq)
+    codes, scales, table = pool.gpu()
+    out = torch.full_like(q, 7.0).cuda()
+    n = len(lens)
+    E.op_kv8_attn(codes, scales, table, q.cuda(), out, _ints(range(n + 1)), _ints(lens), 1, max(lens))
+    want, bound = R.attend(pool.codes, pool.scales, pool.table, q.double().numpy().reshape(n, hq, hd), list(range(n + 1)),
+                           lens, 1, max(lens), True, hd ** -0.5, weight_terms=2)
+    _held(out.double().cpu().numpy().reshape(want.shape), want, bound)
+
+
+@gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype,copies,ql,bound", [("bf16", 260, 100, 1024), ("bf16", 300, 100, 120), ("bf16", 1, 100, 120),
+                                                   ("fp32", 300, 100, 120), ("fp32", 1, 100, 120), ("fp32", 1, 5, 120),
+                                                   ("fp32", 600, 5, 120)])
+def test_attn_nan_in_every_page_of_a_step(dtype, copies, ql, bound, hd):
+    """NaN values in the first, third and fourth page of a step of 64 keys, behind causal masks, and a NaN key; tiles of 128
+    rows (the first case) and fp32 rows among them."""
+    n, hkv = 120, 2
+    rng = np.random.default_rng(130)
+    pool = Pool(131, [n, n], hkv, hd)
+    clean = pool.codes.copy()
+    nans = {(40, 1), (55, 5), (70, 9), (100, 17), (115, 33), (118, hd - 1)}      # (token, dim)
+    for t, dim in nans:
+        pool.codes[pool.table[0, t // 16], 1, 0, R.order(hd, 1)[t % 16, dim]] = 0x7F
+    pool.codes[pool.table[0, (n - 1) // 16], 0, 0, R.order(hd, 0)[(n - 1) % 16, 2]] = 0xFF
+    seq = [0] + [1] * copies
+    q, _ = _rows(rng, ql * len(seq), 4, hd, DT[dtype])
+    res = []
+    for c in (clean, pool.codes):
+        out = torch.empty_like(q)
+        E.op_kv8_attn(torch.from_numpy(c).cuda(), torch.from_numpy(pool.scales).cuda(), torch.from_numpy(pool.table).cuda(),
+                      q, out, _ints(ql * np.arange(len(seq) + 1)), _ints([n] * len(seq)), ql, bound, seq=_ints(seq))
+        res.append(out.double().cpu().numpy().reshape(len(seq), ql, 4, hd))
+    want = res[0].copy()
+    for j in range(ql):
+        for t, dim in nans:
+            if n - ql + j >= t:
+                want[0, j, :2, dim] = np.nan
+    want[0, ql - 1, :2] = np.nan
+    np.testing.assert_array_equal(want, res[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kind", list(LADDERS))
+def test_attn_leaves_rows_of_no_sequence(kind, hd, dtype):
+    """Rows before the first sequence, past the bound of each and behind the last keep every byte; all others are written."""
+    n, ql, keys, _, bound = LADDERS[kind]
+    pool = Pool(140, [keys], 2, hd)
+    codes, scales, table = pool.gpu()
+    gap = 3
+    start = 2 + (ql + gap) * np.arange(n + 1)
+    q, _ = _rows(np.random.default_rng(141), int(start[-1]) + 4, 4, hd, DT[dtype])
+    out = torch.full((q.shape[0], 4 * hd + 8), 7.0, dtype=DT[dtype], device="cuda")
+    E.op_kv8_attn(codes, scales, table, q, out[:, :4 * hd], _ints(start), _ints([keys] * n), ql, bound,
+                  seq=_ints([0] * n))
+    mine = torch.zeros(q.shape[0], dtype=torch.bool)
+    for r in start[:-1]:
+        mine[r:r + ql] = True
+    assert (out[~mine] == 7.0).all() and (out[:, 4 * hd:] == 7.0).all()
+    assert torch.isfinite(out[mine]).all() and not (out[mine][:, :4 * hd] == 7.0).any()
