@@ -1524,24 +1524,27 @@ int kv8_attn(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args, int pl
 }
 
 // Pages of one layer after another: the codes and scales of page pairs[i].x
-// go to page pairs[i].y (negative: nothing is copied).
-__global__ __launch_bounds__(256) void kv8_copy_kernel(uint8_t* codes, float* scales, int num_blocks, int groups,
+// go to page pairs[i].y (negative: nothing is copied).  A workgroup a (K or V,
+// head) group: a denoise call copies before each step, with few environments
+// too (4 layers of 8 heads of 128: 4 environments 4.8 us, 64 6.4 us; with a
+// workgroup a page 5.6 and 7.6).
+__global__ __launch_bounds__(128) void kv8_copy_kernel(uint8_t* codes, float* scales, int num_blocks, int groups,
                                                        int group_bytes, const int2* pairs)
 {
-    const int2 p = pairs[blockIdx.x];
+    const int2 p = pairs[blockIdx.x / groups];
     if (p.x < 0 || p.y < 0 || p.x >= num_blocks || p.y >= num_blocks) return;
-    const size_t layer = (size_t)blockIdx.y * num_blocks;
-    const size_t bytes = (size_t)groups * group_bytes;
-    const uint4* src = reinterpret_cast<const uint4*>(codes + (layer + p.x) * bytes);
-    uint4* dst = reinterpret_cast<uint4*>(codes + (layer + p.y) * bytes);
-    for (size_t i = threadIdx.x; i < bytes / 16; i += 256) dst[i] = src[i];
-    for (int i = threadIdx.x; i < groups; i += 256)
-        scales[(layer + p.y) * groups + i] = scales[(layer + p.x) * groups + i];
+    const size_t layer = (size_t)blockIdx.y * num_blocks, group = blockIdx.x % groups;
+    const size_t from = (layer + p.x) * groups + group, to = (layer + p.y) * groups + group;
+    const uint4* src = reinterpret_cast<const uint4*>(codes + from * group_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(codes + to * group_bytes);
+    for (int i = threadIdx.x; i < group_bytes / 16; i += 128) dst[i] = src[i];
+    if (threadIdx.x == 0) scales[to] = scales[from];
 }
 void kv8_copy_pages(const ebrl_kv8_cache& c, int layers, const int2* pairs, int n, hipStream_t s) {
     if (n <= 0) return;
-    hipLaunchKernelGGL(kv8_copy_kernel, dim3(n, layers), dim3(256), 0, s, (uint8_t*)c.codes, c.scales, c.num_blocks,
-                       2 * c.kv_heads, KV8_PAGE * c.head_dim, pairs);
+    const int groups = 2 * c.kv_heads;
+    hipLaunchKernelGGL(kv8_copy_kernel, dim3((unsigned)n * groups, layers), dim3(128), 0, s, (uint8_t*)c.codes, c.scales,
+                       c.num_blocks, groups, KV8_PAGE * c.head_dim, pairs);
 }
 
 // Value of an e4m3 code, on the host.
