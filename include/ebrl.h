@@ -61,7 +61,10 @@ typedef struct ebrl_config {
                                  softmax, residual stream, norms and logits;
                                  EBRL_DTYPE_BF16_KV8: the same with the decoder's
                                  KV cache in 8 bits (ebrl_kv8.h): half the bytes a
-                                 token, no bound of 4096 tokens on a sequence */
+                                 token, no bound of 4096 tokens on a sequence; the
+                                 QKV projection is rounded to bf16 before its rows
+                                 turn (bf16 policies turn the fp32 sums), and the
+                                 policy holds a buffer of its rows */
     /* vision: n_cams cameras of img x img x 3 float32 pixels, square patches */
     int32_t n_cams, img, patch;
     /* optional ViT encoder before the decoder (0 layers = patch embedding

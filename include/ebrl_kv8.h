@@ -25,8 +25,9 @@
  * sequence of length 0; a page id outside [0, num_blocks) holds no tokens (none
  * are written there or seen; queries at its positions are still turned); a
  * sequence ends with the table's row (queries past it are left as well); row
- * ranges are cut to [0, rows] and to the host's max_* bounds; positions are
- * cut to the rotary tables.
+ * ranges are cut to [0, rows] and to the host's max_* bounds (a sequence's
+ * first max_* rows and keys are what counts, also for a causal mask);
+ * positions are cut to the rotary tables.
  */
 #ifndef EBRL_KV8_H
 #define EBRL_KV8_H
@@ -91,7 +92,7 @@ typedef struct ebrl_kv8_attn_args {
     int32_t n;                   /* sequences */
     int32_t rows;                /* rows of q and out */
     int32_t max_q_len;           /* most query rows of a sequence */
-    int32_t max_kv_len;          /* most keys of a sequence, at most 2^30; more are not seen */
+    int32_t max_kv_len;          /* most keys of a sequence, at most 2^30; a longer one counts as this long */
     int32_t q_heads;             /* a multiple of kv_heads, at most 2^20: query head h reads KV head h / (q_heads / kv_heads) */
     int32_t causal;              /* 0: every row sees all keys; else row j of m sees keys 0 .. kv_len - m + j */
     float scale;                 /* of the scores, > 0 (commonly 1 / sqrt(head_dim)) */
@@ -107,15 +108,18 @@ typedef struct ebrl_kv8_attn_args {
 
 /* Bytes of workspace that a call with these arguments needs (host arithmetic
  * on n, max_q_len, max_kv_len, the heads and the dtype; no pointer is read),
- * or EBRL_E_INVALID.  0: none. */
+ * or EBRL_E_INVALID.  0: none.  Fewer sequences or rows may need more, since
+ * their keys are cut into more parts: a workspace for calls of several sizes
+ * is the largest of what each of them needs. */
 int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args);
 
 /* out = softmax(scale q K^T + mask) V over the cache: one query row a
  * sequence (a decode step), a prompt's rows, or any ragged mix.  Keys a row
  * does not see do not count, whatever their slots hold, NaN included; a row
- * that sees no key gets zeros; one whose query is not finite, or whose scores
- * pass the 32-bit range (the largest upwards, or all downwards), is NaN; rows
- * outside every sequence are left as they were.  Scores, the softmax's maximum and sum and the weighted sum are held
+ * that sees no key gets zeros; one whose query is not finite (fp32: past
+ * bf16's range, 3.39e38), or whose scores pass the 32-bit range (the largest
+ * upwards, or all downwards), is NaN; rows outside every sequence are left as
+ * they were.  Scores, the softmax's maximum and sum and the weighted sum are held
  * in 32 bits; bf16 rows' weights enter the product with V as bf16, in two terms
  * where a KV head has at most 16 rows a sequence.  Weights go up to 2^11: the
  * sum overflows to infinity only where the keys' values, times 2^11 and their

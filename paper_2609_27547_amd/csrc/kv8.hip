@@ -964,7 +964,7 @@ EBRL_DEV uint4 kv8_stream16(const uint8_t* p) {
 // rows, at most 16, and deal the pairs of pages of a part of the keys.  Bound
 // by the bytes of the cache: codes go straight to registers, and a step's
 // registers are loaded again as soon as it is done, so that each wave keeps
-// 8 to 16 KB in flight (head dim 128).  90 us, 5.9 TB/s, on 61 sequences of 500
+// 8 to 16 KB in flight (head dim 128).  95 us, 5.6 TB/s, on 61 sequences of 500
 // to 8000 keys (8 KV heads of 128), where a streaming read reaches 7.1; one
 // sequence of 291 keys 6 us, the latency of lengths, pages and codes in turn.
 template <typename T, int HD, int KW>
@@ -1101,11 +1101,11 @@ __global__ __launch_bounds__(256, 2) void kv8_decode_kernel(Kv8AttnKernelArgs w)
 // and takes P pages at a time; with KG 1 the four waves of a workgroup have
 // rows of their own and take all keys, with KG 2 two waves share rows and take
 // 32 keys of each step.  Bound by issue: with 32 rows a wave (QT 2, head dim 128,
-// 2 x 4096 rows of 32 heads on 8 k keys) 726 us, 1.10 PFLOP/s; matrix
-// instructions take 44 % of a SIMD's cycles and vector instructions 54 %, and
-// they hardly overlap.  148 rows of 37 sequences on 730 keys 34 us, 480 TFLOP/s.
+// 2 x 4096 rows of 32 heads on 8 k keys) 710 to 760 us by card and clock, 1.06
+// to 1.13 PFLOP/s; matrix instructions take 44 to 49 % of a SIMD's cycles and
+// vector instructions 54 to 61 %, and they hardly overlap.  148 rows of 37 sequences on 730 keys 34 us, 480 TFLOP/s.
 // At head dim 64 K's codes go to the scaled product with 32 rows a wave, held to
-// 128 registers (2048 rows of 32 heads on 8 k keys 172 us against 179 with
+// 128 registers (2048 rows of 32 heads on 8 k keys, 168 us now, 172 against 179 with
 // conversions; without the bound 167, but 4 x 2048 rows on themselves 93 against
 // 90); with 16 rows preparing q and two registers more cost what it saves (24
 // prompts of 200 to 424 tokens 20.8 us against 19.1).
@@ -1348,7 +1348,7 @@ static Kv8Plan kv8_plan(const ebrl_kv8_cache& c, const ebrl_kv8_attn_args& a, in
     } else {
         // few workgroups: twice as many of half the rows, two waves sharing
         // them (600 rows of 32 heads on 600 keys 17 us against 29, 512 rows
-        // of 4 heads each on 1512 keys 21.5 against 33; 37 sequences of 148
+        // of 4 heads each on 1512 keys 22.4 against 33; 37 sequences of 148
         // rows on 730 keys, 888 workgroups of 64 rows, 37 against 34; 64
         // sequences of them 75 against 58)
         p.kind = KV8_PAIRS;
