@@ -419,6 +419,13 @@ _KV8_WRITE = struct.Struct("10i4P4q6P")
 _KV8_ATTN = struct.Struct("7if2P2q4Pq")
 
 
+def _kv8_pack(packer, *values) -> bytes:
+    try:
+        return packer.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise EbrlError(-1, f"kv8: sizes pass 32 bits: {e}") from e
+
+
 def _kv8_codes(t) -> bool:
     import torch
     dtype = t.dtype
@@ -442,7 +449,8 @@ def _kv8_cache(codes, scales, table):
     if len(pages) != 2 or table.dtype is not torch.int32 or not table.is_contiguous() or table.get_device() != dev:
         _kv8_bad("block_table is contiguous int32 [sequences, pages] where the codes are", table)
     hd = wide // KV8_PAGE
-    return _KV8_CACHE.pack(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), blocks, *pages, heads, hd), heads, hd, dev
+    c = _kv8_pack(_KV8_CACHE, codes.data_ptr(), scales.data_ptr(), table.data_ptr(), blocks, *pages, heads, hd)
+    return c, heads, hd, dev
 
 
 def _kv8_rows(name, t, dtype, dev, rows, width):
@@ -549,11 +557,11 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
         _kv8_bad("codes are [num_blocks, 2, kv_heads, 16 * head_dim], block_table [sequences, pages]", codes, block_table)
     blocks, _, heads, wide = codes.shape
     hd = wide // KV8_PAGE
-    c = _KV8_CACHE.pack(0, 0, 0, blocks, *block_table.shape, heads, hd)
+    c = _kv8_pack(_KV8_CACHE, 0, 0, 0, blocks, *block_table.shape, heads, hd)
     dtype = _kv8_dtype("q", q)
     if not 0 <= n < 1 << 31:
         _kv8_bad(f"n {n}")
-    a = _KV8_ATTN.pack(dtype, n, q.shape[0], max_q_len, max_kv_len, q.shape[1] // hd, 1, 1.0, *(0,) * 9)
+    a = _kv8_pack(_KV8_ATTN, dtype, n, q.shape[0], max_q_len, max_kv_len, q.shape[1] // hd, 1, 1.0, *(0,) * 9)
     need = lib().ebrl_op_kv8_attn_workspace(c, a)
     if need < 0:
         raise EbrlError(need, "ebrl_op_kv8_attn_workspace")

@@ -1106,3 +1106,24 @@ def test_attn_leaves_rows_of_no_sequence(kind, hd, dtype):
         mine[r:r + ql] = True
     assert (out[~mine] == 7.0).all() and (out[:, 4 * hd:] == 7.0).all()
     assert torch.isfinite(out[mine]).all() and not (out[mine][:, :4 * hd] == 7.0).any()
+
+
+def test_binding_refuses_shapes_past_32_bits():
+    """Refused as other calls are, by the library's error."""
+    codes = torch.empty((4, 2, 2, 1024), dtype=torch.uint8, device="meta")
+    scales = torch.empty((4, 2, 2), device="meta")
+    wide = torch.empty((1, 1 << 31), dtype=torch.int32, device="meta")
+    tall = torch.empty((1 << 31, 2, 2, 1024), dtype=torch.uint8, device="meta")
+    table = torch.empty((1, 4), dtype=torch.int32, device="meta")
+    k = torch.empty((1, 128), dtype=torch.bfloat16, device="meta")
+    i32 = lambda n: torch.empty(n, dtype=torch.int32, device="meta")  # noqa: E731
+    for c, s, t in ((codes, scales, wide), (tall, torch.empty((1 << 31, 2, 2), device="meta"), table)):
+        with pytest.raises(E.EbrlError, match="32 bits"):
+            E.op_kv8_write(c, s, t, k, k, i32(2), i32(1), 1)
+        with pytest.raises(E.EbrlError, match="32 bits"):
+            E.op_kv8_attn(c, s, t, k, torch.empty_like(k), i32(2), i32(1), 1, 1)
+        with pytest.raises(E.EbrlError, match="32 bits"):
+            E.kv8_attn_workspace(c, t, k, 1, 1, 1)
+    rows = torch.empty((1 << 31, 128), dtype=torch.bfloat16, device="meta")
+    with pytest.raises(E.EbrlError):
+        E.kv8_attn_workspace(codes, table, rows, 1, 1, 1)
