@@ -559,6 +559,8 @@ def kv8_attn_workspace(codes, block_table, q, n, max_q_len, max_kv_len):
     hd = wide // KV8_PAGE
     c = _kv8_pack(_KV8_CACHE, 0, 0, 0, blocks, *block_table.shape, heads, hd)
     dtype = _kv8_dtype("q", q)
+    if q.shape[1] % hd:
+        _kv8_bad(f"q has heads of {hd}", q)
     if not 0 <= n < 1 << 31:
         _kv8_bad(f"n {n}")
     a = _kv8_pack(_KV8_ATTN, dtype, n, q.shape[0], max_q_len, max_kv_len, q.shape[1] // hd, 1, 1.0, *(0,) * 9)

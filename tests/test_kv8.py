@@ -1127,3 +1127,10 @@ def test_binding_refuses_shapes_past_32_bits():
     rows = torch.empty((1 << 31, 128), dtype=torch.bfloat16, device="meta")
     with pytest.raises(E.EbrlError):
         E.kv8_attn_workspace(codes, table, rows, 1, 1, 1)
+
+
+def test_workspace_refuses_queries_that_are_no_heads():
+    codes, _ = E.kv8_alloc(4, 2, 64, device="cpu")
+    table = torch.zeros((1, 4), dtype=torch.int32)
+    with pytest.raises(E.EbrlError, match="heads of 64"):
+        E.kv8_attn_workspace(codes, table, torch.zeros((1, 190), dtype=torch.bfloat16), 1, 1, 1)
