@@ -542,15 +542,20 @@ EBRL_DEV Kv8Tile kv8_tile(const Kv8AttnKernelArgs& w, int i, int tile) {
     return t;
 }
 
-// First key of a part of a (sequence, KV head) that is there, or INT_MAX.
+// First key of a part of a (sequence, KV head) that is there, or INT_MAX; by a
+// whole wave, 64 pages at a time.
 EBRL_DEV int kv8_first_key(const Kv8AttnKernelArgs& w, unsigned pair, int part) {
     asm volatile("" : "+s"(pair));   // the table's row is worked out again, not kept through the loop over keys
     const int trow = kv8_table_row(w, pair / w.c.kv_heads);
     if (trow < 0) return INT_MAX;
     const int* const table = w.c.block_table + (size_t)trow * w.c.table_stride;
     const int lo = part * (w.part_keys / KV8_PAGE), hi = min(lo + w.part_keys / KV8_PAGE, w.c.table_stride);
-    for (int p = lo; p < hi; ++p)
-        if (table[p] >= 0 && table[p] < w.c.num_blocks) return p * KV8_PAGE;
+    const int lane = threadIdx.x & 63;
+    for (int p = lo; p < hi; p += 64) {
+        const int page = p + lane < hi ? table[p + lane] : -1;
+        const uint64_t there = __ballot(page >= 0 && page < w.c.num_blocks);
+        if (there) return (p + __builtin_ctzll(there)) * KV8_PAGE;
+    }
     return INT_MAX;
 }
 

@@ -1134,3 +1134,38 @@ def test_workspace_refuses_queries_that_are_no_heads():
     table = torch.zeros((1, 4), dtype=torch.int32)
     with pytest.raises(E.EbrlError, match="heads of 64"):
         E.kv8_attn_workspace(codes, table, torch.zeros((1, 190), dtype=torch.bfloat16), 1, 1, 1)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ql", [1, 40])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attn_pages_that_are_none_before_the_first(ql, hd, dtype):
+    """Sequences of 200 pages of which the 1st, the 64th, the 65th, the 130th or none is there, in parts: a query of
+    -infinity is NaN where a page is, zeros where none is; ordinary ones are a mean of that page's values."""
+    n_pages, there = 200, [0, 63, 64, 129, None]
+    rng = np.random.default_rng(150)
+    pool = Pool(151, [16], 2, hd)
+    page = pool.table[0, 0]
+    table = np.full((5, n_pages), -1, np.int32)
+    for i, p in enumerate(there):
+        if p is not None:
+            table[i, p] = page
+    pool.table = table
+    k = rng.uniform(1, 2, (16, 2, hd))
+    v = rng.standard_normal((16, 2, hd))
+    R.write(pool.codes, pool.scales, np.array([[page]]), k, v, [0, 16], [0], 16)
+    codes, scales, dev = pool.gpu()
+    q, q64 = _rows(rng, 5 * ql, 4, hd, DT[dtype])
+    kv = [n_pages * 16] * 5
+    start = [ql * i for i in range(6)]
+    want, bound = R.attend(pool.codes, pool.scales, table, q64, start, kv, ql, max(kv), True, hd ** -0.5,
+                           bf16=dtype == "bf16")
+    out = torch.full_like(q, 7.0)
+    E.op_kv8_attn(codes, scales, dev, q, out, _ints(start), _ints(kv), ql, max(kv))
+    _held(out.double().cpu().numpy().reshape(want.shape), want, bound)
+    assert (out[4 * ql:] == 0).all()
+    q[:, 3] = float("-inf")
+    E.op_kv8_attn(codes, scales, dev, q, out, _ints(start), _ints(kv), ql, max(kv))
+    assert torch.isnan(out[:4 * ql, :hd]).all()
+    assert (out[4 * ql:] == 0).all() and torch.isfinite(out[:, hd:]).all()
