@@ -80,11 +80,12 @@ typedef struct ebrl_kv8_write_args {
  * the page's scale is that of the tokens up to the last.  Rows of q_out outside
  * every sequence are left as they were.  A page that holds earlier tokens keeps
  * its scale unless a new token needs a larger one: the earlier tokens' codes
- * are then divided by the power of two that it grew by, which is exact down
- * to 2^-6 of the new scale and rounded below.  Writing smaller tokens in the
- * place of larger ones gives neither the scale nor those roundings back: who
- * writes the same slots again (a denoiser's steps) copies the page first.  Two sequences of a call must
- * not write the same page.  Returns EBRL_E_INVALID on bad arguments. */
+ * are then divided by the power of two that it grew by, which is exact down to
+ * 2^-6 of the new scale and rounded below.  Writing smaller tokens in the place
+ * of larger ones gives neither the scale nor those roundings back: who writes
+ * the same slots again (a denoiser's steps) copies the page first.  Two
+ * sequences of a call must not write the same page.  Returns EBRL_E_INVALID on
+ * bad arguments. */
 int ebrl_op_kv8_write(const ebrl_kv8_cache* cache, const ebrl_kv8_write_args* args, void* stream);
 
 typedef struct ebrl_kv8_attn_args {
@@ -113,20 +114,20 @@ typedef struct ebrl_kv8_attn_args {
  * is the largest of what each of them needs. */
 int64_t ebrl_op_kv8_attn_workspace(const ebrl_kv8_cache* cache, const ebrl_kv8_attn_args* args);
 
-/* out = softmax(scale q K^T + mask) V over the cache: one query row a
- * sequence (a decode step), a prompt's rows, or any ragged mix.  Keys a row
- * does not see do not count, whatever their slots hold, NaN included; a row
- * that sees no key gets zeros; one whose query is not finite (fp32: past
- * bf16's range, 3.39e38), or whose scores pass the 32-bit range (the largest
- * upwards, or all downwards), is NaN; rows outside every sequence are left as
- * they were.  Scores, the softmax's maximum and sum and the weighted sum are held
- * in 32 bits; bf16 rows' weights enter the product with V as bf16, in two terms
- * where a KV head has at most 16 rows a sequence.  Weights go up to 2^11: the
- * sum overflows to infinity only where the keys' values, times 2^11 and their
+/* out = softmax(scale q K^T + mask) V over the cache: one query row a sequence
+ * (a decode step), a prompt's rows, or any ragged mix.  Keys a row does not see
+ * do not count, whatever their slots hold, NaN included; a row that sees no key
+ * gets zeros; one whose query is not finite (fp32: past bf16's range, 3.39e38),
+ * or whose scores pass the 32-bit range (the largest upwards, or all
+ * downwards), is NaN; rows outside every sequence are left as they were.
+ * Scores, the softmax's maximum and sum and the weighted sum are held in 32
+ * bits; bf16 rows' weights enter the product with V as bf16, in two terms where
+ * a KV head has at most 16 rows a sequence.  Weights go up to 2^11: the sum
+ * overflows to infinity only where the keys' values, times 2^11 and their
  * number, pass the 32-bit range.  Scores, times log2(e), are floats: from 2^24
- * on they lie whole numbers apart.  With few rows the keys are cut into parts that
- * run at the same time and are joined in their order by a second launch.  The
- * cut follows n, max_q_len, max_kv_len and the heads.
+ * on they lie whole numbers apart.  With few rows the keys are cut into parts
+ * that run at the same time and are joined in their order by a second launch.
+ * The cut follows n, max_q_len, max_kv_len and the heads.
  *
  * The workspace holds the parts; what is in it before a call does not matter.
  * Calls that may overlap in time (other streams, graphs replayed side by side)

@@ -1169,3 +1169,36 @@ def test_attn_pages_that_are_none_before_the_first(ql, hd, dtype):
     E.op_kv8_attn(codes, scales, dev, q, out, _ints(start), _ints(kv), ql, max(kv))
     assert torch.isnan(out[:4 * ql, :hd]).all()
     assert (out[4 * ql:] == 0).all() and torch.isfinite(out[:, hd:]).all()
+
+
+@gpu
+@pytest.mark.parametrize("ql", [1, 40])
+def test_attn_fp32_queries_at_the_end_of_bf16s_range(ql):
+    """Queries enter as bf16 terms: one past bf16's largest number makes its row and head NaN, one just below does not."""
+    pool = Pool(160, [70], 2, 64)
+    pool.scales[:, 0] *= 2.0 ** -92
+    codes, scales, table = pool.gpu()
+    q = torch.randn((ql, 256), device="cuda")
+    q[0, 3], q[ql - 1, 64 + 7] = 3.4e38, 3.38e38
+    out = torch.empty_like(q)
+    E.op_kv8_attn(codes, scales, table, q, out, _ints([0, ql]), _ints([70]), ql, 70)
+    nan = torch.isnan(out).reshape(ql, 4, 64)
+    assert nan[0, 0].all() and nan.sum() == 64
+
+
+@gpu
+@pytest.mark.parametrize("new", [[1, 1], [20, 3]])
+def test_write_turns_keys_without_queries(new):
+    past = [5, 30]
+    pool = Pool(161, past, 2, 128, room=21)
+    rng = np.random.default_rng(162)
+    rows = sum(new)
+    k, k64 = _rows(rng, rows, 2, 128, torch.bfloat16)
+    cos, sin = _tables(64, 128)
+    codes, scales, table = pool.gpu()
+    E.op_kv8_write(codes, scales, table, k, k, _ints([0, new[0], rows]), _ints(past), max(new), sections=(64,),
+                   cos=torch.from_numpy(cos).cuda(), sin=torch.from_numpy(sin).cuda())
+    wc, ws = pool.codes.copy(), pool.scales.copy()
+    R.write(wc, ws, pool.table, k64, k64, [0, new[0], rows], past, max(new), [64], None, cos, sin)
+    _same_codes(_bits(codes), wc)
+    np.testing.assert_array_equal(scales.cpu().numpy(), ws)
