@@ -21,7 +21,7 @@ ARCH = "gfx950"
 HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-Wno-unused-result", "-I", os.path.join(ROOT, "include")]
-HIP_SOURCES = ["gemm.hip", "attention.hip", "misc.hip", "kv8.hip", "engine.cpp"]
+HIP_SOURCES = ["gemm.hip", "attention.hip", "misc.hip", "kv8.hip", "pages.hip", "i8.hip", "engine.cpp"]
 # Per-source additions.  Attention (attention.hip, kv8.hip): MFMA accumulators in VGPRs (gfx950 allows
 # either file), so the softmax rescale and the score reads need no
 # AGPR <-> VGPR copies every key tile.

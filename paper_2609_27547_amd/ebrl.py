@@ -91,6 +91,26 @@ class Kv8AttnArgs(ctypes.Structure):
                [("workspace_bytes", ctypes.c_int64)]
 
 
+class Kv8Pool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("codes", "scales", "block_table", "refs")] + \
+               [(n, ctypes.c_int64) for n in ("layer_codes", "layer_scales")] + \
+               [(n, _I32) for n in ("layers", "num_blocks", "table_rows", "table_stride", "kv_heads", "head_dim")]
+
+
+class I8QuantArgs(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "op", "rows", "cols")] + [("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_void_p) for n in ("x", "up")] + [(n, ctypes.c_int64) for n in ("ldx", "ldup")] + \
+               [(n, ctypes.c_void_p) for n in ("gain", "codes")] + [("ldc", ctypes.c_int64), ("scales", ctypes.c_void_p)]
+
+
+class I8GemmArgs(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "M", "N", "K")] + [(n, ctypes.c_void_p) for n in ("a", "b")] + \
+               [(n, ctypes.c_int64) for n in ("lda", "ldb")] + \
+               [(n, ctypes.c_void_p) for n in ("scale_a", "scale_b", "bias", "residual")] + [("ldr", ctypes.c_int64)] + \
+               [("c", ctypes.c_void_p), ("ldc", ctypes.c_int64), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64)]
+
+
 class EbrlError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{ERRORS.get(code, code)}: {msg}")
@@ -107,6 +127,9 @@ EXPORTED = [
     "ebrl_profile_enable", "ebrl_profile_read", "ebrl_op_gemm", "ebrl_op_gemm_plan",
     "ebrl_op_gemm_noalloc", "ebrl_op_stream_read",
     "ebrl_op_kv8_write", "ebrl_op_kv8_attn", "ebrl_op_kv8_attn_workspace",
+    "ebrl_op_kv8_fork", "ebrl_op_kv8_free", "ebrl_op_kv8_reserve", "ebrl_op_kv8_reserve_workspace",
+    "ebrl_op_kv8_compact", "ebrl_op_kv8_compact_workspace",
+    "ebrl_op_i8_quant", "ebrl_op_i8_gemm", "ebrl_op_i8_gemm_workspace",
     "ebrl_alloc_solve", "ebrl_alloc_objective", "ebrl_alloc_monitor_create", "ebrl_alloc_monitor_observe",
     "ebrl_alloc_monitor_destroy", "ebrl_alloc_refine",
     "ebrl_sched_create", "ebrl_sched_destroy", "ebrl_sched_dispatch", "ebrl_sched_complete",
@@ -152,6 +175,15 @@ def lib():
         "ebrl_op_kv8_write": (i32, [vp, vp, vp]),
         "ebrl_op_kv8_attn": (i32, [vp, vp, vp]),
         "ebrl_op_kv8_attn_workspace": (i64, [vp, vp]),
+        "ebrl_op_kv8_fork": (i32, [vp, vp, vp, vp, i32, vp]),
+        "ebrl_op_kv8_free": (i32, [vp, vp, vp, i32, vp]),
+        "ebrl_op_kv8_reserve": (i32, [vp, vp, vp, vp, i32, i32, vp, vp, i64, vp]),
+        "ebrl_op_kv8_reserve_workspace": (i64, [vp, i32, i32]),
+        "ebrl_op_kv8_compact": (i32, [vp, vp, vp, vp, vp, i64, vp]),
+        "ebrl_op_kv8_compact_workspace": (i64, [vp]),
+        "ebrl_op_i8_quant": (i32, [vp, vp]),
+        "ebrl_op_i8_gemm": (i32, [vp, vp]),
+        "ebrl_op_i8_gemm_workspace": (i64, [vp]),
         "ebrl_alloc_solve": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocLimits),
                                    ctypes.POINTER(AllocResult)]),
         "ebrl_alloc_objective": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocResult)]),
@@ -602,6 +634,294 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
     except (struct.error, OverflowError) as e:
         raise EbrlError(-1, f"kv8: scale {scale}: {e}") from e
     _kv8_call(lib().ebrl_op_kv8_attn, "ebrl_op_kv8_attn", c, a, dev, stream)
+
+
+# ------------------------------------------- pages of the 8-bit KV cache --
+# include/ebrl_kv8_pages.h.  A pool is the caches of one or more layers that share
+# a block table: codes as kv8_alloc makes them, or [layers, num_blocks, 2, kv_heads,
+# 16 * head_dim], scales alike; block_table (entries without a page: -1) and refs,
+# int32 [num_blocks], zero at the start.
+
+_KV8_POOL = struct.Struct("4P2q6i")
+
+
+def _kv8_pool_table(block_table, refs):
+    """Pointers and sizes of a table and its refs, and their GPU's index."""
+    import torch
+    dev = refs.get_device()
+    if refs.dim() != 1 or refs.dtype is not torch.int32 or not refs.is_contiguous():
+        _kv8_bad("refs are contiguous int32 [num_blocks]", refs)
+    if block_table.dim() != 2 or block_table.dtype is not torch.int32 or not block_table.is_contiguous() or \
+            block_table.get_device() != dev:
+        _kv8_bad("block_table is contiguous int32 [sequences, pages] where refs are", block_table)
+    return block_table.data_ptr(), refs.data_ptr(), refs.shape[0], *block_table.shape, dev
+
+
+def _kv8_pool_shape(codes):
+    """Layers, pages, KV heads and head dim; a layer's codes are contiguous, with any distance between layers."""
+    shape = codes.shape
+    if len(shape) not in (4, 5) or shape[-3] != 2 or not shape[-1] or shape[-1] % KV8_PAGE or not _kv8_codes(codes) or \
+            not shape[0]:
+        _kv8_bad("codes are float8_e4m3fn or bytes [layers, num_blocks, 2, kv_heads, 16 * head_dim]", codes)
+    return shape[0] if len(shape) == 5 else 1, shape[-4], shape[-2], shape[-1] // KV8_PAGE
+
+
+def _kv8_pool(codes, scales, block_table, refs):
+    """The packed pool and its GPU's index."""
+    import torch
+    table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
+    layers, pages, heads, hd = _kv8_pool_shape(codes)
+    many = codes.dim() == 5
+    if pages != blocks or not (codes[0] if many else codes).is_contiguous() or codes.get_device() != dev or \
+            codes.stride(0) < 0:
+        _kv8_bad(f"codes of a layer are contiguous [{blocks}, 2, kv_heads, 16 * head_dim] where refs are", codes)
+    if scales.shape != codes.shape[:-1] or scales.dtype is not torch.float32 or \
+            not (scales[0] if many else scales).is_contiguous() or scales.get_device() != dev:
+        _kv8_bad("scales are float32 [layers, num_blocks, 2, kv_heads] where refs are", scales)
+    at, scales_at = (codes.stride(0), scales.stride(0)) if many else (0, 0)
+    return _kv8_pack(_KV8_POOL, codes.data_ptr(), scales.data_ptr(), table_at, refs_at, at, scales_at, layers, blocks,
+                     rows, stride, heads, hd), dev
+
+
+def _kv8_on(fn, name, dev, stream, *args):
+    """fn(*args, stream) on `stream` (None: the current one of the pool's device)."""
+    import torch
+    if dev < 0:
+        _kv8_bad("the pool is not on a GPU")
+    if dev != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return _kv8_on(fn, name, dev, stream, *args)
+    rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream)
+    if rc != EBRL_OK:
+        raise EbrlError(rc, name)
+
+
+def op_kv8_fork(block_table, refs, src, dst, length, stream=None) -> None:
+    """Rows dst of the table take the pages of rows src's first `length` tokens
+    (ebrl_op_kv8_fork).  src, dst, length: int32 [n]."""
+    import torch
+    table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
+    n = dst.numel()
+    at = _kv8_ints(torch.int32, dev, ("src", src, n), ("dst", dst, n), ("length", length, n))
+    c = _kv8_pack(_KV8_POOL, 0, 0, table_at, refs_at, 0, 0, 1, blocks, rows, stride, 1, 64)
+    _kv8_on(lib().ebrl_op_kv8_fork, "ebrl_op_kv8_fork", dev, stream, c, *at, n)
+
+
+def op_kv8_free(block_table, refs, seq, keep=None, stream=None) -> None:
+    """Rows seq of the table release all but the pages of their first `keep` tokens
+    (None: all) (ebrl_op_kv8_free).  seq, keep: int32 [n]."""
+    import torch
+    table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
+    n = seq.numel()
+    at = _kv8_ints(torch.int32, dev, ("seq", seq, n), ("keep", keep, n))
+    c = _kv8_pack(_KV8_POOL, 0, 0, table_at, refs_at, 0, 0, 1, blocks, rows, stride, 1, 64)
+    _kv8_on(lib().ebrl_op_kv8_free, "ebrl_op_kv8_free", dev, stream, c, *at, n)
+
+
+def _kv8_pool_workspace(name, codes, block_table, *sizes):
+    import torch
+    layers, blocks, heads, hd = _kv8_pool_shape(codes)
+    if block_table.dim() != 2:
+        _kv8_bad("block_table is [sequences, pages]", block_table)
+    for x in sizes:
+        if not 0 <= x < 1 << 31:
+            _kv8_bad(f"{name}: {sizes}")
+    need = getattr(lib(), name)(_kv8_pack(_KV8_POOL, 0, 0, 0, 0, 0, 0, layers, blocks, *block_table.shape, heads, hd), *sizes)
+    if need < 0:
+        raise EbrlError(need, name)
+    return torch.empty(need, dtype=torch.uint8, device=codes.device)
+
+
+def kv8_reserve_workspace(codes, block_table, n, max_count):
+    """A workspace for op_kv8_reserve calls of at most n rows and max_count tokens."""
+    return _kv8_pool_workspace("ebrl_op_kv8_reserve_workspace", codes, block_table, n, max_count)
+
+
+def kv8_compact_workspace(codes, block_table):
+    """A workspace for op_kv8_compact."""
+    return _kv8_pool_workspace("ebrl_op_kv8_compact_workspace", codes, block_table)
+
+
+def _kv8_workspace_of(workspace, dev, stream, make):
+    """The given workspace's pointer and size, or a new one's (kept by the third value)."""
+    if workspace is None:
+        if stream is not None:
+            _kv8_bad("a call on an explicit stream needs a workspace")
+        workspace = make()
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _kv8_bad("the workspace is contiguous and where the pool is", workspace)
+    return workspace.data_ptr(), workspace.nbytes, workspace
+
+
+def op_kv8_reserve(codes, scales, block_table, refs, seq, pos0, count, max_count, lacking, workspace=None,
+                   stream=None) -> None:
+    """Pages for tokens pos0 .. pos0 + count - 1 of rows seq, copies of shared ones
+    (ebrl_op_kv8_reserve).  seq, pos0, count: int32 [n]; lacking: int32 [1], how many
+    pages were missing (then nothing has changed).  workspace: from
+    kv8_reserve_workspace, one for each chain of calls that may overlap others; None
+    makes one for this call (not with an explicit stream)."""
+    import torch
+    c, dev = _kv8_pool(codes, scales, block_table, refs)
+    n = seq.numel()
+    if not 0 <= max_count < 1 << 31:
+        _kv8_bad(f"max_count {max_count}")
+    *at, short = _kv8_ints(torch.int32, dev, ("seq", seq, n), ("pos0", pos0, n), ("count", count, n), ("lacking", lacking, 1))
+    work_at, size, keep = _kv8_workspace_of(workspace, dev, stream,
+                                            lambda: kv8_reserve_workspace(codes, block_table, n, max_count))
+    _kv8_on(lib().ebrl_op_kv8_reserve, "ebrl_op_kv8_reserve", dev, stream, c, *at, n, max_count, short, work_at, size)
+
+
+def op_kv8_compact(codes, scales, block_table, refs, new_table, new_refs, used, workspace=None, stream=None) -> None:
+    """The used pages move to the low ids (ebrl_op_kv8_compact); new_table and
+    new_refs (which may be block_table and refs) go with that; used: int32 [1], their
+    number.  workspace: from kv8_compact_workspace, as for op_kv8_reserve."""
+    import torch
+    c, dev = _kv8_pool(codes, scales, block_table, refs)
+    if new_table.shape != block_table.shape or new_refs.shape != refs.shape:
+        _kv8_bad("new_table and new_refs have the shapes of block_table and refs", new_table, new_refs)
+    at = _kv8_ints(torch.int32, dev, ("new_table", new_table, block_table.numel()), ("new_refs", new_refs, refs.numel()),
+                   ("used", used, 1))
+    work_at, size, keep = _kv8_workspace_of(workspace, dev, stream, lambda: kv8_compact_workspace(codes, block_table))
+    _kv8_on(lib().ebrl_op_kv8_compact, "ebrl_op_kv8_compact", dev, stream, c, *at, work_at, size)
+
+
+# ------------------------------------------------- 8-bit integer products --
+# include/ebrl_i8.h.  An operand is int8 codes [rows, K], K a multiple of 16, rows
+# contiguous and 16-byte aligned, and float32 scales [rows].
+
+I8_ROWS, I8_RMSNORM, I8_SWIGLU = range(3)
+_I8_QUANT = struct.Struct("4if2P2q2PqP")
+_I8_GEMM = struct.Struct("4i2P2q4PqPqPq")
+
+
+def i8_alloc(rows: int, cols: int, device="cuda"):
+    """(codes, scales) of an operand of this size, cols rounded up to a multiple of 16."""
+    import torch
+    return (torch.zeros((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device),
+            torch.ones(rows, device=device))
+
+
+def _i8_bad(what: str, *tensors):
+    raise EbrlError(-1, "i8: " + what + "".join(
+        f"; got {None if t is None else (tuple(t.shape), t.stride(), t.dtype, str(t.device))}" for t in tensors))
+
+
+def _i8_pack(packer, *values) -> bytes:
+    try:
+        return packer.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise EbrlError(-1, f"i8: numbers that the structs do not hold: {e}") from e
+
+
+def _i8_codes(name, t, dev):
+    """Pointer, rows, width and row stride of codes."""
+    import torch
+    if t.dim() != 2 or t.dtype is not torch.int8 or t.get_device() != dev:
+        _i8_bad(f"{name} are int8 [rows, K] on one GPU", t)
+    rows, wide = t.shape
+    ld, one = t.stride()
+    if one != 1 and wide > 1:
+        _i8_bad(f"{name} have contiguous rows", t)
+    return t.data_ptr(), rows, wide, ld if rows > 1 else (wide + 15) // 16 * 16
+
+
+def _i8_floats(name, t, n, dev):
+    """Pointer of n float32; 0 for None."""
+    import torch
+    if t is None:
+        return 0
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        _i8_bad(f"{name} is {n} contiguous float32 where the codes are", t)
+    return t.data_ptr()
+
+
+def _i8_rows(name, t, dtype, dev, rows, width):
+    """Pointer and row stride of a [rows, width] tensor whose rows are contiguous; 0 for None."""
+    if t is None:
+        return 0, 0
+    if t.shape != (rows, width) or t.dtype is not dtype or t.get_device() != dev:
+        _i8_bad(f"{name} is {dtype} [{rows}, {width}] where the codes are", t)
+    ld, one = t.stride()
+    if one != 1 and width > 1:
+        _i8_bad(f"{name} has contiguous rows", t)
+    return t.data_ptr(), ld if rows > 1 else width
+
+
+def _i8_dtype(name, t) -> int:
+    import torch
+    dtype = t.dtype
+    if t.dim() != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
+        _i8_bad(f"{name} is bfloat16 or float32 [rows, width]", t)
+    return DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_FP32
+
+
+def _i8_call(fn, name, args, dev, stream):
+    """The call on `stream` (None: the current one of the codes' device)."""
+    import torch
+    if dev < 0:
+        _i8_bad("the codes are not on a GPU")
+    if dev != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return _i8_call(fn, name, args, dev, stream)
+    rc = fn(args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream)
+    if rc != EBRL_OK:
+        raise EbrlError(rc, name)
+
+
+def op_i8_quant(x, codes, scales, up=None, norm_eps=None, gain=None, stream=None) -> None:
+    """Rows x [rows, cols] to codes [rows, K] (K: cols rounded up to a multiple of 16,
+    or more) and scales [rows] (ebrl_op_i8_quant): as they are; with norm_eps, RMS-normed
+    and times gain (float32 [cols] or None); with up, silu(x) * up."""
+    dev = codes.get_device()
+    dtype = _i8_dtype("x", x)
+    rows, cols = x.shape
+    if up is not None and norm_eps is not None or gain is not None and norm_eps is None:
+        _i8_bad("rows are normed (norm_eps, gain) or gated (up), not both")
+    op = I8_SWIGLU if up is not None else I8_RMSNORM if norm_eps is not None else I8_ROWS
+    x_at, ldx = _i8_rows("x", x, x.dtype, dev, rows, cols)
+    up_at, ldup = _i8_rows("up", up, x.dtype, dev, rows, cols)
+    at, n, wide, ldc = _i8_codes("codes", codes, dev)
+    if n != rows or wide < (cols + 15) // 16 * 16:
+        _i8_bad(f"codes are [{rows}, {(cols + 15) // 16 * 16}]", codes)
+    a = _i8_pack(_I8_QUANT, dtype, op, rows, cols, norm_eps or 0.0, x_at, up_at, ldx, ldup,
+                 _i8_floats("gain", gain, cols, dev), at, ldc, _i8_floats("scales", scales, rows, dev))
+    _i8_call(lib().ebrl_op_i8_quant, "ebrl_op_i8_quant", a, dev, stream)
+
+
+def i8_gemm_workspace(a, b):
+    """A workspace for op_i8_gemm of codes a [M, K] and b [N, K], on a's device."""
+    import torch
+    if a.dim() != 2 or b.dim() != 2:
+        _i8_bad("codes are [rows, K]", a, b)
+    need = lib().ebrl_op_i8_gemm_workspace(_i8_pack(_I8_GEMM, 0, a.shape[0], b.shape[0], a.shape[1], *(0,) * 13))
+    if need < 0:
+        raise EbrlError(need, "ebrl_op_i8_gemm_workspace")
+    return torch.empty(need, dtype=torch.uint8, device=a.device)
+
+
+def op_i8_gemm(a, scale_a, b, scale_b, out, bias=None, residual=None, workspace=None, stream=None) -> None:
+    """out = (a scale_a) (b scale_b)^T + bias + residual (ebrl_op_i8_gemm): codes a [M,
+    K], b [N, K]; out [M, N] bfloat16 or float32, residual like out (or out itself).
+    workspace: from i8_gemm_workspace, one for each chain of calls that may overlap
+    others; None makes one for this call (not with an explicit stream)."""
+    dev = a.get_device()
+    a_at, m, k, lda = _i8_codes("a", a, dev)
+    b_at, n, kb, ldb = _i8_codes("b", b, dev)
+    if k != kb:
+        _i8_bad("a and b have rows of one width", a, b)
+    dtype = _i8_dtype("out", out)
+    out_at, ldc = _i8_rows("out", out, out.dtype, dev, m, n)
+    res_at, ldr = _i8_rows("residual", residual, out.dtype, dev, m, n)
+    if workspace is None:
+        if stream is not None:
+            _i8_bad("a call on an explicit stream needs a workspace")
+        workspace = i8_gemm_workspace(a, b)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _i8_bad("the workspace is contiguous and where the codes are", workspace)
+    args = _i8_pack(_I8_GEMM, dtype, m, n, k, a_at, b_at, lda, ldb, _i8_floats("scale_a", scale_a, m, dev),
+                    _i8_floats("scale_b", scale_b, n, dev), _i8_floats("bias", bias, n, dev), res_at, ldr, out_at, ldc,
+                    workspace.data_ptr(), workspace.nbytes)
+    _i8_call(lib().ebrl_op_i8_gemm, "ebrl_op_i8_gemm", args, dev, stream)
 
 
 def create_cu_masked_stream(device: int, mask_words: Sequence[int]) -> int:

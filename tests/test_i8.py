@@ -1,0 +1,370 @@
+"""Projections in 8-bit integers (include/ebrl_i8.h) against their formulas: codes and
+scales of rows, products bit for bit; the calls that are refused."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_27547_amd import ebrl as E
+
+gpu = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+LEAST = 2.0 ** -100
+
+
+# ------------------------------------------------------------ no GPU needed --
+
+def _quant_args(**kw):
+    a = E.I8QuantArgs(dtype=E.DTYPE_BF16, op=E.I8_ROWS, rows=3, cols=40, eps=1e-6, x=4096, ldx=40, codes=8192, ldc=48,
+                      scales=12288)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=2), dict(dtype=-1), dict(op=3), dict(op=-1), dict(rows=-1), dict(cols=0), dict(cols=(1 << 20) + 1),
+    dict(x=0), dict(x=4097), dict(dtype=0, x=4098), dict(ldx=39), dict(codes=0), dict(codes=8200), dict(ldc=40),
+    dict(ldc=32), dict(scales=0), dict(scales=12290), dict(up=4096), dict(gain=4096), dict(op=1, eps=-1.0),
+    dict(op=1, eps=float("nan")), dict(op=1, gain=4098), dict(op=2), dict(op=2, up=4096, ldup=39),
+    dict(op=2, up=4097, ldup=40)])
+def test_quant_refuses_arguments(bad):
+    assert E.lib().ebrl_op_i8_quant(ctypes.byref(_quant_args(**bad)), None) == -1
+
+
+def _gemm_args(**kw):
+    a = E.I8GemmArgs(dtype=E.DTYPE_FP32, M=5, N=7, K=32, a=4096, b=8192, lda=32, ldb=48, scale_a=12288, scale_b=16384,
+                     c=20480, ldc=7)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dtype=2), dict(M=-1), dict(N=-1), dict(K=0), dict(K=24), dict(K=131072), dict(a=0), dict(b=0), dict(a=4104),
+    dict(b=8196), dict(lda=16), dict(lda=40), dict(ldb=-48), dict(lda=1 << 23), dict(ldb=1 << 23), dict(scale_a=0),
+    dict(scale_b=0), dict(scale_a=12290), dict(bias=2), dict(c=0), dict(c=20482), dict(ldc=6), dict(residual=24576),
+    dict(residual=24578, ldr=7), dict(residual=20480, ldr=8), dict(M=1 << 30, N=1 << 30)])
+def test_gemm_refuses_arguments(bad):
+    assert E.lib().ebrl_op_i8_gemm(ctypes.byref(_gemm_args(**bad)), None) == -1
+
+
+def test_calls_of_nothing_are_ok():
+    assert E.lib().ebrl_op_i8_quant(ctypes.byref(_quant_args(rows=0)), None) == 0
+    for kw in (dict(M=0), dict(N=0)):
+        assert E.lib().ebrl_op_i8_gemm(ctypes.byref(_gemm_args(**kw)), None) == 0
+        assert E.lib().ebrl_op_i8_gemm_workspace(ctypes.byref(_gemm_args(**kw))) == 0
+    assert E.lib().ebrl_op_i8_gemm_workspace(ctypes.byref(_gemm_args(K=24))) == -1
+    assert E.lib().ebrl_op_i8_quant(None, None) == -1 and E.lib().ebrl_op_i8_gemm(None, None) == -1
+
+
+def test_binding_refuses():
+    x = torch.zeros((3, 40), dtype=torch.bfloat16)
+    codes, scales = E.i8_alloc(3, 40, device="cpu")
+    assert codes.shape == (3, 48)
+    ok = dict(x=x, codes=codes, scales=scales)
+    for bad in (dict(), dict(x=x.half()), dict(x=x[0]), dict(x=x.t()), dict(x=x[:2]), dict(codes=codes[:, :40]),
+                dict(codes=codes.float()), dict(codes=codes[:2]), dict(scales=scales[:2]), dict(scales=scales.double()),
+                dict(up=x.float()), dict(up=x, norm_eps=1e-6), dict(gain=torch.ones(40)),
+                dict(norm_eps=1e-6, gain=torch.ones(39)), dict(norm_eps=1e-6, gain=torch.ones(40).double())):
+        with pytest.raises(E.EbrlError):
+            E.op_i8_quant(**{**ok, **bad})
+    out = torch.zeros((3, 5))
+    b, sb = E.i8_alloc(5, 40, device="cpu")
+    ok = dict(a=codes, scale_a=scales, b=b, scale_b=sb, out=out)
+    for bad in (dict(), dict(a=codes[:, :32]), dict(b=b.int()), dict(out=out.half()), dict(out=out[:, :4]),
+                dict(out=out.t().contiguous().t()), dict(scale_a=sb), dict(bias=torch.ones(4)),
+                dict(residual=out.bfloat16()), dict(stream=0), dict(a=codes[:, 8:24], b=b[:, :16])):
+        with pytest.raises(E.EbrlError):
+            E.op_i8_gemm(**{**ok, **bad})
+
+
+# --------------------------------------------------------- rows to codes --
+
+def _values(op, x, up, gain, eps):
+    """y in float64, row by row, from the formulas."""
+    x = x.double().cpu().numpy()
+    if op == E.I8_RMSNORM:
+        g = 1.0 if gain is None else gain.double().cpu().numpy()
+        return x / np.sqrt((x * x).mean(1, keepdims=True) + eps) * g
+    if op == E.I8_SWIGLU:
+        with np.errstate(over="ignore"):
+            return x / (1 + np.exp(-x)) * up.double().cpu().numpy()
+    return x
+
+
+def _check_codes(y, codes, scales):
+    """Codes and scales of finite rows y.  y is known to 2^-50 of its size here and in the
+    kernel; a quotient is at most 127, so codes are within 1/2 + 127 * 2^-48 of it, and a
+    scale is within half a step (2^-24, and 2^-48) of max |y| / 127."""
+    cols = y.shape[1]
+    codes, s = codes.cpu().numpy().astype(np.float64), scales.cpu().numpy().astype(np.float64)
+    want = np.maximum(np.abs(y).max(1) / 127, LEAST)
+    assert (np.abs(s - want) <= want * (2.0 ** -24 + 2.0 ** -48)).all()
+    q = y / s[:, None]
+    assert (np.abs(codes[:, :cols] - q) <= 0.5 + 127 * 2.0 ** -48).all()
+    assert (codes[:, cols:(cols + 15) // 16 * 16] == 0).all()
+
+
+def _rows(rows, cols, dtype, g, pad=0, shift=0):
+    """Rows with a few large columns, `pad` elements apart, `shift` elements off an aligned start."""
+    x = torch.randn((rows, cols), generator=g) * torch.where(torch.rand(cols, generator=g) < 0.02, 8.0, 1.0)
+    wide = torch.empty(shift + rows * (cols + pad), dtype=DT[dtype], device="cuda")
+    at = wide.as_strided((rows, cols), (cols + pad, 1), shift)
+    at.copy_(x)
+    return at
+
+
+OPS = {"rows": E.I8_ROWS, "norm": E.I8_RMSNORM, "gate": E.I8_SWIGLU}
+
+
+@gpu
+@pytest.mark.parametrize("op", list(OPS))
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,cols,pad,shift", [
+    (1, 1, 0, 0), (2, 15, 0, 0), (3, 16, 0, 0), (5, 17, 3, 1), (1, 64, 0, 0), (7, 256, 8, 0), (4, 1000, 0, 0),
+    (9, 1024, 0, 0), (9, 1024, 1, 1), (33, 1283, 0, 0), (3, 2048, 16, 8), (70, 4096, 0, 0), (2, 4104, 0, 0),
+    (5, 8191, 1, 0), (6, 8192, 0, 0), (3, 11008, 11008, 0), (2, 16384, 0, 0), (2, 16400, 0, 3), (1, 70000, 0, 0),
+    (300, 48, 0, 0), (1025, 512, 0, 0)])
+def test_codes_are_the_formulas(op, dtype, rows, cols, pad, shift):
+    g = torch.Generator().manual_seed(rows * 7 + cols)
+    x = _rows(rows, cols, dtype, g, pad, shift)
+    up = _rows(rows, cols, dtype, g, pad, shift) if op == "gate" else None
+    gain = 1 + 0.1 * torch.randn(cols, generator=g).cuda() if op == "norm" and rows % 2 else None
+    k = (cols + 15) // 16 * 16
+    held = torch.full((rows, k + 32), 77, dtype=torch.int8, device="cuda")
+    codes, scales = held[:, :k + 16], torch.empty(rows, device="cuda")
+    E.op_i8_quant(x, codes, scales, up=up, gain=gain, norm_eps=1e-6 if op == "norm" else None)
+    torch.cuda.synchronize()
+    _check_codes(_values(OPS[op], x, up, gain, 1e-6), held, scales)
+    assert (held[:, k:] == 77).all()
+    if op == "rows":
+        # both sides' quotients of two floats are the same number in 64 bits
+        s = scales.double().cpu().numpy()
+        assert (held[:, :cols].cpu().numpy() == np.rint(x.double().cpu().numpy() / s[:, None])).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_codes_at_ties(dtype):
+    """Values that are whole and half steps exactly: ties go to the even code."""
+    half = torch.arange(-254, 255, dtype=torch.float32) / 2
+    if dtype == "bf16":
+        half = half[half.bfloat16().float() == half]
+    x = torch.stack([half * 0.25, half * 2.0 ** -90]).to(DT[dtype]).cuda()
+    codes, scales = E.i8_alloc(*x.shape)
+    E.op_i8_quant(x, codes, scales)
+    assert scales.tolist() == [0.25, 2.0 ** -90]
+    assert (codes[:, :x.shape[1]].cpu().float() == torch.round(half)).all()
+
+
+@gpu
+@pytest.mark.parametrize("cols", [24, 1024, 5000, 20000])
+def test_rows_of_any_size_of_number(cols):
+    """Zeros, numbers below the least scale, denormals, the largest floats."""
+    g = torch.Generator().manual_seed(cols)
+    base = torch.randn((8, cols), generator=g).clamp(-4, 4)
+    size = torch.tensor([0.0, 2.0 ** -140, 2.0 ** -100, 2.0 ** -93, 1.0, 2.0 ** 100, 2.0 ** 125, 2.0 ** 20])
+    x = (base * size[:, None]).cuda()
+    for op in ("rows", "norm"):
+        codes, scales = E.i8_alloc(8, cols)
+        E.op_i8_quant(x, codes, scales, norm_eps=1e-30 if op == "norm" else None)
+        _check_codes(_values(OPS[op], x, None, None, float(np.float32(1e-30))), codes, scales)
+    codes, scales = E.i8_alloc(8, cols)
+    E.op_i8_quant(torch.zeros_like(x), codes, scales, norm_eps=0.0)       # 0 / 0
+    assert scales.isnan().all() and (codes == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("op", list(OPS))
+@pytest.mark.parametrize("cols", [33, 512, 1024, 4096, 11008, 20001])
+def test_rows_that_are_not_finite(op, dtype, cols):
+    """One such value, anywhere in a row, gives the row codes of zero and the scale NaN; its
+    neighbours keep theirs."""
+    g = torch.Generator().manual_seed(cols)
+    x = _rows(9, cols, dtype, g)
+    up = _rows(9, cols, dtype, g) if op == "gate" else None
+    bad = {1: float("nan"), 3: float("inf"), 5: -float("inf"), 7: float("nan")}
+    for i, (row, v) in enumerate(bad.items()):
+        (up if op == "gate" and i % 2 == 0 else x)[row, (cols - 1) * i // 3] = v
+    kw = dict(up=up, norm_eps=1e-6 if op == "norm" else None)
+    codes, scales = E.i8_alloc(9, cols)
+    codes.fill_(5)
+    E.op_i8_quant(x, codes, scales, **kw)
+    rows = sorted(bad)
+    good = [r for r in range(9) if r not in bad]
+    assert scales[rows].isnan().all() and (codes[rows] == 0).all()
+    y = _values(OPS[op], x[good], None if up is None else up[good], None, 1e-6)
+    _check_codes(y, codes[good], scales[good])
+
+
+@gpu
+def test_scales_past_the_range():
+    """silu(x) up that no float holds: the row counts as not finite."""
+    x = torch.full((2, 64), 3e38, device="cuda")
+    up = torch.full((2, 64), 3e38, device="cuda")
+    up[1] = 1e-38
+    codes, scales = E.i8_alloc(2, 64)
+    E.op_i8_quant(x, codes, scales, up=up)
+    assert scales[0].isnan() and (codes[0] == 0).all() and (codes[1] == 127).all()
+    _check_codes(_values(2, x[1:], up[1:], None, 0), codes[1:], scales[1:])
+
+
+# -------------------------------------------------------------- products --
+
+def _operand(rows, k, g, ld=0):
+    held = torch.randint(-128, 128, (rows, ld or k), generator=g, dtype=torch.int8).cuda()
+    return held[:, :k], (torch.rand(rows, generator=g) + 0.5).cuda() * 2.0 ** -7
+
+
+def _sums(a, b):
+    """Whole-number products on the GPU in 64-bit floats: below 2^53, so exact."""
+    return torch.matmul(a.double(), b.double().t())
+
+
+def _expected(a, sa, b, sb, bias, residual, dtype):
+    """The steps of the documentation, each rounded to 32 bits."""
+    v = _sums(a, b).float() * sb[None, :]
+    v = v * sa[:, None]
+    if bias is not None:
+        v = v + bias
+    if residual is not None:
+        v = v + residual.float()
+    return v.to(DT[dtype])
+
+
+def _same(x, y):
+    return torch.equal(x.isnan(), y.isnan()) and torch.equal(x.nan_to_num(), y.nan_to_num())
+
+
+SHAPES = [(1, 1, 16), (1, 16, 64), (1, 4096, 4096), (2, 33, 48), (3, 1000, 128), (8, 4096, 11008), (15, 100, 1040),
+          (16, 64, 1024), (17, 257, 256), (31, 22016, 4096), (32, 96, 8192), (33, 1024, 1024), (37, 4100, 272),
+          (48, 512, 131056), (64, 64, 64), (65, 2048, 2048), (100, 1003, 1296), (128, 128, 128), (129, 4096, 4096),
+          (200, 300, 400), (255, 1024, 4096), (256, 1024, 11008), (257, 513, 192), (300, 12288, 4096), (424, 1024, 4096),
+          (591, 1003, 1296), (800, 1000, 2064), (1024, 2048, 1024), (2048, 8192, 272), (2304, 1024, 4096),
+          (3200, 8192, 1024), (4097, 4100, 1040), (5476, 1024, 4096), (9216, 64, 80), (40000, 16, 128)]
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", SHAPES)
+def test_products_bit_for_bit(m, n, k):
+    g = torch.Generator().manual_seed(m + n + k)
+    for dtype, extra, bias, resid in (("fp32", 0, False, True), ("bf16", 32, True, False), ("bf16", 0, False, True)):
+        a, sa = _operand(m, k, g, k + extra)
+        b, sb = _operand(n, k, g, k + extra)
+        if not extra and m > 2:
+            sa[m // 2] = float("nan")
+        bias = torch.randn(n, generator=g).cuda() if bias else None
+        pad = 3 if extra else 0
+        held = torch.full((m, n + pad), 9.0, dtype=DT[dtype], device="cuda")
+        res = torch.randn((m, n), generator=g).to(DT[dtype]).cuda() if resid else None
+        want = _expected(a, sa, b, sb, bias, res, dtype)
+        work = E.i8_gemm_workspace(a, b)
+        work.fill_(0xA5)
+        E.op_i8_gemm(a, sa, b, sb, held[:, :n], bias=bias, residual=res, workspace=work)
+        assert _same(held[:, :n], want), f"{dtype} {extra}"
+        assert (held[:, n:] == 9).all()
+        if resid:   # in place
+            E.op_i8_gemm(a, sa, b, sb, res, bias=bias, residual=res, workspace=work)
+            assert _same(res, want)
+
+
+@gpu
+def test_sums_at_the_end_of_the_range():
+    """-128 times -128 at the longest K: 2^31 - 2^18, exactly; and the most negative sum."""
+    k = 131056
+    a = torch.full((2, k), -128, dtype=torch.int8, device="cuda")
+    b = torch.full((40, k), -128, dtype=torch.int8, device="cuda")
+    b[7] = 127
+    one = torch.ones(40, device="cuda")
+    out = torch.empty((2, 40), device="cuda")
+    E.op_i8_gemm(a, one[:2], b, one, out)
+    want = torch.full((40,), float(128 * 128 * k), dtype=torch.float64)
+    want[7] = -128.0 * 127 * k
+    assert (out.cpu().double() == want.float().double()).all()
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 4096, 11008), (64, 1024, 2048), (591, 1003, 1296), (2304, 2048, 1024)])
+def test_rows_do_not_depend_on_the_call(m, n, k):
+    """A row's outputs are the same in a call of its own, on a few compute units, and on another stream."""
+    g = torch.Generator().manual_seed(k)
+    a, sa = _operand(m, k, g)
+    b, sb = _operand(n, k, g)
+    out = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    E.op_i8_gemm(a, sa, b, sb, out)
+    i = m // 2
+    one = torch.empty((1, n), dtype=torch.bfloat16, device="cuda")
+    E.op_i8_gemm(a[i:i + 1], sa[i:i + 1], b, sb, one)
+    assert torch.equal(one[0], out[i])
+    again = torch.empty_like(out)
+    work = E.i8_gemm_workspace(a, b)
+    torch.cuda.synchronize()
+    s = E.create_cu_masked_stream(0, [0xFFFF] + [0] * 7)
+    try:
+        E.op_i8_gemm(a, sa, b, sb, again, workspace=work, stream=s)
+        torch.cuda.synchronize()
+    finally:
+        E.destroy_stream(s)
+    assert torch.equal(again, out)
+    side = torch.cuda.Stream()
+    again.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        E.op_i8_gemm(a, sa, b, sb, again, workspace=work)
+    side.synchronize()
+    assert torch.equal(again, out)
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 37, 600])
+def test_captured_linear_is_replayed(m):
+    """Quantised rows and their product in a graph, replayed on new inputs beside eager calls."""
+    g = torch.Generator().manual_seed(m)
+    k, n = 1024, 1000
+    x = torch.randn((m, k), generator=g).cuda()
+    b, sb = _operand(n, k, g)
+    a, sa = E.i8_alloc(m, k)
+    out = torch.empty((m, n), device="cuda")
+    work = E.i8_gemm_workspace(a, b)
+
+    def step(to, codes, scales, w):
+        E.op_i8_quant(x, codes, scales, norm_eps=1e-6)
+        E.op_i8_gemm(codes, scales, b, sb, to, workspace=w)
+    step(out, a, sa, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, a, sa, work)
+    other, (a2, sa2) = torch.empty_like(out), E.i8_alloc(m, k)
+    for i in range(4):
+        x.copy_(torch.randn((m, k), generator=g))
+        step(other, a2, sa2, None)
+        if i == 2:
+            torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, other) and torch.equal(a, a2)
+
+
+@gpu
+def test_quantised_linear_layer():
+    """Weights and rows by op_i8_quant: within the steps' bound of the layer in 64 bits.  Each code is off by
+    half a step of its row's scale, so an output by at most sum (|a| sb + |b| sa + sa sb / 2) / 2, and its own
+    rounding."""
+    g = torch.Generator().manual_seed(5)
+    m, n, k = 50, 200, 1000
+    x, w = torch.randn((m, k), generator=g).cuda(), torch.randn((n, k), generator=g).cuda()
+    a, sa = E.i8_alloc(m, k)
+    b, sb = E.i8_alloc(n, k)
+    E.op_i8_quant(x, a, sa)
+    E.op_i8_quant(w, b, sb)
+    out = torch.empty((m, n), device="cuda")
+    E.op_i8_gemm(a, sa, b, sb, out)
+    xd, wd, s, t = x.double(), w.double(), sa.double()[:, None], sb.double()[None]
+    bound = (xd.abs().sum(1)[:, None] * t + wd.abs().sum(1)[None] * s + k * s * t / 2) / 2
+    want = xd @ wd.t()
+    assert ((out.double() - want).abs() <= bound + want.abs() * 2.0 ** -21 + bound * 2.0 ** -21).all()
