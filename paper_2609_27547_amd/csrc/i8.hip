@@ -7,6 +7,7 @@
 #include "../../include/ebrl.h"
 #include "../../include/ebrl_i8.h"
 #include "kernels.h"
+#include "tile.h"
 
 namespace ebrl {
 
@@ -81,71 +82,441 @@ __global__ __launch_bounds__(256) void i8_quant_kernel(ebrl_i8_quant_args a)
 }
 
 // -------------------------------------------------------------- product --
+// All kernels hold the weights' rows as the first operand of
+// v_mfma_i32_16x16x64_i8: a lane (r, g) gives bytes 16 g .. of row r, and gets
+// outputs n = 4 g .. of row m = r.  Sums are whole numbers: any order gives the
+// same, so tiles and cuts of K are free to follow the size of a call.
+//
+// K tiles are 128 bytes, a cache line of each row.  The last one may be shorter:
+// its loads past K repeat the last 16 bytes of the row, and the first operand's
+// fragments past K are zeros.
 
-// One element's epilogue and its store; `m`, `n` inside.
+// The outputs that a lane stores: four neighbours of a row.
 template <typename T> struct I8Epi {
     const float *scale_a, *scale_b, *bias;
     const T* residual;
     T* c;
     int64_t ldr, ldc;
-    EBRL_DEV void operator()(int m, int n, int sum) const {
+    bool wide;              // rows of c and residual are 16-byte aligned (so is N a multiple of four)
+
+    struct Cols { f32x4 s, b; };
+    EBRL_DEV Cols cols(int n, int N) const {
+        Cols k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int at = min(n + e, N - 1);
+            k.s[e] = scale_b[at];
+            k.b[e] = bias ? bias[at] : 0.f;
+        }
+        return k;
+    }
+    EBRL_DEV f32x4 value(i32x4 sum, const Cols& k, float sa) const {
 #pragma clang fp contract(off)
-        float v = (float)sum * scale_b[n] * scale_a[m];
-        if (bias) v += bias[n];
-        if (residual) v += ld_elem<T>(residual + (size_t)m * ldr + n);
-        st_elem<T>(c + (size_t)m * ldc + n, v);
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * k.s[e] * sa;
+        if (bias) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += k.b[e];
+        }
+        return v;
+    }
+    // Four outputs inside, all aligned.
+    EBRL_DEV void store_wide(int m, int n, i32x4 sum, const Cols& k, float sa) const {
+        f32x4 v = value(sum, k, sa);
+        if (residual) {
+            const T* r = residual + (size_t)m * ldr + n;
+            if constexpr (sizeof(T) == 4) {
+                v += *reinterpret_cast<const f32x4*>(r);
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(r);
+                v[0] += __uint_as_float(w.x << 16); v[1] += __uint_as_float(w.x & 0xFFFF0000u);
+                v[2] += __uint_as_float(w.y << 16); v[3] += __uint_as_float(w.y & 0xFFFF0000u);
+            }
+        }
+        st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
+    }
+    EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Cols& k, float sa) const {
+        if (m >= M || n >= N) return;
+        if (wide) { store_wide(m, n, sum, k, sa); return; }
+        const f32x4 v = value(sum, k, sa);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) {
+                float x = v[e];
+                if (residual) x += ld_elem<T>(residual + (size_t)m * ldr + n + e);
+                st_elem<T>(c + (size_t)m * ldc + n + e, x);
+            }
     }
 };
 
-// 64 x 64 tiles on four waves of 32 x 32, K 64 at a time through LDS.  The
-// weights' rows are the first operand: a lane (r, g) of
-// v_mfma_i32_16x16x64_i8 gives bytes 16 g .. of row r, and gets outputs n = 4 g ..
-// of row m = r.
+EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32x4*>(lds); }
+
+// 256 x 256 tiles, eight waves of 128 x 64 in two groups of four that run half a
+// phase apart, as in the large bf16 kernel: while one group multiplies from
+// registers, the other reads its next fragments from LDS and issues DMA.  A K tile
+// is two phases: all of a wave's columns with its first 64 rows, then its last 64.
+// Two LDS stages of 64 KB, refilled by half operands as soon as both groups have
+// read them.  Workgroups are persistent; the next tile's first DMAs go out before
+// the epilogue, whose stores drain behind them.  `full` tiles are dealt evenly, those
+// of the last round cut in `split`.
 template <typename T>
-__global__ __launch_bounds__(256) void i8_gemm_kernel(const int8_t* __restrict__ A, int64_t lda,
-                                                      const int8_t* __restrict__ B, int64_t ldb, int M, int N, int K,
-                                                      I8Epi<T> epi)
+__global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict__ A, uint32_t lda,
+                                                        const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
+                                                        int full, int split, I8Epi<T> epi)
 {
-    __shared__ __attribute__((aligned(16))) int8_t sA[64 * 80], sB[64 * 80];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int tiles_n = (N + 63) / 64;
-    const int m0 = blockIdx.x / tiles_n * 64, n0 = blockIdx.x % tiles_n * 64;
-    const int wm = wave >> 1, wn = wave & 1, r = lane & 15, g = lane >> 4;
-    const int row = tid >> 2, ch = tid & 3;
-    const int8_t* pa = A + (size_t)min(m0 + row, M - 1) * lda + ch * 16;
-    const int8_t* pb = B + (size_t)min(n0 + row, N - 1) * ldb + ch * 16;
-    i32x4 acc[2][2] = {};
-    for (int k = 0; k < K; k += 64) {
-        i32x4 va = {}, vb = {};
-        if (k + ch * 16 < K) {
-            va = *reinterpret_cast<const i32x4*>(pa + k);
-            vb = *reinterpret_cast<const i32x4*>(pb + k);
-        }
-        __syncthreads();
-        *reinterpret_cast<i32x4*>(sA + row * 80 + ch * 16) = va;
-        *reinterpret_cast<i32x4*>(sB + row * 80 + ch * 16) = vb;
-        __syncthreads();
-        i32x4 fa[2], fb[2];
+    constexpr int STAGES = 2 * 65536;   // operand stages; 4 KB of epilogue staging per wave follow
+    __shared__ __attribute__((aligned(1024))) char smem[STAGES + 8 * 4096];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 2, wc = wave & 3;   // group (row half of the tile) and column quarter
+    const int r = lane & 15, g = lane >> 4;
+    const int tiles_m = (M + 255) >> 8, tiles_n = (N + 255) >> 8;
+    const int nk = (K + 127) >> 7, rest = K - (nk - 1) * 128;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)smem);
+    // byte in the K tile that this lane loads, and how far past the last one's end that is
+    const uint32_t kb = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t past = (uint32_t)max(0, (int)kb - (rest - 16));
+
+    auto run = [&](auto FAC, auto FBC, int m0, int n0, auto next) {
+        constexpr int FA = decltype(FAC)::value, FB = decltype(FBC)::value;
+        constexpr int HA = 16 * FA, HB = 16 * FB;        // a wave's rows / columns per half
+        constexpr int NA = FA / 2, NB = FB;              // DMA instructions per wave and half
+        constexpr int AHALF = 2 * HA * 128, BHALF = 4 * HB * 128, SB = 2 * (AHALF + BHALF);
+        constexpr int W = 2 * NA + 2 * NB;               // DMA instructions per wave and K tile
+        static_assert(2 * SB <= STAGES, "stages");
+        // stores of an interior tile's epilogue, at least: they may still be in
+        // flight behind the next tile's first loads
+        constexpr int EST = 2 * FA * 4 * FB / 2;
+        static_assert(W + EST < 64, "vmcnt range");
+        uint32_t va[2][NA], vb[2][NB];
+        const char *pA, *pB;
+        auto dmaA = [&](int t, int h) {
+            const char* p = pA + (size_t)t * 128;
+            const uint32_t l = lds0 + (t & 1) * SB + h * AHALF + wave * NA * 1024;
+            const uint32_t back = t == nk - 1 ? past : 0u;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fa[i] = *reinterpret_cast<const i32x4*>(sA + (wm * 32 + i * 16 + r) * 80 + g * 16);
-            fb[i] = *reinterpret_cast<const i32x4*>(sB + (wn * 32 + i * 16 + r) * 80 + g * 16);
-        }
+            for (int j = 0; j < NA; ++j) dma16_to_lds_s(p, va[h][j] - back, l + j * 1024);
+        };
+        auto dmaB = [&](int t, int h) {
+            const char* p = pB + (size_t)t * 128;
+            const uint32_t l = lds0 + (t & 1) * SB + 2 * AHALF + h * BHALF + wave * NB * 1024;
+            const uint32_t back = t == nk - 1 ? past : 0u;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < NB; ++j) dma16_to_lds_s(p, vb[h][j] - back, l + j * 1024);
+        };
+        // K tiles 0 and 1 but for the second half of A's tile 1; rows past the
+        // operand repeat its last one.  LDS row q of a half h holds tile row
+        // (q / HA) 2 HA + h HA + q % HA: each wave's rows are contiguous.
+        auto prologue = [&]() {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    }
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+                for (int j = 0; j < NA; ++j) {
+                    const int q = (wave * NA + j) * 8 + (lane >> 3);
+                    const int row = (q / HA) * 2 * HA + h * HA + q % HA;
+                    va[h][j] = (uint32_t)min(row, M - 1 - m0) * lda + kb;
+                }
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int m = m0 + wm * 32 + i * 16 + r, n = n0 + wn * 32 + j * 16 + 4 * g + e;
-                if (m < M && n < N) epi(m, n, acc[i][j][e]);
+                for (int j = 0; j < NB; ++j) {
+                    const int q = (wave * NB + j) * 8 + (lane >> 3);
+                    const int row = (q / HB) * 2 * HB + h * HB + q % HB;
+                    vb[h][j] = (uint32_t)min(row, N - 1 - n0) * ldb + kb;
+                }
             }
+            pA = uniform_ptr(A + (size_t)m0 * lda);
+            pB = uniform_ptr(B + (size_t)n0 * ldb);
+            dmaB(0, 0); dmaA(0, 0); dmaB(0, 1); dmaA(0, 1);
+            if (nk > 1) { dmaB(1, 0); dmaA(1, 0); dmaB(1, 1); }
+        };
+        uint32_t a_off[2], b_off[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            a_off[ks] = (uint32_t)((wr * HA + r) * 128 + (((ks * 4 + g) ^ (r & 7)) << 4));
+            b_off[ks] = (uint32_t)(2 * AHALF + (wc * HB + r) * 128 + (((ks * 4 + g) ^ (r & 7)) << 4));
+        }
+        i32x4 acc[2][2][FA][FB];
+        i32x4 fa[2][FA], fb0[2][FB], fb1[2][FB];
+        auto readA = [&](int st, int h) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < FA; ++i) fa[ks][i] = i8_fragment(smem + st + a_off[ks] + h * AHALF + i * 2048);
+        };
+        auto readB = [&](int st, int h, i32x4 (&f)[2][FB]) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int j = 0; j < FB; ++j) f[ks][j] = i8_fragment(smem + st + b_off[ks] + h * BHALF + j * 2048);
+        };
+        // fragments past K to zero
+        auto cut = [&](i32x4 (&f)[2][FB]) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+                if (ks * 64 + g * 16 >= rest) {
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) f[ks][j] = i32x4{0, 0, 0, 0};
+                }
+        };
+        auto mma = [&](i32x4 (&c)[FA][FB], const i32x4 (&f)[2][FB]) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < FB; ++j)
+                        c[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f[ks][j], fa[ks][i], c[i][j], 0, 0, 0);
+        };
+        // Phase p of a group: read fragments, issue DMA, wait for the DMA that
+        // phase p + 1 reads, barrier, multiply, barrier.  A group's reads are
+        // complete before its first barrier, so what phase p reads may be refilled
+        // from phase p + 1 on, by either group.  One K tile with L further ones (0,
+        // 1, 2 = two or more); ov: the previous output tile's stores sit between
+        // this tile's DMAs.
+        auto ktile = [&](int t, bool ov, auto LC) {
+            constexpr int L = decltype(LC)::value;
+            const int st = (t & 1) * SB;
+            readB(st, 0, fb0); readA(st, 0); readB(st, 1, fb1);
+            if constexpr (L >= 1) dmaA(t + 1, 1);
+            if constexpr (L >= 2) { if (ov) wait_vmcnt<W + EST>(); else wait_vmcnt<W>(); }
+            else if constexpr (L == 1) wait_vmcnt<W>();
+            else wait_vmcnt<0>();
+            wait_lds();
+            wg_barrier();
+            if constexpr (L == 0) { cut(fb0); cut(fb1); }
+            mma(acc[0][0], fb0); mma(acc[0][1], fb1);
+            wg_barrier();
+            readA(st, 1);
+            if constexpr (L >= 2) {
+                dmaB(t + 2, 0); dmaA(t + 2, 0); dmaB(t + 2, 1);
+                if (ov) wait_vmcnt<W + EST>(); else wait_vmcnt<W>();
+            } else if constexpr (L == 1) wait_vmcnt<NA>();
+            wait_lds();
+            wg_barrier();
+            mma(acc[1][0], fb0); mma(acc[1][1], fb1);
+            wg_barrier();
+        };
+        prologue();
+        bool over = false;   // an interior tile's stores were issued behind the prologue
+        for (;;) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < FA; ++i)
+#pragma unroll
+                        for (int j = 0; j < FB; ++j) acc[a][b][i][j] = i32x4{0, 0, 0, 0};
+            // first B halves and first A half of K tile 0
+            if (nk > 1) { if (over) wait_vmcnt<W + EST>(); else wait_vmcnt<W>(); }
+            else wait_vmcnt<NA>();
+            wg_barrier();
+            if (wr == 1) wg_barrier();   // the second group runs half a phase behind
+            int t = 0;
+            for (; t + 2 < nk; ++t) ktile(t, over && t == 0, std::integral_constant<int, 2>{});
+            if (t + 1 < nk) { ktile(t, false, std::integral_constant<int, 1>{}); ++t; }
+            ktile(t, false, std::integral_constant<int, 0>{});
+            if (wr == 0) wg_barrier();   // both groups are done with the stages
+            const int mw = m0 + wr * 2 * HA, nw = n0 + wc * 2 * HB;
+            const bool inside = epi.wide && m0 + 4 * HA <= M && n0 + 8 * HB <= N;
+            // this lane's columns, and the scales of the wave's rows lane and 64 + lane
+            constexpr int LPR = 2 * HB / 4, RPP = 64 / LPR;   // lanes a row, rows a pass
+            const int col = nw + lane % LPR * 4;
+            const auto cols = epi.cols(col, N);
+            constexpr int RV = FA / 2;
+            float row_scale[RV];
+#pragma unroll
+            for (int v = 0; v < RV; ++v) row_scale[v] = epi.scale_a[min(mw + v * 64 + lane, M - 1)];
+            const bool more = next(m0, n0);
+            if (more) prologue();
+            // Through the wave's own staging LDS, 16 rows at a time; chunks swizzled
+            // by row so that the fragment-layout writes and the row-contiguous reads
+            // spread over all banks.
+            char* const stage = smem + STAGES + wave * 4096;
+            auto swz = [](int row) { return ((row & 1) << 2) | ((row >> 1) & 3) | (row & 8); };
+            auto epilogue = [&](auto IN) {
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < FA; ++i) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int j = 0; j < FB; ++j)
+                                *reinterpret_cast<i32x4*>(stage + r * 256 + ((((b * FB + j) * 4 + g) ^ swz(r)) << 4)) =
+                                    acc[a][b][i][j];
+                        const int row0 = a * HA + i * 16;
+#pragma unroll
+                        for (int pass = 0; pass < 16 / RPP; ++pass) {
+                            const int row = pass * RPP + lane / LPR;
+                            const i32x4 sum = *reinterpret_cast<const i32x4*>(
+                                stage + row * 256 + (((lane % LPR) ^ swz(row)) << 4));
+                            const float sa = __shfl(row_scale[row0 / 64], row0 % 64 + row, 64);
+                            if constexpr (decltype(IN)::value) epi.store_wide(mw + row0 + row, col, sum, cols, sa);
+                            else epi.store(mw + row0 + row, col, M, N, sum, cols, sa);
+                        }
+                    }
+            };
+            if (inside) epilogue(std::true_type{});
+            else epilogue(std::false_type{});
+            if (!more) break;
+            over = inside;
+        }
+    };
+
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I4 = std::integral_constant<int, 4>;
+    // The dispatcher deals workgroup ids round-robin over the 8 XCDs: XCD x's
+    // workgroups walk a contiguous range of tiles together and share its L2.
+    const int P = gridDim.x, bid = blockIdx.x;
+    if (full > 0) {
+        const int rounds = full / P;
+        int i = 0;
+        auto origin = [&](int k, int& m, int& n) {
+            const int v = (P & 7) == 0 ? (bid & 7) * (full >> 3) + k * (P >> 3) + (bid >> 3) : k * P + bid;
+            tile_origin(v, tiles_m, tiles_n, 256, 256, m, n);
+        };
+        int m0, n0;
+        origin(0, m0, n0);
+        run(I4{}, I2{}, m0, n0, [&](int& m, int& n) {
+            if (++i >= rounds) return false;
+            origin(i, m, n);
+            return true;
+        });
+    }
+    // The last round: at most one (part of a) tile per workgroup.
+    const int items = (tiles_m * tiles_n - full) * split;
+    if (bid >= items) return;
+    const int x = bid & 7;
+    const int s = x * (items >> 3) + min(x, items & 7) + (bid >> 3);
+    int m0, n0;
+    tile_origin(full + s / split, tiles_m, tiles_n, 256, 256, m0, n0);
+    auto none = [](int&, int&) { return false; };
+    const int part = s % split;
+    m0 += (part & 1) * 128;
+    n0 += (part >> 1) * 128;
+    if (m0 >= M || n0 >= N) return;
+    if (split == 1) run(I4{}, I2{}, m0, n0, none);
+    else if (split == 2) run(I2{}, I2{}, m0, n0, none);
+    else run(I2{}, I1{}, m0, n0, none);
+}
+
+// Small outputs (fewer 256 x 256 tiles than CUs): BM x BN tiles on four waves
+// (2 x 2), a ring of ST K tiles in LDS with ST - 1 of them in flight, one barrier a
+// K tile.
+template <typename T, int BM, int BN, int ST>
+__global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restrict__ A, uint32_t lda,
+                                                         const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
+                                                         I8Epi<T> epi)
+{
+    constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 16, TN = WTN / 16;
+    constexpr int SB = (BM + BN) * 128;                // bytes of a stage
+    constexpr int PER = (BM + BN) / 32;                // DMA instructions per wave and K tile
+    static_assert((BM + BN) % 32 == 0 && BM % 8 == 0 && ST >= 2 && ST <= 4, "ring");
+    __shared__ __attribute__((aligned(1024))) char smem[ST * SB];
+    const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+    int bid = blockIdx.x;
+    {
+        // XCD x takes the x-th contiguous range of tiles
+        const int nb = gridDim.x, x = bid & 7;
+        bid = x * (nb >> 3) + min(x, nb & 7) + (bid >> 3);
+    }
+    int m0, n0;
+    tile_origin(bid, tiles_m, tiles_n, BM, BN, m0, n0);
+    const int nk = (K + 127) >> 7, rest = K - (nk - 1) * 128;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int r = lane & 15, g = lane >> 4;
+    const uint32_t kb = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t past = (uint32_t)max(0, (int)kb - (rest - 16));
+
+    // 8-row groups of a stage, A's first: PER per wave
+    uint32_t vo[PER];
+    const char* base[PER];
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)smem + wave * PER * 1024);
+    const char* const pA = uniform_ptr(A + (size_t)m0 * lda);
+    const char* const pB = uniform_ptr(B + (size_t)n0 * ldb);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int q0 = (wave * PER + j) * 8, q = q0 + (lane >> 3);
+        vo[j] = (q0 < BM ? (uint32_t)min(q, M - 1 - m0) * lda : (uint32_t)min(q - BM, N - 1 - n0) * ldb) + kb;
+        base[j] = q0 < BM ? pA : pB;
+    }
+    auto dma = [&](int t, int st) {
+        const uint32_t back = t == nk - 1 ? past : 0u;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) dma16_to_lds_s(base[j] + (size_t)t * 128, vo[j] - back, lds0 + st * SB + j * 1024);
+    };
+    uint32_t a_off[2], b_off[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        a_off[ks] = (uint32_t)((wm * WTM + r) * 128 + (((ks * 4 + g) ^ (r & 7)) << 4));
+        b_off[ks] = (uint32_t)((BM + wn * WTN + r) * 128 + (((ks * 4 + g) ^ (r & 7)) << 4));
+    }
+    i32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    for (int p = 0; p < ST - 1 && p < nk; ++p) dma(p, p);
+    int st = 0, nst = ST - 1;
+    for (int t = 0; t < nk; ++t) {
+        // this wave's part of tile t has landed (the tiles issued after it may
+        // stay in flight); after the barrier every wave's has, and all have
+        // read tile t - 1, whose stage is refilled next
+        const int later = min(ST - 2, nk - 1 - t);
+        if (ST >= 4 && later >= 2) wait_vmcnt<2 * PER>();
+        else if (ST >= 3 && later >= 1) wait_vmcnt<PER>();
+        else wait_vmcnt<0>();
+        wg_barrier();
+        if (t + ST - 1 < nk) dma(t + ST - 1, nst);
+        const char* const s = smem + st * SB;
+        i32x4 w[2][TN], x[2][TM];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) w[ks][j] = i8_fragment(s + b_off[ks] + j * 2048);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x[ks][i] = i8_fragment(s + a_off[ks] + i * 2048);
+        }
+        if (t == nk - 1) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+                if (ks * 64 + g * 16 >= rest) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) w[ks][j] = i32x4{0, 0, 0, 0};
+                }
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[ks][j], x[ks][i], acc[i][j], 0, 0, 0);
+        nst = st;
+        st = st + 1 == ST ? 0 : st + 1;
+    }
+    // epilogue staging in the stages: rows padded by one chunk
+    constexpr int SROW = WTN + 4, LPR = WTN / 4, RPP = 64 / LPR;
+    static_assert(4 * 16 * SROW * 4 <= ST * SB, "staging space");
+    const int col = n0 + wn * WTN + lane % LPR * 4;
+    const auto cols = epi.cols(col, N);
+    wg_barrier();
+    int* const stage = reinterpret_cast<int*>(smem) + wave * 16 * SROW;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4*>(stage + r * SROW + j * 16 + 4 * g) = acc[i][j];
+#pragma unroll
+        for (int pass = 0; pass < 16 / RPP; ++pass) {
+            const int row = pass * RPP + lane / LPR, m = m0 + wm * WTM + i * 16 + row;
+            const i32x4 sum = *reinterpret_cast<const i32x4*>(stage + row * SROW + lane % LPR * 4);
+            epi.store(m, col, M, N, sum, cols, epi.scale_a[min(m, M - 1)]);
+        }
+    }
 }
 
 // ------------------------------------------------------------- the checks --
@@ -183,10 +554,69 @@ static bool i8_shape_ok(const ebrl_i8_gemm_args* a) {
            (((int64_t)a->M + 31) / 32) * (((int64_t)a->N + 63) / 64) <= I8_MAX_TILES;
 }
 
+struct I8Plan {
+    int bm, bn;              // tile
+    int grid, full, split;   // 256 x 256: workgroups, evenly dealt tiles, cut of the last round's tiles
+};
+
+static I8Plan i8_plan(int M, int N, int K) {
+    constexpr int CUS = 256;
+    I8Plan p{};
+    const double nk = (K + 127) / 128;
+    auto up = [](long a, long b) { return (a + b - 1) / b; };
+    const long tiles = up(M, 256) * up(N, 256);
+    const long rounds = tiles / CUS, full = rounds * CUS, rest = tiles - full;
+    p.bm = p.bn = 256;
+    p.full = (int)full;
+    double best = 0;
+    struct Cut { int split; double c, alone, busy; } cuts[] = {{1, 8.0, 0.75, 1.24}, {2, 5.6, 0.50, 0.78}, {4, 4.0, 0.38, 0.55}};
+    for (const Cut& v : cuts) {
+        if (v.split > 1 && (!rest || rest * v.split > CUS)) continue;
+        const long pieces = full || v.split == 1 ? rest * v.split : up(M, 128) * up(N, v.split == 2 ? 256 : 128);
+        double t = v.c + rounds * (8.7 + 1.39 * nk);
+        if (rest) t += nk * (v.alone + (v.busy - v.alone) * pieces / CUS);
+        if (v.split == 1 || t < best) {
+            best = t;
+            p.split = v.split;
+        }
+    }
+    p.grid = (int)(full ? CUS : rest * p.split);
+    struct Ring { int bm, bn; double c, epi, one, two; } rings[] = {{64, 128, 2.4, 1.7, 0.353, 0.610},
+                                                                    {64, 64, 2.3, 1.0, 0.225, 0.355},
+                                                                    {32, 64, 2.4, 0.7, 0.175, 0.262}};
+    for (const Ring& v : rings) {
+        const long wgs = up(M, v.bm) * up(N, v.bn), pairs = wgs / (2 * CUS);
+        const double left = (double)(wgs - pairs * 2 * CUS) / CUS;
+        double t = v.c + pairs * (v.epi + nk * v.two);
+        if (left > 1) t += v.epi + nk * (v.one + (v.two - v.one) * (0.6 + 0.4 * (left - 1)));
+        else if (left > 0) t += v.epi / 2 + nk * v.one;
+        if (t < best) {
+            best = t;
+            p.bm = v.bm;
+            p.bn = v.bn;
+        }
+    }
+    return p;
+}
+
 template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, hipStream_t s) {
-    const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc};
-    const unsigned tiles = (unsigned)((((int64_t)a.M + 63) / 64) * (((int64_t)a.N + 63) / 64));
-    hipLaunchKernelGGL(i8_gemm_kernel<T>, dim3(tiles), dim3(256), 0, s, a.a, a.lda, a.b, a.ldb, a.M, a.N, a.K, epi);
+    const int esz = sizeof(T);
+    auto wide = [&](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; };
+    const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc,
+                       a.N % 4 == 0 && wide(a.c, a.ldc) && (!a.residual || wide(a.residual, a.ldr))};
+    const I8Plan p = i8_plan(a.M, a.N, a.K);
+    if (p.bm == 256) {
+        hipLaunchKernelGGL(i8_big_kernel<T>, dim3(p.grid), dim3(512), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M,
+                           a.N, a.K, p.full, p.split, epi);
+        return;
+    }
+    const dim3 grid((unsigned)((((int64_t)a.M + p.bm - 1) / p.bm) * (((int64_t)a.N + p.bn - 1) / p.bn)));
+    auto ring = [&](auto kern) {
+        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M, a.N, a.K, epi);
+    };
+    if (p.bn == 128) ring(i8_ring_kernel<T, 64, 128, 3>);
+    else if (p.bm == 64) ring(i8_ring_kernel<T, 64, 64, 3>);
+    else ring(i8_ring_kernel<T, 32, 64, 4>);
 }
 
 static int i8_gemm(const ebrl_i8_gemm_args* args, hipStream_t s) {
