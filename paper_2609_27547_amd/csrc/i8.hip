@@ -19,19 +19,49 @@ constexpr int64_t I8_MAX_LD = 1 << 23;      // a tile's byte offsets are 32-bit 
 constexpr int64_t I8_MAX_TILES = 1 << 23;
 
 // ------------------------------------------------------- rows to codes --
-// y in 64 bits: a code is off by one where y / s is nearer to a border than its
-// error, and one such code moves a product by about 1e-4 of its size.  With 32-bit
-// y that is a code in 1e5, with 64-bit ones none.
+// y, its largest size and the quotients are 64-bit: a code is off by one where y /
+// s is nearer to a border than its error, and one such code moves a product by
+// about 1e-4 of its size.  With 32-bit y that is one code in 1e5, with 64-bit ones
+// none.  The vector units do 64-bit adds and products at the rate of 32-bit ones.
 
-EBRL_DEV double i8_value(int op, float x, float up, double factor, float gain) {
-    if (op == EBRL_I8_RMSNORM) return (double)x * factor * (double)gain;
-    if (op == EBRL_I8_SWIGLU) return (double)x / (1.0 + exp(-(double)x)) * (double)up;
-    return (double)x;
+// silu(g) u.  exp(-g) = 2^n 2^f, |f| <= 1/2, 2^f by its Taylor series: the first
+// term left out is 2e-16.  The exponent is held to +-690, where silu is g or below
+// every scale.  1 / ln(2) in two parts keeps f to all its bits.
+EBRL_DEV double i8_gate(float g32, float u32) {
+    const double g = g32, h = fmin(fmax(g, -690.0), 690.0);
+    const double n = rint(h * -1.4426950408889634);
+    const double f = fma(h, -2.0355273740931033e-17, fma(h, -1.4426950408889634, -n));
+    double p = 2.5678435993488205141e-11;       // ln(2)^k / k!, k = 12 .. 0
+    p = fma(p, f, 4.4455382718708114976e-10);
+    p = fma(p, f, 7.0549116208011233299e-9);
+    p = fma(p, f, 1.0178086009239699728e-7);
+    p = fma(p, f, 1.3215486790144309488e-6);
+    p = fma(p, f, 1.5252733804059840280e-5);
+    p = fma(p, f, 1.5403530393381609954e-4);
+    p = fma(p, f, 1.3333558146428443423e-3);
+    p = fma(p, f, 9.6181291076284771619e-3);
+    p = fma(p, f, 5.5504108664821579953e-2);
+    p = fma(p, f, 2.4022650695910071233e-1);
+    p = fma(p, f, 6.9314718055994530942e-1);
+    p = fma(p, f, 1.0);
+    const double d = 1.0 + ldexp(p, (int)n);
+    double r = __builtin_amdgcn_rcp(d);         // two steps of Newton's: 2^-23, 2^-46, then all bits
+    r = fma(r, fma(-d, r, 1.0), r);
+    r = fma(r, fma(-d, r, 1.0), r);
+    return g * r * (double)u32;
 }
-EBRL_DEV double i8_wave_max(double v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = fmax(v, __shfl_xor(v, m, 64));
-    return v;
+// y / s to the nearest whole number, ties to even.  The product with 1 / s is
+// corrected by its remainder, which makes a quotient that is a half exactly that;
+// adding 1.5 * 2^52 rounds it into the low bits.
+EBRL_DEV int i8_code(double y, double s, double inv) {
+    double q = y * inv;
+    q = fma(fma(-q, s, y), inv, q);
+    return (int)(uint32_t)__builtin_bit_cast(uint64_t, q + 6755399441055744.0);
+}
+// The scale that rows with |y| <= top need; infinity: none, the row is not finite.
+EBRL_DEV float i8_scale(double top, bool bad) {
+    const float s = fmaxf((float)(top / 127.0), 0x1p-100f);
+    return bad || !(s <= 3.40282347e38f) ? INFINITY : s;
 }
 EBRL_DEV double i8_wave_sum(double v) {
 #pragma unroll
@@ -39,46 +69,173 @@ EBRL_DEV double i8_wave_sum(double v) {
     return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void i8_quant_kernel(ebrl_i8_quant_args a)
-{
-    __shared__ double red[4];
-    const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
-    const T* x = (const T*)a.x + (size_t)row * a.ldx;
-    const T* up = a.op == EBRL_I8_SWIGLU ? (const T*)a.up + (size_t)row * a.ldup : nullptr;
-    auto value = [&](int j, double factor) {
-        return i8_value(a.op, ld_elem<T>(x + j), up ? ld_elem<T>(up + j) : 0.f, factor, a.gain ? a.gain[j] : 1.f);
-    };
-    double factor = 1.0;
-    if (a.op == EBRL_I8_RMSNORM) {
-        double ss = 0.0;
-        for (int j = tid; j < a.cols; j += 256) {
-            const double v = ld_elem<T>(x + j);
-            ss += v * v;
+// Eight neighbours of a row; those from `left` on are zeros.
+template <typename T> EBRL_DEV void i8_load8(const T* p, int left, bool aligned, float (&v)[8]) {
+    if (aligned && left >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+        } else {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(w[e] << 16);
+                v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+            }
         }
-        ss = i8_wave_sum(ss);
-        if ((tid & 63) == 0) red[wave] = ss;
-        __syncthreads();
-        factor = 1.0 / sqrt((red[0] + red[1] + red[2] + red[3]) / a.cols + (double)a.eps);
-        __syncthreads();
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? ld_elem<T>(p + e) : 0.f;
     }
-    double top = 0.0;
-    bool bad = false;
-    for (int j = tid; j < a.cols; j += 256) {
-        const double v = fabs(value(j, factor));
-        bad |= !(v <= 1.7976931348623157e308);
-        top = fmax(top, v);
+}
+// Eight codes; columns from `left` on are zeros, those from `fill` on left as they are.
+EBRL_DEV void i8_store8(int8_t* p, const double (&y)[8], int left, int fill, double s, double inv, bool bad) {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left && !bad) w[e >> 2] |= (uint32_t)(i8_code(y[e], s, inv) & 255) << (e & 3) * 8;
+    if (fill > 0) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+}
+
+// What a launch needs, beside the call's arguments.
+struct I8Quant {
+    ebrl_i8_quant_args a;
+    bool aligned, gain_aligned;
+};
+
+// The largest scale, and the sum, over a row's waves; `red`: a word for each.
+template <int WAVES, typename V> EBRL_DEV V i8_over_waves(V v, V* red, bool sum) {
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = sum ? v + red[w] : (V)fmax(v, red[w]);
     }
-    top = i8_wave_max(top);
-    if ((tid & 63) == 0) red[wave] = top;
-    bad = __syncthreads_or(bad);
-    top = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
-    const float s = fmaxf((float)(top / 127.0), 0x1p-100f);
-    bad |= !(s <= 3.40282347e38f);
+    return v;
+}
+
+// Rows of at most 512 WAVES CHUNKS columns, held in registers from one read to the
+// codes: a thread has eight neighbours in each of CHUNKS places.  One wave: four
+// rows a workgroup.
+template <typename T, int OP, int WAVES, int CHUNKS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel(I8Quant w)
+{
+    __shared__ double red_sum[WAVES];
+    __shared__ float red_max[WAVES];
+    const ebrl_i8_quant_args& a = w.a;
+    const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int row = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (row >= a.rows) return;
+    const T* const x = (const T*)a.x + (size_t)row * a.ldx;
+    float v[CHUNKS][8];
+    float u[CHUNKS][8];     // the gated rows' other factor, or the norm's gain
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int j = (c * 64 * WAVES + tid) * 8;
+        i8_load8<T>(x + j, a.cols - j, w.aligned, v[c]);
+        if constexpr (OP == EBRL_I8_SWIGLU)
+            i8_load8<T>((const T*)a.up + (size_t)row * a.ldup + j, a.cols - j, w.aligned, u[c]);
+        if constexpr (OP == EBRL_I8_RMSNORM)
+            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, w.gain_aligned, u[c]);
+    }
+    double factor = 1.0;
+    if constexpr (OP == EBRL_I8_RMSNORM) {
+        double ss = 0.0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fma((double)v[c][e], (double)v[c][e], ss);
+        ss = i8_over_waves<WAVES>(i8_wave_sum(ss), red_sum, true);
+        factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
+    }
+    double y[CHUNKS][8], top = 0.0, nan = 0.0;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (OP == EBRL_I8_SWIGLU) y[c][e] = i8_gate(v[c][e], u[c][e]);
+            else if constexpr (OP == EBRL_I8_RMSNORM) {
+                y[c][e] = v[c][e] * factor;
+                if (a.gain) y[c][e] *= (double)u[c][e];
+            } else y[c][e] = v[c][e];
+            top = fmax(top, fabs(y[c][e]));
+            nan = fma(y[c][e], 0.0, nan);
+        }
+    float s = wave_max(i8_scale(top, !(nan == 0.0)));
+    s = i8_over_waves<WAVES>(s, red_max, false);
+    const bool bad = s == INFINITY;
+    const double sd = s, inv = 1.0 / sd;
     if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
-    int8_t* out = a.codes + (size_t)row * a.ldc;
-    for (int j = tid; j < (a.cols + 15) / 16 * 16; j += 256)
-        out[j] = j < a.cols && !bad ? (int8_t)(int)rint(value(j, factor) / (double)s) : (int8_t)0;
+    int8_t* const out = a.codes + (size_t)row * a.ldc;
+    const int wide = (a.cols + 15) / 16 * 16;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int j = (c * 64 * WAVES + tid) * 8;
+        i8_store8(out + j, y[c], a.cols - j, wide - j, sd, inv, bad);
+    }
+}
+
+// Longer rows: read once more for each step.
+template <typename T, int OP>
+__global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
+{
+    __shared__ double red_sum[16];
+    __shared__ float red_max[16];
+    const ebrl_i8_quant_args& a = w.a;
+    const int tid = threadIdx.x, row = blockIdx.x;
+    const T* const x = (const T*)a.x + (size_t)row * a.ldx;
+    double factor = 1.0;
+    if constexpr (OP == EBRL_I8_RMSNORM) {
+        double ss = 0.0;
+        for (int j = tid * 8; j < a.cols; j += 8192) {
+            float v[8];
+            i8_load8<T>(x + j, a.cols - j, w.aligned, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fma((double)v[e], (double)v[e], ss);
+        }
+        ss = i8_over_waves<16>(i8_wave_sum(ss), red_sum, true);
+        factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
+    }
+    auto values = [&](int j, double (&y)[8]) {
+        float v[8], u[8];
+        i8_load8<T>(x + j, a.cols - j, w.aligned, v);
+        if constexpr (OP == EBRL_I8_SWIGLU)
+            i8_load8<T>((const T*)a.up + (size_t)row * a.ldup + j, a.cols - j, w.aligned, u);
+        if constexpr (OP == EBRL_I8_RMSNORM)
+            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, w.gain_aligned, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (OP == EBRL_I8_SWIGLU) y[e] = i8_gate(v[e], u[e]);
+            else if constexpr (OP == EBRL_I8_RMSNORM) {
+                y[e] = v[e] * factor;
+                if (a.gain) y[e] *= (double)u[e];
+            } else y[e] = v[e];
+        }
+    };
+    double top = 0.0, nan = 0.0;
+    for (int j = tid * 8; j < a.cols; j += 8192) {
+        double y[8];
+        values(j, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            top = fmax(top, fabs(y[e]));
+            nan = fma(y[e], 0.0, nan);
+        }
+    }
+    const float s = i8_over_waves<16>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+    const bool bad = s == INFINITY;
+    const double sd = s, inv = 1.0 / sd;
+    if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
+    int8_t* const out = a.codes + (size_t)row * a.ldc;
+    const int wide = (a.cols + 15) / 16 * 16;
+    for (int j = tid * 8; j < wide; j += 8192) {
+        double y[8];
+        values(j, y);
+        i8_store8(out + j, y, a.cols - j, wide - j, sd, inv, bad);
+    }
 }
 
 // -------------------------------------------------------------- product --
@@ -531,6 +688,28 @@ static bool i8_codes_ok(const void* p, int64_t ld, int64_t width) {
     return p && (uintptr_t)p % 16 == 0 && ld >= width && ld % 16 == 0;
 }
 
+template <typename T, int OP> static void i8_quant_op(const I8Quant& w, hipStream_t s) {
+    const int cols = w.a.cols;
+    const unsigned rows = w.a.rows;
+    auto go = [&](auto kern, unsigned groups, int threads) {
+        hipLaunchKernelGGL(kern, dim3(groups), dim3(threads), 0, s, w);
+    };
+    if (cols <= 512) go(i8_quant_kernel<T, OP, 1, 1>, (rows + 3) / 4, 256);
+    else if (cols <= 1024) go(i8_quant_kernel<T, OP, 1, 2>, (rows + 3) / 4, 256);
+    else if (cols <= 2048) go(i8_quant_kernel<T, OP, 4, 1>, rows, 256);
+    else if (cols <= 4096) go(i8_quant_kernel<T, OP, 4, 2>, rows, 256);
+    else if (cols <= 8192) go(i8_quant_kernel<T, OP, 8, 2>, rows, 512);
+    else if (cols <= 12288) go(i8_quant_kernel<T, OP, 8, 3>, rows, 512);
+    else go(i8_quant_long_kernel<T, OP>, rows, 1024);
+}
+template <typename T> static void i8_quant_launch(const ebrl_i8_quant_args& a, hipStream_t s) {
+    auto aligned = [](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
+    const I8Quant w{a, aligned(a.x, a.ldx) && (a.op != EBRL_I8_SWIGLU || aligned(a.up, a.ldup)), (uintptr_t)a.gain % 16 == 0};
+    if (a.op == EBRL_I8_ROWS) i8_quant_op<T, EBRL_I8_ROWS>(w, s);
+    else if (a.op == EBRL_I8_RMSNORM) i8_quant_op<T, EBRL_I8_RMSNORM>(w, s);
+    else i8_quant_op<T, EBRL_I8_SWIGLU>(w, s);
+}
+
 static int i8_quant(const ebrl_i8_quant_args* args, hipStream_t s) {
     if (!args) return EBRL_E_INVALID;
     const ebrl_i8_quant_args& a = *args;
@@ -544,8 +723,8 @@ static int i8_quant(const ebrl_i8_quant_args* args, hipStream_t s) {
         (uintptr_t)a.gain % 4 || !i8_codes_ok(a.codes, a.ldc, (a.cols + 15) / 16 * 16) || a.ldc >= ((int64_t)1 << 40) ||
         !a.scales || (uintptr_t)a.scales % 4)
         return EBRL_E_INVALID;
-    if (esz == 2) hipLaunchKernelGGL(i8_quant_kernel<bf16_t>, dim3(a.rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(i8_quant_kernel<float>, dim3(a.rows), dim3(256), 0, s, a);
+    if (esz == 2) i8_quant_launch<bf16_t>(a, s);
+    else i8_quant_launch<float>(a, s);
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
 }
 
