@@ -110,85 +110,101 @@ struct I8Quant {
 };
 
 // The largest value, and the sum, over a row's waves; `red`: a word for each.
-template <typename V> EBRL_DEV V i8_over_waves(int waves, V v, V* red, bool sum) {
-    if (waves == 1) return v;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-    for (int w = 1; w < waves; ++w) v = sum ? v + red[w] : (V)fmax(v, red[w]);
+template <int WAVES, typename V> EBRL_DEV V i8_over_waves(V v, V* red, bool sum) {
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = sum ? v + red[w] : (V)fmax(v, red[w]);
+    }
     return v;
 }
 EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(m, fabsf(v)); }   // NaN stays
 
-// Rows of at most 1024 columns a wave (CHUNKS 2), held in registers from one read to
-// the codes: a thread has eight neighbours in each of CHUNKS places.  ONE: a wave a
-// row, four a workgroup; else a workgroup a row, of as many waves as it takes.
+// Rows of at most 512 CHUNKS columns a wave, held in registers from one read to the
+// codes: a thread has eight neighbours in each of CHUNKS places.  One wave: four rows a
+// workgroup, else a workgroup a row.
 //
-// Values, their maximum and the codes are computed in 32 bits, and what lies nearer to
-// a border than these are exact (EB, twice their error and more) is computed once more
-// in 64 bits: one code in 1e5 of plain and normed rows, one in 1e4 of gated ones.  So is
-// a whole row where 32 bits do not do (near the ends of their range, or not finite).
-template <typename T, int OP, int CHUNKS, bool ONE>
-__global__ __launch_bounds__(ONE ? 256 : 1024) void i8_quant_kernel(I8Quant w)
+// Plain and normed rows are 64-bit throughout.  Gated rows, whose 64-bit exponentials
+// would take twice the time of reading them, have 32-bit values, maximum and codes; what
+// lies nearer to a border than these are exact (EB, twice their error) is computed once
+// more in 64 bits, one code in 1e4, and so is a whole row where 32 bits do not do
+// (near the ends of their range, or not finite).
+template <typename T, int OP, int WAVES, int CHUNKS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel(I8Quant w)
 {
-    constexpr float EB = OP == EBRL_I8_SWIGLU ? 0x1p-16f : OP == EBRL_I8_RMSNORM ? 0x1p-20f : 0x1p-22f;
-    __shared__ double red_sum[16];
-    __shared__ float red_max[16];
+    constexpr bool ONE = WAVES == 1;
+    constexpr int threads = 64 * WAVES;
+    constexpr bool GATE = OP == EBRL_I8_SWIGLU;
+    constexpr float EB = 0x1p-16f;
+    __shared__ double red_sum[WAVES];
+    __shared__ float red_max[WAVES];
     const ebrl_i8_quant_args& a = w.a;
-    const int waves = ONE ? 1 : blockDim.x >> 6, threads = waves * 64;
     const int tid = ONE ? threadIdx.x & 63 : threadIdx.x;
     const int row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (row >= a.rows) return;
     const T* const x = (const T*)a.x + (size_t)row * a.ldx;
-    const T* const up = OP == EBRL_I8_SWIGLU ? (const T*)a.up + (size_t)row * a.ldup : nullptr;
+    const T* const up = GATE ? (const T*)a.up + (size_t)row * a.ldup : nullptr;
+    int8_t* const out = a.codes + (size_t)row * a.ldc;
+    const int wide = (a.cols + 15) / 16 * 16;
     float z[CHUNKS][8], u[CHUNKS][8];     // u: the gated rows' other factor, or the norm's gain
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int j = (c * threads + tid) * 8;
         i8_load8<T>(x + j, a.cols - j, w.aligned, z[c]);
-        if constexpr (OP == EBRL_I8_SWIGLU) i8_load8<T>(up + j, a.cols - j, w.aligned, u[c]);
+        if constexpr (GATE) i8_load8<T>(up + j, a.cols - j, w.aligned, u[c]);
         if constexpr (OP == EBRL_I8_RMSNORM)
             if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, w.gain_aligned, u[c]);
     }
-    double factor = 1.0;
-    if constexpr (OP == EBRL_I8_RMSNORM) {
-        double ss = 0.0;
+    if constexpr (!GATE) {
+        double factor = 1.0;
+        if constexpr (OP == EBRL_I8_RMSNORM) {
+            double ss = 0.0;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fma((double)z[c][e], (double)z[c][e], ss);
+            ss = i8_over_waves<WAVES>(i8_wave_sum(ss), red_sum, true);
+            factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
+        }
+        double y[CHUNKS][8], top = 0.0, nan = 0.0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fma((double)z[c][e], (double)z[c][e], ss);
-        ss = i8_over_waves(waves, i8_wave_sum(ss), red_sum, true);
-        factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
-    }
-    auto exactly = [&](int j) {
-        if constexpr (OP == EBRL_I8_SWIGLU) return i8_gate(ld_elem<T>(x + j), ld_elem<T>(up + j));
-        else if constexpr (OP == EBRL_I8_RMSNORM)
-            return a.gain ? ld_elem<T>(x + j) * factor * (double)a.gain[j] : ld_elem<T>(x + j) * factor;
-        else return (double)ld_elem<T>(x + j);
-    };
-    int8_t* const out = a.codes + (size_t)row * a.ldc;
-    const int wide = (a.cols + 15) / 16 * 16;
-    const float ff = (float)factor;
-    float most = 0.f, gate = 0.f;
+            for (int e = 0; e < 8; ++e) {
+                y[c][e] = z[c][e];
+                if constexpr (OP == EBRL_I8_RMSNORM) {
+                    y[c][e] *= factor;
+                    if (a.gain) y[c][e] *= (double)u[c][e];
+                }
+                top = fmax(top, fabs(y[c][e]));
+                nan = fma(y[c][e], 0.0, nan);
+            }
+        const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+        const bool bad = s == INFINITY;
+        const double sd = s, inv = 1.0 / sd;
+        if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int j = (c * threads + tid) * 8;
+            i8_store8(out + j, y[c], a.cols - j, wide - j, sd, inv, bad);
+        }
+    } else {
+        auto exactly = [&](int j) { return i8_gate(ld_elem<T>(x + j), ld_elem<T>(up + j)); };
+        float most = 0.f, gate = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (OP == EBRL_I8_SWIGLU) {
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
                 gate = i8_most(gate, z[c][e]);
                 z[c][e] = i8_gate_fast(z[c][e], u[c][e]);
-            } else if constexpr (OP == EBRL_I8_RMSNORM) {
-                z[c][e] *= ff;
-                if (a.gain) z[c][e] *= u[c][e];
+                most = i8_most(most, z[c][e]);
             }
-            most = i8_most(most, z[c][e]);
-        }
-    const bool fits = most <= 0x1p120f && gate <= 80.f && ff >= 0x1p-100f && ff <= 0x1p100f;
-    const float m = i8_over_waves(waves, wave_max(fits ? most : INFINITY), red_max, false);
-    if (m <= 0x1p120f && m >= 0x1p-80f) {
-        float s = i8_scale(m, false);
-        if constexpr (OP != EBRL_I8_ROWS) {
+        const bool fits = most <= 0x1p120f && gate <= 80.f;
+        const float m = i8_over_waves<WAVES>(wave_max(fits ? most : INFINITY), red_max, false);
+        if (m <= 0x1p120f && m >= 0x1p-80f) {
             // what may be the largest one, from the row read again
             const float may = m * (1.0f - EB);
             double top = 0.0;
@@ -202,57 +218,57 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void i8_quant_kernel(I8Quant w)
                         top = fmax(top, fabs(exactly((c * threads + tid) * 8 + __builtin_ctz(these))));
                 }
             }
-            s = i8_over_waves(waves, wave_max(i8_scale(top, false)), red_max, false);
-        }
-        const double sd = s, inv = 1.0 / sd;
-        const float invf = (float)inv, eb = invf * EB;
-        if (tid == 0) a.scales[row] = s;
+            const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, false)), red_max, false);
+            const double sd = s, inv = 1.0 / sd;
+            const float invf = (float)inv, eb = invf * EB;
+            if (tid == 0) a.scales[row] = s;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int j = (c * threads + tid) * 8;
-            uint32_t k[8];
-            float border[8], near = 0.f;
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int j = (c * threads + tid) * 8;
+                uint32_t k[8];
+                float border[8], near = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // adding 1.5 * 2^23 rounds to a whole number in the low bits
-                const float t = fmaf(z[c][e], invf, 12582912.0f);
-                k[e] = __float_as_uint(t);
-                border[e] = fmaf(fabsf(z[c][e]), eb, fabsf(fmaf(z[c][e], invf, -(t - 12582912.0f))));
-                near = fmaxf(near, border[e]);
-            }
-            uint32_t lo = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[3], k[2], 0x0c0c0400),
-                                                __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0400), 0x05040100);
-            uint32_t hi = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[7], k[6], 0x0c0c0400),
-                                                __builtin_amdgcn_perm(k[5], k[4], 0x0c0c0400), 0x05040100);
-            if (near >= 0.5f) {
-                unsigned these = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) these |= (border[e] >= 0.5f ? 1u : 0u) << e;
-                for (; these; these &= these - 1) {
-                    const int e = __builtin_ctz(these), at = (e & 3) * 8;
-                    const uint32_t code = (uint32_t)i8_code(exactly(j + e), sd, inv) & 255;
-                    if (e < 4) lo = (lo & ~(255u << at)) | code << at;
-                    else hi = (hi & ~(255u << at)) | code << at;
+                for (int e = 0; e < 8; ++e) {
+                    // adding 1.5 * 2^23 rounds to a whole number in the low bits
+                    const float t = fmaf(z[c][e], invf, 12582912.0f);
+                    k[e] = __float_as_uint(t);
+                    border[e] = fmaf(fabsf(z[c][e]), eb, fabsf(fmaf(z[c][e], invf, -(t - 12582912.0f))));
+                    near = fmaxf(near, border[e]);
                 }
+                uint32_t lo = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[3], k[2], 0x0c0c0400),
+                                                    __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0400), 0x05040100);
+                uint32_t hi = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[7], k[6], 0x0c0c0400),
+                                                    __builtin_amdgcn_perm(k[5], k[4], 0x0c0c0400), 0x05040100);
+                if (near >= 0.5f) {
+                    unsigned these = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) these |= (border[e] >= 0.5f ? 1u : 0u) << e;
+                    for (; these; these &= these - 1) {
+                        const int e = __builtin_ctz(these), at = (e & 3) * 8;
+                        const uint32_t code = (uint32_t)i8_code(exactly(j + e), sd, inv) & 255;
+                        if (e < 4) lo = (lo & ~(255u << at)) | code << at;
+                        else hi = (hi & ~(255u << at)) | code << at;
+                    }
+                }
+                if (j < wide) *reinterpret_cast<uint2*>(out + j) = make_uint2(lo, hi);
             }
-            if (j < wide) *reinterpret_cast<uint2*>(out + j) = make_uint2(lo, hi);
+            return;
         }
-        return;
-    }
-    double top = 0.0, nan = 0.0;
+        double top = 0.0, nan = 0.0;
 #pragma unroll 1
-    for (int j = tid; j < a.cols; j += threads) {
-        const double y = exactly(j);
-        top = fmax(top, fabs(y));
-        nan = fma(y, 0.0, nan);
-    }
-    const float s = i8_over_waves(waves, wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
-    const bool bad = s == INFINITY;
-    const double sd = s, inv = 1.0 / sd;
-    if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
+        for (int j = tid; j < a.cols; j += threads) {
+            const double y = exactly(j);
+            top = fmax(top, fabs(y));
+            nan = fma(y, 0.0, nan);
+        }
+        const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+        const bool bad = s == INFINITY;
+        const double sd = s, inv = 1.0 / sd;
+        if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll 1
-    for (int j = tid; j < wide; j += threads)
-        out[j] = j < a.cols && !bad ? (int8_t)i8_code(exactly(j), sd, inv) : (int8_t)0;
+        for (int j = tid; j < wide; j += threads)
+            out[j] = j < a.cols && !bad ? (int8_t)i8_code(exactly(j), sd, inv) : (int8_t)0;
+    }
 }
 
 // Longer rows: read once more for each step.
@@ -273,7 +289,7 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fma((double)v[e], (double)v[e], ss);
         }
-        ss = i8_over_waves(16, i8_wave_sum(ss), red_sum, true);
+        ss = i8_over_waves<16>(i8_wave_sum(ss), red_sum, true);
         factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
     }
     auto values = [&](int j, double (&y)[8]) {
@@ -302,7 +318,7 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
             nan = fma(y[e], 0.0, nan);
         }
     }
-    const float s = i8_over_waves(16, wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+    const float s = i8_over_waves<16>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
     const bool bad = s == INFINITY;
     const double sd = s, inv = 1.0 / sd;
     if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
@@ -771,9 +787,13 @@ template <typename T, int OP> static void i8_quant_op(const I8Quant& w, hipStrea
     auto go = [&](auto kern, unsigned groups, int threads) {
         hipLaunchKernelGGL(kern, dim3(groups), dim3(threads), 0, s, w);
     };
-    if (cols <= 512) go(i8_quant_kernel<T, OP, 1, true>, (rows + 3) / 4, 256);
-    else if (cols <= 1024) go(i8_quant_kernel<T, OP, 2, true>, (rows + 3) / 4, 256);
-    else if (cols <= 16384) go(i8_quant_kernel<T, OP, 2, false>, rows, (cols + 1023) / 1024 * 64);
+    if (cols <= 512) go(i8_quant_kernel<T, OP, 1, 1>, (rows + 3) / 4, 256);
+    else if (cols <= 1024) go(i8_quant_kernel<T, OP, 1, 2>, (rows + 3) / 4, 256);
+    else if (cols <= 2048) go(i8_quant_kernel<T, OP, 4, 1>, rows, 256);
+    else if (cols <= 4096) go(i8_quant_kernel<T, OP, 4, 2>, rows, 256);
+    else if (cols <= 8192) go(i8_quant_kernel<T, OP, 8, 2>, rows, 512);
+    else if (cols <= 12288) go(i8_quant_kernel<T, OP, 12, 2>, rows, 768);
+    else if (cols <= 16384) go(i8_quant_kernel<T, OP, 16, 2>, rows, 1024);
     else go(i8_quant_long_kernel<T, OP>, rows, 1024);
 }
 template <typename T> static void i8_quant_launch(const ebrl_i8_quant_args& a, hipStream_t s) {
