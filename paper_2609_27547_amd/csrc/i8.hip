@@ -769,6 +769,156 @@ __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restric
     }
 }
 
+// Few rows: the weights are streamed once.  A workgroup has a slice of BN columns, at
+// most 16 TM rows and a range of K; its waves split that range and run pipelines of
+// their own: each DMAs its weights' and activations' rows into LDS of its own, one
+// instruction 8 rows x 128 bytes, STAGES - 1 K tiles ahead, and multiplies from
+// there.  XR rows of activations are loaded, 8 of them for up to 8 rows (the upper
+// half of the fragment then repeats the lower one and is not stored).  The waves'
+// tiles are summed through LDS.  With several ranges of K (splits) the sums go to the
+// workspace and i8_join_kernel adds them up.  NT: each weight is read by one workgroup.
+template <typename T, int XR, int BN, int STAGES, bool NT>
+__global__ __launch_bounds__(256) void i8_decode_kernel(const int8_t* __restrict__ A, uint32_t lda,
+                                                               const int8_t* __restrict__ B, uint32_t ldb, int M, int N,
+                                                               int K, int tiles_per_split, int splits, int m_tiles,
+                                                               int* __restrict__ ws, I8Epi<T> epi)
+{
+    constexpr int WAVES = 4;
+    constexpr int TM = XR < 16 ? 1 : XR / 16, TN = BN / 16, FR = TM * TN;
+    constexpr int WI = BN / 8, XI = XR / 8;                  // DMA instructions per K tile
+    constexpr int STAGE = (BN + XR) * 128;                   // bytes per wave and K tile
+    constexpr int RB = FR * 1024;                            // bytes of a wave's sums
+    constexpr int LDS = WAVES * (STAGES * STAGE > RB ? STAGES * STAGE : RB);
+    static_assert(LDS <= 160 * 1024 && STAGES >= 2, "LDS");
+    __shared__ __attribute__((aligned(1024))) char smem[LDS];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    // XCD x takes the x-th contiguous range of units, so that the row tiles of one
+    // slice, which read the same weights, run on one XCD
+    int bid = blockIdx.x;
+    {
+        const int nb = gridDim.x, x = bid & 7;
+        bid = x * (nb >> 3) + min(x, nb & 7) + (bid >> 3);
+    }
+    const int mt = bid % m_tiles, unit = bid / m_tiles;
+    const int split = unit % splits, nt = unit / splits;
+    const int m0 = mt * 16 * TM, n0 = nt * BN;
+    const int nk = (K + 127) >> 7, rest = K - (nk - 1) * 128;
+    const int s_begin = split * tiles_per_split, s_end = min(nk, s_begin + tiles_per_split);
+    const int per_wave = (s_end - s_begin + WAVES - 1) / WAVES;
+    const int w_begin = min(s_end, s_begin + wave * per_wave), w_end = min(s_end, w_begin + per_wave);
+    const uint32_t kb = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t past = (uint32_t)max(0, (int)kb - (rest - 16));
+
+    uint32_t vw[WI], vx[XI];
+#pragma unroll
+    for (int j = 0; j < WI; ++j) vw[j] = (uint32_t)min(j * 8 + (lane >> 3), N - 1 - n0) * ldb + kb;
+#pragma unroll
+    for (int j = 0; j < XI; ++j) vx[j] = (uint32_t)min(j * 8 + (lane >> 3), M - 1 - m0) * lda + kb;
+    const char* const pB = uniform_ptr(B + (size_t)n0 * ldb);
+    const char* const pA = uniform_ptr(A + (size_t)m0 * lda);
+    const uint32_t lds0 =
+        __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)smem + wave * STAGES * STAGE);
+    auto dma = [&](int t, int st) {
+        const uint32_t back = t == nk - 1 ? past : 0u;
+        const uint32_t l = lds0 + st * STAGE;
+#pragma unroll
+        for (int j = 0; j < WI; ++j) {
+            if constexpr (NT) dma16_to_lds_s_nt(pB + (size_t)t * 128, vw[j] - back, l + j * 1024);
+            else dma16_to_lds_s(pB + (size_t)t * 128, vw[j] - back, l + j * 1024);
+        }
+#pragma unroll
+        for (int j = 0; j < XI; ++j) dma16_to_lds_s(pA + (size_t)t * 128, vx[j] - back, l + (WI + j) * 1024);
+    };
+    uint32_t off[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) off[ks] = (uint32_t)((r & 7) * 128 + (((ks * 4 + g) ^ (r & 7)) << 4));
+    const uint32_t upper = (r >> 3) * 1024;                  // second 8-row group of a fragment
+    i32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    auto multiply = [&](int t, int st) {
+        const char* const s = smem + (wave * STAGES + st) * STAGE;
+        i32x4 w[2][TN], x[2][TM];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) w[ks][j] = i8_fragment(s + off[ks] + upper + j * 2048);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                x[ks][i] = i8_fragment(s + BN * 128 + off[ks] + (XR < 16 ? 0 : upper) + i * 2048);
+        }
+        if (t == nk - 1) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+                if (ks * 64 + g * 16 >= rest) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) w[ks][j] = i32x4{0, 0, 0, 0};
+                }
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[ks][j], x[ks][i], acc[i][j], 0, 0, 0);
+    };
+    // Tile w_begin + i sits in stage i % STAGES; the one STAGES - 1 further on goes
+    // into the stage that the tile before it has left (wait_lds: it has been read).
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (w_begin + i < w_end) dma(w_begin + i, i);
+    for (int t = w_begin; t < w_end; t += STAGES) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) {
+            if (t + i >= w_end) break;
+            wait_lds();
+            if (t + i + STAGES - 1 < w_end) dma(t + i + STAGES - 1, (i + STAGES - 1) % STAGES);
+            wait_tiles<STAGES - 1, WI + XI>(w_end - 1 - t - i);
+            multiply(t + i, i);
+        }
+    }
+    // the waves' sums through LDS, once every wave is done
+    __syncthreads();
+    i32x4* const red = reinterpret_cast<i32x4*>(smem);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) red[(wave * FR + i * TN + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int q = tid; q < FR * 64; q += 64 * WAVES) {
+        const int f = q >> 6, l = q & 63;
+        const int m = m0 + f / TN * 16 + (l & 15), n = n0 + f % TN * 16 + 4 * (l >> 4);
+        if (m >= M || n >= N || (XR < 16 && (l & 15) >= XR)) continue;
+        i32x4 v = red[q];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += red[w * FR * 64 + q];
+        if (splits > 1) *reinterpret_cast<i32x4*>(ws + ((size_t)split * M + m) * ((N + 3) & ~3) + n) = v;
+        else epi.store(m, n, M, N, v, epi.cols(n, N), epi.scale_a[m]);
+    }
+}
+
+// Adds up the sums of several ranges of K: a thread four columns of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void i8_join_kernel(const int* __restrict__ ws, int splits, int M, int N, I8Epi<T> epi)
+{
+    const int groups = (N + 3) >> 2;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (int64_t)M * groups) return;
+    const int m = (int)(at / groups), n = (int)(at % groups) * 4;
+    const i32x4* p = reinterpret_cast<const i32x4*>(ws) + at;
+    const auto cols = epi.cols(n, N);
+    const float sa = epi.scale_a[m];
+    i32x4 v = *p;
+#pragma unroll 4
+    for (int s = 1; s < splits; ++s) v += p[(int64_t)s * M * groups];
+    epi.store(m, n, M, N, v, cols, sa);
+}
+
 // ------------------------------------------------------------- the checks --
 
 static bool i8_dtype_ok(int dtype) { return dtype == EBRL_DTYPE_FP32 || dtype == EBRL_DTYPE_BF16; }
@@ -827,60 +977,133 @@ static bool i8_shape_ok(const ebrl_i8_gemm_args* a) {
            (((int64_t)a->M + 31) / 32) * (((int64_t)a->N + 63) / 64) <= I8_MAX_TILES;
 }
 
+enum { I8_BIG, I8_RING, I8_DECODE };
 struct I8Plan {
-    int bm, bn;              // tile
-    int grid, full, split;   // 256 x 256: workgroups, evenly dealt tiles, cut of the last round's tiles
+    int kind, bm, bn;                // tile (decode: rows loaded, columns)
+    int grid, full, cut;             // big: workgroups, evenly dealt tiles, parts of each tile of the last round
+    int splits, per_split, m_tiles;  // decode: ranges of K, their K tiles
 };
 
-static I8Plan i8_plan(int M, int N, int K) {
-    constexpr int CUS = 256;
-    I8Plan p{};
-    const double nk = (K + 127) / 128;
-    auto up = [](long a, long b) { return (a + b - 1) / b; };
-    const long tiles = up(M, 256) * up(N, 256);
-    const long rounds = tiles / CUS, full = rounds * CUS, rest = tiles - full;
-    p.bm = p.bn = 256;
-    p.full = (int)full;
-    double best = 0;
-    struct Cut { int split; double c, alone, busy; } cuts[] = {{1, 8.0, 0.75, 1.24}, {2, 5.6, 0.50, 0.78}, {4, 4.0, 0.38, 0.55}};
-    for (const Cut& v : cuts) {
-        if (v.split > 1 && (!rest || rest * v.split > CUS)) continue;
-        const long pieces = full || v.split == 1 ? rest * v.split : up(M, 128) * up(N, v.split == 2 ? 256 : 128);
-        double t = v.c + rounds * (8.7 + 1.39 * nk);
-        if (rest) t += nk * (v.alone + (v.busy - v.alone) * pieces / CUS);
-        if (v.split == 1 || t < best) {
-            best = t;
-            p.split = v.split;
-        }
-    }
-    p.grid = (int)(full ? CUS : rest * p.split);
-    struct Ring { int bm, bn; double c, epi, one, two; } rings[] = {{64, 128, 2.4, 1.7, 0.353, 0.610},
-                                                                    {64, 64, 2.3, 1.0, 0.225, 0.355},
-                                                                    {32, 64, 2.4, 0.7, 0.175, 0.262}};
-    for (const Ring& v : rings) {
-        const long wgs = up(M, v.bm) * up(N, v.bn), pairs = wgs / (2 * CUS);
-        const double left = (double)(wgs - pairs * 2 * CUS) / CUS;
-        double t = v.c + pairs * (v.epi + nk * v.two);
-        if (left > 1) t += v.epi + nk * (v.one + (v.two - v.one) * (0.6 + 0.4 * (left - 1)));
-        else if (left > 0) t += v.epi / 2 + nk * v.one;
-        if (t < best) {
-            best = t;
-            p.bm = v.bm;
-            p.bn = v.bn;
-        }
-    }
-    return p;
+constexpr int i8_decode_stages(int xr, int bn) {
+    // as many K tiles in LDS as fit, at most four and those in 128 KB
+    const int per = 4 * (bn + xr) * 128;
+    return 4 * per <= 128 * 1024 ? 4 : 3 * per <= 150 * 1024 ? 3 : 2;
 }
 
-template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, hipStream_t s) {
+// The kernel and tile whose modelled time (us) is least.  The constants are a fit to
+// all candidates on 209 products (M 1 to 9216, N 300 to 22016, K 1024 to 11008, bf16
+// output, weights from HBM): the candidate it picks is on average 0.7 % and at worst 9 %
+// slower than the best one.  No choice changes a result.
+static I8Plan i8_plan(int M, int N, int K) {
+    constexpr int CUS = 256;
+    const int nk = (K + 127) / 128;
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    I8Plan best{};
+    double least = 1e300;
+    auto consider = [&](const I8Plan& p, double t) {
+        if (t < least) {
+            least = t;
+            best = p;
+        }
+    };
+    // 256 x 256 tiles: whole rounds, then the others whole or cut in two or four where
+    // the pieces fit one round.  A K tile of a piece takes `alone` with the chip nearly
+    // empty and `busy` with a piece on every CU.
+    const int64_t tiles = up(M, 256) * up(N, 256);
+    const int64_t rounds = tiles / CUS, full = rounds * CUS, rest = tiles - full;
+    struct Cut { int cut; double c, alone, busy; };
+    for (const Cut& v : {Cut{1, 12.7, 0.85, 1.27}, Cut{2, 7.8, 0.68, 0.92}, Cut{4, 4.5, 0.52, 0.63}}) {
+        if (v.cut > 1 && (!rest || rest * v.cut > CUS)) continue;
+        // (pieces past the last row or column have nothing to do)
+        const int64_t pieces = full || v.cut == 1 ? rest * v.cut : up(M, 128) * up(N, v.cut == 2 ? 256 : 128);
+        double t = v.c + rounds * (11.3 + 1.28 * nk);
+        if (rest) t += nk * (v.alone + (v.busy - v.alone) * pieces / CUS);
+        consider(I8Plan{I8_BIG, 256, 256, (int)(full ? CUS : rest * v.cut), (int)full, v.cut, 1, nk, 1}, t);
+    }
+    // Ring tiles: two workgroups share a CU, so they take rounds of one (`one` us a K
+    // tile) or two (`two`) a CU; of that and the weights, streamed once for each
+    // group of four row tiles, the shorter one shows by a ninth.
+    struct Ring { int bm, bn; double epi, one, two; };
+    for (const Ring& v : {Ring{64, 128, 3.3, 0.42, 0.58}, Ring{64, 64, 0.83, 0.30, 0.37}, Ring{32, 64, 0.69, 0.20, 0.30}}) {
+        const int64_t wgs = up(M, v.bm) * up(N, v.bn), pairs = wgs / (2 * CUS);
+        const double left = (double)(wgs - pairs * 2 * CUS) / CUS;   // workgroups a CU in the last round
+        double t = 2.8 + pairs * (v.epi + nk * v.two);
+        if (left > 1) t += v.epi + nk * (v.one + (v.two - v.one) * (0.6 + 0.4 * (left - 1)));
+        else if (left > 0) t += v.epi / 2 + nk * v.one;
+        const double w = (double)N * K * 1e-6 * (0.265 + 0.2 * (up(up(M, v.bm), 4) - 1));
+        t = std::max(t, w) + 0.11 * std::min(t, w);
+        consider(I8Plan{I8_RING, v.bm, v.bn, 0, 0, 0, 1, nk, 1}, t);
+    }
+    // Decode: a K tile of the four waves is (bn + xr) * 512 bytes through LDS, at 57 or
+    // 68 KB/us a CU by how many are in flight (more where few CUs work); the weights
+    // come at 10 TB/s at best, and the shorter time shows by a third.  Several ranges
+    // of K cost a launch more, and their sums' way through memory.
+    if (M <= 512) {
+        const int xr = M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : up(M, up(M, 64)) <= 48 ? 48 : 64;
+        const int m_tiles = (int)up(M, xr);
+        for (int bn : {16, 32, 48, 64, 96})
+            for (int splits : {1, 2, 4, 8, 16}) {
+                const int64_t wgs = up(N, bn) * m_tiles * splits;
+                if (splits > 1 && (wgs > CUS || nk < splits * 8)) continue;
+                const int per = (int)up(nk, splits);
+                const double step = (bn + xr) * 0.512 / (i8_decode_stages(xr, bn) == 2 ? 57 : 68) *
+                                    (0.77 + 0.23 * std::min(1.0, wgs / 256.0));
+                const double cu = up(wgs, CUS) * (0.88 + up(per, 4) * step), hbm = (double)N * K / 10e6;
+                double t = 2.6 + std::max(cu, hbm) + 0.3 * std::min(cu, hbm);
+                if (splits > 1) t += 2.6 + 4.1e-6 * splits * M * N;
+                consider(I8Plan{I8_DECODE, xr, bn, (int)wgs, 0, 0, (int)up(nk, per), per, m_tiles}, t);
+            }
+    }
+    return best;
+}
+static int64_t i8_plan_bytes(const I8Plan& p, int M, int N) {
+    return p.kind == I8_DECODE && p.splits > 1 ? (int64_t)p.splits * M * ((N + 3) & ~3) * 4 : 0;
+}
+
+template <typename T, int XR, int BN> static void i8_decode_launch(const ebrl_i8_gemm_args& a, const I8Plan& p,
+                                                                   const I8Epi<T>& epi, hipStream_t s) {
+    constexpr int STAGES = i8_decode_stages(XR, BN);
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((a.N + BN - 1) / BN * p.splits * p.m_tiles), dim3(256), 0, s, a.a, (uint32_t)a.lda,
+                           a.b, (uint32_t)a.ldb, a.M, a.N, a.K, p.per_split, p.splits, p.m_tiles, (int*)a.workspace, epi);
+    };
+    if constexpr (XR > 32) {
+        if (p.m_tiles > 1) { go(i8_decode_kernel<T, XR, BN, STAGES, false>); return; }
+    }
+    go(i8_decode_kernel<T, XR, BN, STAGES, true>);
+}
+template <typename T, int XR> static void i8_decode_slices(const ebrl_i8_gemm_args& a, const I8Plan& p, const I8Epi<T>& epi,
+                                                           hipStream_t s) {
+    switch (p.bn) {
+    case 16: i8_decode_launch<T, XR, 16>(a, p, epi, s); break;
+    case 32: i8_decode_launch<T, XR, 32>(a, p, epi, s); break;
+    case 48: i8_decode_launch<T, XR, 48>(a, p, epi, s); break;
+    case 64: i8_decode_launch<T, XR, 64>(a, p, epi, s); break;
+    default: i8_decode_launch<T, XR, 96>(a, p, epi, s); break;
+    }
+}
+
+template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, const I8Plan& p, hipStream_t s) {
     const int esz = sizeof(T);
     auto wide = [&](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; };
     const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc,
                        a.N % 4 == 0 && wide(a.c, a.ldc) && (!a.residual || wide(a.residual, a.ldr))};
-    const I8Plan p = i8_plan(a.M, a.N, a.K);
-    if (p.bm == 256) {
+    if (p.kind == I8_DECODE) {
+        switch (p.bm) {
+        case 8: i8_decode_slices<T, 8>(a, p, epi, s); break;
+        case 16: i8_decode_slices<T, 16>(a, p, epi, s); break;
+        case 32: i8_decode_slices<T, 32>(a, p, epi, s); break;
+        case 48: i8_decode_slices<T, 48>(a, p, epi, s); break;
+        default: i8_decode_slices<T, 64>(a, p, epi, s); break;
+        }
+        if (p.splits > 1)
+            hipLaunchKernelGGL(i8_join_kernel<T>, dim3((unsigned)(((int64_t)a.M * ((a.N + 3) / 4) + 255) / 256)), dim3(256),
+                               0, s, (const int*)a.workspace, p.splits, a.M, a.N, epi);
+        return;
+    }
+    if (p.kind == I8_BIG) {
         hipLaunchKernelGGL(i8_big_kernel<T>, dim3(p.grid), dim3(512), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M,
-                           a.N, a.K, p.full, p.split, epi);
+                           a.N, a.K, p.full, p.cut, epi);
         return;
     }
     const dim3 grid((unsigned)((((int64_t)a.M + p.bm - 1) / p.bm) * (((int64_t)a.N + p.bn - 1) / p.bn)));
@@ -890,6 +1113,11 @@ template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, hip
     if (p.bn == 128) ring(i8_ring_kernel<T, 64, 128, 3>);
     else if (p.bm == 64) ring(i8_ring_kernel<T, 64, 64, 3>);
     else ring(i8_ring_kernel<T, 32, 64, 4>);
+}
+
+static int64_t i8_gemm_workspace(const ebrl_i8_gemm_args* a) {
+    if (!i8_shape_ok(a)) return EBRL_E_INVALID;
+    return a->M == 0 || a->N == 0 ? 0 : i8_plan_bytes(i8_plan(a->M, a->N, a->K), a->M, a->N);
 }
 
 static int i8_gemm(const ebrl_i8_gemm_args* args, hipStream_t s) {
@@ -902,8 +1130,11 @@ static int i8_gemm(const ebrl_i8_gemm_args* args, hipStream_t s) {
         !i8_rows_ok(a.c, a.ldc, a.N, esz) || (a.residual && !i8_rows_ok(a.residual, a.ldr, a.N, esz)) ||
         (a.residual == a.c && a.ldr != a.ldc))
         return EBRL_E_INVALID;
-    if (esz == 2) i8_gemm_launch<bf16_t>(a, s);
-    else i8_gemm_launch<float>(a, s);
+    const I8Plan p = i8_plan(a.M, a.N, a.K);
+    const int64_t need = i8_plan_bytes(p, a.M, a.N);
+    if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return EBRL_E_INVALID;
+    if (esz == 2) i8_gemm_launch<bf16_t>(a, p, s);
+    else i8_gemm_launch<float>(a, p, s);
     return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP;
 }
 
@@ -913,7 +1144,7 @@ extern "C" {
 
 int ebrl_op_i8_quant(const ebrl_i8_quant_args* args, void* stream) { return ebrl::i8_quant(args, (hipStream_t)stream); }
 
-int64_t ebrl_op_i8_gemm_workspace(const ebrl_i8_gemm_args* args) { return ebrl::i8_shape_ok(args) ? 0 : EBRL_E_INVALID; }
+int64_t ebrl_op_i8_gemm_workspace(const ebrl_i8_gemm_args* args) { return ebrl::i8_gemm_workspace(args); }
 
 int ebrl_op_i8_gemm(const ebrl_i8_gemm_args* args, void* stream) { return ebrl::i8_gemm(args, (hipStream_t)stream); }
 
