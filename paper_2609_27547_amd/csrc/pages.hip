@@ -14,24 +14,16 @@
 
 namespace ebrl {
 
-constexpr int PG_CHUNK = 4096;      // refs that a workgroup of 256 threads counts
-constexpr int PG_PIECE = 32768;     // bytes that a workgroup copies at a time
+constexpr int PG_CHUNK = 4096;      // refs that a workgroup counts: sixteen neighbours a thread
+constexpr int PG_PIECE = 16384;     // bytes that a workgroup copies at a time: four loads a thread
 constexpr int PG_MAX_ROWS = 1 << 16;
 constexpr int64_t PG_MAX_GROUPS = 1 << 23;
 
 // ------------------------------------------------------- workgroup helpers --
 
-// Sum over the workgroup's 256 threads, for each of them; `red`: 4 words.
-EBRL_DEV int pg_sum(int v, int* red) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return red[0] + red[1] + red[2] + red[3];
-}
-// Sum of the values of the threads before this one; `red`: 4 words.
-EBRL_DEV int pg_before(int v, int* red) {
+// Of each thread's value: the sum of those of the threads before it, and of all.
+// `red`: a word for each wave.
+template <int WAVES> EBRL_DEV int2 pg_scan(int v, int* red) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int s = v;
 #pragma unroll
@@ -42,11 +34,16 @@ EBRL_DEV int pg_before(int v, int* red) {
     __syncthreads();
     if (lane == 63) red[wave] = s;
     __syncthreads();
-    int base = 0;
-    for (int w = 0; w < wave; ++w) base += red[w];
-    return base + s - v;
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const int t = red[w];
+        all += t;
+        if (w < wave) before += t;
+    }
+    return make_int2(before + s - v, all);
 }
-// Sums of v[0 .. at) and of v[0 .. n).
+// Sums of v[0 .. at) and of v[0 .. n), for workgroups of 256.
 EBRL_DEV int2 pg_prefix(const int* v, int at, int n, int* red) {
     int a = 0, b = 0;
     for (int i = threadIdx.x; i < n; i += 256) {
@@ -54,9 +51,7 @@ EBRL_DEV int2 pg_prefix(const int* v, int at, int n, int* red) {
         b += x;
         if (i < at) a += x;
     }
-    a = pg_sum(a, red);
-    b = pg_sum(b, red);
-    return make_int2(a, b);
+    return make_int2(pg_scan<4>(a, red).y, pg_scan<4>(b, red).y);
 }
 // Whether v[0 .. n) holds x, for every thread of the workgroup.
 EBRL_DEV bool pg_holds(const int* v, int n, int x) {
@@ -71,14 +66,52 @@ EBRL_DEV int pg_pages(int64_t tokens, int stride) {
 }
 EBRL_DEV bool pg_page(int p, int num) { return (unsigned)p < (unsigned)num; }
 
+// Which of pages p .. p + 15 are in use, a bit each; those past the pool are not.
+EBRL_DEV unsigned pg_used16(const ebrl_kv8_pool& c, int p) {
+    unsigned m = 0;
+    if (p + 16 <= c.num_blocks && (uintptr_t)c.refs % 16 == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int4 r = *reinterpret_cast<const int4*>(c.refs + p + 4 * k);
+            m |= ((r.x > 0 ? 1u : 0u) | (r.y > 0 ? 2u : 0u) | (r.z > 0 ? 4u : 0u) | (r.w > 0 ? 8u : 0u)) << 4 * k;
+        }
+    } else {
+        for (int k = 0; k < 16 && p + k < c.num_blocks; ++k) m |= (c.refs[p + k] > 0 ? 1u : 0u) << k;
+    }
+    return m;
+}
+// Which of them exist.
+EBRL_DEV unsigned pg_there16(const ebrl_kv8_pool& c, int p) {
+    const int n = c.num_blocks - p;
+    return n >= 16 ? 0xFFFFu : n > 0 ? (1u << n) - 1 : 0u;
+}
+
 // Copies piece `piece` of a page in one layer; `bytes`: of a page's codes, a
-// multiple of 1024.  The first piece takes the scales along.
-EBRL_DEV void pg_copy(const ebrl_kv8_pool& c, int from, int to, int layer, int piece, int bytes) {
-    const char* src = (const char*)c.codes + (size_t)layer * c.layer_codes + (size_t)from * bytes;
-    char* dst = (char*)c.codes + (size_t)layer * c.layer_codes + (size_t)to * bytes;
-    const int end = min(bytes, (piece + 1) * PG_PIECE);
-    for (int o = piece * PG_PIECE + threadIdx.x * 16; o < end; o += 4096)
-        *reinterpret_cast<uint4*>(dst + o) = *reinterpret_cast<const uint4*>(src + o);
+// multiple of 1024.  The first piece takes the scales along.  Bound by memory: a
+// thread's loads are in flight before its first store, and what is written is not read
+// again here (900 pages of 32 KB in 18 layers 191 us with non-temporal loads and stores,
+// 209 with plain ones; 256 copies of 16 pages in 32 layers 54 us with plain loads, whose
+// pages stay in the caches, 82 without).  ONCE: no other copy reads the same page.
+template <bool ONCE> EBRL_DEV void pg_copy(const ebrl_kv8_pool& c, int from, int to, int layer, int piece, int bytes) {
+    constexpr int N = PG_PIECE / 4096;
+    const size_t base = (size_t)layer * c.layer_codes + (size_t)piece * PG_PIECE;
+    const char* src = (const char*)c.codes + base + (size_t)from * bytes + threadIdx.x * 16;
+    char* dst = (char*)c.codes + base + (size_t)to * bytes + threadIdx.x * 16;
+    auto load = [](const char* p) {
+        const u32x4* q = reinterpret_cast<const u32x4*>(p);
+        return ONCE ? __builtin_nontemporal_load(q) : *q;
+    };
+    const int left = bytes - piece * PG_PIECE;
+    if (left >= PG_PIECE) {
+        u32x4 v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = load(src + k * 4096);
+#pragma unroll
+        for (int k = 0; k < N; ++k) __builtin_nontemporal_store(v[k], reinterpret_cast<u32x4*>(dst + k * 4096));
+    } else {
+        for (int o = 0; o + (int)threadIdx.x * 16 < left; o += 4096)
+            __builtin_nontemporal_store(load(src + o), reinterpret_cast<u32x4*>(dst + o));
+    }
     if (piece == 0) {
         const int words = 2 * c.kv_heads;
         float* s = c.scales + (size_t)layer * c.layer_scales;
@@ -121,59 +154,134 @@ __global__ __launch_bounds__(256) void pages_free_kernel(ebrl_kv8_pool c, const 
 
 // ---------------------------------------------------------------- reserve --
 
-// Workspace of a reservation: `chunks` counts of free pages; for each of n rows
-// the number of pages that it needs and the page to copy (or -1); the local rank
-// of each of its `pages` entries among those that need one (or -1); what is
-// needed and free in all; the needed free ids.
+// A reservation's numbers in the workspace.
 struct PgReserve {
     int n, pages, chunks;
-    int *free_count, *need, *copy, *rank, *total, *list;
+    int* free_count;    // [chunks] free pages of each
+    int* need;          // [n] pages that row i needs
+    int* before;        // [n] ... and the rows before it
+    int* copy;          // [n] the page to copy, or -1
+    int* total;         // pages needed and free in all
+    int* rank;          // [n][pages] an entry's number among those of its row that need a page, or -1
+    int* list;          // the free ids, as many as are needed
 };
+// Entries of row i that the call looks at: `pages` of them from j0 on, none if it is
+// left out.
+struct PgSpan { int row, pos, j0, pages; };
+EBRL_DEV PgSpan pg_span(const ebrl_kv8_pool& c, const int* seq, const int* pos0, const int* count, int max_count, int i) {
+    PgSpan r;
+    r.row = seq[i];
+    r.pos = max(pos0[i], 0);
+    r.j0 = r.pos / EBRL_KV8_PAGE;
+    const int64_t end = min((int64_t)r.pos + min(max(count[i], 0), max_count), (int64_t)c.table_stride * EBRL_KV8_PAGE);
+    r.pages = !pg_page(r.row, c.table_rows) || end <= r.pos ? 0 : (int)((end + EBRL_KV8_PAGE - 1) / EBRL_KV8_PAGE) - r.j0;
+    return r;
+}
+// Whether entry j of the span needs a page; the first one tells what to copy.
+EBRL_DEV bool pg_need(const ebrl_kv8_pool& c, const PgSpan& r, int j, int* copy) {
+    bool need = false;
+    int from = -1;
+    if (j < r.pages) {
+        const int p = c.block_table[(size_t)r.row * c.table_stride + r.j0 + j];
+        const bool held = pg_page(p, c.num_blocks);
+        need = !held || c.refs[p] > 1;
+        if (need && held && r.pos % EBRL_KV8_PAGE) from = p;
+    }
+    if (j == 0) *copy = from;
+    return need;
+}
 
+// Small calls (PG_SMALL_*): everything that is decided, in one workgroup of sixteen
+// waves, a row a wave at a time, then sixteen pages a thread.
+constexpr int PG_SMALL_ROWS = 1024, PG_SMALL_POOL = 1 << 16, PG_SMALL_ENTRIES = 1 << 14;
+__global__ __launch_bounds__(1024) void pages_reserve_small_kernel(ebrl_kv8_pool c, const int* seq, const int* pos0,
+                                                                   const int* count, int max_count, int* lacking,
+                                                                   PgReserve w)
+{
+    __shared__ int s_seq[PG_SMALL_ROWS], s_need[PG_SMALL_ROWS], red[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // what the later steps read, asked for now
+    const unsigned first = pg_used16(c, tid * 16);
+    if (tid < w.n) s_seq[tid] = seq[tid];
+    __syncthreads();
+    for (int i = wave; i < w.n; i += 16) {
+        PgSpan r = pg_span(c, seq, pos0, count, max_count, i);
+        bool again = false;
+        for (int k = lane; k < i; k += 64) again |= s_seq[k] == r.row;
+        if (__any(again)) r.pages = 0;
+        int base = 0;
+        for (int q = 0; q < w.pages; q += 64) {
+            const int j = q + lane;
+            const bool need = pg_need(c, r, j, w.copy + i);
+            const uint64_t m = __ballot(need);
+            if (j < w.pages) w.rank[(size_t)i * w.pages + j] = need ? base + (int)__popcll(m & ((1ull << lane) - 1)) : -1;
+            base += (int)__popcll(m);
+        }
+        if (lane == 0) s_need[i] = base;
+    }
+    __syncthreads();
+    const int2 r = pg_scan<16>(tid < w.n ? s_need[tid] : 0, red);
+    if (tid < w.n) {
+        w.need[tid] = s_need[tid];
+        w.before[tid] = r.x;
+    }
+    int base = 0;
+    for (int q = 0; q < c.num_blocks; q += 16384) {
+        const int p = q + tid * 16;
+        unsigned m = (q ? pg_used16(c, p) : first) ^ pg_there16(c, p);
+        const int2 f = pg_scan<16>(__popc(m), red);
+        for (int at = base + f.x; m && at < r.y; m &= m - 1, ++at) w.list[at] = p + __builtin_ctz(m);
+        base += f.y;
+    }
+    if (tid == 0) {
+        w.total[0] = r.y;
+        w.total[1] = base;
+        *lacking = max(0, r.y - base);
+    }
+}
+
+// The others: counts, by chunks of pages and by rows ...
 __global__ __launch_bounds__(256) void pages_reserve_count_kernel(ebrl_kv8_pool c, const int* seq, const int* pos0,
                                                                   const int* count, int max_count, PgReserve w)
 {
     __shared__ int red[4];
     if ((int)blockIdx.x < w.chunks) {
-        const int p0 = blockIdx.x * PG_CHUNK;
-        int free = 0;
-        for (int p = threadIdx.x; p < PG_CHUNK; p += 256)
-            if (p0 + p < c.num_blocks) free += c.refs[p0 + p] <= 0;
-        free = pg_sum(free, red);
+        const int p = blockIdx.x * PG_CHUNK + threadIdx.x * 16;
+        const int free = pg_scan<4>(__popc(pg_used16(c, p) ^ pg_there16(c, p)), red).y;
         if (threadIdx.x == 0) w.free_count[blockIdx.x] = free;
         return;
     }
-    const int i = blockIdx.x - w.chunks, s = seq[i];
-    const bool out = !pg_page(s, c.table_rows) || pg_holds(seq, i, s);
-    const int pos = max(pos0[i], 0);
-    const int64_t cap = (int64_t)c.table_stride * EBRL_KV8_PAGE;
-    const int64_t end = min((int64_t)pos + min(max(count[i], 0), max_count), cap);
-    const int j0 = pos / EBRL_KV8_PAGE;
-    const int pages = out || end <= pos ? 0 : (int)((end + EBRL_KV8_PAGE - 1) / EBRL_KV8_PAGE) - j0;
+    const int i = blockIdx.x - w.chunks;
+    PgSpan r = pg_span(c, seq, pos0, count, max_count, i);
+    if (pg_holds(seq, i, r.row)) r.pages = 0;
     int base = 0;
     for (int q = 0; q < w.pages; q += 256) {
         const int j = q + threadIdx.x;
-        bool need = false;
-        if (j < pages) {
-            const int p = c.block_table[(size_t)s * c.table_stride + j0 + j];
-            const bool held = pg_page(p, c.num_blocks);
-            need = !held || c.refs[p] > 1;
-            if (j == 0) w.copy[i] = need && held && pos % EBRL_KV8_PAGE ? p : -1;
-        } else if (j == 0) {
-            w.copy[i] = -1;
-        }
-        const int at = pg_before(need, red);
-        if (j < w.pages) w.rank[(size_t)i * w.pages + j] = need ? base + at : -1;
-        base += pg_sum(need, red);
+        const bool need = pg_need(c, r, j, w.copy + i);
+        const int2 at = pg_scan<4>(need, red);
+        if (j < w.pages) w.rank[(size_t)i * w.pages + j] = need ? base + at.x : -1;
+        base += at.y;
     }
     if (threadIdx.x == 0) w.need[i] = base;
 }
-
-// Free ids into the list, as many as are needed; needs of the rows before each.
+// ... then free ids into the list, as many as are needed, and (the last workgroup) the
+// needs of the rows before each.
 __global__ __launch_bounds__(256) void pages_reserve_list_kernel(ebrl_kv8_pool c, int* lacking, PgReserve w)
 {
     __shared__ int red[4];
     const int chunk = blockIdx.x;
+    if (chunk == w.chunks) {
+        int base = 0;
+        for (int q = 0; q < w.n; q += 256) {
+            const int i = q + threadIdx.x;
+            const int2 r = pg_scan<4>(i < w.n ? w.need[i] : 0, red);
+            if (i < w.n) w.before[i] = base + r.x;
+            base += r.y;
+        }
+        return;
+    }
+    const int p = chunk * PG_CHUNK + threadIdx.x * 16;
+    unsigned m = pg_used16(c, p) ^ pg_there16(c, p);
     const int2 f = pg_prefix(w.free_count, chunk, w.chunks, red);
     const int needed = pg_prefix(w.need, 0, w.n, red).y;
     if (chunk == 0 && threadIdx.x == 0) {
@@ -181,28 +289,20 @@ __global__ __launch_bounds__(256) void pages_reserve_list_kernel(ebrl_kv8_pool c
         w.total[1] = f.y;
         *lacking = max(0, needed - f.y);
     }
-    if (needed > f.y) return;
-    int base = f.x;
-    for (int q = 0; q < PG_CHUNK && base < needed; q += 256) {
-        const int p = chunk * PG_CHUNK + q + threadIdx.x;
-        const bool free = p < c.num_blocks && c.refs[p] <= 0;
-        const int at = base + pg_before(free, red);
-        if (free && at < needed) w.list[at] = p;
-        base += pg_sum(free, red);
-    }
+    int at = f.x + pg_scan<4>(__popc(m), red).x;
+    for (; m && at < needed; m &= m - 1, ++at) w.list[at] = p + __builtin_ctz(m);
 }
 
-// A row's new entries (piece 0 of layer 0) and the copy of its first page.
+// A row's new entries (piece 0 of the first layers) and the copy of its first page, in
+// `step` layers.
 __global__ __launch_bounds__(256) void pages_reserve_kernel(ebrl_kv8_pool c, const int* seq, const int* pos0, int bytes,
-                                                            int pieces, PgReserve w)
+                                                            int pieces, int step, PgReserve w)
 {
-    __shared__ int red[4];
-    const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces, layer = blockIdx.y;
-    if (w.total[0] > w.total[1]) return;
-    const int from = w.copy[i];
+    const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces, layer = blockIdx.y * step;
+    const int from = w.copy[i], need = w.need[i], before = w.before[i], needed = w.total[0], free = w.total[1];
     const bool entries = piece == 0 && layer == 0;
-    if (w.need[i] == 0 || (!entries && from < 0)) return;
-    const int before = pg_prefix(w.need, i, i, red).x;
+    if (needed > free || need == 0 || (!entries && from < 0)) return;
+    const int to = w.list[before];
     if (entries) {
         int* row = c.block_table + (size_t)seq[i] * c.table_stride + max(pos0[i], 0) / EBRL_KV8_PAGE;
         for (int j = threadIdx.x; j < w.pages; j += 256) {
@@ -214,61 +314,93 @@ __global__ __launch_bounds__(256) void pages_reserve_kernel(ebrl_kv8_pool c, con
             row[j] = p;
         }
     }
-    if (from >= 0) pg_copy(c, from, w.list[before], layer, piece, bytes);
+    if (from < 0) return;
+    const int end = min(layer + step, c.layers);
+    for (int l = layer; l < end; ++l) pg_copy<false>(c, from, to, l, piece, bytes);
 }
 
 // ---------------------------------------------------------------- compact --
 
-// Workspace of a compaction: counts of used pages by chunk; for each page its
-// rank: of a free one below the end among those, of a used one past the end
-// counted from the last of these, -1 for others; free ids below the end by rank;
-// used ids past it, and their refs, by rank; {end, moves}.
+// A compaction's numbers in the workspace.
 struct PgCompact {
     int chunks;
-    int *count, *rank, *hole, *mover, *mover_refs, *total;
+    int* count;         // [chunks] used pages of each
+    int* rank;          // [num_blocks] of a free page below the end: its number among those; of a used one
+                        // past it: its number, from the last of those; -1 of others
+    int* hole;          // the free ids below the end
+    int* mover;         // the used ones past it, the last first
+    int* mover_refs;    // ... their refs
+    int* total;         // the end (pages in use) and the moves
 };
+// Sixteen pages' ranks and places in the lists; m: which are in use, `before`: how many
+// below them are.
+EBRL_DEV void pg_place16(const ebrl_kv8_pool& c, const PgCompact& w, int p, unsigned m, int before, int end) {
+    const unsigned there = pg_there16(c, p);
+#pragma unroll 1
+    for (int k = 0; k < 16; ++k) {
+        if (!(there >> k & 1)) break;
+        const bool used = m >> k & 1;
+        int rank = -1;
+        if (p + k < end && !used) {
+            rank = p + k - before;
+            w.hole[rank] = p + k;
+        } else if (p + k >= end && used) {
+            rank = end - 1 - before;
+            w.mover[rank] = p + k;
+            w.mover_refs[rank] = c.refs[p + k];
+        }
+        w.rank[p + k] = rank;
+        before += used;
+        // free pages below the end: as many as there are moves
+        if (p + k == end - 1) w.total[1] = end - before;
+    }
+}
 
+// Small pools: in one workgroup, sixteen pages a thread at a time.
+__global__ __launch_bounds__(1024) void pages_compact_small_kernel(ebrl_kv8_pool c, int* used, PgCompact w)
+{
+    constexpr int N = PG_SMALL_POOL / 16384;
+    __shared__ int red[16];
+    const int tid = threadIdx.x;
+    unsigned m[N];
+    int before[N], end = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m[k] = pg_used16(c, k * 16384 + tid * 16);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int2 r = pg_scan<16>(__popc(m[k]), red);
+        before[k] = end + r.x;
+        end += r.y;
+    }
+    if (tid == 0) {
+        w.total[0] = end;
+        if (end == 0) w.total[1] = 0;
+        *used = end;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) pg_place16(c, w, k * 16384 + tid * 16, m[k], before[k], end);
+}
+
+// The others: counts by chunks, then ranks and lists.
 __global__ __launch_bounds__(256) void pages_compact_count_kernel(ebrl_kv8_pool c, PgCompact w)
 {
     __shared__ int red[4];
-    const int p0 = blockIdx.x * PG_CHUNK;
-    int used = 0;
-    for (int p = threadIdx.x; p < PG_CHUNK; p += 256)
-        if (p0 + p < c.num_blocks) used += c.refs[p0 + p] > 0;
-    used = pg_sum(used, red);
+    const int used = pg_scan<4>(__popc(pg_used16(c, blockIdx.x * PG_CHUNK + threadIdx.x * 16)), red).y;
     if (threadIdx.x == 0) w.count[blockIdx.x] = used;
 }
-
 __global__ __launch_bounds__(256) void pages_compact_list_kernel(ebrl_kv8_pool c, int* used, PgCompact w)
 {
     __shared__ int red[4];
-    const int p0 = blockIdx.x * PG_CHUNK;
+    const int p = blockIdx.x * PG_CHUNK + threadIdx.x * 16;
+    const unsigned m = pg_used16(c, p);
     const int2 u = pg_prefix(w.count, blockIdx.x, w.chunks, red);
     const int end = u.y;
-    int base = u.x;
-    for (int q = 0; q < PG_CHUNK; q += 256) {
-        const int p = p0 + q + threadIdx.x;
-        const int r = p < c.num_blocks ? c.refs[p] : 0;
-        const int before = base + pg_before(r > 0, red);   // used pages below p
-        int rank = -1;
-        if (p < end && r <= 0) {
-            rank = p - before;
-            w.hole[rank] = p;
-        } else if (p >= end && r > 0) {
-            rank = end - 1 - before;
-            w.mover[rank] = p;
-            w.mover_refs[rank] = r;
-        }
-        if (p < c.num_blocks) w.rank[p] = rank;
-        // free pages below the end: as many as there are moves
-        if (p == end - 1) w.total[1] = end - (before + (r > 0));
-        base += pg_sum(r > 0, red);
-    }
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         w.total[0] = end;
         if (end == 0) w.total[1] = 0;
         *used = end;
     }
+    pg_place16(c, w, p, m, u.x + pg_scan<4>(__popc(m), red).x, end);
 }
 
 // Workgroups below `table_groups`: table and refs; the others: pages.
@@ -296,12 +428,18 @@ __global__ __launch_bounds__(256) void pages_compact_kernel(ebrl_kv8_pool c, int
         }
         return;
     }
-    const int64_t units = (int64_t)moves * c.layers * pieces;
-    for (int64_t u = blockIdx.x - table_groups; u < units; u += gridDim.x - table_groups) {
-        const int piece = (int)(u % pieces);
-        const int64_t v = u / pieces;
-        const int layer = (int)(v / moves), k = (int)(v % moves);
-        pg_copy(c, w.mover[moves - 1 - k], w.hole[k], layer, piece, bytes);
+    // pieces of the moves, layer after layer
+    const int groups = gridDim.x - table_groups, per_layer = moves * pieces;
+    if (moves == 0) return;
+    int u = blockIdx.x - table_groups, layer = u / per_layer;
+    for (u -= layer * per_layer; layer < c.layers;) {
+        const int k = u / pieces;
+        pg_copy<true>(c, w.mover[moves - 1 - k], w.hole[k], layer, u - k * pieces, bytes);
+        u += groups;
+        if (u >= per_layer) {
+            layer += u / per_layer;
+            u %= per_layer;
+        }
     }
 }
 
@@ -333,7 +471,7 @@ static int64_t pg_most_pages(const ebrl_kv8_pool* c, int32_t max_count) {
     return std::min<int64_t>(((int64_t)max_count + 2 * EBRL_KV8_PAGE - 2) / EBRL_KV8_PAGE, c->table_stride);
 }
 static int64_t pg_reserve_words(const ebrl_kv8_pool* c, int64_t n, int64_t pages) {
-    return pg_chunks(c) + 2 * n + n * pages + 2 + std::min<int64_t>(n * pages, c->num_blocks);
+    return pg_chunks(c) + 3 * n + n * pages + 2 + std::min<int64_t>(n * pages, c->num_blocks);
 }
 static int64_t pg_compact_words(const ebrl_kv8_pool* c) {
     return pg_chunks(c) + c->num_blocks + 3 * ((int64_t)c->num_blocks / 2 + 1) + 2;
@@ -391,15 +529,23 @@ int ebrl_op_kv8_reserve(const ebrl_kv8_pool* pool, const int32_t* seq, const int
     w.chunks = pg_chunks(pool);
     w.free_count = (int*)workspace;
     w.need = w.free_count + w.chunks;
-    w.copy = w.need + n;
+    w.before = w.need + n;
+    w.copy = w.before + n;
     w.total = w.copy + n;
     w.rank = w.total + 2;
     w.list = w.rank + (int64_t)n * pages;
-    hipLaunchKernelGGL(pages_reserve_count_kernel, dim3(w.chunks + n), dim3(256), 0, s, *pool, seq, pos0, count, max_count, w);
-    hipLaunchKernelGGL(pages_reserve_list_kernel, dim3(w.chunks), dim3(256), 0, s, *pool, lacking, w);
-    if (n > 0)
-        hipLaunchKernelGGL(pages_reserve_kernel, dim3((unsigned)groups, pool->layers), dim3(256), 0, s, *pool, seq, pos0,
-                           (int)pg_bytes(pool), pieces, w);
+    if (n <= PG_SMALL_ROWS && pool->num_blocks <= PG_SMALL_POOL && n * pages <= PG_SMALL_ENTRIES) {
+        hipLaunchKernelGGL(pages_reserve_small_kernel, dim3(1), dim3(1024), 0, s, *pool, seq, pos0, count, max_count, lacking, w);
+    } else {
+        hipLaunchKernelGGL(pages_reserve_count_kernel, dim3(w.chunks + n), dim3(256), 0, s, *pool, seq, pos0, count, max_count, w);
+        hipLaunchKernelGGL(pages_reserve_list_kernel, dim3(w.chunks + 1), dim3(256), 0, s, *pool, lacking, w);
+    }
+    if (n > 0) {
+        // several layers a workgroup where there are many: what it looks up serves them all
+        const int step = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * pool->layers / 2048));
+        hipLaunchKernelGGL(pages_reserve_kernel, dim3((unsigned)groups, (pool->layers + step - 1) / step), dim3(256), 0, s,
+                           *pool, seq, pos0, (int)pg_bytes(pool), pieces, step, w);
+    }
     return pg_status();
 }
 
@@ -424,10 +570,15 @@ int ebrl_op_kv8_compact(const ebrl_kv8_pool* pool, int32_t* new_table, int32_t* 
     const int pieces = pg_pieces(pool);
     const int64_t entries = std::max<int64_t>((int64_t)pool->table_rows * pool->table_stride, pool->num_blocks);
     const int table_groups = (int)std::min<int64_t>(256, (entries + 1023) / 1024);
-    const int64_t most = (int64_t)(pool->num_blocks / 2) * pool->layers * pieces;
-    const int copy_groups = (int)std::min<int64_t>(2048, most);
-    hipLaunchKernelGGL(pages_compact_count_kernel, dim3(w.chunks), dim3(256), 0, s, *pool, w);
-    hipLaunchKernelGGL(pages_compact_list_kernel, dim3(w.chunks), dim3(256), 0, s, *pool, used, w);
+    const int64_t most = (int64_t)(pool->num_blocks / 2) * pieces;
+    if (most > (1 << 30)) return EBRL_E_INVALID;   // (16 TB a layer)
+    const int copy_groups = (int)std::min<int64_t>(2048, most * pool->layers);
+    if (pool->num_blocks <= PG_SMALL_POOL) {
+        hipLaunchKernelGGL(pages_compact_small_kernel, dim3(1), dim3(1024), 0, s, *pool, used, w);
+    } else {
+        hipLaunchKernelGGL(pages_compact_count_kernel, dim3(w.chunks), dim3(256), 0, s, *pool, w);
+        hipLaunchKernelGGL(pages_compact_list_kernel, dim3(w.chunks), dim3(256), 0, s, *pool, used, w);
+    }
     hipLaunchKernelGGL(pages_compact_kernel, dim3(table_groups + copy_groups), dim3(256), 0, s, *pool, new_table,
                        new_refs, (int)pg_bytes(pool), pieces, table_groups, w);
     return pg_status();

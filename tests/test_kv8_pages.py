@@ -120,29 +120,32 @@ class Lists:
         self.codes = self.store[:, :num]
         self.scales = torch.zeros((layers, num + gap, 2, heads), device="cuda")[:, :num]
         self.content = list(range(num))                # what each page holds
-        for p in range(num):
-            self.fill(p, p)
+        for lo in range(0, num, 4096):
+            self.codes[:, lo:lo + 4096], self.scales[:, lo:lo + 4096] = self._pattern(
+                torch.arange(lo, min(num, lo + 4096), device="cuda")[:, None, None])
         self.d_table = torch.full((rows, stride), -1, dtype=torch.int32, device="cuda")
         self.d_refs = torch.zeros(num, dtype=torch.int32, device="cuda")
         self.lacking = torch.full((1,), 99, dtype=torch.int32, device="cuda")
 
     def _pattern(self, v):
         n = self.layers * 2 * self.heads
-        which = torch.arange(n, device="cuda").reshape(self.layers, 2, self.heads)
+        which = torch.arange(n, device="cuda").reshape(self.layers, 1, 2, self.heads)
         at = torch.arange(PAGE * self.hd, device="cuda")
-        return ((v * 31 + which[..., None] * 7 + at * (v % 5 + 1)) % 251).to(torch.uint8), (v * 1000 + which).float()
+        c, s = (v * 31 + which) * 7, v * 1000 + which
+        return ((c[..., None] + at * ((v % 5 + 1)[..., None])) % 251).to(torch.uint8), s.float()
 
     def fill(self, p, v):
-        self.codes[:, p], self.scales[:, p] = self._pattern(v)
+        self.codes[:, p:p + 1], self.scales[:, p:p + 1] = self._pattern(torch.tensor([v], device="cuda")[:, None, None])
         self.content[p] = v
 
     def check(self):
         torch.cuda.synchronize()
         assert self.d_table.tolist() == self.table
         assert self.d_refs.tolist() == self.refs
-        for p, v in enumerate(self.content):
-            c, s = self._pattern(v)
-            assert torch.equal(self.codes[:, p], c) and torch.equal(self.scales[:, p], s), f"page {p}"
+        for lo in range(0, self.num, 4096):
+            c, s = self._pattern(torch.tensor(self.content[lo:lo + 4096], device="cuda")[:, None, None])
+            same = (self.codes[:, lo:lo + 4096] == c).flatten(2).all(2) & (self.scales[:, lo:lo + 4096] == s).flatten(2).all(2)
+            assert same.all(), f"pages {(lo + torch.nonzero(~same.all(0)).flatten()).tolist()[:9]}"
         # nothing behind a layer's last page was touched
         assert (self.store[:, self.num:] == 0).all()
 
@@ -222,7 +225,8 @@ def _i32(v):
 
 
 SIZES = [(1, 40, 6, 8, 1, 64, 0), (3, 60, 10, 12, 4, 128, 2), (2, 500, 20, 40, 2, 64, 0), (1, 9000, 12, 700, 1, 64, 1),
-         (5, 30, 4, 300, 16, 128, 0), (2, 4097, 9, 5, 1, 64, 0)]
+         (5, 30, 4, 300, 16, 128, 0), (2, 4097, 9, 5, 1, 64, 0),
+         (1, 65536, 5, 9000, 1, 64, 0), (1, 70001, 5, 9000, 1, 64, 3), (2, 300, 70, 60, 17, 128, 0)]
 
 
 @gpu
@@ -254,6 +258,40 @@ def test_calls_in_turn(sizes, seed):
                 p.fill(q, r.randrange(1 << 16))
     p.check()
     assert sum(x for x in p.refs) == sum(q >= 0 for row in p.table for q in row)
+
+
+@gpu
+@pytest.mark.parametrize("rows,num", [(1024, 4000), (1025, 4000), (1300, 5000), (1500, 70000)])
+def test_many_rows(rows, num):
+    r = random.Random(rows)
+    p = Lists(1, num, rows, 3, 1, 64)
+    first = [r.randrange(-2, rows + 2) for _ in range(rows - 200)] + [5] * 200
+    p.reserve(first, [0] * rows, [r.randrange(0, 49) for _ in range(rows)], 48)
+    src = [i for i in range(100) if p.table[i][0] >= 0]
+    dst = [r.randrange(100, rows) for _ in src]
+    p.fork(src, dst, [r.randrange(1, 49) for _ in src])
+    p.check()
+    order = r.sample(range(rows), rows)
+    p.reserve(order, [r.randrange(0, 40) for _ in order], [r.randrange(0, 20) for _ in order], 20)
+    p.check()
+    p.free(r.sample(range(rows), rows // 2))
+    p.compact()
+    p.check()
+    assert sum(p.refs) == sum(q >= 0 for row in p.table for q in row)
+
+
+@gpu
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_refs_of_any_alignment(shift):
+    """refs at any element of a larger tensor."""
+    p = Lists(1, 100, 6, 20, 1, 64)
+    p.d_refs = torch.zeros(100 + shift, dtype=torch.int32, device="cuda")[shift:]
+    p.reserve([0, 1, 2], [0, 0, 0], [300, 200, 77], 320)
+    p.fork([0, 1], [3, 4], [300, 133])
+    p.reserve([3, 4], [300, 133], [9, 9], 9)
+    p.free([0, 2])
+    p.compact()
+    p.check()
 
 
 @gpu
