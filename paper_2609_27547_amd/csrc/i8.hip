@@ -371,25 +371,24 @@ template <typename T> struct I8Epi {
         }
         return v;
     }
-    // Four outputs inside, all aligned.
-    EBRL_DEV void store_wide(int m, int n, i32x4 sum, const Cols& k, float sa) const {
-        f32x4 v = value(sum, k, sa);
-        if (residual) {
-            const T* r = residual + (size_t)m * ldr + n;
-            if constexpr (sizeof(T) == 4) {
-                v += *reinterpret_cast<const f32x4*>(r);
-            } else {
-                const uint2 w = *reinterpret_cast<const uint2*>(r);
-                v[0] += __uint_as_float(w.x << 16); v[1] += __uint_as_float(w.x & 0xFFFF0000u);
-                v[2] += __uint_as_float(w.y << 16); v[3] += __uint_as_float(w.y & 0xFFFF0000u);
-            }
-        }
-        st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
+    // Four neighbours of the residual, as they lie in memory, and as floats.
+    typedef typename std::conditional<sizeof(T) == 4, f32x4, uint2>::type Four;
+    EBRL_DEV Four load_residual(int m, int n) const {
+        return *reinterpret_cast<const Four*>(residual + (size_t)m * ldr + n);
     }
-    EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Cols& k, float sa) const {
+    static EBRL_DEV f32x4 floats(f32x4 v) { return v; }
+    static EBRL_DEV f32x4 floats(uint2 v) {
+        return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                     __uint_as_float(v.y & 0xFFFF0000u)};
+    }
+    // Up to four outputs, those that are inside: v but for the residual.
+    EBRL_DEV void store_some(int m, int n, int M, int N, f32x4 v) const {
         if (m >= M || n >= N) return;
-        if (wide) { store_wide(m, n, sum, k, sa); return; }
-        const f32x4 v = value(sum, k, sa);
+        if (wide) {
+            if (residual) v += floats(load_residual(m, n));
+            st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (n + e < N) {
@@ -397,6 +396,9 @@ template <typename T> struct I8Epi {
                 if (residual) x += ld_elem<T>(residual + (size_t)m * ldr + n + e);
                 st_elem<T>(c + (size_t)m * ldc + n + e, x);
             }
+    }
+    EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Cols& k, float sa) const {
+        store_some(m, n, M, N, value(sum, k, sa));
     }
 };
 
@@ -410,7 +412,7 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 // read them.  Workgroups are persistent; the next tile's first DMAs go out before
 // the epilogue, whose stores drain behind them.  `full` tiles are dealt evenly, those
 // of the last round cut in `split`.
-template <typename T>
+template <typename T, bool RES>
 __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict__ A, uint32_t lda,
                                                         const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
                                                         int full, int split, I8Epi<T> epi)
@@ -435,10 +437,16 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
         constexpr int AHALF = 2 * HA * 128, BHALF = 4 * HB * 128, SB = 2 * (AHALF + BHALF);
         constexpr int W = 2 * NA + 2 * NB;               // DMA instructions per wave and K tile
         static_assert(2 * SB <= STAGES, "stages");
-        // stores of an interior tile's epilogue, at least: they may still be in
-        // flight behind the next tile's first loads
-        constexpr int EST = 2 * FA * 4 * FB / 2;
-        static_assert(W + EST < 64, "vmcnt range");
+        // The epilogue's 16-row groups, the group before which the next tile's first
+        // loads go out (RES: when the residual's are all on their way), and the stores
+        // of an interior tile behind those, which may still be in flight with them.
+        constexpr int GROUPS = 2 * FA, AT = RES ? 5 : 0;
+        constexpr int HALF = sizeof(T) == 2 && !RES;     // staged as results, not as floats
+        constexpr int PASSES = FB * (HALF ? 1 : 2);
+        constexpr int EST = (GROUPS - AT) * PASSES;
+        // scales that are loaded behind them, without the bias
+        constexpr int RV = FA / 2, SCL = RV + 1;
+        static_assert(W + EST + SCL < 64, "vmcnt range");
         uint32_t va[2][NA], vb[2][NB];
         const char *pA, *pB;
         auto dmaA = [&](int t, int h) {
@@ -521,14 +529,19 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
         // phase p + 1 reads, barrier, multiply, barrier.  A group's reads are
         // complete before its first barrier, so what phase p reads may be refilled
         // from phase p + 1 on, by either group.  One K tile with L further ones (0,
-        // 1, 2 = two or more); ov: the previous output tile's stores sit between
-        // this tile's DMAs.
-        auto ktile = [&](int t, bool ov, auto LC) {
+        // 1, 2 = two or more); first, ov: the scales', and the previous output tile's
+        // stores, sit between this tile's DMAs.
+        auto wait = [&](bool first, bool ov) {
+            if (!first) wait_vmcnt<W>();
+            else if (ov) wait_vmcnt<W + EST + SCL>();
+            else wait_vmcnt<W + SCL>();
+        };
+        auto ktile = [&](int t, bool first, bool ov, auto LC) {
             constexpr int L = decltype(LC)::value;
             const int st = (t & 1) * SB;
             readB(st, 0, fb0); readA(st, 0); readB(st, 1, fb1);
             if constexpr (L >= 1) dmaA(t + 1, 1);
-            if constexpr (L >= 2) { if (ov) wait_vmcnt<W + EST>(); else wait_vmcnt<W>(); }
+            if constexpr (L >= 2) wait(first, ov);
             else if constexpr (L == 1) wait_vmcnt<W>();
             else wait_vmcnt<0>();
             wait_lds();
@@ -539,7 +552,7 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             readA(st, 1);
             if constexpr (L >= 2) {
                 dmaB(t + 2, 0); dmaA(t + 2, 0); dmaB(t + 2, 1);
-                if (ov) wait_vmcnt<W + EST>(); else wait_vmcnt<W>();
+                wait(first, ov);
             } else if constexpr (L == 1) wait_vmcnt<NA>();
             wait_lds();
             wg_barrier();
@@ -557,58 +570,116 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
                     for (int i = 0; i < FA; ++i)
 #pragma unroll
                         for (int j = 0; j < FB; ++j) acc[a][b][i][j] = i32x4{0, 0, 0, 0};
+            // The scales of the wave's rows and columns, and the bias, into its staging
+            // LDS: loads of the compiler's would wait for the DMAs that it does not see.
+            const int mw = m0 + wr * 2 * HA, nw = n0 + wc * 2 * HB;
+            const uint32_t stage0 = lds0 + STAGES + wave * 4096;
+            char* const stage = smem + STAGES + wave * 4096;
+#pragma unroll
+            for (int v = 0; v < RV; ++v) dma4_to_lds(epi.scale_a + min(mw + v * 64 + lane, M - 1), stage0 + v * 256);
+            const int at_col = min(nw + lane % (2 * HB), N - 1);
+            dma4_to_lds(epi.scale_b + at_col, stage0 + 512);
+            if (epi.bias) dma4_to_lds(epi.bias + at_col, stage0 + 768);
             // first B halves and first A half of K tile 0
-            if (nk > 1) { if (over) wait_vmcnt<W + EST>(); else wait_vmcnt<W>(); }
-            else wait_vmcnt<NA>();
+            if (nk > 1) wait(true, over);
+            else wait_vmcnt<0>();
             wg_barrier();
             if (wr == 1) wg_barrier();   // the second group runs half a phase behind
             int t = 0;
-            for (; t + 2 < nk; ++t) ktile(t, over && t == 0, std::integral_constant<int, 2>{});
-            if (t + 1 < nk) { ktile(t, false, std::integral_constant<int, 1>{}); ++t; }
-            ktile(t, false, std::integral_constant<int, 0>{});
+            for (; t + 2 < nk; ++t) ktile(t, t == 0, over, std::integral_constant<int, 2>{});
+            if (t + 1 < nk) { ktile(t, false, false, std::integral_constant<int, 1>{}); ++t; }
+            ktile(t, false, false, std::integral_constant<int, 0>{});
             if (wr == 0) wg_barrier();   // both groups are done with the stages
-            const int mw = m0 + wr * 2 * HA, nw = n0 + wc * 2 * HB;
             const bool inside = epi.wide && m0 + 4 * HA <= M && n0 + 8 * HB <= N;
-            // this lane's columns, and the scales of the wave's rows lane and 64 + lane
-            constexpr int LPR = 2 * HB / 4, RPP = 64 / LPR;   // lanes a row, rows a pass
-            const int col = nw + lane % LPR * 4;
-            const auto cols = epi.cols(col, N);
-            constexpr int RV = FA / 2;
-            float row_scale[RV];
+            float sa[GROUPS];
+            f32x4 sb[2 * FB], bias[2 * FB];
 #pragma unroll
-            for (int v = 0; v < RV; ++v) row_scale[v] = epi.scale_a[min(mw + v * 64 + lane, M - 1)];
+            for (int k = 0; k < GROUPS; ++k) sa[k] = *reinterpret_cast<const float*>(stage + (k * 16 + r) * 4);
+#pragma unroll
+            for (int j = 0; j < 2 * FB; ++j) {
+                sb[j] = *reinterpret_cast<const f32x4*>(stage + 512 + (j * 16 + 4 * g) * 4);
+                if (epi.bias) bias[j] = *reinterpret_cast<const f32x4*>(stage + 768 + (j * 16 + 4 * g) * 4);
+            }
+            wait_lds();
             const bool more = next(m0, n0);
-            if (more) prologue();
-            // Through the wave's own staging LDS, 16 rows at a time; chunks swizzled
-            // by row so that the fragment-layout writes and the row-contiguous reads
-            // spread over all banks.
-            char* const stage = smem + STAGES + wave * 4096;
-            auto swz = [](int row) { return ((row & 1) << 2) | ((row >> 1) & 3) | (row & 8); };
-            auto epilogue = [&](auto IN) {
+            // Sixteen rows at a time, scaled, through the staging LDS, so that stores are
+            // of whole row segments; 16-byte chunks swizzled by row, which spreads the
+            // writes (a lane a row) and the reads (several a row) over all banks.
+            auto value = [&](int k, int j) {
+#pragma clang fp contract(off)
+                const i32x4 sum = acc[k / FA][j / FB][k % FA][j % FB];
+                f32x4 v;
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int i = 0; i < FA; ++i) {
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int j = 0; j < FB; ++j)
-                                *reinterpret_cast<i32x4*>(stage + r * 256 + ((((b * FB + j) * 4 + g) ^ swz(r)) << 4)) =
-                                    acc[a][b][i][j];
-                        const int row0 = a * HA + i * 16;
-#pragma unroll
-                        for (int pass = 0; pass < 16 / RPP; ++pass) {
-                            const int row = pass * RPP + lane / LPR;
-                            const i32x4 sum = *reinterpret_cast<const i32x4*>(
-                                stage + row * 256 + (((lane % LPR) ^ swz(row)) << 4));
-                            const float sa = __shfl(row_scale[row0 / 64], row0 % 64 + row, 64);
-                            if constexpr (decltype(IN)::value) epi.store_wide(mw + row0 + row, col, sum, cols, sa);
-                            else epi.store(mw + row0 + row, col, M, N, sum, cols, sa);
-                        }
-                    }
+                for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * sb[j][e] * sa[k];
+                if (epi.bias) v += bias[j];
+                return v;
             };
-            if (inside) epilogue(std::true_type{});
-            else epilogue(std::false_type{});
+            auto swz = [](int row) { return ((row & 1) << 2) | ((row >> 1) & 3) | (row & 8); };
+            auto put = [&](int k) {
+#pragma unroll
+                for (int j = 0; j < 2 * FB; ++j)
+                    *reinterpret_cast<f32x4*>(stage + r * 256 + (((j * 4 + g) ^ swz(r)) << 4)) = value(k, j);
+            };
+            auto get = [&](int row, int ch) {
+                return *reinterpret_cast<const f32x4*>(stage + row * 256 + ((ch ^ swz(row)) << 4));
+            };
+            constexpr int LPR = 2 * HB / 4, RPP = 64 / LPR;   // lanes a row of floats, rows a pass
+            const int lr = lane / LPR, lc = lane % LPR;
+            if (inside && HALF) {
+                // results of 2 bytes: eight neighbours a lane
+                constexpr int L8 = 2 * HB / 8, R8 = 64 / L8;
+                if (more) prologue();
+#pragma unroll
+                for (int k = 0; k < GROUPS; ++k) {
+#pragma unroll
+                    for (int j = 0; j < 2 * FB; ++j) {
+                        const f32x4 v = value(k, j);
+                        st4<bf16_t>(reinterpret_cast<bf16_t*>(stage + r * 128 + (((j * 2 + (g >> 1)) ^ (r & 7)) << 4) + (g & 1) * 8),
+                                    v[0], v[1], v[2], v[3]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 16 / R8; ++p) {
+                        const int row = p * R8 + lane / L8;
+                        const u32x4 v = *reinterpret_cast<const u32x4*>(stage + row * 128 + (((lane % L8) ^ (row & 7)) << 4));
+                        *reinterpret_cast<u32x4*>(epi.c + (size_t)(mw + k * 16 + row) * epi.ldc + nw + lane % L8 * 8) = v;
+                    }
+                }
+            } else if (inside) {
+                typename I8Epi<T>::Four ahead[4][16 / RPP];
+                auto fetch = [&](int k) {
+#pragma unroll
+                    for (int p = 0; p < 16 / RPP; ++p)
+                        ahead[k & 3][p] = epi.load_residual(mw + k * 16 + p * RPP + lr, nw + lc * 4);
+                };
+                if constexpr (RES) {
+#pragma unroll
+                    for (int k = 0; k < 3 && k < GROUPS; ++k) fetch(k);
+                }
+#pragma unroll
+                for (int k = 0; k < GROUPS; ++k) {
+                    if (k == AT && more) prologue();
+                    put(k);
+                    if constexpr (RES) { if (k + 3 < GROUPS) fetch(k + 3); }
+#pragma unroll
+                    for (int p = 0; p < 16 / RPP; ++p) {
+                        const int row = p * RPP + lr;
+                        f32x4 v = get(row, lc);
+                        if constexpr (RES) v += I8Epi<T>::floats(ahead[k & 3][p]);
+                        st4<T>(epi.c + (size_t)(mw + k * 16 + row) * epi.ldc + nw + lc * 4, v[0], v[1], v[2], v[3]);
+                    }
+                }
+            } else {
+                if (more) prologue();
+#pragma unroll
+                for (int k = 0; k < GROUPS; ++k) {
+                    put(k);
+#pragma unroll 1
+                    for (int p = 0; p < 16 / RPP; ++p) {
+                        const int row = p * RPP + lr;
+                        epi.store_some(mw + k * 16 + row, nw + lc * 4, M, N, get(row, lc));
+                    }
+                }
+            }
             if (!more) break;
             over = inside;
         }
@@ -1102,8 +1173,12 @@ template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, con
         return;
     }
     if (p.kind == I8_BIG) {
-        hipLaunchKernelGGL(i8_big_kernel<T>, dim3(p.grid), dim3(512), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M,
-                           a.N, a.K, p.full, p.cut, epi);
+        auto big = [&](auto kern) {
+            hipLaunchKernelGGL(kern, dim3(p.grid), dim3(512), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M, a.N, a.K,
+                               p.full, p.cut, epi);
+        };
+        if (a.residual) big(i8_big_kernel<T, true>);
+        else big(i8_big_kernel<T, false>);
         return;
     }
     const dim3 grid((unsigned)((((int64_t)a.M + p.bm - 1) / p.bm) * (((int64_t)a.N + p.bn - 1) / p.bn)));

@@ -58,6 +58,11 @@ EBRL_DEV void dma16_to_lds_s_nt(const void* sbase, uint32_t voff, uint32_t lds_a
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
                  :: "v"(voff), "s"(sbase), "s"(lds_addr) : "memory", "m0");
 }
+// Four bytes a lane, lane i's at lds_addr + 4 i.
+EBRL_DEV void dma4_to_lds(const void* g, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+                 :: "v"(g), "s"(lds_addr) : "memory", "m0");
+}
 // A wave-uniform address pinned to SGPRs (readfirstlane returns int: each half
 // goes through uint32_t, so the low half is zero-extended).
 EBRL_DEV const char* uniform_ptr(const void* p) {
