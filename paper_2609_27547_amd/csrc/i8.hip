@@ -68,10 +68,24 @@ EBRL_DEV float i8_scale(double top, bool bad) {
     const float s = fmaxf((float)(top / 127.0), 0x1p-100f);
     return bad || !(s <= 3.40282347e38f) ? INFINITY : s;
 }
+// As wave_sum, on both halves of a double.
+template <int CTRL> EBRL_DEV double i8_dpp(double v) {
+    const uint2 w = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(
+        (unsigned)__builtin_amdgcn_update_dpp(0, (int)w.x, CTRL, 0xF, 0xF, false),
+        (unsigned)__builtin_amdgcn_update_dpp(0, (int)w.y, CTRL, 0xF, 0xF, false)));
+}
 EBRL_DEV double i8_wave_sum(double v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
-    return v;
+    v += i8_dpp<DPP_SWAP1>(v);
+    v += i8_dpp<DPP_SWAP2>(v);
+    v += i8_dpp<DPP_HALF_MIRROR>(v);
+    v += i8_dpp<DPP_MIRROR>(v);
+    const uint2 w = __builtin_bit_cast(uint2, v);
+    auto lane = [&](int l) {
+        return __builtin_bit_cast(double, make_uint2((unsigned)__builtin_amdgcn_readlane((int)w.x, l),
+                                                     (unsigned)__builtin_amdgcn_readlane((int)w.y, l)));
+    };
+    return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
 
 // Eight neighbours of a row; those from `left` on are zeros.
@@ -347,11 +361,17 @@ template <typename T> struct I8Epi {
     const T* residual;
     T* c;
     int64_t ldr, ldc;
-    bool wide;              // rows of c and residual are 16-byte aligned (so is N a multiple of four)
+    bool wide;              // rows of c and residual are 16-byte aligned, and N a multiple of four
+    bool wide_cols;         // scale_b and bias are 16-byte aligned
 
     struct Cols { f32x4 s, b; };
     EBRL_DEV Cols cols(int n, int N) const {
         Cols k;
+        if (wide_cols && n + 4 <= N) {
+            k.s = *reinterpret_cast<const f32x4*>(scale_b + n);
+            k.b = bias ? *reinterpret_cast<const f32x4*>(bias + n) : f32x4{0.f, 0.f, 0.f, 0.f};
+            return k;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int at = min(n + e, N - 1);
@@ -399,6 +419,25 @@ template <typename T> struct I8Epi {
     }
     EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Cols& k, float sa) const {
         store_some(m, n, M, N, value(sum, k, sa));
+    }
+    // What four outputs need beside their sums, asked for before these are there, and
+    // their store.
+    struct Ahead { Cols k; float sa; Four r; };
+    EBRL_DEV Ahead ahead(int m, int n, int M, int N) const {
+        Ahead x{};
+        if (m < M && n < N) {
+            x.k = cols(n, N);
+            x.sa = scale_a[m];
+            if (residual && wide) x.r = load_residual(m, n);
+        }
+        return x;
+    }
+    EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Ahead& x) const {
+        if (!wide) { store(m, n, M, N, sum, x.k, x.sa); return; }
+        if (m >= M || n >= N) return;
+        f32x4 v = value(sum, x.k, x.sa);
+        if (residual) v += floats(x.r);
+        st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
     }
 };
 
@@ -781,6 +820,16 @@ __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restric
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    // the epilogue's scales and residual, ahead of the operands
+    constexpr int SROW = WTN + 4, LPR = WTN / 4, RPP = 64 / LPR, PASSES = 16 / RPP;
+    static_assert(4 * 16 * SROW * 4 <= ST * SB, "staging space");
+    const int col = n0 + wn * WTN + lane % LPR * 4;
+    typename I8Epi<T>::Ahead ahead[TM][PASSES];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+            ahead[i][p] = epi.ahead(m0 + wm * WTM + i * 16 + p * RPP + lane / LPR, col, M, N);
     for (int p = 0; p < ST - 1 && p < nk; ++p) dma(p, p);
     int st = 0, nst = ST - 1;
     for (int t = 0; t < nk; ++t) {
@@ -820,22 +869,18 @@ __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restric
         nst = st;
         st = st + 1 == ST ? 0 : st + 1;
     }
-    // epilogue staging in the stages: rows padded by one chunk
-    constexpr int SROW = WTN + 4, LPR = WTN / 4, RPP = 64 / LPR;
-    static_assert(4 * 16 * SROW * 4 <= ST * SB, "staging space");
-    const int col = n0 + wn * WTN + lane % LPR * 4;
-    const auto cols = epi.cols(col, N);
     wg_barrier();
+    // epilogue staging in the stages: rows padded by one chunk
     int* const stage = reinterpret_cast<int*>(smem) + wave * 16 * SROW;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4*>(stage + r * SROW + j * 16 + 4 * g) = acc[i][j];
 #pragma unroll
-        for (int pass = 0; pass < 16 / RPP; ++pass) {
-            const int row = pass * RPP + lane / LPR, m = m0 + wm * WTM + i * 16 + row;
+        for (int p = 0; p < PASSES; ++p) {
+            const int row = p * RPP + lane / LPR;
             const i32x4 sum = *reinterpret_cast<const i32x4*>(stage + row * SROW + lane % LPR * 4);
-            epi.store(m, col, M, N, sum, cols, epi.scale_a[min(m, M - 1)]);
+            epi.store(m0 + wm * WTM + i * 16 + row, col, M, N, sum, ahead[i][p]);
         }
     }
 }
@@ -953,6 +998,23 @@ __global__ __launch_bounds__(256) void i8_decode_kernel(const int8_t* __restrict
             multiply(t + i, i);
         }
     }
+    // The outputs that this thread stores, four each, and what they need beside the
+    // sums, asked for while these are exchanged.
+    constexpr int UNITS = FR * 64, PER = (UNITS + 255) / 256;
+    typename I8Epi<T>::Ahead ahead[PER];
+    auto place = [&](int q, int& m, int& n) {
+        const int f = q >> 6, l = q & 63;
+        m = m0 + f / TN * 16 + (l & 15);
+        n = n0 + f % TN * 16 + 4 * (l >> 4);
+        return q < UNITS && m < M && n < N && (XR >= 16 || (l & 15) < XR);
+    };
+    if (splits == 1) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            int m, n;
+            if (place(tid + 256 * u, m, n)) ahead[u] = epi.ahead(m, n, M, N);
+        }
+    }
     // the waves' sums through LDS, once every wave is done
     __syncthreads();
     i32x4* const red = reinterpret_cast<i32x4*>(smem);
@@ -961,15 +1023,16 @@ __global__ __launch_bounds__(256) void i8_decode_kernel(const int8_t* __restrict
 #pragma unroll
         for (int j = 0; j < TN; ++j) red[(wave * FR + i * TN + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    for (int q = tid; q < FR * 64; q += 64 * WAVES) {
-        const int f = q >> 6, l = q & 63;
-        const int m = m0 + f / TN * 16 + (l & 15), n = n0 + f % TN * 16 + 4 * (l >> 4);
-        if (m >= M || n >= N || (XR < 16 && (l & 15) >= XR)) continue;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        int m, n;
+        const int q = tid + 256 * u;
+        if (!place(q, m, n)) continue;
         i32x4 v = red[q];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += red[w * FR * 64 + q];
+        for (int w = 1; w < WAVES; ++w) v += red[w * UNITS + q];
         if (splits > 1) *reinterpret_cast<i32x4*>(ws + ((size_t)split * M + m) * ((N + 3) & ~3) + n) = v;
-        else epi.store(m, n, M, N, v, epi.cols(n, N), epi.scale_a[m]);
+        else epi.store(m, n, M, N, v, ahead[u]);
     }
 }
 
@@ -1158,7 +1221,8 @@ template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, con
     const int esz = sizeof(T);
     auto wide = [&](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; };
     const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc,
-                       a.N % 4 == 0 && wide(a.c, a.ldc) && (!a.residual || wide(a.residual, a.ldr))};
+                       a.N % 4 == 0 && wide(a.c, a.ldc) && (!a.residual || wide(a.residual, a.ldr)),
+                       ((uintptr_t)a.scale_b | (uintptr_t)a.bias) % 16 == 0};
     if (p.kind == I8_DECODE) {
         switch (p.bm) {
         case 8: i8_decode_slices<T, 8>(a, p, epi, s); break;

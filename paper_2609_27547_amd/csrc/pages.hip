@@ -192,51 +192,91 @@ EBRL_DEV bool pg_need(const ebrl_kv8_pool& c, const PgSpan& r, int j, int* copy)
 }
 
 // Small calls (PG_SMALL_*): everything that is decided, in one workgroup of sixteen
-// waves, a row a wave at a time, then sixteen pages a thread.
+// waves: a row and then an entry a thread, ids a page a lane.  Bound by latency: 256
+// rows of 5 entries 21.7 us with a row a wave at a time, 7 so.
 constexpr int PG_SMALL_ROWS = 1024, PG_SMALL_POOL = 1 << 16, PG_SMALL_ENTRIES = 1 << 14;
+
+// Pages wave `wave` of sixteen looks at, 64 at a time: first and last of them.
+EBRL_DEV int2 pg_wave_pages(int num, int wave) {
+    const int per = (num + 1023) / 1024 * 64;
+    return make_int2(min(num, wave * per), min(num, (wave + 1) * per));
+}
+// Number of lanes below this one whose bit is set.
+EBRL_DEV int pg_below(uint64_t m) {
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+// Pages in use among r.x .. r.y - 1, for a whole wave.
+EBRL_DEV int pg_wave_used(const ebrl_kv8_pool& c, int2 r) {
+    int used = 0;
+    const int lane = threadIdx.x & 63;
+    for (int p = r.x; p < r.y; p += 512) {
+        int v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c.refs[min(p + k * 64 + lane, r.y - 1)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) used += (int)__popcll(__ballot(p + k * 64 + lane < r.y && v[k] > 0));
+    }
+    return used;
+}
+
 __global__ __launch_bounds__(1024) void pages_reserve_small_kernel(ebrl_kv8_pool c, const int* seq, const int* pos0,
                                                                    const int* count, int max_count, int* lacking,
                                                                    PgReserve w)
 {
-    __shared__ int s_seq[PG_SMALL_ROWS], s_need[PG_SMALL_ROWS], red[16];
+    __shared__ int s_seq[PG_SMALL_ROWS], red[16];
+    __shared__ bool s_again[PG_SMALL_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    // what the later steps read, asked for now
-    const unsigned first = pg_used16(c, tid * 16);
-    if (tid < w.n) s_seq[tid] = seq[tid];
-    __syncthreads();
-    for (int i = wave; i < w.n; i += 16) {
-        PgSpan r = pg_span(c, seq, pos0, count, max_count, i);
-        bool again = false;
-        for (int k = lane; k < i; k += 64) again |= s_seq[k] == r.row;
-        if (__any(again)) r.pages = 0;
-        int base = 0;
-        for (int q = 0; q < w.pages; q += 64) {
-            const int j = q + lane;
-            const bool need = pg_need(c, r, j, w.copy + i);
-            const uint64_t m = __ballot(need);
-            if (j < w.pages) w.rank[(size_t)i * w.pages + j] = need ? base + (int)__popcll(m & ((1ull << lane) - 1)) : -1;
-            base += (int)__popcll(m);
-        }
-        if (lane == 0) s_need[i] = base;
-    }
-    __syncthreads();
-    const int2 r = pg_scan<16>(tid < w.n ? s_need[tid] : 0, red);
+    const int2 mine = pg_wave_pages(c.num_blocks, wave);
     if (tid < w.n) {
-        w.need[tid] = s_need[tid];
-        w.before[tid] = r.x;
+        s_seq[tid] = seq[tid];
+        s_again[tid] = false;
+        w.before[tid] = 0;      // ranks count through all rows
     }
-    int base = 0;
-    for (int q = 0; q < c.num_blocks; q += 16384) {
-        const int p = q + tid * 16;
-        unsigned m = (q ? pg_used16(c, p) : first) ^ pg_there16(c, p);
-        const int2 f = pg_scan<16>(__popc(m), red);
-        for (int at = base + f.x; m && at < r.y; m &= m - 1, ++at) w.list[at] = p + __builtin_ctz(m);
-        base += f.y;
+    // free pages of the waves before this one, and of all
+    const int free = mine.y - mine.x - pg_wave_used(c, mine);
+    const int2 f = pg_scan<16>(lane == 0 ? free : 0, red);
+    const int free_before = __builtin_amdgcn_readfirstlane(f.x);
+    __syncthreads();
+    // rows that an earlier number names too: several threads a row where rows are few
+    const int span = (w.n + 63) & ~63, parts = 1024 / max(span, 64), i0 = tid % max(span, 64);
+    if (i0 < w.n) {
+        bool again = false;
+        for (int k = tid / max(span, 64); k < i0; k += parts) again |= s_seq[k] == s_seq[i0];
+        if (again) s_again[i0] = true;
+    }
+    __syncthreads();
+    int needed = 0;
+    for (int q = 0; q < w.n * w.pages; q += 1024) {
+        const int e = q + tid, i = min(e / w.pages, w.n - 1), j = e - i * w.pages;
+        bool need = false;
+        if (e < w.n * w.pages) {
+            PgSpan r = pg_span(c, seq, pos0, count, max_count, i);
+            if (s_again[i]) r.pages = 0;
+            need = pg_need(c, r, j, w.copy + i);
+        }
+        const int2 at = pg_scan<16>(need, red);
+        if (e < w.n * w.pages) w.rank[e] = need ? needed + at.x : -1;
+        needed += at.y;
     }
     if (tid == 0) {
-        w.total[0] = r.y;
-        w.total[1] = base;
-        *lacking = max(0, r.y - base);
+        w.total[0] = needed;
+        w.total[1] = f.y;
+        *lacking = max(0, needed - f.y);
+    }
+    int at = free_before;
+    for (int q = mine.x; q < mine.y && at < needed; q += 256) {
+        int v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = c.refs[min(q + k * 64 + lane, mine.y - 1)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int p = q + k * 64 + lane;
+            const bool is = p < mine.y && v[k] <= 0;
+            const uint64_t m = __ballot(is);
+            const int to = at + pg_below(m);
+            if (is && to < needed) w.list[to] = p;
+            at += (int)__popcll(m);
+        }
     }
 }
 
@@ -299,10 +339,9 @@ __global__ __launch_bounds__(256) void pages_reserve_kernel(ebrl_kv8_pool c, con
                                                             int pieces, int step, PgReserve w)
 {
     const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces, layer = blockIdx.y * step;
-    const int from = w.copy[i], need = w.need[i], before = w.before[i], needed = w.total[0], free = w.total[1];
+    const int from = w.copy[i], before = w.before[i], first = w.rank[(size_t)i * w.pages];
     const bool entries = piece == 0 && layer == 0;
-    if (needed > free || need == 0 || (!entries && from < 0)) return;
-    const int to = w.list[before];
+    if (w.total[0] > w.total[1] || (!entries && from < 0)) return;
     if (entries) {
         int* row = c.block_table + (size_t)seq[i] * c.table_stride + max(pos0[i], 0) / EBRL_KV8_PAGE;
         for (int j = threadIdx.x; j < w.pages; j += 256) {
@@ -315,6 +354,7 @@ __global__ __launch_bounds__(256) void pages_reserve_kernel(ebrl_kv8_pool c, con
         }
     }
     if (from < 0) return;
+    const int to = w.list[before + first];
     const int end = min(layer + step, c.layers);
     for (int l = layer; l < end; ++l) pg_copy<false>(c, from, to, l, piece, bytes);
 }
@@ -356,29 +396,46 @@ EBRL_DEV void pg_place16(const ebrl_kv8_pool& c, const PgCompact& w, int p, unsi
     }
 }
 
-// Small pools: in one workgroup, sixteen pages a thread at a time.
+// Small pools: in one workgroup, a page a lane.
 __global__ __launch_bounds__(1024) void pages_compact_small_kernel(ebrl_kv8_pool c, int* used, PgCompact w)
 {
-    constexpr int N = PG_SMALL_POOL / 16384;
     __shared__ int red[16];
-    const int tid = threadIdx.x;
-    unsigned m[N];
-    int before[N], end = 0;
-#pragma unroll
-    for (int k = 0; k < N; ++k) m[k] = pg_used16(c, k * 16384 + tid * 16);
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const int2 r = pg_scan<16>(__popc(m[k]), red);
-        before[k] = end + r.x;
-        end += r.y;
-    }
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int2 mine = pg_wave_pages(c.num_blocks, tid >> 6);
+    const int of_wave = pg_wave_used(c, mine);
+    const int2 u = pg_scan<16>(lane == 0 ? of_wave : 0, red);
+    const int end = u.y;
     if (tid == 0) {
         w.total[0] = end;
         if (end == 0) w.total[1] = 0;
         *used = end;
     }
+    int below = __builtin_amdgcn_readfirstlane(u.x);
+    for (int q = mine.x; q < mine.y; q += 256) {
+        int v[4];
 #pragma unroll
-    for (int k = 0; k < N; ++k) pg_place16(c, w, k * 16384 + tid * 16, m[k], before[k], end);
+        for (int k = 0; k < 4; ++k) v[k] = c.refs[min(q + k * 64 + lane, mine.y - 1)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int p = q + k * 64 + lane;
+            const bool is = p < mine.y && v[k] > 0;
+            const uint64_t m = __ballot(is);
+            const int before = below + pg_below(m);
+            below += (int)__popcll(m);
+            if (p >= mine.y) continue;
+            int rank = -1;
+            if (p < end && !is) {
+                rank = p - before;
+                w.hole[rank] = p;
+            } else if (p >= end && is) {
+                rank = end - 1 - before;
+                w.mover[rank] = p;
+                w.mover_refs[rank] = v[k];
+            }
+            w.rank[p] = rank;
+            if (p == end - 1) w.total[1] = end - before - is;   // free pages below the end: as many as there are moves
+        }
+    }
 }
 
 // The others: counts by chunks, then ranks and lists.

@@ -646,41 +646,49 @@ _KV8_POOL = struct.Struct("4P2q6i")
 
 
 def _kv8_pool_table(block_table, refs):
-    """Pointers and sizes of a table and its refs, and their GPU's index."""
+    """Pointers of a table and its refs, the pool's pages, the table's shape and their GPU's index."""
     import torch
-    dev = refs.get_device()
-    if refs.dim() != 1 or refs.dtype is not torch.int32 or not refs.is_contiguous():
+    int32, dev = torch.int32, refs.get_device()
+    blocks, table = refs.shape, block_table.shape
+    if len(blocks) != 1 or refs.dtype is not int32 or not refs.is_contiguous():
         _kv8_bad("refs are contiguous int32 [num_blocks]", refs)
-    if block_table.dim() != 2 or block_table.dtype is not torch.int32 or not block_table.is_contiguous() or \
+    if len(table) != 2 or block_table.dtype is not int32 or not block_table.is_contiguous() or \
             block_table.get_device() != dev:
         _kv8_bad("block_table is contiguous int32 [sequences, pages] where refs are", block_table)
-    return block_table.data_ptr(), refs.data_ptr(), refs.shape[0], *block_table.shape, dev
+    return block_table.data_ptr(), refs.data_ptr(), blocks[0], *table, dev
 
 
 def _kv8_pool_shape(codes):
-    """Layers, pages, KV heads and head dim; a layer's codes are contiguous, with any distance between layers."""
+    """Layers, pages, KV heads and the codes of a page's head."""
     shape = codes.shape
-    if len(shape) not in (4, 5) or shape[-3] != 2 or not shape[-1] or shape[-1] % KV8_PAGE or not _kv8_codes(codes) or \
-            not shape[0]:
+    if len(shape) == 5:
+        layers, blocks, two, heads, wide = shape
+    elif len(shape) == 4:
+        layers, (blocks, two, heads, wide) = 1, shape
+    else:
+        layers = blocks = two = heads = wide = 0
+    if two != 2 or not layers or not wide or wide % KV8_PAGE or not _kv8_codes(codes):
         _kv8_bad("codes are float8_e4m3fn or bytes [layers, num_blocks, 2, kv_heads, 16 * head_dim]", codes)
-    return shape[0] if len(shape) == 5 else 1, shape[-4], shape[-2], shape[-1] // KV8_PAGE
+    return layers, blocks, heads, wide
 
 
 def _kv8_pool(codes, scales, block_table, refs):
     """The packed pool and its GPU's index."""
     import torch
-    table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
-    layers, pages, heads, hd = _kv8_pool_shape(codes)
-    many = codes.dim() == 5
-    if pages != blocks or not (codes[0] if many else codes).is_contiguous() or codes.get_device() != dev or \
-            codes.stride(0) < 0:
+    table_at, refs_at, blocks, rows, pages, dev = _kv8_pool_table(block_table, refs)
+    layers, num, heads, wide = _kv8_pool_shape(codes)
+    st, sst = codes.stride(), scales.stride()
+    many = len(st) == 5
+    # (strides that a contiguous layer has; those of dimensions of 1 may be others)
+    if num != blocks or codes.get_device() != dev or st[0] < 0 or \
+            (st[many:] != (2 * heads * wide, heads * wide, wide, 1) and not (codes[0] if many else codes).is_contiguous()):
         _kv8_bad(f"codes of a layer are contiguous [{blocks}, 2, kv_heads, 16 * head_dim] where refs are", codes)
-    if scales.shape != codes.shape[:-1] or scales.dtype is not torch.float32 or \
-            not (scales[0] if many else scales).is_contiguous() or scales.get_device() != dev:
+    if scales.shape != codes.shape[:-1] or scales.dtype is not torch.float32 or scales.get_device() != dev or sst[0] < 0 or \
+            (sst[many:] != (2 * heads, heads, 1) and not (scales[0] if many else scales).is_contiguous()):
         _kv8_bad("scales are float32 [layers, num_blocks, 2, kv_heads] where refs are", scales)
-    at, scales_at = (codes.stride(0), scales.stride(0)) if many else (0, 0)
+    at, scales_at = (st[0], sst[0]) if many else (0, 0)
     return _kv8_pack(_KV8_POOL, codes.data_ptr(), scales.data_ptr(), table_at, refs_at, at, scales_at, layers, blocks,
-                     rows, stride, heads, hd), dev
+                     rows, pages, heads, wide // KV8_PAGE), dev
 
 
 def _kv8_on(fn, name, dev, stream, *args):
@@ -720,13 +728,14 @@ def op_kv8_free(block_table, refs, seq, keep=None, stream=None) -> None:
 
 def _kv8_pool_workspace(name, codes, block_table, *sizes):
     import torch
-    layers, blocks, heads, hd = _kv8_pool_shape(codes)
+    layers, blocks, heads, wide = _kv8_pool_shape(codes)
     if block_table.dim() != 2:
         _kv8_bad("block_table is [sequences, pages]", block_table)
     for x in sizes:
         if not 0 <= x < 1 << 31:
             _kv8_bad(f"{name}: {sizes}")
-    need = getattr(lib(), name)(_kv8_pack(_KV8_POOL, 0, 0, 0, 0, 0, 0, layers, blocks, *block_table.shape, heads, hd), *sizes)
+    pool = _kv8_pack(_KV8_POOL, 0, 0, 0, 0, 0, 0, layers, blocks, *block_table.shape, heads, wide // KV8_PAGE)
+    need = getattr(lib(), name)(pool, *sizes)
     if need < 0:
         raise EbrlError(need, name)
     return torch.empty(need, dtype=torch.uint8, device=codes.device)
@@ -816,29 +825,25 @@ def _i8_pack(packer, *values) -> bytes:
 def _i8_codes(name, t, dev):
     """Pointer, rows, width and row stride of codes."""
     import torch
-    if t.dim() != 2 or t.dtype is not torch.int8 or t.get_device() != dev:
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not torch.int8 or t.get_device() != dev:
         _i8_bad(f"{name} are int8 [rows, K] on one GPU", t)
-    rows, wide = t.shape
+    rows, wide = shape
     ld, one = t.stride()
     if one != 1 and wide > 1:
         _i8_bad(f"{name} have contiguous rows", t)
     return t.data_ptr(), rows, wide, ld if rows > 1 else (wide + 15) // 16 * 16
 
 
-def _i8_floats(name, t, n, dev):
-    """Pointer of n float32; 0 for None."""
-    import torch
-    if t is None:
-        return 0
-    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+def _i8_floats(name, t, n, dev, float32):
+    """Pointer of n float32."""
+    if t.dtype is not float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
         _i8_bad(f"{name} is {n} contiguous float32 where the codes are", t)
     return t.data_ptr()
 
 
 def _i8_rows(name, t, dtype, dev, rows, width):
-    """Pointer and row stride of a [rows, width] tensor whose rows are contiguous; 0 for None."""
-    if t is None:
-        return 0, 0
+    """Pointer and row stride of a [rows, width] tensor whose rows are contiguous."""
     if t.shape != (rows, width) or t.dtype is not dtype or t.get_device() != dev:
         _i8_bad(f"{name} is {dtype} [{rows}, {width}] where the codes are", t)
     ld, one = t.stride()
@@ -847,8 +852,7 @@ def _i8_rows(name, t, dtype, dev, rows, width):
     return t.data_ptr(), ld if rows > 1 else width
 
 
-def _i8_dtype(name, t) -> int:
-    import torch
+def _i8_dtype(name, t, torch) -> int:
     dtype = t.dtype
     if t.dim() != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
         _i8_bad(f"{name} is bfloat16 or float32 [rows, width]", t)
@@ -872,19 +876,26 @@ def op_i8_quant(x, codes, scales, up=None, norm_eps=None, gain=None, stream=None
     """Rows x [rows, cols] to codes [rows, K] (K: cols rounded up to a multiple of 16,
     or more) and scales [rows] (ebrl_op_i8_quant): as they are; with norm_eps, RMS-normed
     and times gain (float32 [cols] or None); with up, silu(x) * up."""
+    import torch
     dev = codes.get_device()
-    dtype = _i8_dtype("x", x)
+    dtype = _i8_dtype("x", x, torch)
     rows, cols = x.shape
-    if up is not None and norm_eps is not None or gain is not None and norm_eps is None:
-        _i8_bad("rows are normed (norm_eps, gain) or gated (up), not both")
-    op = I8_SWIGLU if up is not None else I8_RMSNORM if norm_eps is not None else I8_ROWS
-    x_at, ldx = _i8_rows("x", x, x.dtype, dev, rows, cols)
-    up_at, ldup = _i8_rows("up", up, x.dtype, dev, rows, cols)
     at, n, wide, ldc = _i8_codes("codes", codes, dev)
     if n != rows or wide < (cols + 15) // 16 * 16:
         _i8_bad(f"codes are [{rows}, {(cols + 15) // 16 * 16}]", codes)
-    a = _i8_pack(_I8_QUANT, dtype, op, rows, cols, norm_eps or 0.0, x_at, up_at, ldx, ldup,
-                 _i8_floats("gain", gain, cols, dev), at, ldc, _i8_floats("scales", scales, rows, dev))
+    x_at, ldx = _i8_rows("x", x, x.dtype, dev, rows, cols)
+    op, eps, up_at, ldup, gain_at = I8_ROWS, 0.0, 0, 0, 0
+    if norm_eps is not None:
+        op, eps = I8_RMSNORM, norm_eps
+        if gain is not None:
+            gain_at = _i8_floats("gain", gain, cols, dev, torch.float32)
+    elif up is not None:
+        op = I8_SWIGLU
+        up_at, ldup = _i8_rows("up", up, x.dtype, dev, rows, cols)
+    if up is not None and norm_eps is not None or gain is not None and norm_eps is None:
+        _i8_bad("rows are normed (norm_eps, gain) or gated (up), not both")
+    a = _i8_pack(_I8_QUANT, dtype, op, rows, cols, eps, x_at, up_at, ldx, ldup, gain_at, at, ldc,
+                 _i8_floats("scales", scales, rows, dev, torch.float32))
     _i8_call(lib().ebrl_op_i8_quant, "ebrl_op_i8_quant", a, dev, stream)
 
 
@@ -904,22 +915,27 @@ def op_i8_gemm(a, scale_a, b, scale_b, out, bias=None, residual=None, workspace=
     K], b [N, K]; out [M, N] bfloat16 or float32, residual like out (or out itself).
     workspace: from i8_gemm_workspace, one for each chain of calls that may overlap
     others; None makes one for this call (not with an explicit stream)."""
-    dev = a.get_device()
+    import torch
+    dev, f32 = a.get_device(), torch.float32
     a_at, m, k, lda = _i8_codes("a", a, dev)
     b_at, n, kb, ldb = _i8_codes("b", b, dev)
     if k != kb:
         _i8_bad("a and b have rows of one width", a, b)
-    dtype = _i8_dtype("out", out)
+    dtype = _i8_dtype("out", out, torch)
     out_at, ldc = _i8_rows("out", out, out.dtype, dev, m, n)
-    res_at, ldr = _i8_rows("residual", residual, out.dtype, dev, m, n)
+    res_at = ldr = bias_at = 0
+    if residual is not None:
+        res_at, ldr = _i8_rows("residual", residual, out.dtype, dev, m, n)
+    if bias is not None:
+        bias_at = _i8_floats("bias", bias, n, dev, f32)
     if workspace is None:
         if stream is not None:
             _i8_bad("a call on an explicit stream needs a workspace")
         workspace = i8_gemm_workspace(a, b)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _i8_bad("the workspace is contiguous and where the codes are", workspace)
-    args = _i8_pack(_I8_GEMM, dtype, m, n, k, a_at, b_at, lda, ldb, _i8_floats("scale_a", scale_a, m, dev),
-                    _i8_floats("scale_b", scale_b, n, dev), _i8_floats("bias", bias, n, dev), res_at, ldr, out_at, ldc,
+    args = _i8_pack(_I8_GEMM, dtype, m, n, k, a_at, b_at, lda, ldb, _i8_floats("scale_a", scale_a, m, dev, f32),
+                    _i8_floats("scale_b", scale_b, n, dev, f32), bias_at, res_at, ldr, out_at, ldc,
                     workspace.data_ptr(), workspace.nbytes)
     _i8_call(lib().ebrl_op_i8_gemm, "ebrl_op_i8_gemm", args, dev, stream)
 
