@@ -465,9 +465,19 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
     const int tiles_m = (M + 255) >> 8, tiles_n = (N + 255) >> 8;
     const int nk = (K + 127) >> 7, rest = K - (nk - 1) * 128;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)smem);
-    // byte in the K tile that this lane loads, and how far past the last one's end that is
-    const uint32_t kb = ((lane & 7) ^ (lane >> 3)) * 16;
-    const uint32_t past = (uint32_t)max(0, (int)kb - (rest - 16));
+    // The lane, made anew: what is derived from it once a tile would otherwise be kept in
+    // registers through the K loop, that is, spilled, and its way back waits for every
+    // load in flight.
+    auto fresh_lane = [&]() {
+        int l = 0;
+        asm volatile("" : "+v"(l));
+        return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, (uint32_t)l));
+    };
+    // How far past the end of the last K tile, if it is a short one, this lane's bytes are.
+    auto past = [&]() {
+        const int l = fresh_lane();
+        return (uint32_t)max(0, ((l & 7) ^ (l >> 3)) * 16 - (rest - 16));
+    };
 
     auto run = [&](auto FAC, auto FBC, int m0, int n0, auto next) {
         constexpr int FA = decltype(FAC)::value, FB = decltype(FBC)::value;
@@ -491,21 +501,33 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
         auto dmaA = [&](int t, int h) {
             const char* p = pA + (size_t)t * 128;
             const uint32_t l = lds0 + (t & 1) * SB + h * AHALF + wave * NA * 1024;
-            const uint32_t back = t == nk - 1 ? past : 0u;
+            if (rest < 128 && t == nk - 1) {
+                const uint32_t back = past();
 #pragma unroll
-            for (int j = 0; j < NA; ++j) dma16_to_lds_s(p, va[h][j] - back, l + j * 1024);
+                for (int j = 0; j < NA; ++j) dma16_to_lds_s(p, va[h][j] - back, l + j * 1024);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NA; ++j) dma16_to_lds_s(p, va[h][j], l + j * 1024);
+            }
         };
         auto dmaB = [&](int t, int h) {
             const char* p = pB + (size_t)t * 128;
             const uint32_t l = lds0 + (t & 1) * SB + 2 * AHALF + h * BHALF + wave * NB * 1024;
-            const uint32_t back = t == nk - 1 ? past : 0u;
+            if (rest < 128 && t == nk - 1) {
+                const uint32_t back = past();
 #pragma unroll
-            for (int j = 0; j < NB; ++j) dma16_to_lds_s(p, vb[h][j] - back, l + j * 1024);
+                for (int j = 0; j < NB; ++j) dma16_to_lds_s(p, vb[h][j] - back, l + j * 1024);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) dma16_to_lds_s(p, vb[h][j], l + j * 1024);
+            }
         };
         // K tiles 0 and 1 but for the second half of A's tile 1; rows past the
         // operand repeat its last one.  LDS row q of a half h holds tile row
         // (q / HA) 2 HA + h HA + q % HA: each wave's rows are contiguous.
         auto prologue = [&]() {
+            const int lane = fresh_lane();
+            const uint32_t kb = ((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -614,9 +636,10 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             const int mw = m0 + wr * 2 * HA, nw = n0 + wc * 2 * HB;
             const uint32_t stage0 = lds0 + STAGES + wave * 4096;
             char* const stage = smem + STAGES + wave * 4096;
+            const int early = fresh_lane();
 #pragma unroll
-            for (int v = 0; v < RV; ++v) dma4_to_lds(epi.scale_a + min(mw + v * 64 + lane, M - 1), stage0 + v * 256);
-            const int at_col = min(nw + lane % (2 * HB), N - 1);
+            for (int v = 0; v < RV; ++v) dma4_to_lds(epi.scale_a + min(mw + v * 64 + early, M - 1), stage0 + v * 256);
+            const int at_col = min(nw + early % (2 * HB), N - 1);
             dma4_to_lds(epi.scale_b + at_col, stage0 + 512);
             if (epi.bias) dma4_to_lds(epi.bias + at_col, stage0 + 768);
             // first B halves and first A half of K tile 0
@@ -630,6 +653,7 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             ktile(t, false, false, std::integral_constant<int, 0>{});
             if (wr == 0) wg_barrier();   // both groups are done with the stages
             const bool inside = epi.wide && m0 + 4 * HA <= M && n0 + 8 * HB <= N;
+            const int lane = fresh_lane(), r = lane & 15, g = lane >> 4;
             float sa[GROUPS];
             f32x4 sb[2 * FB], bias[2 * FB];
 #pragma unroll
@@ -667,6 +691,8 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             if (inside && HALF) {
                 // results of 2 bytes: eight neighbours a lane
                 constexpr int L8 = 2 * HB / 8, R8 = 64 / L8;
+                T* to = epi.c + (size_t)(mw + lane / L8) * epi.ldc + nw + lane % L8 * 8;
+                const int64_t step = R8 * epi.ldc;
                 if (more) prologue();
 #pragma unroll
                 for (int k = 0; k < GROUPS; ++k) {
@@ -680,15 +706,23 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
                     for (int p = 0; p < 16 / R8; ++p) {
                         const int row = p * R8 + lane / L8;
                         const u32x4 v = *reinterpret_cast<const u32x4*>(stage + row * 128 + (((lane % L8) ^ (row & 7)) << 4));
-                        *reinterpret_cast<u32x4*>(epi.c + (size_t)(mw + k * 16 + row) * epi.ldc + nw + lane % L8 * 8) = v;
+                        *reinterpret_cast<u32x4*>(to) = v;
+                        to += step;
+                        asm volatile("" : "+v"(to));     // the next rows' addresses are not kept
                     }
                 }
             } else if (inside) {
                 typename I8Epi<T>::Four ahead[4][16 / RPP];
+                T* to = epi.c + (size_t)(mw + lr) * epi.ldc + nw + lc * 4;
+                const T* from = RES ? epi.residual + (size_t)(mw + lr) * epi.ldr + nw + lc * 4 : nullptr;
+                const int64_t step = RPP * epi.ldc, step_r = RPP * epi.ldr;
                 auto fetch = [&](int k) {
 #pragma unroll
-                    for (int p = 0; p < 16 / RPP; ++p)
-                        ahead[k & 3][p] = epi.load_residual(mw + k * 16 + p * RPP + lr, nw + lc * 4);
+                    for (int p = 0; p < 16 / RPP; ++p) {
+                        ahead[k & 3][p] = *reinterpret_cast<const typename I8Epi<T>::Four*>(from);
+                        from += step_r;
+                        asm volatile("" : "+v"(from));   // the next rows' addresses are not kept
+                    }
                 };
                 if constexpr (RES) {
 #pragma unroll
@@ -704,7 +738,9 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
                         const int row = p * RPP + lr;
                         f32x4 v = get(row, lc);
                         if constexpr (RES) v += I8Epi<T>::floats(ahead[k & 3][p]);
-                        st4<T>(epi.c + (size_t)(mw + k * 16 + row) * epi.ldc + nw + lc * 4, v[0], v[1], v[2], v[3]);
+                        st4<T>(to, v[0], v[1], v[2], v[3]);
+                        to += step;
+                        asm volatile("" : "+v"(to));
                     }
                 }
             } else {
@@ -1125,8 +1161,8 @@ constexpr int i8_decode_stages(int xr, int bn) {
 }
 
 // The kernel and tile whose modelled time (us) is least.  The constants are a fit to
-// all candidates on 209 products (M 1 to 9216, N 300 to 22016, K 1024 to 11008, bf16
-// output, weights from HBM): the candidate it picks is on average 0.7 % and at worst 9 %
+// all candidates on 385 products (M 1 to 9216, N 300 to 22016, K 1024 to 11008, bf16
+// output, weights from HBM): the candidate it picks is on average 0.7 % and at worst 11 %
 // slower than the best one.  No choice changes a result.
 static I8Plan i8_plan(int M, int N, int K) {
     constexpr int CUS = 256;
@@ -1146,31 +1182,31 @@ static I8Plan i8_plan(int M, int N, int K) {
     const int64_t tiles = up(M, 256) * up(N, 256);
     const int64_t rounds = tiles / CUS, full = rounds * CUS, rest = tiles - full;
     struct Cut { int cut; double c, alone, busy; };
-    for (const Cut& v : {Cut{1, 12.7, 0.85, 1.27}, Cut{2, 7.8, 0.68, 0.92}, Cut{4, 4.5, 0.52, 0.63}}) {
+    for (const Cut& v : {Cut{1, 10.3, 0.86, 1.32}, Cut{2, 6.8, 0.67, 0.92}, Cut{4, 5.1, 0.48, 0.635}}) {
         if (v.cut > 1 && (!rest || rest * v.cut > CUS)) continue;
         // (pieces past the last row or column have nothing to do)
         const int64_t pieces = full || v.cut == 1 ? rest * v.cut : up(M, 128) * up(N, v.cut == 2 ? 256 : 128);
-        double t = v.c + rounds * (11.3 + 1.28 * nk);
+        double t = v.c + rounds * (9.1 + 1.3 * nk);
         if (rest) t += nk * (v.alone + (v.busy - v.alone) * pieces / CUS);
         consider(I8Plan{I8_BIG, 256, 256, (int)(full ? CUS : rest * v.cut), (int)full, v.cut, 1, nk, 1}, t);
     }
     // Ring tiles: two workgroups share a CU, so they take rounds of one (`one` us a K
     // tile) or two (`two`) a CU; of that and the weights, streamed once for each
-    // group of four row tiles, the shorter one shows by a ninth.
+    // group of four row tiles, the shorter one shows by a seventh.
     struct Ring { int bm, bn; double epi, one, two; };
-    for (const Ring& v : {Ring{64, 128, 3.3, 0.42, 0.58}, Ring{64, 64, 0.83, 0.30, 0.37}, Ring{32, 64, 0.69, 0.20, 0.30}}) {
+    for (const Ring& v : {Ring{64, 128, 3.3, 0.42, 0.70}, Ring{64, 64, 1.0, 0.30, 0.385}, Ring{32, 64, 0.76, 0.20, 0.30}}) {
         const int64_t wgs = up(M, v.bm) * up(N, v.bn), pairs = wgs / (2 * CUS);
         const double left = (double)(wgs - pairs * 2 * CUS) / CUS;   // workgroups a CU in the last round
-        double t = 2.8 + pairs * (v.epi + nk * v.two);
+        double t = 2.9 + pairs * (v.epi + nk * v.two);
         if (left > 1) t += v.epi + nk * (v.one + (v.two - v.one) * (0.6 + 0.4 * (left - 1)));
         else if (left > 0) t += v.epi / 2 + nk * v.one;
-        const double w = (double)N * K * 1e-6 * (0.265 + 0.2 * (up(up(M, v.bm), 4) - 1));
-        t = std::max(t, w) + 0.11 * std::min(t, w);
+        const double w = (double)N * K * 1e-6 * (0.26 + 0.163 * (up(up(M, v.bm), 4) - 1));
+        t = std::max(t, w) + 0.14 * std::min(t, w);
         consider(I8Plan{I8_RING, v.bm, v.bn, 0, 0, 0, 1, nk, 1}, t);
     }
     // Decode: a K tile of the four waves is (bn + xr) * 512 bytes through LDS, at 57 or
-    // 68 KB/us a CU by how many are in flight (more where few CUs work); the weights
-    // come at 10 TB/s at best, and the shorter time shows by a third.  Several ranges
+    // 69 KB/us a CU by how many are in flight (more where few CUs work); the weights
+    // come at 10 TB/s at best, and the shorter time shows by two fifths.  Several ranges
     // of K cost a launch more, and their sums' way through memory.
     if (M <= 512) {
         const int xr = M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : up(M, up(M, 64)) <= 48 ? 48 : 64;
@@ -1180,11 +1216,11 @@ static I8Plan i8_plan(int M, int N, int K) {
                 const int64_t wgs = up(N, bn) * m_tiles * splits;
                 if (splits > 1 && (wgs > CUS || nk < splits * 8)) continue;
                 const int per = (int)up(nk, splits);
-                const double step = (bn + xr) * 0.512 / (i8_decode_stages(xr, bn) == 2 ? 57 : 68) *
-                                    (0.77 + 0.23 * std::min(1.0, wgs / 256.0));
-                const double cu = up(wgs, CUS) * (0.88 + up(per, 4) * step), hbm = (double)N * K / 10e6;
-                double t = 2.6 + std::max(cu, hbm) + 0.3 * std::min(cu, hbm);
-                if (splits > 1) t += 2.6 + 4.1e-6 * splits * M * N;
+                const double step = (bn + xr) * 0.512 / (i8_decode_stages(xr, bn) == 2 ? 57 : 69) *
+                                    (0.83 + 0.17 * std::min(1.0, wgs / 256.0));
+                const double cu = up(wgs, CUS) * (0.96 + up(per, 4) * step), hbm = (double)N * K / 9.83e6;
+                double t = 2.55 + std::max(cu, hbm) + 0.39 * std::min(cu, hbm);
+                if (splits > 1) t += 2.2 + 5.3e-6 * splits * M * N;
                 consider(I8Plan{I8_DECODE, xr, bn, (int)wgs, 0, 0, (int)up(nk, per), per, m_tiles}, t);
             }
     }
