@@ -73,6 +73,13 @@ typedef struct ebrl_i8_gemm_args {
  * more. */
 int64_t ebrl_op_i8_gemm_workspace(const ebrl_i8_gemm_args* args);
 
+/* The kernel that computes a product, for tests and timings that have to know which
+ * one they reach; host arithmetic, no GPU needed.  plan[0] 0: 256 x 256 tiles, 1: LDS
+ * ring, 2: decode; [1], [2] tile rows and columns (decode: rows loaded); [3] ranges
+ * that K is cut into; [4] workgroups; [5] kernel 0: the parts each tile of the last
+ * round is cut into.  Returns EBRL_E_INVALID on bad arguments. */
+int ebrl_op_i8_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t plan[6]);
+
 /* c[m, n] = scale_a[m] scale_b[n] sum_k a[m, k] b[n, k] + bias[n] + residual[m, n].
  * The sum is exact (32-bit integers, which K's bound keeps from overflowing, codes
  * of -128 among them); it is rounded to a float, multiplied by scale_b, then by

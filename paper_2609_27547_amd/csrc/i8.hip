@@ -1101,8 +1101,22 @@ static bool i8_codes_ok(const void* p, int64_t ld, int64_t width) {
     return p && (uintptr_t)p % 16 == 0 && ld >= width && ld % 16 == 0;
 }
 
-template <typename T, int OP> static void i8_quant_op(const I8Quant& w, hipStream_t s) {
+template <typename T, int OP> static void i8_quant_op(I8Quant w, hipStream_t s) {
     const int cols = w.a.cols;
+    // a launch has under 2^32 threads
+    constexpr int MOST = 1 << 21;
+    if (w.a.rows > MOST) {
+        I8Quant part = w;
+        for (int64_t r = 0; r < w.a.rows; r += MOST) {
+            part.a.rows = (int)std::min<int64_t>(MOST, w.a.rows - r);
+            part.a.x = (const T*)w.a.x + r * w.a.ldx;
+            if (OP == EBRL_I8_SWIGLU) part.a.up = (const T*)w.a.up + r * w.a.ldup;
+            part.a.codes = w.a.codes + r * w.a.ldc;
+            part.a.scales = w.a.scales + r;
+            i8_quant_op<T, OP>(part, s);
+        }
+        return;
+    }
     const unsigned rows = w.a.rows;
     auto go = [&](auto kern, unsigned groups, int threads) {
         hipLaunchKernelGGL(kern, dim3(groups), dim3(threads), 0, s, w);
@@ -1150,7 +1164,8 @@ static bool i8_shape_ok(const ebrl_i8_gemm_args* a) {
 enum { I8_BIG, I8_RING, I8_DECODE };
 struct I8Plan {
     int kind, bm, bn;                // tile (decode: rows loaded, columns)
-    int grid, full, cut;             // big: workgroups, evenly dealt tiles, parts of each tile of the last round
+    int grid;                        // workgroups
+    int full, cut;                   // big: evenly dealt tiles, parts of each tile of the last round
     int splits, per_split, m_tiles;  // decode: ranges of K, their K tiles
 };
 
@@ -1202,7 +1217,7 @@ static I8Plan i8_plan(int M, int N, int K) {
         else if (left > 0) t += v.epi / 2 + nk * v.one;
         const double w = (double)N * K * 1e-6 * (0.26 + 0.163 * (up(up(M, v.bm), 4) - 1));
         t = std::max(t, w) + 0.14 * std::min(t, w);
-        consider(I8Plan{I8_RING, v.bm, v.bn, 0, 0, 0, 1, nk, 1}, t);
+        consider(I8Plan{I8_RING, v.bm, v.bn, (int)wgs, 0, 0, 1, nk, 1}, t);
     }
     // Decode: a K tile of the four waves is (bn + xr) * 512 bytes through LDS, at 57 or
     // 69 KB/us a CU by how many are in flight (more where few CUs work); the weights
@@ -1214,7 +1229,7 @@ static I8Plan i8_plan(int M, int N, int K) {
         for (int bn : {16, 32, 48, 64, 96})
             for (int splits : {1, 2, 4, 8, 16}) {
                 const int64_t wgs = up(N, bn) * m_tiles * splits;
-                if (splits > 1 && (wgs > CUS || nk < splits * 8)) continue;
+                if (wgs > I8_MAX_TILES || (splits > 1 && (wgs > CUS || nk < splits * 8))) continue;
                 const int per = (int)up(nk, splits);
                 const double step = (bn + xr) * 0.512 / (i8_decode_stages(xr, bn) == 2 ? 57 : 69) *
                                     (0.83 + 0.17 * std::min(1.0, wgs / 256.0));
@@ -1234,7 +1249,7 @@ template <typename T, int XR, int BN> static void i8_decode_launch(const ebrl_i8
                                                                    const I8Epi<T>& epi, hipStream_t s) {
     constexpr int STAGES = i8_decode_stages(XR, BN);
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((a.N + BN - 1) / BN * p.splits * p.m_tiles), dim3(256), 0, s, a.a, (uint32_t)a.lda,
+        hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)a.N + BN - 1) / BN * p.splits * p.m_tiles)), dim3(256), 0, s, a.a, (uint32_t)a.lda,
                            a.b, (uint32_t)a.ldb, a.M, a.N, a.K, p.per_split, p.splits, p.m_tiles, (int*)a.workspace, epi);
     };
     if constexpr (XR > 32) {
@@ -1281,9 +1296,8 @@ template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, con
         else big(i8_big_kernel<T, false>);
         return;
     }
-    const dim3 grid((unsigned)((((int64_t)a.M + p.bm - 1) / p.bm) * (((int64_t)a.N + p.bn - 1) / p.bn)));
     auto ring = [&](auto kern) {
-        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M, a.N, a.K, epi);
+        hipLaunchKernelGGL(kern, dim3(p.grid), dim3(256), 0, s, a.a, (uint32_t)a.lda, a.b, (uint32_t)a.ldb, a.M, a.N, a.K, epi);
     };
     if (p.bn == 128) ring(i8_ring_kernel<T, 64, 128, 3>);
     else if (p.bm == 64) ring(i8_ring_kernel<T, 64, 64, 3>);
@@ -1320,6 +1334,18 @@ extern "C" {
 int ebrl_op_i8_quant(const ebrl_i8_quant_args* args, void* stream) { return ebrl::i8_quant(args, (hipStream_t)stream); }
 
 int64_t ebrl_op_i8_gemm_workspace(const ebrl_i8_gemm_args* args) { return ebrl::i8_gemm_workspace(args); }
+
+int ebrl_op_i8_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t plan[6]) {
+    ebrl_i8_gemm_args a{};
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    if (!plan || !ebrl::i8_shape_ok(&a) || M == 0 || N == 0) return EBRL_E_INVALID;
+    const ebrl::I8Plan p = ebrl::i8_plan(M, N, K);
+    const int32_t out[6] = {p.kind, p.bm, p.bn, p.splits, p.grid, p.cut};
+    std::copy(out, out + 6, plan);
+    return EBRL_OK;
+}
 
 int ebrl_op_i8_gemm(const ebrl_i8_gemm_args* args, void* stream) { return ebrl::i8_gemm(args, (hipStream_t)stream); }
 

@@ -129,7 +129,7 @@ EXPORTED = [
     "ebrl_op_kv8_write", "ebrl_op_kv8_attn", "ebrl_op_kv8_attn_workspace",
     "ebrl_op_kv8_fork", "ebrl_op_kv8_free", "ebrl_op_kv8_reserve", "ebrl_op_kv8_reserve_workspace",
     "ebrl_op_kv8_compact", "ebrl_op_kv8_compact_workspace",
-    "ebrl_op_i8_quant", "ebrl_op_i8_gemm", "ebrl_op_i8_gemm_workspace",
+    "ebrl_op_i8_quant", "ebrl_op_i8_gemm", "ebrl_op_i8_gemm_workspace", "ebrl_op_i8_gemm_plan",
     "ebrl_alloc_solve", "ebrl_alloc_objective", "ebrl_alloc_monitor_create", "ebrl_alloc_monitor_observe",
     "ebrl_alloc_monitor_destroy", "ebrl_alloc_refine",
     "ebrl_sched_create", "ebrl_sched_destroy", "ebrl_sched_dispatch", "ebrl_sched_complete",
@@ -184,6 +184,7 @@ def lib():
         "ebrl_op_i8_quant": (i32, [vp, vp]),
         "ebrl_op_i8_gemm": (i32, [vp, vp]),
         "ebrl_op_i8_gemm_workspace": (i64, [vp]),
+        "ebrl_op_i8_gemm_plan": (i32, [i32, i32, i32, vp]),
         "ebrl_alloc_solve": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocLimits),
                                    ctypes.POINTER(AllocResult)]),
         "ebrl_alloc_objective": (i32, [ctypes.POINTER(AllocProfiles), ctypes.POINTER(AllocResult)]),
@@ -897,6 +898,17 @@ def op_i8_quant(x, codes, scales, up=None, norm_eps=None, gain=None, stream=None
     a = _i8_pack(_I8_QUANT, dtype, op, rows, cols, eps, x_at, up_at, ldx, ldup, gain_at, at, ldc,
                  _i8_floats("scales", scales, rows, dev, torch.float32))
     _i8_call(lib().ebrl_op_i8_quant, "ebrl_op_i8_quant", a, dev, stream)
+
+
+def i8_gemm_plan(M, N, K) -> dict:
+    """The kernel that computes an M x N x K product of codes (no GPU needed)."""
+    plan = (ctypes.c_int32 * 6)()
+    rc = lib().ebrl_op_i8_gemm_plan(M, N, K, plan)
+    if rc != EBRL_OK:
+        raise EbrlError(rc, "ebrl_op_i8_gemm_plan")
+    out = dict(zip(("kernel", "rows", "cols", "splits", "workgroups", "cut"), plan))
+    out["kernel"] = ("large", "ring", "decode")[out["kernel"]]
+    return out
 
 
 def i8_gemm_workspace(a, b):

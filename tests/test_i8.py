@@ -1,6 +1,8 @@
 """Projections in 8-bit integers (include/ebrl_i8.h) against their formulas: codes and
 scales of rows, products bit for bit; the calls that are refused."""
 import ctypes
+import math
+import random
 
 import numpy as np
 import pytest
@@ -57,6 +59,41 @@ def test_calls_of_nothing_are_ok():
         assert E.lib().ebrl_op_i8_gemm_workspace(ctypes.byref(_gemm_args(**kw))) == 0
     assert E.lib().ebrl_op_i8_gemm_workspace(ctypes.byref(_gemm_args(K=24))) == -1
     assert E.lib().ebrl_op_i8_quant(None, None) == -1 and E.lib().ebrl_op_i8_gemm(None, None) == -1
+
+
+def test_plans_are_refused():
+    plan = (ctypes.c_int32 * 6)()
+    for m, n, k in ((0, 1, 16), (1, 0, 16), (-1, 1, 16), (1, 1, 15), (1, 1, 131072), (1 << 30, 1 << 30, 16)):
+        assert E.lib().ebrl_op_i8_gemm_plan(m, n, k, plan) == -1
+    assert E.lib().ebrl_op_i8_gemm_plan(1, 1, 16, None) == -1
+
+
+@pytest.mark.parametrize("m,n,k,kernel", [
+    # kernels that are 10 % or more ahead of the others
+    (1, 4096, 4096, "decode"), (8, 4096, 11008, "decode"), (37, 22016, 4096, "decode"), (256, 1024, 4096, "decode"),
+    (591, 1024, 4096, "ring"), (800, 1024, 1024, "ring"), (800, 12288, 4096, "large"), (3200, 8192, 1024, "large"),
+    (9216, 12288, 4096, "large")])
+def test_plan_is_the_measured_best(m, n, k, kernel):
+    assert E.i8_gemm_plan(m, n, k)["kernel"] == kernel
+
+
+@pytest.mark.parametrize("m", [1, 7, 64, 300, 512, 513, 5000])
+def test_workgroups_cover_the_output(m):
+    """Every plan's workgroups, and its workspace, for sizes up to the largest."""
+    for n in (1, 63, 1000, 22016, 1 << 20, 1 << 25):
+        for k in (16, 1040, 11008, 131056):
+            if -(-m // 32) * -(-n // 64) > 1 << 23:
+                continue
+            p = E.i8_gemm_plan(m, n, k)
+            tiles = -(-m // p["rows"]) * -(-n // p["cols"])
+            assert 1 <= p["workgroups"] <= 1 << 23
+            if p["kernel"] != "large":
+                assert p["workgroups"] == tiles * p["splits"]
+            else:
+                assert p["workgroups"] == (256 if tiles >= 256 else tiles * p["cut"]) and p["cut"] in (1, 2, 4)
+            a = _gemm_args(M=m, N=n, K=k)
+            need = E.lib().ebrl_op_i8_gemm_workspace(ctypes.byref(a))
+            assert need == (p["splits"] * m * ((n + 3) // 4 * 4) * 4 if p["splits"] > 1 else 0)
 
 
 def test_binding_refuses():
@@ -201,6 +238,55 @@ def test_rows_that_are_not_finite(op, dtype, cols):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [500, 1000, 2000, 4000, 8000, 11008, 16384])
+def test_gates_of_every_size(dtype, cols):
+    """Gates over and past the range in which 32 bits do for most codes, products spread over the codes:
+    up = t / silu(gate) makes them t, but for up's rounding."""
+    g = torch.Generator().manual_seed(cols)
+    for lo, hi in ((-80, 80), (-79.9, -60), (-3, 3), (30, 80), (-100, 100), (-700, 5), (79.5, 80.5)):
+        gate = torch.linspace(lo, hi, 4 * cols).reshape(cols, 4).t().contiguous().to(DT[dtype])
+        silu = gate.double() / (1 + torch.exp(-gate.double()))
+        t = torch.rand((4, cols), generator=g).double() * 2 - 1
+        up = (t / torch.where(silu.abs() < 1e-37, 1.0, silu)).clamp(-3e38, 3e38).to(DT[dtype])
+        codes, scales = E.i8_alloc(4, cols)
+        E.op_i8_quant(gate.cuda(), codes, scales, up=up.cuda())
+        _check_codes(_values(E.I8_SWIGLU, gate, up, None, 0), codes, scales)
+
+
+@gpu
+@pytest.mark.parametrize("op", list(OPS))
+@pytest.mark.parametrize("cols", [512, 1024, 4096, 11008])
+def test_many_rows_of_codes(op, cols):
+    """A million codes each: none next to a border is off."""
+    g = torch.Generator().manual_seed(cols)
+    rows = (1 << 20) // cols
+    x, up = _rows(rows, cols, "bf16", g), _rows(rows, cols, "bf16", g) if op == "gate" else None
+    codes, scales = E.i8_alloc(rows, cols)
+    E.op_i8_quant(x, codes, scales, up=up, norm_eps=1e-6 if op == "norm" else None)
+    _check_codes(_values(OPS[op], x, up, None, 1e-6), codes, scales)
+    # rows whose values are all alike, and one value alone
+    x.fill_(0.75)
+    if up is not None:
+        up.fill_(-3.0)
+    x[1::2, 1:] = 0
+    E.op_i8_quant(x, codes, scales, up=up, norm_eps=1e-6 if op == "norm" else None)
+    _check_codes(_values(OPS[op], x, up, None, 1e-6), codes, scales)
+    assert (codes[0].abs() == 127).all() and codes[1, 0].abs() == 127 and (codes[1, 1:] == 0).all()
+
+
+@gpu
+def test_more_rows_than_a_launch_takes():
+    rows = (1 << 21) + 1000
+    x = torch.zeros((rows, 16), dtype=torch.bfloat16, device="cuda")
+    x[:, 3] = 1 + torch.arange(rows, device="cuda") % 100
+    codes, scales = E.i8_alloc(rows, 16)
+    E.op_i8_quant(x, codes, scales)
+    assert (codes[:, 3] == 127).all() and (codes.int().abs().sum(1) == 127).all()
+    assert torch.equal(scales, (x[:, 3].double() / 127).float())
+
+
+@gpu
 def test_scales_past_the_range():
     """silu(x) up that no float holds: the row counts as not finite."""
     x = torch.full((2, 64), 3e38, device="cuda")
@@ -269,6 +355,63 @@ def test_products_bit_for_bit(m, n, k):
         if resid:   # in place
             E.op_i8_gemm(a, sa, b, sb, res, bias=bias, residual=res, workspace=work)
             assert _same(res, want)
+
+
+def _reaching():
+    """The smallest of many shapes for each kernel and tile that the plan has."""
+    r, found = random.Random(0), {}
+
+    def size(lo, hi):
+        return int(math.exp(r.uniform(math.log(lo), math.log(hi))))
+    for _ in range(20000):
+        m, n, k = size(1, 11000), size(1, 23000), 16 * size(1, 700)
+        p = E.i8_gemm_plan(m, n, k)
+        key = (p["kernel"], p["rows"], p["cols"], p["splits"] > 1, p["cut"], p["workgroups"] == 256,
+               p["kernel"] == "decode" and m > p["rows"])
+        if key not in found or m * n * k < math.prod(found[key]):
+            found[key] = (m, n, k)
+    return found
+
+
+@gpu
+def test_products_of_every_kernel():
+    """Bit for bit, at odd sizes, with a bias and a residual in turn, outputs and floats of any alignment."""
+    g = torch.Generator().manual_seed(1)
+    found = _reaching()
+    assert {k[0] for k in found} == {"large", "ring", "decode"} and len(found) > 40
+    for i, (key, (m, n, k)) in enumerate(sorted(found.items(), key=str)):
+        a, sa = _operand(m, k, g, k + 16 * (i % 3))
+        b, sb = _operand(n, k, g)
+        for dtype, shift in (("fp32", 0), ("bf16", 1)):
+            bias = torch.randn(n + shift, generator=g).cuda()[shift:] if i % 2 == shift else None
+            res = torch.randn((m, n), generator=g).to(DT[dtype]).cuda() if i % 4 < 2 else None
+            sb2 = torch.cat([sb[:shift], sb])[shift:]
+            held = torch.full((m * n + 8,), 3.0, dtype=DT[dtype], device="cuda")
+            out = held[shift:shift + m * n].view(m, n)
+            E.op_i8_gemm(a, sa, b, sb2, out, bias=bias, residual=res)
+            assert _same(out, _expected(a, sa, b, sb2, bias, res, dtype)), f"{key} {m} x {n} x {k} {dtype}"
+            assert (held[:shift] == 3).all() and (held[shift + m * n:] == 3).all()
+
+
+@gpu
+def test_rows_far_apart():
+    """Rows of operands 8 MB apart: offsets in a tile that pass 31 bits."""
+    g = torch.Generator().manual_seed(2)
+    ld, k = (1 << 23) - 16, 256
+    held = torch.zeros(ld * 299 + k, dtype=torch.int8, device="cuda")
+    far = held.as_strided((300, k), (ld, 1))
+    far.copy_(torch.randint(-128, 128, (300, k), generator=g, dtype=torch.int8))
+    for m, n in ((300, 300), (300, 8192), (8, 300), (2048, 300)):
+        a, b = (far if m == 300 else _operand(m, k, g)[0]), (far if n == 300 else _operand(n, k, g)[0])
+        sa, sb = torch.ones(m, device="cuda"), torch.ones(n, device="cuda")
+        out = torch.empty((m, n), device="cuda")
+        E.op_i8_gemm(a, sa, b, sb, out)
+        assert torch.equal(out, _sums(a, b).float())
+    wide = held.as_strided((256, k), (ld, 1))
+    a, sa = _operand(16384, k, g)
+    out = torch.empty((16384, 256), device="cuda")
+    E.op_i8_gemm(a, sa, wide, torch.ones(256, device="cuda"), out)
+    assert torch.equal(out, _expected(a, sa, wide, torch.ones(256, device="cuda"), None, None, "fp32"))
 
 
 @gpu
