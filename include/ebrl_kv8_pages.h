@@ -16,6 +16,9 @@
  * caller that edits the table itself keeps them right too (a page of negative
  * refs counts as free).
  *
+ * Calls on one pool follow one another on a stream, or are ordered by the caller:
+ * each reads what the one before it has written.
+ *
  * All choices are fixed by the arguments: page ids do not depend on timing.
  * Numbers on the device that a call cannot check on the host never lead to an
  * access out of bounds: rows of the table outside [0, table_rows) are left out,

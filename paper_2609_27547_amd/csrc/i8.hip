@@ -1227,16 +1227,16 @@ static I8Plan i8_plan(int M, int N, int K) {
         const int xr = M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : up(M, up(M, 64)) <= 48 ? 48 : 64;
         const int m_tiles = (int)up(M, xr);
         for (int bn : {16, 32, 48, 64, 96})
-            for (int splits : {1, 2, 4, 8, 16}) {
+            for (int want : {1, 2, 4, 8, 16}) {
+                const int per = (int)up(nk, want), splits = (int)up(nk, per);
                 const int64_t wgs = up(N, bn) * m_tiles * splits;
-                if (wgs > I8_MAX_TILES || (splits > 1 && (wgs > CUS || nk < splits * 8))) continue;
-                const int per = (int)up(nk, splits);
+                if (wgs > I8_MAX_TILES || (want > 1 && (wgs > CUS || nk < want * 8))) continue;
                 const double step = (bn + xr) * 0.512 / (i8_decode_stages(xr, bn) == 2 ? 57 : 69) *
                                     (0.83 + 0.17 * std::min(1.0, wgs / 256.0));
                 const double cu = up(wgs, CUS) * (0.96 + up(per, 4) * step), hbm = (double)N * K / 9.83e6;
                 double t = 2.55 + std::max(cu, hbm) + 0.39 * std::min(cu, hbm);
                 if (splits > 1) t += 2.2 + 5.3e-6 * splits * M * N;
-                consider(I8Plan{I8_DECODE, xr, bn, (int)wgs, 0, 0, (int)up(nk, per), per, m_tiles}, t);
+                consider(I8Plan{I8_DECODE, xr, bn, (int)wgs, 0, 0, splits, per, m_tiles}, t);
             }
     }
     return best;
@@ -1249,7 +1249,7 @@ template <typename T, int XR, int BN> static void i8_decode_launch(const ebrl_i8
                                                                    const I8Epi<T>& epi, hipStream_t s) {
     constexpr int STAGES = i8_decode_stages(XR, BN);
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)a.N + BN - 1) / BN * p.splits * p.m_tiles)), dim3(256), 0, s, a.a, (uint32_t)a.lda,
+        hipLaunchKernelGGL(kern, dim3(p.grid), dim3(256), 0, s, a.a, (uint32_t)a.lda,
                            a.b, (uint32_t)a.ldb, a.M, a.N, a.K, p.per_split, p.splits, p.m_tiles, (int*)a.workspace, epi);
     };
     if constexpr (XR > 32) {

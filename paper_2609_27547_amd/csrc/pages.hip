@@ -571,7 +571,7 @@ int64_t ebrl_op_kv8_reserve_workspace(const ebrl_kv8_pool* pool, int32_t n, int3
 int ebrl_op_kv8_reserve(const ebrl_kv8_pool* pool, const int32_t* seq, const int32_t* pos0, const int32_t* count,
                         int32_t n, int32_t max_count, int32_t* lacking, void* workspace, int64_t workspace_bytes,
                         void* stream) {
-    if (!pg_reserve_ok(pool, n, max_count) || !pg_pool_ok(pool) || !lacking) return EBRL_E_INVALID;
+    if (!pg_reserve_ok(pool, n, max_count) || !pg_pool_ok(pool) || !lacking || (uintptr_t)lacking % 4) return EBRL_E_INVALID;
     const int64_t pages = pg_most_pages(pool, max_count);
     const int pieces = pg_pieces(pool);
     const int64_t groups = std::max<int64_t>(1, (int64_t)n * pieces);
@@ -612,7 +612,9 @@ int64_t ebrl_op_kv8_compact_workspace(const ebrl_kv8_pool* pool) {
 
 int ebrl_op_kv8_compact(const ebrl_kv8_pool* pool, int32_t* new_table, int32_t* new_refs, int32_t* used,
                         void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!pg_pool_ok(pool) || !new_table || !new_refs || !used) return EBRL_E_INVALID;
+    if (!pg_pool_ok(pool) || !new_table || !new_refs || !used ||
+        ((uintptr_t)new_table | (uintptr_t)new_refs | (uintptr_t)used) % 4)
+        return EBRL_E_INVALID;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < pg_compact_words(pool) * 4) return EBRL_E_INVALID;
     const hipStream_t s = (hipStream_t)stream;
     const int64_t half = pool->num_blocks / 2 + 1;

@@ -63,11 +63,11 @@ def test_numbers_are_refused():
         assert _free(p, **kw) == -1
     need = E.lib().ebrl_op_kv8_reserve_workspace(ctypes.byref(p), 2, 40)
     assert 0 < need < 1 << 12
-    for kw in (dict(n=-1), dict(n=65537), dict(most=-1), dict(seq=0), dict(pos0=0), dict(count=0), dict(lacking=0),
+    for kw in (dict(n=-1), dict(n=65537), dict(most=-1), dict(seq=0), dict(pos0=0), dict(count=0), dict(lacking=0), dict(lacking=2),
                dict(work=0), dict(work=4104), dict(size=need - 1)):
         assert _reserve(p, **kw) == -1
     need = E.lib().ebrl_op_kv8_compact_workspace(ctypes.byref(p))
-    for kw in (dict(table=0), dict(refs=0), dict(used=0), dict(work=0), dict(work=8), dict(size=need - 1)):
+    for kw in (dict(table=0), dict(refs=0), dict(used=0), dict(table=2), dict(refs=1), dict(used=6), dict(work=0), dict(work=8), dict(size=need - 1)):
         assert _compact(p, **kw) == -1
     many = _pool(table_stride=1 << 20, num_blocks=1 << 20)
     assert E.lib().ebrl_op_kv8_reserve_workspace(ctypes.byref(many), 65536, 1 << 30) == -1
