@@ -1,5 +1,6 @@
 // Projections in 8-bit integers (include/ebrl_i8.h): rows to codes, and the
-// product of two operands of codes.
+// product of two operands of codes.  Three kernels multiply, by the shape (i8_plan):
+// 256 x 256 tiles, LDS rings of smaller ones, and slices of the weights for few rows.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -23,6 +24,10 @@ constexpr int64_t I8_MAX_TILES = 1 << 23;
 // s is nearer to a border than its error, and one such code moves a product by
 // about 1e-4 of its size.  With 32-bit y that is one code in 1e5, with 64-bit ones
 // none.  The vector units do 64-bit adds and products at the rate of 32-bit ones.
+//
+// Bound by memory from some thousand rows on: fp32 rows of 4096, normed, 37 to 40 us
+// for 9216 (4.7 to 5.1 TB/s of a copy's 4.8), bf16 ones as they are 26 (4.3); a row
+// alone 3.2 us, a launch and two memory latencies.
 
 // silu(g) u.  exp(-g) = 2^n 2^f, |f| <= 1/2, 2^f by its Taylor series: the first
 // term left out is 2e-16.  The exponent is held to +-690, where silu is g or below
@@ -139,13 +144,20 @@ EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(
 
 // Rows of at most 512 CHUNKS columns a wave, held in registers from one read to the
 // codes: a thread has eight neighbours in each of CHUNKS places.  One wave: four rows a
-// workgroup, else a workgroup a row.
+// workgroup, else a workgroup a row.  Rows of 1025 to 2048 columns on four waves with
+// one place (591 rows of 1283: 3.8 us; three with two 4.8); the count of waves is a
+// constant, because a loop over it waits for each wave's word in turn (a row of 4096 3.2
+// us against 3.6) and sixteen doubles at once take the registers of a wave in four.
 //
 // Plain and normed rows are 64-bit throughout.  Gated rows, whose 64-bit exponentials
 // would take twice the time of reading them, have 32-bit values, maximum and codes; what
 // lies nearer to a border than these are exact (EB, twice their error) is computed once
 // more in 64 bits, one code in 1e4, and so is a whole row where 32 bits do not do
-// (near the ends of their range, or not finite).
+// (near the ends of their range, or not finite).  9216 rows of 11008 (bf16): 127 us, 4.0
+// TB/s, 195 with 64 bits throughout.  Two workgroups of twelve waves share a CU, whose
+// vector units are half busy: the rest is the wait for a row and the two exchanges.
+// Eight waves with three places 149 (159 held to three workgroups a CU), six with four
+// 186; persistent workgroups with the next row in flight 152.
 template <typename T, int OP, int WAVES, int CHUNKS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel(I8Quant w)
 {
@@ -451,6 +463,24 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 // read them.  Workgroups are persistent; the next tile's first DMAs go out before
 // the epilogue, whose stores drain behind them.  `full` tiles are dealt evenly, those
 // of the last round cut in `split`.
+//  * What bounds it: power.  8192 x 8192 x 8192 takes 364 us, 3.02 POPS (the library's
+//    product of that size 522 to 540, 2.04 to 2.11); 9216 x 12288 x 4096 345 (420 to 431).
+//    The matrix units are busy 70 % of the cycles, at a clock that the card holds at 1.85
+//    GHz; a K tile takes 1.3 us with one on every CU, of which 1.1 are products.
+//  * The epilogue loads nothing that the compiler waits for, since its waits count the
+//    DMAs too, which it does not see: scales and bias come through LDS, the residual is
+//    asked for three row groups ahead, the next tile's DMAs go out behind its last
+//    loads (9216 x 12288 x 4096 380 -> 361 us, 5476 x 8192 x 1024 62 -> 53).  Scaled
+//    results are staged, bf16 ones as such: half the LDS traffic, 16 bytes a store.
+//  * What a tile derives from the lane is made anew each time: kept in registers it was
+//    spilled, and each reload waited for every DMA (35 spilled registers, 374 us at 8192^3;
+//    none, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x 1024 51 -> 48,
+//    nothing at long K).
+//  * With a residual the tiles of a round meet in memory at the end: 9216 x 4096 x 11008,
+//    fp32, 345 us, of which 302 MB of residual and results are 63.  Half the XCDs
+//    taking their part of the last round first, so that the rounds do not end together:
+//    425 us (the code of the parts twice in the loop, and spills); starts 1 to 20 us
+//    apart: no change.
 template <typename T, bool RES>
 __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict__ A, uint32_t lda,
                                                         const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
@@ -608,7 +638,9 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             wait_lds();
             wg_barrier();
             if constexpr (L == 0) { cut(fb0); cut(fb1); }
+            __builtin_amdgcn_s_setprio(1);
             mma(acc[0][0], fb0); mma(acc[0][1], fb1);
+            __builtin_amdgcn_s_setprio(0);
             wg_barrier();
             readA(st, 1);
             if constexpr (L >= 2) {
@@ -617,7 +649,9 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             } else if constexpr (L == 1) wait_vmcnt<NA>();
             wait_lds();
             wg_barrier();
+            __builtin_amdgcn_s_setprio(1);
             mma(acc[1][0], fb0); mma(acc[1][1], fb1);
+            __builtin_amdgcn_s_setprio(0);
             wg_barrier();
         };
         prologue();
@@ -800,7 +834,10 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
 
 // Small outputs (fewer 256 x 256 tiles than CUs): BM x BN tiles on four waves
 // (2 x 2), a ring of ST K tiles in LDS with ST - 1 of them in flight, one barrier a
-// K tile.
+// K tile; scales and residual ahead of the first operands.  Bound by what a CU draws
+// through LDS, 70 to 90 GB/s: a K tile takes 0.2 (32 x 64), 0.3 (64 x 64) and 0.42 us (64
+// x 128) with one workgroup on a CU, 0.3, 0.39 and 0.7 with two.  800 x 1024 x 4096 12.9
+// us, 591 x 1003 x 1296 8.0.
 template <typename T, int BM, int BN, int ST>
 __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restrict__ A, uint32_t lda,
                                                          const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
@@ -929,6 +966,14 @@ __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restric
 // half of the fragment then repeats the lower one and is not stored).  The waves'
 // tiles are summed through LDS.  With several ranges of K (splits) the sums go to the
 // workspace and i8_join_kernel adds them up.  NT: each weight is read by one workgroup.
+//
+// Bound by memory where the slices fill the chip in one round (1 x 12288 x 4096 9.9 us,
+// 5.1 TB/s with launch and tail; 8 x 4096 x 11008 9.4, 4.8), by what a CU draws through
+// LDS, 57 to 70 GB/s, where activations are half of it and more (64 x 12288 x 4096 14 to 15).
+// Slices of 16, 48 or 96 columns are those that make one round of 256 workgroups of 4096,
+// 12288 and 22016 outputs: 37 x 22016 x 4096 19.8 us with 96, 22.2 with 48, 25 with 64; 17 x
+// 4096 x 4096 6.2 with 16, 7.8 with 32.  Eight waves instead of four: never faster (1 x
+// 12288 x 4096 13.0, 10.9 and 11.3 us with slices of 16, 48 and 64 against 9.8, 9.9 and 10.2).
 template <typename T, int XR, int BN, int STAGES, bool NT>
 __global__ __launch_bounds__(256) void i8_decode_kernel(const int8_t* __restrict__ A, uint32_t lda,
                                                                const int8_t* __restrict__ B, uint32_t ldb, int M, int N,
