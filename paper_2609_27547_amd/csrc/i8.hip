@@ -56,9 +56,12 @@ EBRL_DEV double i8_gate(float g32, float u32) {
     return g * r * (double)u32;
 }
 // The same in 32 bits, for |g| <= 80, off by less than 2^-17 of its size: the
-// exponent by 2^-18 and the constant's 2^-20, the others by a few ulps.
+// exponent by 2^-18 and the constant's 2^-20, the others by a few ulps.  The gate
+// comes last: what is below the normal floats before it, off by 2^-149, stays below
+// any code of rows that this is used for; silu(g) of a denormal g would lose bits
+// that a large u brings up again.
 EBRL_DEV float i8_gate_fast(float g, float u) {
-    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;
+    return g * (__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u);
 }
 // y / s to the nearest whole number, ties to even.  The product with 1 / s is
 // corrected by its remainder, which makes a quotient that is a half exactly that;

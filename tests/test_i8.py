@@ -255,6 +255,20 @@ def test_gates_of_every_size(dtype, cols):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [500, 4000, 11008, 20000])
+def test_gates_below_the_normal_floats(dtype, cols):
+    """Denormal gates of few bits, whose halves no float holds, against factors near the largest float."""
+    g = torch.Generator().manual_seed(cols)
+    least = 2.0 ** (-149 if dtype == "fp32" else -133)
+    gate = (torch.randint(-100, 101, (4, cols), generator=g).double() * least).to(DT[dtype])
+    up = ((torch.rand((4, cols), generator=g) + 0.5) * 2.0 ** 127).to(DT[dtype])
+    codes, scales = E.i8_alloc(4, cols)
+    E.op_i8_quant(gate.cuda(), codes, scales, up=up.cuda())
+    _check_codes(_values(E.I8_SWIGLU, gate, up, None, 0), codes, scales)
+
+
+@gpu
 @pytest.mark.parametrize("op", list(OPS))
 @pytest.mark.parametrize("cols", [512, 1024, 4096, 11008])
 def test_many_rows_of_codes(op, cols):
