@@ -14,6 +14,18 @@ namespace ebrl {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+// Vectors that lie in memory at the alignment of an element: global loads and stores
+// take any, and a row segment stays one instruction.  9216 rows of 4095 columns, fp32, normed
+// 48 us (4096: 49; by elements 76); bf16, gated 67 (44; 102).
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef __bf16 bf16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> EBRL_DEV void st4_any(T* p, f32x4 v) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any*>(p) = v;
+    else *reinterpret_cast<bf16x4_any*>(p) = bf16x4_any{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+}
+
 constexpr int I8_MAX_COLS = 1 << 20;
 constexpr int I8_MAX_K = 131056;            // 2^14 K < 2^31, K a multiple of 16
 constexpr int64_t I8_MAX_LD = 1 << 23;      // a tile's byte offsets are 32-bit numbers
@@ -97,14 +109,14 @@ EBRL_DEV double i8_wave_sum(double v) {
 }
 
 // Eight neighbours of a row; those from `left` on are zeros.
-template <typename T> EBRL_DEV void i8_load8(const T* p, int left, bool aligned, float (&v)[8]) {
-    if (aligned && left >= 8) {
+template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]) {
+    if (left >= 8) {
         if constexpr (sizeof(T) == 4) {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+            const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
         } else {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+            const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 v[2 * e] = __uint_as_float(w[e] << 16);
@@ -124,12 +136,6 @@ EBRL_DEV void i8_store8(int8_t* p, const double (&y)[8], int left, int fill, dou
         if (e < left && !bad) w[e >> 2] |= (uint32_t)(i8_code(y[e], s, inv) & 255) << (e & 3) * 8;
     if (fill > 0) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
-
-// What a launch needs, beside the call's arguments.
-struct I8Quant {
-    ebrl_i8_quant_args a;
-    bool aligned, gain_aligned;
-};
 
 // The largest value, and the sum, over a row's waves; `red`: a word for each.
 template <int WAVES, typename V> EBRL_DEV V i8_over_waves(V v, V* red, bool sum) {
@@ -162,7 +168,7 @@ EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(
 // Eight waves with three places 149 (159 held to three workgroups a CU), six with four
 // 186; persistent workgroups with the next row in flight 152.
 template <typename T, int OP, int WAVES, int CHUNKS>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel(I8Quant w)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel(ebrl_i8_quant_args a)
 {
     constexpr bool ONE = WAVES == 1;
     constexpr int threads = 64 * WAVES;
@@ -170,7 +176,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
     constexpr float EB = 0x1p-16f;
     __shared__ double red_sum[WAVES];
     __shared__ float red_max[WAVES];
-    const ebrl_i8_quant_args& a = w.a;
     const int tid = ONE ? threadIdx.x & 63 : threadIdx.x;
     const int row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (row >= a.rows) return;
@@ -182,10 +187,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int j = (c * threads + tid) * 8;
-        i8_load8<T>(x + j, a.cols - j, w.aligned, z[c]);
-        if constexpr (GATE) i8_load8<T>(up + j, a.cols - j, w.aligned, u[c]);
+        i8_load8<T>(x + j, a.cols - j, z[c]);
+        if constexpr (GATE) i8_load8<T>(up + j, a.cols - j, u[c]);
         if constexpr (OP == EBRL_I8_RMSNORM)
-            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, w.gain_aligned, u[c]);
+            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, u[c]);
     }
     if constexpr (!GATE) {
         double factor = 1.0;
@@ -302,11 +307,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
 
 // Longer rows: read once more for each step.
 template <typename T, int OP>
-__global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
+__global__ __launch_bounds__(1024) void i8_quant_long_kernel(ebrl_i8_quant_args a)
 {
     __shared__ double red_sum[16];
     __shared__ float red_max[16];
-    const ebrl_i8_quant_args& a = w.a;
     const int tid = threadIdx.x, row = blockIdx.x;
     const T* const x = (const T*)a.x + (size_t)row * a.ldx;
     double factor = 1.0;
@@ -314,7 +318,7 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
         double ss = 0.0;
         for (int j = tid * 8; j < a.cols; j += 8192) {
             float v[8];
-            i8_load8<T>(x + j, a.cols - j, w.aligned, v);
+            i8_load8<T>(x + j, a.cols - j, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fma((double)v[e], (double)v[e], ss);
         }
@@ -323,11 +327,11 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(I8Quant w)
     }
     auto values = [&](int j, double (&y)[8]) {
         float v[8], u[8];
-        i8_load8<T>(x + j, a.cols - j, w.aligned, v);
+        i8_load8<T>(x + j, a.cols - j, v);
         if constexpr (OP == EBRL_I8_SWIGLU)
-            i8_load8<T>((const T*)a.up + (size_t)row * a.ldup + j, a.cols - j, w.aligned, u);
+            i8_load8<T>((const T*)a.up + (size_t)row * a.ldup + j, a.cols - j, u);
         if constexpr (OP == EBRL_I8_RMSNORM)
-            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, w.gain_aligned, u);
+            if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if constexpr (OP == EBRL_I8_SWIGLU) y[e] = i8_gate(v[e], u[e]);
@@ -376,15 +380,13 @@ template <typename T> struct I8Epi {
     const T* residual;
     T* c;
     int64_t ldr, ldc;
-    bool wide;              // rows of c and residual are 16-byte aligned, and N a multiple of four
-    bool wide_cols;         // scale_b and bias are 16-byte aligned
 
     struct Cols { f32x4 s, b; };
     EBRL_DEV Cols cols(int n, int N) const {
         Cols k;
-        if (wide_cols && n + 4 <= N) {
-            k.s = *reinterpret_cast<const f32x4*>(scale_b + n);
-            k.b = bias ? *reinterpret_cast<const f32x4*>(bias + n) : f32x4{0.f, 0.f, 0.f, 0.f};
+        if (n + 4 <= N) {
+            k.s = *reinterpret_cast<const f32x4_any*>(scale_b + n);
+            k.b = bias ? *reinterpret_cast<const f32x4_any*>(bias + n) : f32x4{0.f, 0.f, 0.f, 0.f};
             return k;
         }
 #pragma unroll
@@ -408,9 +410,15 @@ template <typename T> struct I8Epi {
     }
     // Four neighbours of the residual, as they lie in memory, and as floats.
     typedef typename std::conditional<sizeof(T) == 4, f32x4, uint2>::type Four;
-    EBRL_DEV Four load_residual(int m, int n) const {
-        return *reinterpret_cast<const Four*>(residual + (size_t)m * ldr + n);
+    static EBRL_DEV Four load4(const T* p) {
+        if constexpr (sizeof(T) == 4) {
+            return *reinterpret_cast<const f32x4_any*>(p);
+        } else {
+            const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
+            return make_uint2(w[0], w[1]);
+        }
     }
+    EBRL_DEV Four load_residual(int m, int n) const { return load4(residual + (size_t)m * ldr + n); }
     static EBRL_DEV f32x4 floats(f32x4 v) { return v; }
     static EBRL_DEV f32x4 floats(uint2 v) {
         return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
@@ -419,9 +427,9 @@ template <typename T> struct I8Epi {
     // Up to four outputs, those that are inside: v but for the residual.
     EBRL_DEV void store_some(int m, int n, int M, int N, f32x4 v) const {
         if (m >= M || n >= N) return;
-        if (wide) {
+        if (n + 4 <= N) {
             if (residual) v += floats(load_residual(m, n));
-            st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
+            st4_any<T>(c + (size_t)m * ldc + n, v);
             return;
         }
 #pragma unroll
@@ -443,16 +451,30 @@ template <typename T> struct I8Epi {
         if (m < M && n < N) {
             x.k = cols(n, N);
             x.sa = scale_a[m];
-            if (residual && wide) x.r = load_residual(m, n);
+            if (residual && n + 4 <= N) {
+                x.r = load_residual(m, n);
+            } else if (residual) {
+                const T* p = residual + (size_t)m * ldr + n;
+                T some[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) some[e] = n + e < N ? p[e] : T{};
+                x.r = __builtin_bit_cast(Four, some);
+            }
         }
         return x;
     }
     EBRL_DEV void store(int m, int n, int M, int N, i32x4 sum, const Ahead& x) const {
-        if (!wide) { store(m, n, M, N, sum, x.k, x.sa); return; }
         if (m >= M || n >= N) return;
         f32x4 v = value(sum, x.k, x.sa);
         if (residual) v += floats(x.r);
-        st4<T>(c + (size_t)m * ldc + n, v[0], v[1], v[2], v[3]);
+        T* p = c + (size_t)m * ldc + n;
+        if (n + 4 <= N) {
+            st4_any<T>(p, v);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (n + e < N) st_elem<T>(p + e, v[e]);
     }
 };
 
@@ -475,9 +497,12 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 //    asked for three row groups ahead, the next tile's DMAs go out behind its last
 //    loads (9216 x 12288 x 4096 380 -> 361 us, 5476 x 8192 x 1024 62 -> 53).  Scaled
 //    results are staged, bf16 ones as such: half the LDS traffic, 16 bytes a store.
+//    Tiles at the edges do the same with what is there, four columns at a time (9216 x
+//    4095 x 4096, fp32 with a residual, 179 us; 224 by elements, one load after the other;
+//    4096 columns 176).
 //  * What a tile derives from the lane is made anew each time: kept in registers it was
 //    spilled, and each reload waited for every DMA (35 spilled registers, 374 us at 8192^3;
-//    none, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x 1024 51 -> 48,
+//    none in the K loop, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x 1024 51 -> 48,
 //    nothing at long K).
 //  * With a residual the tiles of a round meet in memory at the end: 9216 x 4096 x 11008,
 //    fp32, 345 us, of which 302 MB of residual and results are 63.  Half the XCDs
@@ -522,7 +547,7 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
         // The epilogue's 16-row groups, the group before which the next tile's first
         // loads go out (RES: when the residual's are all on their way), and the stores
         // of an interior tile behind those, which may still be in flight with them.
-        constexpr int GROUPS = 2 * FA, AT = RES ? 5 : 0;
+        constexpr int GROUPS = 2 * FA, AT = RES ? GROUPS - 3 : 0;
         constexpr int HALF = sizeof(T) == 2 && !RES;     // staged as results, not as floats
         constexpr int PASSES = FB * (HALF ? 1 : 2);
         constexpr int EST = (GROUPS - AT) * PASSES;
@@ -689,7 +714,7 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             if (t + 1 < nk) { ktile(t, false, false, std::integral_constant<int, 1>{}); ++t; }
             ktile(t, false, false, std::integral_constant<int, 0>{});
             if (wr == 0) wg_barrier();   // both groups are done with the stages
-            const bool inside = epi.wide && m0 + 4 * HA <= M && n0 + 8 * HB <= N;
+            const bool inside = m0 + 4 * HA <= M && n0 + 8 * HB <= N;
             const int lane = fresh_lane(), r = lane & 15, g = lane >> 4;
             float sa[GROUPS];
             f32x4 sb[2 * FB], bias[2 * FB];
@@ -725,6 +750,59 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
             };
             constexpr int LPR = 2 * HB / 4, RPP = 64 / LPR;   // lanes a row of floats, rows a pass
             const int lr = lane / LPR, lc = lane % LPR;
+            // Edges: rows and columns that are there; a lane whose four columns end past
+            // the last one takes the last four (those that its neighbour has too are the
+            // same, and loaded before either stores).
+            auto rows = [&](auto EDGE) {
+                constexpr bool edge = decltype(EDGE)::value;
+                constexpr int DEPTH = edge ? 1 : 3;              // row groups of the residual in flight
+                typename I8Epi<T>::Four ahead[4][16 / RPP];
+                const int col = edge ? min(lc * 4, N - 4 - nw) : lc * 4;
+                const int there = !edge ? 16 * GROUPS : nw + lc * 4 < N ? M - mw - lr : 0;
+                T* to = epi.c + (size_t)(mw + lr) * epi.ldc + nw + col;
+                const T* from = RES ? epi.residual + (size_t)(mw + lr) * epi.ldr + nw + col : nullptr;
+                const int64_t step = RPP * epi.ldc, step_r = RPP * epi.ldr;
+                auto fetch = [&](int k) {
+#pragma unroll
+                    for (int p = 0; p < 16 / RPP; ++p) {
+                        if (!edge || k * 16 + p * RPP < there)
+                            ahead[k & 3][p] = I8Epi<T>::load4(from);
+                        from += step_r;
+                        asm volatile("" : "+v"(from));   // the next rows' addresses are not kept
+                    }
+                };
+                if constexpr (RES) {
+#pragma unroll
+                    for (int k = 0; k < DEPTH && k < GROUPS; ++k) fetch(k);
+                }
+#pragma unroll
+                for (int k = 0; k < GROUPS; ++k) {
+                    if (k == (RES ? GROUPS - DEPTH : 0) && more) prologue();
+                    put(k);
+                    if constexpr (RES) { if (k + DEPTH < GROUPS) fetch(k + DEPTH); }
+#pragma unroll
+                    for (int p = 0; p < 16 / RPP; ++p) {
+                        const int row = p * RPP + lr;
+                        f32x4 v;
+                        if constexpr (edge) {
+                            int at = col;
+                            asm volatile("" : "+v"(at));         // nor those in LDS
+#pragma unroll
+                            for (int e = 0; e < 4; ++e, ++at)
+                                v[e] = *reinterpret_cast<const float*>(stage + row * 256 + (((at >> 2) ^ swz(row)) << 4) +
+                                                                       (at & 3) * 4);
+                        } else {
+                            v = get(row, lc);
+                        }
+                        if (!edge || k * 16 + p * RPP < there) {
+                            if constexpr (RES) v += I8Epi<T>::floats(ahead[k & 3][p]);
+                            st4_any<T>(to, v);
+                        }
+                        to += step;
+                        asm volatile("" : "+v"(to));
+                    }
+                }
+            };
             if (inside && HALF) {
                 // results of 2 bytes: eight neighbours a lane
                 constexpr int L8 = 2 * HB / 8, R8 = 64 / L8;
@@ -743,43 +821,15 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
                     for (int p = 0; p < 16 / R8; ++p) {
                         const int row = p * R8 + lane / L8;
                         const u32x4 v = *reinterpret_cast<const u32x4*>(stage + row * 128 + (((lane % L8) ^ (row & 7)) << 4));
-                        *reinterpret_cast<u32x4*>(to) = v;
+                        *reinterpret_cast<u32x4_any*>(to) = v;
                         to += step;
                         asm volatile("" : "+v"(to));     // the next rows' addresses are not kept
                     }
                 }
             } else if (inside) {
-                typename I8Epi<T>::Four ahead[4][16 / RPP];
-                T* to = epi.c + (size_t)(mw + lr) * epi.ldc + nw + lc * 4;
-                const T* from = RES ? epi.residual + (size_t)(mw + lr) * epi.ldr + nw + lc * 4 : nullptr;
-                const int64_t step = RPP * epi.ldc, step_r = RPP * epi.ldr;
-                auto fetch = [&](int k) {
-#pragma unroll
-                    for (int p = 0; p < 16 / RPP; ++p) {
-                        ahead[k & 3][p] = *reinterpret_cast<const typename I8Epi<T>::Four*>(from);
-                        from += step_r;
-                        asm volatile("" : "+v"(from));   // the next rows' addresses are not kept
-                    }
-                };
-                if constexpr (RES) {
-#pragma unroll
-                    for (int k = 0; k < 3 && k < GROUPS; ++k) fetch(k);
-                }
-#pragma unroll
-                for (int k = 0; k < GROUPS; ++k) {
-                    if (k == AT && more) prologue();
-                    put(k);
-                    if constexpr (RES) { if (k + 3 < GROUPS) fetch(k + 3); }
-#pragma unroll
-                    for (int p = 0; p < 16 / RPP; ++p) {
-                        const int row = p * RPP + lr;
-                        f32x4 v = get(row, lc);
-                        if constexpr (RES) v += I8Epi<T>::floats(ahead[k & 3][p]);
-                        st4<T>(to, v[0], v[1], v[2], v[3]);
-                        to += step;
-                        asm volatile("" : "+v"(to));
-                    }
-                }
+                rows(std::integral_constant<bool, false>{});
+            } else if (N - nw >= 4) {
+                rows(std::integral_constant<bool, true>{});
             } else {
                 if (more) prologue();
 #pragma unroll
@@ -1149,25 +1199,25 @@ static bool i8_codes_ok(const void* p, int64_t ld, int64_t width) {
     return p && (uintptr_t)p % 16 == 0 && ld >= width && ld % 16 == 0;
 }
 
-template <typename T, int OP> static void i8_quant_op(I8Quant w, hipStream_t s) {
-    const int cols = w.a.cols;
+template <typename T, int OP> static void i8_quant_op(const ebrl_i8_quant_args& a, hipStream_t s) {
+    const int cols = a.cols;
     // a launch has under 2^32 threads
     constexpr int MOST = 1 << 21;
-    if (w.a.rows > MOST) {
-        I8Quant part = w;
-        for (int64_t r = 0; r < w.a.rows; r += MOST) {
-            part.a.rows = (int)std::min<int64_t>(MOST, w.a.rows - r);
-            part.a.x = (const T*)w.a.x + r * w.a.ldx;
-            if (OP == EBRL_I8_SWIGLU) part.a.up = (const T*)w.a.up + r * w.a.ldup;
-            part.a.codes = w.a.codes + r * w.a.ldc;
-            part.a.scales = w.a.scales + r;
+    if (a.rows > MOST) {
+        ebrl_i8_quant_args part = a;
+        for (int64_t r = 0; r < a.rows; r += MOST) {
+            part.rows = (int)std::min<int64_t>(MOST, a.rows - r);
+            part.x = (const T*)a.x + r * a.ldx;
+            if (OP == EBRL_I8_SWIGLU) part.up = (const T*)a.up + r * a.ldup;
+            part.codes = a.codes + r * a.ldc;
+            part.scales = a.scales + r;
             i8_quant_op<T, OP>(part, s);
         }
         return;
     }
-    const unsigned rows = w.a.rows;
+    const unsigned rows = a.rows;
     auto go = [&](auto kern, unsigned groups, int threads) {
-        hipLaunchKernelGGL(kern, dim3(groups), dim3(threads), 0, s, w);
+        hipLaunchKernelGGL(kern, dim3(groups), dim3(threads), 0, s, a);
     };
     if (cols <= 512) go(i8_quant_kernel<T, OP, 1, 1>, (rows + 3) / 4, 256);
     else if (cols <= 1024) go(i8_quant_kernel<T, OP, 1, 2>, (rows + 3) / 4, 256);
@@ -1179,11 +1229,9 @@ template <typename T, int OP> static void i8_quant_op(I8Quant w, hipStream_t s) 
     else go(i8_quant_long_kernel<T, OP>, rows, 1024);
 }
 template <typename T> static void i8_quant_launch(const ebrl_i8_quant_args& a, hipStream_t s) {
-    auto aligned = [](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
-    const I8Quant w{a, aligned(a.x, a.ldx) && (a.op != EBRL_I8_SWIGLU || aligned(a.up, a.ldup)), (uintptr_t)a.gain % 16 == 0};
-    if (a.op == EBRL_I8_ROWS) i8_quant_op<T, EBRL_I8_ROWS>(w, s);
-    else if (a.op == EBRL_I8_RMSNORM) i8_quant_op<T, EBRL_I8_RMSNORM>(w, s);
-    else i8_quant_op<T, EBRL_I8_SWIGLU>(w, s);
+    if (a.op == EBRL_I8_ROWS) i8_quant_op<T, EBRL_I8_ROWS>(a, s);
+    else if (a.op == EBRL_I8_RMSNORM) i8_quant_op<T, EBRL_I8_RMSNORM>(a, s);
+    else i8_quant_op<T, EBRL_I8_SWIGLU>(a, s);
 }
 
 static int i8_quant(const ebrl_i8_quant_args* args, hipStream_t s) {
@@ -1317,11 +1365,7 @@ template <typename T, int XR> static void i8_decode_slices(const ebrl_i8_gemm_ar
 }
 
 template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, const I8Plan& p, hipStream_t s) {
-    const int esz = sizeof(T);
-    auto wide = [&](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0; };
-    const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc,
-                       a.N % 4 == 0 && wide(a.c, a.ldc) && (!a.residual || wide(a.residual, a.ldr)),
-                       ((uintptr_t)a.scale_b | (uintptr_t)a.bias) % 16 == 0};
+    const I8Epi<T> epi{a.scale_a, a.scale_b, a.bias, (const T*)a.residual, (T*)a.c, a.ldr, a.ldc};
     if (p.kind == I8_DECODE) {
         switch (p.bm) {
         case 8: i8_decode_slices<T, 8>(a, p, epi, s); break;

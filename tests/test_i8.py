@@ -408,6 +408,33 @@ def test_products_of_every_kernel():
 
 
 @gpu
+@pytest.mark.parametrize("m,k", [(2085, 512), (591, 1296), (1100, 2064), (4200, 272)])
+@pytest.mark.parametrize("n", [4093, 4094, 4095, 4097, 4098, 4099, 4031, 4036, 4161])
+def test_edges_of_large_products(m, n, k):
+    """Last rows and columns of large tiles: one to three columns behind whole fours, of a wave, of a tile; bit for
+    bit, the residual in place, rows of c at any element."""
+    assert E.i8_gemm_plan(m, n, k)["kernel"] == "large"
+    g = torch.Generator().manual_seed(n + m)
+    (a, sa), (b, sb) = _operand(m, k, g), _operand(n, k, g)
+    for dtype, resid, shift in (("fp32", True, 1), ("bf16", True, 3), ("fp32", False, 0), ("bf16", False, 1)):
+        bias = torch.randn(n, generator=g).cuda() if shift else None
+        ld = n + 2 * shift + 1
+        held = torch.full((shift + m * ld,), 5.0, dtype=DT[dtype], device="cuda")
+        out = held.as_strided((m, n), (ld, 1), shift)
+        res = torch.randn((m, n), generator=g).to(DT[dtype]).cuda() if resid else None
+        want = _expected(a, sa, b, sb, bias, res, dtype)
+        if resid:
+            out.copy_(res)
+        E.op_i8_gemm(a, sa, b, sb, out, bias=bias, residual=out if resid else None)
+        assert _same(out, want), f"{dtype} {resid}"
+        assert (held[:shift] == 5).all() and (held[shift:].view(m, ld)[:, n:] == 5).all()
+        if resid:   # of another stride
+            other = torch.empty((m, n), dtype=DT[dtype], device="cuda")
+            E.op_i8_gemm(a, sa, b, sb, other, bias=bias, residual=res)
+            assert _same(other, want)
+
+
+@gpu
 def test_rows_far_apart():
     """Rows of operands 8 MB apart: offsets in a tile that pass 31 bits."""
     g = torch.Generator().manual_seed(2)
