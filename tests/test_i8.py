@@ -71,7 +71,7 @@ def test_plans_are_refused():
 @pytest.mark.parametrize("m,n,k,kernel", [
     # kernels that are 10 % or more ahead of the others
     (1, 4096, 4096, "decode"), (8, 4096, 11008, "decode"), (37, 22016, 4096, "decode"), (256, 1024, 4096, "decode"),
-    (591, 1024, 4096, "ring"), (800, 1024, 1024, "ring"), (800, 12288, 4096, "large"), (3200, 8192, 1024, "large"),
+    (781, 33, 11056, "decode"), (4094, 21, 8624, "decode"), (591, 1024, 4096, "ring"), (800, 1024, 1024, "ring"), (800, 12288, 4096, "large"), (3200, 8192, 1024, "large"),
     (9216, 12288, 4096, "large")])
 def test_plan_is_the_measured_best(m, n, k, kernel):
     assert E.i8_gemm_plan(m, n, k)["kernel"] == kernel
@@ -344,6 +344,7 @@ SHAPES = [(1, 1, 16), (1, 16, 64), (1, 4096, 4096), (2, 33, 48), (3, 1000, 128),
           (48, 512, 131056), (64, 64, 64), (65, 2048, 2048), (100, 1003, 1296), (128, 128, 128), (129, 4096, 4096),
           (200, 300, 400), (255, 1024, 4096), (256, 1024, 11008), (257, 513, 192), (300, 12288, 4096), (424, 1024, 4096),
           (591, 1003, 1296), (800, 1000, 2064), (1024, 2048, 1024), (2048, 8192, 272), (2304, 1024, 4096),
+          (781, 33, 11056), (1650, 16, 3328), (2151, 55, 10784), (8446, 26, 9024),
           (3200, 8192, 1024), (4097, 4100, 1040), (5476, 1024, 4096), (9216, 64, 80), (40000, 16, 128)]
 
 
