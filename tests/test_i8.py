@@ -436,6 +436,24 @@ def test_edges_of_large_products(m, n, k):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,m,n,ld", [("fp32", 8300, 4100, 4128), ("bf16", 16500, 4099, 4160), ("bf16", 16640, 4352, 4352)])
+def test_results_past_the_cache(dtype, m, n, ld):
+    """128 MB and more in whole cache lines, with tiles at the edges; then read by the next call."""
+    g = torch.Generator().manual_seed(n)
+    (a, sa), (b, sb) = _operand(m, 272, g), _operand(n, 272, g)
+    held = torch.full((m, ld), 5.0, dtype=DT[dtype], device="cuda")
+    want = _expected(a, sa, b, sb, None, None, dtype)
+    E.op_i8_gemm(a, sa, b, sb, held[:, :n])
+    assert _same(held[:, :n], want) and (held[:, n:] == 5).all()
+    codes, scales = E.i8_alloc(m, n)
+    E.op_i8_gemm(a, sa, b, sb, held[:, :n], bias=sb)
+    E.op_i8_quant(held[:, :n], codes, scales)
+    y = _expected(a, sa, b, sb, sb, None, dtype).double()
+    assert torch.equal(scales, (y.abs().amax(1) / 127).float().clamp_min(LEAST))
+    assert torch.equal(codes[:, :n].double(), torch.round(y / scales.double()[:, None]))
+
+
+@gpu
 def test_rows_far_apart():
     """Rows of operands 8 MB apart: offsets in a tile that pass 31 bits."""
     g = torch.Generator().manual_seed(2)
