@@ -75,13 +75,19 @@ EBRL_DEV double i8_gate(float g32, float u32) {
 EBRL_DEV float i8_gate_fast(float g, float u) {
     return g * (__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u);
 }
-// y / s to the nearest whole number, ties to even.  The product with 1 / s is
-// corrected by its remainder, which makes a quotient that is a half exactly that;
-// adding 1.5 * 2^52 rounds it into the low bits.
-EBRL_DEV int i8_code(double y, double s, double inv) {
+// y / s to the nearest whole number, ties to even, in the low bits: adding 1.5 * 2^52
+// rounds it there.  TIES: the product with 1 / s is corrected by its remainder, which
+// makes a quotient that is a half exactly that; a y that is rounded itself has none to keep.
+template <bool TIES> EBRL_DEV uint32_t i8_code(double y, double s, double inv) {
+    constexpr double magic = 6755399441055744.0;
+    if constexpr (!TIES) return (uint32_t)__builtin_bit_cast(uint64_t, fma(y, inv, magic));
     double q = y * inv;
     q = fma(fma(-q, s, y), inv, q);
-    return (int)(uint32_t)__builtin_bit_cast(uint64_t, q + 6755399441055744.0);
+    return (uint32_t)__builtin_bit_cast(uint64_t, q + magic);
+}
+// The low bytes of four words.
+EBRL_DEV uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
 }
 // The scale that rows with |y| <= top need; infinity: none, the row is not finite.
 EBRL_DEV float i8_scale(double top, bool bad) {
@@ -128,13 +134,15 @@ template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]
         for (int e = 0; e < 8; ++e) v[e] = e < left ? ld_elem<T>(p + e) : 0.f;
     }
 }
-// Eight codes; columns from `left` on are zeros, those from `fill` on left as they are.
-EBRL_DEV void i8_store8(int8_t* p, const double (&y)[8], int left, int fill, double s, double inv, bool bad) {
-    uint32_t w[2] = {0, 0};
+// Eight codes (those of columns past the last are codes of zeros); columns from `fill` on
+// are left as they are.
+template <bool TIES> EBRL_DEV void i8_store8(int8_t* p, const double (&y)[8], int fill, double s, double inv, bool bad) {
+    if (fill <= 0) return;
+    uint32_t k[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < left && !bad) w[e >> 2] |= (uint32_t)(i8_code(y[e], s, inv) & 255) << (e & 3) * 8;
-    if (fill > 0) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    for (int e = 0; e < 8; ++e) k[e] = i8_code<TIES>(y[e], s, inv);
+    const uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
+    *reinterpret_cast<uint2*>(p) = bad ? make_uint2(0, 0) : make_uint2(lo, hi);
 }
 
 // The largest value, and the sum, over a row's waves; `red`: a word for each.
@@ -223,7 +231,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int j = (c * threads + tid) * 8;
-            i8_store8(out + j, y[c], a.cols - j, wide - j, sd, inv, bad);
+            i8_store8<OP == EBRL_I8_ROWS>(out + j, y[c], wide - j, sd, inv, bad);
         }
     } else {
         auto exactly = [&](int j) { return i8_gate(ld_elem<T>(x + j), ld_elem<T>(up + j)); };
@@ -269,17 +277,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                     border[e] = fmaf(fabsf(z[c][e]), eb, fabsf(fmaf(z[c][e], invf, -(t - 12582912.0f))));
                     near = fmaxf(near, border[e]);
                 }
-                uint32_t lo = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[3], k[2], 0x0c0c0400),
-                                                    __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0400), 0x05040100);
-                uint32_t hi = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[7], k[6], 0x0c0c0400),
-                                                    __builtin_amdgcn_perm(k[5], k[4], 0x0c0c0400), 0x05040100);
+                uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
                 if (near >= 0.5f) {
                     unsigned these = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) these |= (border[e] >= 0.5f ? 1u : 0u) << e;
                     for (; these; these &= these - 1) {
                         const int e = __builtin_ctz(these), at = (e & 3) * 8;
-                        const uint32_t code = (uint32_t)i8_code(exactly(j + e), sd, inv) & 255;
+                        const uint32_t code = i8_code<false>(exactly(j + e), sd, inv) & 255;
                         if (e < 4) lo = (lo & ~(255u << at)) | code << at;
                         else hi = (hi & ~(255u << at)) | code << at;
                     }
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll 1
         for (int j = tid; j < wide; j += threads)
-            out[j] = j < a.cols && !bad ? (int8_t)i8_code(exactly(j), sd, inv) : (int8_t)0;
+            out[j] = j < a.cols && !bad ? (int8_t)i8_code<false>(exactly(j), sd, inv) : (int8_t)0;
     }
 }
 
@@ -360,7 +365,7 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(ebrl_i8_quant_args 
     for (int j = tid * 8; j < wide; j += 8192) {
         double y[8];
         values(j, y);
-        i8_store8(out + j, y, a.cols - j, wide - j, sd, inv, bad);
+        i8_store8<OP == EBRL_I8_ROWS>(out + j, y, wide - j, sd, inv, bad);
     }
 }
 
