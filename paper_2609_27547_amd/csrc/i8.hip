@@ -101,18 +101,20 @@ template <int CTRL> EBRL_DEV double i8_dpp(double v) {
         (unsigned)__builtin_amdgcn_update_dpp(0, (int)w.x, CTRL, 0xF, 0xF, false),
         (unsigned)__builtin_amdgcn_update_dpp(0, (int)w.y, CTRL, 0xF, 0xF, false)));
 }
-EBRL_DEV double i8_wave_sum(double v) {
-    v += i8_dpp<DPP_SWAP1>(v);
-    v += i8_dpp<DPP_SWAP2>(v);
-    v += i8_dpp<DPP_HALF_MIRROR>(v);
-    v += i8_dpp<DPP_MIRROR>(v);
+template <typename F> EBRL_DEV double i8_over_wave(double v, F op) {
+    v = op(v, i8_dpp<DPP_SWAP1>(v));
+    v = op(v, i8_dpp<DPP_SWAP2>(v));
+    v = op(v, i8_dpp<DPP_HALF_MIRROR>(v));
+    v = op(v, i8_dpp<DPP_MIRROR>(v));
     const uint2 w = __builtin_bit_cast(uint2, v);
     auto lane = [&](int l) {
         return __builtin_bit_cast(double, make_uint2((unsigned)__builtin_amdgcn_readlane((int)w.x, l),
                                                      (unsigned)__builtin_amdgcn_readlane((int)w.y, l)));
     };
-    return (lane(0) + lane(16)) + (lane(32) + lane(48));
+    return op(op(lane(0), lane(16)), op(lane(32), lane(48)));
 }
+EBRL_DEV double i8_wave_sum(double v) { return i8_over_wave(v, [](double a, double b) { return a + b; }); }
+EBRL_DEV double i8_wave_max(double v) { return i8_over_wave(v, [](double a, double b) { return fmax(a, b); }); }
 
 // Eight neighbours of a row; those from `left` on are zeros.
 template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]) {
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
     constexpr int threads = 64 * WAVES;
     constexpr bool GATE = OP == EBRL_I8_SWIGLU;
     constexpr float EB = 0x1p-16f;
-    __shared__ double red_sum[WAVES];
+    __shared__ double red_sum[WAVES], red_top[WAVES];
     __shared__ float red_max[WAVES];
     const int tid = ONE ? threadIdx.x & 63 : threadIdx.x;
     const int row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
@@ -201,32 +203,47 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
             if (a.gain) i8_load8<float>(a.gain + j, a.cols - j, u[c]);
     }
     if constexpr (!GATE) {
-        double factor = 1.0;
-        if constexpr (OP == EBRL_I8_RMSNORM) {
-            double ss = 0.0;
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fma((double)z[c][e], (double)z[c][e], ss);
-            ss = i8_over_waves<WAVES>(i8_wave_sum(ss), red_sum, true);
-            factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
-        }
-        double y[CHUNKS][8], top = 0.0, nan = 0.0;
+        // normed rows: factor x gain, whose product x gain is exact in 64 bits, so that the
+        // largest is known with the sum of squares, in one exchange
+        double y[CHUNKS][8], top = 0.0, nan = 0.0, ss = 0.0, factor = 1.0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 y[c][e] = z[c][e];
                 if constexpr (OP == EBRL_I8_RMSNORM) {
-                    y[c][e] *= factor;
+                    ss = fma(y[c][e], y[c][e], ss);
                     if (a.gain) y[c][e] *= (double)u[c][e];
                 }
                 top = fmax(top, fabs(y[c][e]));
                 nan = fma(y[c][e], 0.0, nan);
             }
-        const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+        float s;
+        if constexpr (OP == EBRL_I8_RMSNORM) {
+            ss = i8_wave_sum(ss);
+            top = i8_wave_max(nan == 0.0 ? top : (double)INFINITY);
+            if constexpr (WAVES > 1) {
+                if ((threadIdx.x & 63) == 0) {
+                    red_sum[threadIdx.x >> 6] = ss;
+                    red_top[threadIdx.x >> 6] = top;
+                }
+                __syncthreads();
+                ss = red_sum[0];
+                top = red_top[0];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) {
+                    ss += red_sum[w];
+                    top = fmax(top, red_top[w]);
+                }
+            }
+            factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
+            top *= factor;      // NaN for squares that are none or infinite
+            s = i8_scale(top, !(top < (double)INFINITY));
+        } else {
+            s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+        }
         const bool bad = s == INFINITY;
-        const double sd = s, inv = 1.0 / sd;
+        const double sd = s, inv = factor / sd;
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
