@@ -41,6 +41,17 @@ constexpr int64_t I8_MAX_TILES = 1 << 23;
 // for 9216 (4.7 to 5.1 TB/s of a copy's 4.8), bf16 ones as they are 26 (4.3); a row
 // alone 3.2 us, a launch and two memory latencies.
 
+// 1 / d and 1 / sqrt(d): two steps of Newton's, 2^-23, 2^-46, then all bits.
+EBRL_DEV double i8_rcp(double d) {
+    double r = __builtin_amdgcn_rcp(d);
+    r = fma(r, fma(-d, r, 1.0), r);
+    return fma(r, fma(-d, r, 1.0), r);
+}
+EBRL_DEV double i8_rsqrt(double d) {
+    double r = __builtin_amdgcn_rsq(d);
+    r = fma(0.5 * r, fma(-d * r, r, 1.0), r);
+    return fma(0.5 * r, fma(-d * r, r, 1.0), r);
+}
 // silu(g) u.  exp(-g) = 2^n 2^f, |f| <= 1/2, 2^f by its Taylor series: the first
 // term left out is 2e-16.  The exponent is held to +-690, where silu is g or below
 // every scale.  1 / ln(2) in two parts keeps f to all its bits.
@@ -61,11 +72,7 @@ EBRL_DEV double i8_gate(float g32, float u32) {
     p = fma(p, f, 2.4022650695910071233e-1);
     p = fma(p, f, 6.9314718055994530942e-1);
     p = fma(p, f, 1.0);
-    const double d = 1.0 + ldexp(p, (int)n);
-    double r = __builtin_amdgcn_rcp(d);         // two steps of Newton's: 2^-23, 2^-46, then all bits
-    r = fma(r, fma(-d, r, 1.0), r);
-    r = fma(r, fma(-d, r, 1.0), r);
-    return g * r * (double)u32;
+    return g * i8_rcp(1.0 + ldexp(p, (int)n)) * (double)u32;
 }
 // The same in 32 bits, for |g| <= 80, off by less than 2^-17 of its size: the
 // exponent by 2^-18 and the constant's 2^-20, the others by a few ulps.  The gate
@@ -206,6 +213,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
         // normed rows: factor x gain, whose product x gain is exact in 64 bits, so that the
         // largest is known with the sum of squares, in one exchange
         double y[CHUNKS][8], top = 0.0, nan = 0.0, ss = 0.0, factor = 1.0;
+        const double mean = 1.0 / a.cols;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -236,14 +244,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                     top = fmax(top, red_top[w]);
                 }
             }
-            factor = 1.0 / sqrt(ss / a.cols + (double)a.eps);
+            factor = i8_rsqrt(fma(ss, mean, (double)a.eps));
             top *= factor;      // NaN for squares that are none or infinite
             s = i8_scale(top, !(top < (double)INFINITY));
         } else {
             s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
         }
         const bool bad = s == INFINITY;
-        const double sd = s, inv = factor / sd;
+        const double sd = s, inv = factor * i8_rcp(sd);
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
