@@ -192,7 +192,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
     constexpr bool GATE = OP == EBRL_I8_SWIGLU;
     constexpr float EB = 0x1p-16f;
     __shared__ double red_sum[WAVES], red_top[WAVES];
-    __shared__ float red_max[WAVES];
+    __shared__ float red_max[WAVES], red_scale[WAVES];
     const int tid = ONE ? threadIdx.x & 63 : threadIdx.x;
     const int row = ONE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (row >= a.rows) return;
@@ -270,9 +270,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                 most = i8_most(most, z[c][e]);
             }
         const bool fits = most <= 0x1p120f && gate <= 80.f;
-        const float m = i8_over_waves<WAVES>(wave_max(fits ? most : INFINITY), red_max, false);
-        if (m <= 0x1p120f && m >= 0x1p-80f) {
-            // what may be the largest one, from the row read again
+        float m = wave_max(fits ? most : INFINITY), s = 0.f;
+        if (m <= 0x1p120f && m >= 0x1p-81f) {
+            // what may be the wave's largest one, from the row read again; those of waves
+            // that are left out are below every wave's that counts
             const float may = m * (1.0f - EB);
             double top = 0.0;
             if (most >= may) {
@@ -285,8 +286,24 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                         top = fmax(top, fabs(exactly((c * threads + tid) * 8 + __builtin_ctz(these))));
                 }
             }
-            const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, false)), red_max, false);
-            const double sd = s, inv = 1.0 / sd;
+            s = wave_max(i8_scale(top, false));
+        }
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                red_max[threadIdx.x >> 6] = m;
+                red_scale[threadIdx.x >> 6] = s;
+            }
+            __syncthreads();
+            m = red_max[0];
+            s = red_scale[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                m = fmaxf(m, red_max[w]);
+                s = fmaxf(s, red_scale[w]);
+            }
+        }
+        if (m <= 0x1p120f && m >= 0x1p-80f) {
+            const double sd = s, inv = i8_rcp(sd);
             const float invf = (float)inv, eb = invf * EB;
             if (tid == 0) a.scales[row] = s;
 #pragma unroll
@@ -325,7 +342,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
             top = fmax(top, fabs(y));
             nan = fma(y, 0.0, nan);
         }
-        const float s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+        s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
         const bool bad = s == INFINITY;
         const double sd = s, inv = 1.0 / sd;
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
