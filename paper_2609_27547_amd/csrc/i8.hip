@@ -37,9 +37,9 @@ constexpr int64_t I8_MAX_TILES = 1 << 23;
 // about 1e-4 of its size.  With 32-bit y that is one code in 1e5, with 64-bit ones
 // none.  The vector units do 64-bit adds and products at the rate of 32-bit ones.
 //
-// Bound by memory from some thousand rows on: fp32 rows of 4096, normed, 37 to 40 us
-// for 9216 (4.7 to 5.1 TB/s of a copy's 4.8), bf16 ones as they are 26 (4.3); a row
-// alone 3.2 us, a launch and two memory latencies.
+// Bound by memory from some thousand rows on: 9216 fp32 rows of 4092, normed, 39 us (4.8
+// TB/s; of 4096, whose rows start on the same channels, 45), as they are 33 (5.7), bf16 ones
+// as they are 22 (5.2); a row alone 2.7 us, a launch and two memory latencies.
 
 // 1 / d and 1 / sqrt(d): two steps of Newton's, 2^-23, 2^-46, then all bits.
 EBRL_DEV double i8_rcp(double d) {
@@ -175,13 +175,14 @@ EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(
 // constant, because a loop over it waits for each wave's word in turn (a row of 4096 3.2
 // us against 3.6) and sixteen doubles at once take the registers of a wave in four.
 //
-// Plain and normed rows are 64-bit throughout.  Gated rows, whose 64-bit exponentials
+// Plain and normed rows are 64-bit throughout.  A row's waves meet once (9216 normed fp32
+// rows of 11008: 117 us; sum and maximum one after the other 161).  Gated rows, whose 64-bit exponentials
 // would take twice the time of reading them, have 32-bit values, maximum and codes; what
 // lies nearer to a border than these are exact (EB, twice their error) is computed once
 // more in 64 bits, one code in 1e4, and so is a whole row where 32 bits do not do
-// (near the ends of their range, or not finite).  9216 rows of 11008 (bf16): 127 us, 4.0
+// (near the ends of their range, or not finite).  9216 rows of 11008 (bf16): 124 us, 4.1
 // TB/s, 195 with 64 bits throughout.  Two workgroups of twelve waves share a CU, whose
-// vector units are half busy: the rest is the wait for a row and the two exchanges.
+// vector units are half busy: the rest is the wait for a row and the exchange.
 // Eight waves with three places 149 (159 held to three workgroups a CU), six with four
 // 186; persistent workgroups with the next row in flight 152.
 template <typename T, int OP, int WAVES, int CHUNKS>
@@ -549,8 +550,8 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 //    4096 columns 176).
 //  * What a tile derives from the lane is made anew each time: kept in registers it was
 //    spilled, and each reload waited for every DMA (35 spilled registers, 374 us at 8192^3;
-//    none in the K loop, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x 1024 51 -> 48,
-//    nothing at long K).
+//    none in the K loop, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x
+//    1024 51 -> 48, nothing at long K).
 //  * With a residual the tiles of a round meet in memory at the end: 9216 x 4096 x 11008,
 //    fp32, 345 us, of which 302 MB of residual and results are 63.  Half the XCDs
 //    taking their part of the last round first, so that the rounds do not end together:
