@@ -37,9 +37,9 @@ constexpr int64_t I8_MAX_TILES = 1 << 23;
 // about 1e-4 of its size.  With 32-bit y that is one code in 1e5, with 64-bit ones
 // none.  The vector units do 64-bit adds and products at the rate of 32-bit ones.
 //
-// Bound by memory from some thousand rows on: 9216 fp32 rows of 4092, normed, 39 us (4.8
-// TB/s; of 4096, whose rows start on the same channels, 45), as they are 33 (5.7), bf16 ones
-// as they are 22 (5.2); a row alone 2.7 us, a launch and two memory latencies.
+// Bound by memory from some thousand rows on: 9216 fp32 rows of 4096, normed, 39 us (4.8
+// TB/s), as they are 32 (5.9), bf16 ones as they are 20 (5.7); bf16 ones, normed, by their
+// vector instructions, 32; a row alone 2.7 us, a launch and two memory latencies.
 
 // 1 / d and 1 / sqrt(d): two steps of Newton's, 2^-23, 2^-46, then all bits.
 EBRL_DEV double i8_rcp(double d) {
@@ -82,19 +82,12 @@ EBRL_DEV double i8_gate(float g32, float u32) {
 EBRL_DEV float i8_gate_fast(float g, float u) {
     return g * (__builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u);
 }
-// y / s to the nearest whole number, ties to even, in the low bits: adding 1.5 * 2^52
-// rounds it there.  TIES: the product with 1 / s is corrected by its remainder, which
-// makes a quotient that is a half exactly that; a y that is rounded itself has none to keep.
-template <bool TIES> EBRL_DEV uint32_t i8_code(double y, double s, double inv) {
-    constexpr double magic = 6755399441055744.0;
-    if constexpr (!TIES) return (uint32_t)__builtin_bit_cast(uint64_t, fma(y, inv, magic));
-    double q = y * inv;
-    q = fma(fma(-q, s, y), inv, q);
-    return (uint32_t)__builtin_bit_cast(uint64_t, q + magic);
-}
-// The low bytes of four words.
-EBRL_DEV uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
+// y / s to the nearest whole number, ties to even.
+EBRL_DEV uint32_t i8_code(double y, double s) { return (uint32_t)(int)rint(y / s); }
+// Byte BYTE of four words.
+template <int BYTE> EBRL_DEV uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    constexpr uint32_t two = 0x0c0c0400 + BYTE * 0x0101;
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, two), __builtin_amdgcn_perm(b, a, two), 0x05040100);
 }
 // The scale that rows with |y| <= top need; infinity: none, the row is not finite.
 EBRL_DEV float i8_scale(double top, bool bad) {
@@ -143,17 +136,48 @@ template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]
         for (int e = 0; e < 8; ++e) v[e] = e < left ? ld_elem<T>(p + e) : 0.f;
     }
 }
-// Eight codes (those of columns past the last are codes of zeros); columns from `fill` on
-// are left as they are.
-template <bool TIES> EBRL_DEV void i8_store8(int8_t* p, const double (&y)[8], int fill, double s, double inv, bool bad) {
-    if (fill <= 0) return;
-    uint32_t k[8];
+// The codes of eight neighbours in each of CHUNKS places, `step` columns apart from j on (those
+// of columns past the last are codes of zeros); columns from `wide` on are left as they are.
+// Adding 1.5 * 2^28 and a half rounds y inv + 1/2 to 2^-24ths, with the whole number in the low
+// word's last byte.  The product is off by less than 2^-42, so that is the one nearest to y / s
+// unless the fraction is 0: then y / s may be a tie, or on either side of one, and
+// `exactly(column)` gives its code by divisions, stored over the first (one in 2^24, but for data
+// of few bits).
+template <int CHUNKS, typename F>
+EBRL_DEV void i8_store(int8_t* out, const double (&y)[CHUNKS][8], int j, int step, int wide, double inv, bool bad, F exactly) {
+    auto code = [&](int c, int e) { return (uint32_t)__builtin_bit_cast(uint64_t, fma(y[c][e], inv, 402653184.5)); };
+    uint32_t least = ~0u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = i8_code<TIES>(y[e], s, inv);
-    const uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
-    *reinterpret_cast<uint2*>(p) = bad ? make_uint2(0, 0) : make_uint2(lo, hi);
+    for (int c = 0; c < CHUNKS; ++c) {
+        uint32_t k[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            k[e] = code(c, e);
+            least = min(least, k[e] << 8);
+        }
+        const uint32_t lo = i8_pack<3>(k[0], k[1], k[2], k[3]), hi = i8_pack<3>(k[4], k[5], k[6], k[7]);
+        if (j + c * step < wide) *reinterpret_cast<uint2*>(out + j + c * step) = bad ? make_uint2(0, 0) : make_uint2(lo, hi);
+    }
+    if (least == 0 && !bad) {
+        unsigned these = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) these |= (code(c, e) << 8 == 0 ? 1u : 0u) << (8 * c + e);
+        for (; these; these &= these - 1) {
+            const int i = __builtin_ctz(these), at = j + (i >> 3) * step + (i & 7);
+            out[at] = (int8_t)exactly(at);
+        }
+    }
 }
 
+// y of a row as it is or normed, read again; ss: its sum of squares.  With the division
+// last, y is exact wherever it and the root are numbers of 64 bits.
+template <typename T, int OP> EBRL_DEV double i8_value(const ebrl_i8_quant_args& a, const T* x, int j, double ss) {
+    const double v = ld_elem<T>(x + j);
+    if constexpr (OP == EBRL_I8_ROWS) return v;
+    else return (a.gain ? v * (double)a.gain[j] : v) / sqrt(ss / a.cols + (double)a.eps);
+}
 // The largest value, and the sum, over a row's waves; `red`: a word for each.
 template <int WAVES, typename V> EBRL_DEV V i8_over_waves(V v, V* red, bool sum) {
     if constexpr (WAVES > 1) {
@@ -175,9 +199,10 @@ EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(
 // constant, because a loop over it waits for each wave's word in turn (a row of 4096 3.2
 // us against 3.6) and sixteen doubles at once take the registers of a wave in four.
 //
-// Plain and normed rows are 64-bit throughout.  A row's waves meet once (9216 normed fp32
-// rows of 11008: 117 us; sum and maximum one after the other 161).  Gated rows, whose 64-bit exponentials
-// would take twice the time of reading them, have 32-bit values, maximum and codes; what
+// Plain and normed rows are 64-bit throughout, but for the maximum of plain ones, which is a
+// float.  A row's waves meet once (9216 normed fp32 rows of 11008: 114 us; sum and maximum one
+// after the other 161).  Gated rows, whose 64-bit exponentials would take twice the
+// time of reading them, have 32-bit values, maximum and codes; what
 // lies nearer to a border than these are exact (EB, twice their error) is computed once
 // more in 64 bits, one code in 1e4, and so is a whole row where 32 bits do not do
 // (near the ends of their range, or not finite).  9216 rows of 11008 (bf16): 124 us, 4.1
@@ -213,7 +238,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
     if constexpr (!GATE) {
         // normed rows: factor x gain, whose product x gain is exact in 64 bits, so that the
         // largest is known with the sum of squares, in one exchange
-        double y[CHUNKS][8], top = 0.0, nan = 0.0, ss = 0.0, factor = 1.0;
+        double y[CHUNKS][8], top = 0.0, ss = 0.0, factor = 1.0;
+        float most = 0.f;       // of what is not finite wherever a y is, for all that ss does not tell
         const double mean = 1.0 / a.cols;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
@@ -222,15 +248,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                 y[c][e] = z[c][e];
                 if constexpr (OP == EBRL_I8_RMSNORM) {
                     ss = fma(y[c][e], y[c][e], ss);
-                    if (a.gain) y[c][e] *= (double)u[c][e];
+                    if (a.gain) {
+                        y[c][e] *= (double)u[c][e];
+                        most = i8_most(most, u[c][e]);
+                    }
+                    top = fmax(top, fabs(y[c][e]));
+                } else {
+                    most = i8_most(most, z[c][e]);
                 }
-                top = fmax(top, fabs(y[c][e]));
-                nan = fma(y[c][e], 0.0, nan);
             }
         float s;
         if constexpr (OP == EBRL_I8_RMSNORM) {
             ss = i8_wave_sum(ss);
-            top = i8_wave_max(nan == 0.0 ? top : (double)INFINITY);
+            top = i8_wave_max(most < INFINITY ? top : (double)INFINITY);
             if constexpr (WAVES > 1) {
                 if ((threadIdx.x & 63) == 0) {
                     red_sum[threadIdx.x >> 6] = ss;
@@ -249,16 +279,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
             top *= factor;      // NaN for squares that are none or infinite
             s = i8_scale(top, !(top < (double)INFINITY));
         } else {
-            s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
+            s = i8_over_waves<WAVES>(wave_max(i8_scale(most, !(most < INFINITY))), red_max, false);
         }
         const bool bad = s == INFINITY;
         const double sd = s, inv = factor * i8_rcp(sd);
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int j = (c * threads + tid) * 8;
-            i8_store8<OP == EBRL_I8_ROWS>(out + j, y[c], wide - j, sd, inv, bad);
-        }
+        i8_store<CHUNKS>(out, y, tid * 8, threads * 8, wide, inv, bad,
+                         [&](int j) { return i8_code(i8_value<T, OP>(a, x, j, ss), sd); });
     } else {
         auto exactly = [&](int j) { return i8_gate(ld_elem<T>(x + j), ld_elem<T>(up + j)); };
         float most = 0.f, gate = 0.f;
@@ -304,8 +331,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
             }
         }
         if (m <= 0x1p120f && m >= 0x1p-80f) {
-            const double sd = s, inv = i8_rcp(sd);
-            const float invf = (float)inv, eb = invf * EB;
+            const double sd = s;
+            const float invf = (float)i8_rcp(sd), eb = invf * EB;
             if (tid == 0) a.scales[row] = s;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
@@ -320,14 +347,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                     border[e] = fmaf(fabsf(z[c][e]), eb, fabsf(fmaf(z[c][e], invf, -(t - 12582912.0f))));
                     near = fmaxf(near, border[e]);
                 }
-                uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
+                uint32_t lo = i8_pack<0>(k[0], k[1], k[2], k[3]), hi = i8_pack<0>(k[4], k[5], k[6], k[7]);
                 if (near >= 0.5f) {
                     unsigned these = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) these |= (border[e] >= 0.5f ? 1u : 0u) << e;
                     for (; these; these &= these - 1) {
                         const int e = __builtin_ctz(these), at = (e & 3) * 8;
-                        const uint32_t code = i8_code<false>(exactly(j + e), sd, inv) & 255;
+                        const uint32_t code = i8_code(exactly(j + e), sd) & 255;
                         if (e < 4) lo = (lo & ~(255u << at)) | code << at;
                         else hi = (hi & ~(255u << at)) | code << at;
                     }
@@ -345,11 +372,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
         }
         s = i8_over_waves<WAVES>(wave_max(i8_scale(top, !(nan == 0.0))), red_max, false);
         const bool bad = s == INFINITY;
-        const double sd = s, inv = 1.0 / sd;
+        const double sd = s;
         if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
 #pragma unroll 1
         for (int j = tid; j < wide; j += threads)
-            out[j] = j < a.cols && !bad ? (int8_t)i8_code<false>(exactly(j), sd, inv) : (int8_t)0;
+            out[j] = j < a.cols && !bad ? (int8_t)i8_code(exactly(j), sd) : (int8_t)0;
     }
 }
 
@@ -361,9 +388,8 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(ebrl_i8_quant_args 
     __shared__ float red_max[16];
     const int tid = threadIdx.x, row = blockIdx.x;
     const T* const x = (const T*)a.x + (size_t)row * a.ldx;
-    double factor = 1.0;
+    double factor = 1.0, ss = 0.0;
     if constexpr (OP == EBRL_I8_RMSNORM) {
-        double ss = 0.0;
         for (int j = tid * 8; j < a.cols; j += 8192) {
             float v[8];
             i8_load8<T>(x + j, a.cols - j, v);
@@ -406,9 +432,13 @@ __global__ __launch_bounds__(1024) void i8_quant_long_kernel(ebrl_i8_quant_args 
     int8_t* const out = a.codes + (size_t)row * a.ldc;
     const int wide = (a.cols + 15) / 16 * 16;
     for (int j = tid * 8; j < wide; j += 8192) {
-        double y[8];
-        values(j, y);
-        i8_store8<OP == EBRL_I8_ROWS>(out + j, y, wide - j, sd, inv, bad);
+        double y[1][8];
+        values(j, y[0]);
+        i8_store<1>(out, y, j, 0, wide, inv, bad, [&](int at) {
+            if constexpr (OP == EBRL_I8_SWIGLU)
+                return i8_code(i8_gate(ld_elem<T>(x + at), ld_elem<T>((const T*)a.up + (size_t)row * a.ldup + at)), sd);
+            else return i8_code(i8_value<T, OP>(a, x, at, ss), sd);
+        });
     }
 }
 

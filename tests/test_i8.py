@@ -197,6 +197,42 @@ def test_codes_at_ties(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("op", list(OPS))
+@pytest.mark.parametrize("cols", [512, 1000, 2048, 4095, 8192, 11008, 16384, 20001])
+def test_halves_go_to_the_even_code(op, dtype, cols):
+    """Quotients that are halves exactly, scales whose reciprocal no number holds.  Normed rows of one size r and eps
+    0, whose root is r; gates of 40 and more, whose silu is the gate itself in 64 bits.  Every y is s k / 2, k a whole
+    number up to 254, so the scale is s and each code k / 2, halves to even."""
+    g = torch.Generator().manual_seed(cols)
+    rows = 12
+    k = torch.randint(-253, 254, (rows, cols), generator=g).double()
+    k[:, cols // 3] = 254
+    r = torch.tensor([1, 2, 3, 5, 0.75, 7, 12, 96, 1, 11, 2.5, 40]).double()[:, None]
+    if op == "norm":
+        # the gain is one for all rows
+        k[:] = k[0]
+        s = torch.full((rows, 1), 3.0 if cols % 2 else 0.6875).double()
+        sign = torch.where(torch.rand((rows, cols), generator=g) < 0.5, -1.0, 1.0).double()
+        kw = dict(norm_eps=0.0, gain=(s[0] * k[0] / 2).float().cuda())
+        x, k = r * sign, k * sign
+    elif op == "gate":
+        gate = torch.tensor([40, 44, 48, 52, 56, 60, 72, 80, 88, 96, 120, 1000]).double()[:, None]
+        s = gate / 4
+        x, kw = gate.expand(rows, cols), dict(up=(k / 8).to(DT[dtype]).cuda())
+    else:
+        # (bf16's eight bits hold 127 s for scales of one bit)
+        s = torch.tensor([3, 5, 7, 9, 11, 13, 1.25, 0.375, 6, 10, 14, 1.75] if dtype == "fp32" else
+                         [1, 2, 4, 0.5, 0.25, 8, 16, 32, 1, 2, 4, 8]).double()[:, None]
+        x, kw = s * k / 2, {}
+    codes, scales = E.i8_alloc(rows, cols)
+    E.op_i8_quant(x.to(DT[dtype]).cuda(), codes, scales, **kw)
+    assert torch.equal(scales.cpu().double(), s[:, 0])
+    wrong = codes[:, :cols].cpu().double() != torch.round(k / 2)
+    assert not wrong.any(), f"{int(wrong.sum())} of {wrong.numel()} codes"
+
+
+@gpu
 @pytest.mark.parametrize("cols", [24, 1024, 5000, 20000])
 def test_rows_of_any_size_of_number(cols):
     """Zeros, numbers below the least scale, denormals, the largest floats."""
@@ -235,6 +271,29 @@ def test_rows_that_are_not_finite(op, dtype, cols):
     assert scales[rows].isnan().all() and (codes[rows] == 0).all()
     y = _values(OPS[op], x[good], None if up is None else up[good], None, 1e-6)
     _check_codes(y, codes[good], scales[good])
+
+
+@gpu
+@pytest.mark.parametrize("cols", [33, 1024, 4096, 11008, 20001])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_gains_that_are_not_finite(cols, bad):
+    """A gain of NaN or infinity, also where the row has a zero, leaves no row finite; a gain of zero takes a
+    column out, but not an infinity in it."""
+    g = torch.Generator().manual_seed(cols)
+    x = _rows(4, cols, "fp32", g)
+    gain = torch.ones(cols, device="cuda")
+    gain[cols // 2] = bad
+    x[1, cols // 2] = 0
+    codes, scales = E.i8_alloc(4, cols)
+    codes.fill_(5)
+    E.op_i8_quant(x, codes, scales, norm_eps=1e-6, gain=gain)
+    assert scales.isnan().all() and (codes == 0).all()
+    gain[cols // 2] = 0
+    x[2, cols // 2] = bad
+    E.op_i8_quant(x, codes, scales, norm_eps=1e-6, gain=gain)
+    assert scales[2].isnan() and (codes[2] == 0).all()
+    good = [0, 1, 3]
+    _check_codes(_values(E.I8_RMSNORM, x[good], None, gain, 1e-6), codes[good], scales[good])
 
 
 @gpu
