@@ -33,7 +33,7 @@ typedef struct ebrl_i8_quant_args {
     int32_t dtype;           /* EBRL_DTYPE_FP32 or _BF16: type of x and up */
     int32_t op;              /* EBRL_I8_* */
     int32_t rows, cols;      /* cols 1 to 2^20 */
-    float eps;               /* EBRL_I8_RMSNORM: >= 0 */
+    float eps;               /* EBRL_I8_RMSNORM: >= 0, finite */
     const void *x, *up;      /* device rows; up: EBRL_I8_SWIGLU alone */
     int64_t ldx, ldup;       /* row strides in elements, >= cols */
     const float* gain;       /* device [cols] (EBRL_I8_RMSNORM), or NULL: ones */

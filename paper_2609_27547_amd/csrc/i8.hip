@@ -1320,7 +1320,7 @@ static int i8_quant(const ebrl_i8_quant_args* args, hipStream_t s) {
     if (!args) return EBRL_E_INVALID;
     const ebrl_i8_quant_args& a = *args;
     if (!i8_dtype_ok(a.dtype) || a.op < EBRL_I8_ROWS || a.op > EBRL_I8_SWIGLU || a.rows < 0 || a.cols < 1 ||
-        a.cols > I8_MAX_COLS || (a.op == EBRL_I8_RMSNORM && !(a.eps >= 0.f)) || (a.op != EBRL_I8_SWIGLU && a.up) ||
+        a.cols > I8_MAX_COLS || (a.op == EBRL_I8_RMSNORM && !(a.eps >= 0.f && a.eps < INFINITY)) || (a.op != EBRL_I8_SWIGLU && a.up) ||
         (a.op != EBRL_I8_RMSNORM && a.gain))
         return EBRL_E_INVALID;
     if (a.rows == 0) return EBRL_OK;

@@ -35,6 +35,14 @@ def test_quant_refuses_arguments(bad):
     assert E.lib().ebrl_op_i8_quant(ctypes.byref(_quant_args(**bad)), None) == -1
 
 
+@pytest.mark.parametrize("eps", [float("inf"), -float("inf"), float("nan"), -1e-30])
+def test_quant_refuses_an_eps_that_is_not_finite(eps):
+    """At every width: a root of infinity would give zeros."""
+    for cols in (1, 40, 5000, 20000):
+        a = _quant_args(op=E.I8_RMSNORM, eps=eps, rows=0, cols=cols, ldx=cols, ldc=(cols + 15) // 16 * 16)
+        assert E.lib().ebrl_op_i8_quant(ctypes.byref(a), None) == -1
+
+
 def _gemm_args(**kw):
     a = E.I8GemmArgs(dtype=E.DTYPE_FP32, M=5, N=7, K=32, a=4096, b=8192, lda=32, ldb=48, scale_a=12288, scale_b=16384,
                      c=20480, ldc=7)
