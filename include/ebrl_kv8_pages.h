@@ -43,7 +43,9 @@ typedef struct ebrl_kv8_pool {
     int64_t layer_codes;     /* bytes, a multiple of 16; any value with one layer */
     int64_t layer_scales;    /* floats */
     int32_t layers;          /* 1 to 65535 */
-    int32_t num_blocks, table_rows, table_stride, kv_heads, head_dim;
+    int32_t num_blocks;      /* 1 to 2^30 */
+    int32_t table_rows, table_stride;   /* from 1 on; table_stride below 2^27 */
+    int32_t kv_heads, head_dim;         /* kv_heads 1 to 2^17, head_dim 64 or 128 */
 } ebrl_kv8_pool;
 
 /* Row dst[i] takes the pages of row src[i]'s first len[i] tokens, the last of them
@@ -51,7 +53,8 @@ typedef struct ebrl_kv8_pool {
  * held before are released.  src, dst, len: device int32 [n].  A fork whose source
  * is a destination of the call is left out, and of several forks to one row all
  * but the first.  Codes and scales are not touched (codes, scales and their
- * strides may be 0).  Returns EBRL_E_INVALID on bad arguments. */
+ * strides may be 0).  n: at most 65536, here and below.  Returns EBRL_E_INVALID on
+ * bad arguments. */
 int ebrl_op_kv8_fork(const ebrl_kv8_pool* pool, const int32_t* src, const int32_t* dst, const int32_t* len, int32_t n,
                      void* stream);
 
@@ -64,7 +67,10 @@ int ebrl_op_kv8_free(const ebrl_kv8_pool* pool, const int32_t* seq, const int32_
 
 /* Bytes of workspace for ebrl_op_kv8_reserve calls of at most n rows and max_count
  * tokens each (host arithmetic on the pool's numbers; no pointer is read), or
- * EBRL_E_INVALID. */
+ * EBRL_E_INVALID: for numbers out of range, n rows whose max_count tokens lie in more
+ * than 2^30 pages, or n pages of more than 2^23 pieces of 16 KB, counted once for
+ * each eight layers.  A call of a size that gets a workspace is not refused for its
+ * size. */
 int64_t ebrl_op_kv8_reserve_workspace(const ebrl_kv8_pool* pool, int32_t n, int32_t max_count);
 
 /* Makes ready the pages that tokens pos0[i] .. pos0[i] + count[i] - 1 of row seq[i]
@@ -87,7 +93,8 @@ int ebrl_op_kv8_reserve(const ebrl_kv8_pool* pool, const int32_t* seq, const int
                         void* stream);
 
 /* Bytes of workspace for ebrl_op_kv8_compact (host arithmetic on the pool's
- * numbers), or EBRL_E_INVALID. */
+ * numbers), or EBRL_E_INVALID: for numbers out of range, or layers of more than 2^31
+ * pieces of 16 KB. */
 int64_t ebrl_op_kv8_compact_workspace(const ebrl_kv8_pool* pool);
 
 /* Moves the used pages to ids 0 .. *used - 1: of the pages in use from id *used on

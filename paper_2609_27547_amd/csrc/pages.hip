@@ -539,11 +539,20 @@ static int64_t pg_reserve_words(const ebrl_kv8_pool* c, int64_t n, int64_t pages
 static int64_t pg_compact_words(const ebrl_kv8_pool* c) {
     return pg_chunks(c) + c->num_blocks + 3 * ((int64_t)c->num_blocks / 2 + 1) + 2;
 }
+static bool pg_compact_ok(const ebrl_kv8_pool* c) {
+    return pg_shape_ok(c) && (int64_t)(c->num_blocks / 2) * pg_pieces(c) <= (1 << 30);      // (16 TB a layer)
+}
 static int pg_status() { return hipGetLastError() == hipSuccess ? EBRL_OK : EBRL_E_HIP; }
 
+// Layers that a workgroup of a reservation copies in: several where there are many, since what
+// it looks up serves them all.
+static int pg_reserve_step(const ebrl_kv8_pool* c, int32_t n) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(8, (int64_t)n * pg_pieces(c) * c->layers / 2048));
+}
 static bool pg_reserve_ok(const ebrl_kv8_pool* c, int32_t n, int32_t max_count) {
-    return pg_shape_ok(c) && n >= 0 && n <= PG_MAX_ROWS && max_count >= 0 &&
-           n * pg_most_pages(c, max_count) <= (1 << 30);
+    if (!pg_shape_ok(c) || n < 0 || n > PG_MAX_ROWS || max_count < 0 || n * pg_most_pages(c, max_count) > (1 << 30)) return false;
+    const int step = pg_reserve_step(c, n);
+    return (int64_t)n * pg_pieces(c) * ((c->layers + step - 1) / step) <= PG_MAX_GROUPS;
 }
 
 }  // namespace ebrl
@@ -580,8 +589,6 @@ int ebrl_op_kv8_reserve(const ebrl_kv8_pool* pool, const int32_t* seq, const int
     if (!pg_reserve_ok(pool, n, max_count) || !pg_pool_ok(pool) || !lacking || (uintptr_t)lacking % 4) return EBRL_E_INVALID;
     const int64_t pages = pg_most_pages(pool, max_count);
     const int pieces = pg_pieces(pool);
-    const int64_t groups = std::max<int64_t>(1, (int64_t)n * pieces);
-    if (groups * pool->layers > PG_MAX_GROUPS) return EBRL_E_INVALID;
     if (n > 0 && (!seq || !pos0 || !count)) return EBRL_E_INVALID;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < pg_reserve_words(pool, n, pages) * 4)
         return EBRL_E_INVALID;
@@ -604,21 +611,20 @@ int ebrl_op_kv8_reserve(const ebrl_kv8_pool* pool, const int32_t* seq, const int
         hipLaunchKernelGGL(pages_reserve_list_kernel, dim3(w.chunks + 1), dim3(256), 0, s, *pool, lacking, w);
     }
     if (n > 0) {
-        // several layers a workgroup where there are many: what it looks up serves them all
-        const int step = (int)std::max<int64_t>(1, std::min<int64_t>(8, groups * pool->layers / 2048));
-        hipLaunchKernelGGL(pages_reserve_kernel, dim3((unsigned)groups, (pool->layers + step - 1) / step), dim3(256), 0, s,
+        const int step = pg_reserve_step(pool, n);
+        hipLaunchKernelGGL(pages_reserve_kernel, dim3((unsigned)n * pieces, (pool->layers + step - 1) / step), dim3(256), 0, s,
                            *pool, seq, pos0, (int)pg_bytes(pool), pieces, step, w);
     }
     return pg_status();
 }
 
 int64_t ebrl_op_kv8_compact_workspace(const ebrl_kv8_pool* pool) {
-    return pg_shape_ok(pool) ? pg_compact_words(pool) * 4 : EBRL_E_INVALID;
+    return pg_compact_ok(pool) ? pg_compact_words(pool) * 4 : EBRL_E_INVALID;
 }
 
 int ebrl_op_kv8_compact(const ebrl_kv8_pool* pool, int32_t* new_table, int32_t* new_refs, int32_t* used,
                         void* workspace, int64_t workspace_bytes, void* stream) {
-    if (!pg_pool_ok(pool) || !new_table || !new_refs || !used ||
+    if (!pg_compact_ok(pool) || !pg_pool_ok(pool) || !new_table || !new_refs || !used ||
         ((uintptr_t)new_table | (uintptr_t)new_refs | (uintptr_t)used) % 4)
         return EBRL_E_INVALID;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < pg_compact_words(pool) * 4) return EBRL_E_INVALID;
@@ -636,7 +642,6 @@ int ebrl_op_kv8_compact(const ebrl_kv8_pool* pool, int32_t* new_table, int32_t* 
     const int64_t entries = std::max<int64_t>((int64_t)pool->table_rows * pool->table_stride, pool->num_blocks);
     const int table_groups = (int)std::min<int64_t>(256, (entries + 1023) / 1024);
     const int64_t most = (int64_t)(pool->num_blocks / 2) * pieces;
-    if (most > (1 << 30)) return EBRL_E_INVALID;   // (16 TB a layer)
     const int copy_groups = (int)std::min<int64_t>(2048, most * pool->layers);
     if (pool->num_blocks <= PG_SMALL_POOL) {
         hipLaunchKernelGGL(pages_compact_small_kernel, dim3(1), dim3(1024), 0, s, *pool, used, w);

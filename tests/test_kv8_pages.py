@@ -76,6 +76,30 @@ def test_numbers_are_refused():
     assert _fork(p, n=0) == _free(p, n=0) == 0 and E.lib().ebrl_op_kv8_reserve_workspace(ctypes.byref(p), 0, 0) >= 0
 
 
+def test_sizes_that_get_a_workspace_are_taken():
+    """What the host refuses for size alone, the workspace's call refuses too.  The calls get a workspace of no bytes,
+    so none of them goes on to the GPU."""
+    for kw in (dict(num_blocks=1 << 30, kv_heads=1 << 17, head_dim=128), dict(num_blocks=1 << 21, kv_heads=1 << 17),
+               dict(num_blocks=1 << 30, kv_heads=1), dict(num_blocks=(1 << 30) + 1), dict(table_stride=1 << 27)):
+        p = _pool(**kw)
+        need = E.lib().ebrl_op_kv8_compact_workspace(ctypes.byref(p))
+        pieces = -(-2 * p.kv_heads * PAGE * p.head_dim // 16384)
+        ok = p.num_blocks <= 1 << 30 and p.table_stride < 1 << 27 and p.num_blocks // 2 * pieces <= 1 << 30
+        assert (need > 0) == ok and (ok or need == -1)
+    for n, most, kw in ((18000, 1, dict(layers=60, kv_heads=32, head_dim=128)), (65536, 1, dict(layers=8, kv_heads=512, head_dim=128)),
+                        (65536, 1, dict(layers=9, kv_heads=512, head_dim=128)), (65536, 1, dict(layers=1, kv_heads=512, head_dim=128)),
+                        (65536, 1, dict(layers=65535, kv_heads=1)), (2000, 40, dict(layers=60000, kv_heads=1 << 10)),
+                        (1, 1, dict(layers=65535, kv_heads=1 << 17, head_dim=128)), (65537, 1, {}), (65536, 0, {}), (0, 0, {}),
+                        (65536, 1 << 30, dict(table_stride=1 << 20))):
+        p = _pool(**kw)
+        need = E.lib().ebrl_op_kv8_reserve_workspace(ctypes.byref(p), n, most)
+        pages = min((most + 30) // 16, p.table_stride)
+        pieces = -(-2 * p.kv_heads * PAGE * p.head_dim // 16384)
+        ok = n <= 65536 and n * pages <= 1 << 30 and n * pieces * -(-p.layers // 8) <= 1 << 23
+        assert (need > 0) == ok and (ok or need == -1)
+        assert _reserve(p, n=n, most=most, size=0) == -1
+
+
 def test_binding_refuses():
     codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
     table, refs = torch.full((2, 3), -1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
@@ -395,6 +419,37 @@ def test_captured_calls_are_replayed():
         plain()                                               # the same again on what the replay left
         assert torch.equal(after[0], p.d_table) and torch.equal(after[1], p.d_refs) and torch.equal(after[2], p.codes)
         p.check()
+
+
+@gpu
+@pytest.mark.parametrize("rows,layers,heads", [(18000, 60, 32), (65536, 20, 128), (4000, 300, 64)])
+def test_reservations_of_many_workgroups(rows, layers, heads):
+    """Rows x pieces of a page x layers past 2^23, which eight layers a workgroup bring below it: many rows of which a
+    few need a page; every layer of a copy is there."""
+    num, hd = 6, 128
+    codes = torch.zeros((layers, num, 2, heads, PAGE * hd), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((layers, num, 2, heads), device="cuda")
+    codes[:, 1] = (torch.arange(layers, device="cuda") % 251 + 1).to(torch.uint8)[:, None, None, None]
+    codes[:, 1, 1, heads - 1, -1] = 255
+    scales[:, 1] = torch.arange(1, layers + 1, device="cuda")[:, None, None]
+    table = torch.full((rows, 2), -1, dtype=torch.int32, device="cuda")
+    refs = torch.zeros(num, dtype=torch.int32, device="cuda")
+    sharers = [0, rows // 2, rows - 1]
+    table[sharers, 0] = 1
+    refs[1] = 3
+    count = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    count[[rows // 2, rows - 1, rows // 3]] = 1
+    lacking = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    E.op_kv8_reserve(codes, scales, table, refs, torch.arange(rows, dtype=torch.int32, device="cuda"),
+                     torch.full((rows,), 7, dtype=torch.int32, device="cuda"), count, 1, lacking)
+    # in the rows' order: a third of them down a page of its own, then two copies
+    assert lacking.item() == 0 and refs.tolist() == [1, 1, 1, 1, 0, 0]
+    want = torch.full_like(table, -1)
+    want[rows // 3, 0], want[rows // 2, 0], want[rows - 1, 0], want[0, 0] = 0, 2, 3, 1
+    assert torch.equal(table, want)
+    for p in (2, 3):
+        assert torch.equal(codes[:, p], codes[:, 1]) and torch.equal(scales[:, p], scales[:, 1])
+    assert not codes[:, [0, 4, 5]].any() and not scales[:, [0, 4, 5]].any()
 
 
 @gpu
