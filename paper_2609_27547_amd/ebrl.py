@@ -644,6 +644,15 @@ def op_kv8_attn(codes, scales, block_table, q, out, row_start, kv_len, max_q_len
 # int32 [num_blocks], zero at the start.
 
 _KV8_POOL = struct.Struct("4P2q6i")
+_KV8_MAX_ROWS = 1 << 16
+
+
+def _kv8_rows_of(t) -> int:
+    """Rows that a call names."""
+    n = t.numel()
+    if n > _KV8_MAX_ROWS:
+        _kv8_bad(f"a call takes at most {_KV8_MAX_ROWS} rows", t)
+    return n
 
 
 def _kv8_pool_table(block_table, refs):
@@ -710,7 +719,7 @@ def op_kv8_fork(block_table, refs, src, dst, length, stream=None) -> None:
     (ebrl_op_kv8_fork).  src, dst, length: int32 [n]."""
     import torch
     table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
-    n = dst.numel()
+    n = _kv8_rows_of(dst)
     at = _kv8_ints(torch.int32, dev, ("src", src, n), ("dst", dst, n), ("length", length, n))
     c = _kv8_pack(_KV8_POOL, 0, 0, table_at, refs_at, 0, 0, 1, blocks, rows, stride, 1, 64)
     _kv8_on(lib().ebrl_op_kv8_fork, "ebrl_op_kv8_fork", dev, stream, c, *at, n)
@@ -721,7 +730,7 @@ def op_kv8_free(block_table, refs, seq, keep=None, stream=None) -> None:
     (None: all) (ebrl_op_kv8_free).  seq, keep: int32 [n]."""
     import torch
     table_at, refs_at, blocks, rows, stride, dev = _kv8_pool_table(block_table, refs)
-    n = seq.numel()
+    n = _kv8_rows_of(seq)
     at = _kv8_ints(torch.int32, dev, ("seq", seq, n), ("keep", keep, n))
     c = _kv8_pack(_KV8_POOL, 0, 0, table_at, refs_at, 0, 0, 1, blocks, rows, stride, 1, 64)
     _kv8_on(lib().ebrl_op_kv8_free, "ebrl_op_kv8_free", dev, stream, c, *at, n)
@@ -772,7 +781,7 @@ def op_kv8_reserve(codes, scales, block_table, refs, seq, pos0, count, max_count
     makes one for this call (not with an explicit stream)."""
     import torch
     c, dev = _kv8_pool(codes, scales, block_table, refs)
-    n = seq.numel()
+    n = _kv8_rows_of(seq)
     if not 0 <= max_count < 1 << 31:
         _kv8_bad(f"max_count {max_count}")
     *at, short = _kv8_ints(torch.int32, dev, ("seq", seq, n), ("pos0", pos0, n), ("count", count, n), ("lacking", lacking, 1))

@@ -131,6 +131,18 @@ def test_binding_refuses():
     refused(E.kv8_compact_workspace, codes[0], table)
 
 
+@pytest.mark.parametrize("n", [65537, (1 << 32) + 1])
+def test_more_rows_than_a_call_takes(n):
+    """Refused for their number, also where its low 32 bits are a small one (tensors without memory)."""
+    table, refs, ids, one = (torch.empty(s, dtype=torch.int32, device="meta") for s in ((2, 3), (4,), (n,), (1,)))
+    codes = torch.empty((4, 2, 2, 1024), dtype=torch.uint8, device="meta")
+    scales = torch.empty((4, 2, 2), device="meta")
+    for call in (lambda: E.op_kv8_fork(table, refs, ids, ids, ids), lambda: E.op_kv8_free(table, refs, ids),
+                 lambda: E.op_kv8_reserve(codes, scales, table, refs, ids, ids, ids, 1, one, workspace=one)):
+        with pytest.raises(E.EbrlError, match="at most 65536 rows"):
+            call()
+
+
 # ------------------------------------------------------------- plain lists --
 
 class Lists:
