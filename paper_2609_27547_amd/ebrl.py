@@ -811,6 +811,7 @@ def op_kv8_compact(codes, scales, block_table, refs, new_table, new_refs, used, 
 I8_ROWS, I8_RMSNORM, I8_SWIGLU = range(3)
 _I8_QUANT = struct.Struct("4if2P2q2PqP")
 _I8_GEMM = struct.Struct("4i2P2q4PqPqPq")
+_I8_SIZES = struct.Struct("3i")
 
 
 def i8_alloc(rows: int, cols: int, device="cuda"):
@@ -912,6 +913,7 @@ def op_i8_quant(x, codes, scales, up=None, norm_eps=None, gain=None, stream=None
 def i8_gemm_plan(M, N, K) -> dict:
     """The kernel that computes an M x N x K product of codes (no GPU needed)."""
     plan = (ctypes.c_int32 * 6)()
+    _i8_pack(_I8_SIZES, M, N, K)      # (a number past 32 bits would be cut to them)
     rc = lib().ebrl_op_i8_gemm_plan(M, N, K, plan)
     if rc != EBRL_OK:
         raise EbrlError(rc, "ebrl_op_i8_gemm_plan")

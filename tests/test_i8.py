@@ -76,6 +76,12 @@ def test_plans_are_refused():
     assert E.lib().ebrl_op_i8_gemm_plan(1, 1, 16, None) == -1
 
 
+def test_plan_refuses_sizes_past_32_bits():
+    for size in (((1 << 32) + 5, 64, 64), (5, (1 << 32) + 64, 64), (5, 64, (1 << 32) + 64), (-(1 << 32) + 5, 64, 64)):
+        with pytest.raises(E.EbrlError, match="do not hold"):
+            E.i8_gemm_plan(*size)
+
+
 @pytest.mark.parametrize("m,n,k,kernel", [
     # kernels that are 10 % or more ahead of the others
     (1, 4096, 4096, "decode"), (8, 4096, 11008, "decode"), (37, 22016, 4096, "decode"), (256, 1024, 4096, "decode"),
