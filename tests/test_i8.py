@@ -526,6 +526,57 @@ def test_results_past_the_cache(dtype, m, n, ld):
     assert torch.equal(codes[:, :n].double(), torch.round(y / scales.double()[:, None]))
 
 
+ROUNDS = [(8300, 4099), (9216, 4096), (12544, 4090), (5476, 8192), (16900, 2049), (9216, 8192)]
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(m, n, k) for m, n in ROUNDS for k in (112, 240, 272, 400, 1040) if n > 2049 or k > 112])
+def test_rounds_of_large_products(m, n, k):
+    """Workgroups with two and three large tiles one after the other, inner ones before inner ones and before the
+    last rows' and columns', of one, two, three, four and nine K tiles; results that stay in the caches and, of
+    9216 x 8192, that are stored past them; rows of any alignment; the residual in place and apart.  The next tile's loads are in flight behind the results of the one before."""
+    assert E.i8_gemm_plan(m, n, k)["kernel"] == "large" and -(-m // 256) * -(-n // 256) >= 512
+    g = torch.Generator().manual_seed(m + k)
+    (a, sa), (b, sb) = _operand(m, k, g), _operand(n, k, g, k + 16)
+    vec, large = torch.randn(n, generator=g).cuda(), torch.Generator("cuda").manual_seed(k)
+    for i, (dtype, resid, shift) in enumerate((d, r, s) for d in ("fp32", "bf16") for r in (None, "apart", "in place")
+                                              for s in (0, 1)):
+        bias = vec if i % 3 == 0 else None
+        res = torch.randn((m, n), generator=large, device="cuda").to(DT[dtype]) if resid else None
+        # shift: rows that start off an aligned element, so that no result goes past the caches
+        held = torch.full((shift + m * (n + shift) + 8,), 5.0, dtype=DT[dtype], device="cuda")
+        out = held.as_strided((m, n), (n + shift, 1), shift)
+        want = _expected(a, sa, b, sb, bias, res, dtype)
+        if resid == "in place":
+            out.copy_(res)
+            res = out
+        E.op_i8_gemm(a, sa, b, sb, out, bias=bias, residual=res)
+        assert _same(out, want), f"{dtype} {resid} {shift}"
+        assert (held[:shift] == 5).all() and (held[shift + m * (n + shift):] == 5).all()
+        if shift:
+            assert (held[1:1 + m * (n + 1)].view(m, n + 1)[:, n:] == 5).all()
+
+
+@gpu
+@pytest.mark.parametrize("far", ["a", "b"])
+def test_rows_far_apart_on_large_tiles(far):
+    """256 rows of a tile, 8 MB apart, of either operand: offsets in a tile up to 2139091072, just below 2^31, and tiles
+    4 GB apart."""
+    g = torch.Generator().manual_seed(3)
+    ld, k, few, many = (1 << 23) - 16, 240, 768, 65536
+    held = torch.zeros(ld * (few - 1) + k, dtype=torch.int8, device="cuda")
+    spread = held.as_strided((few, k), (ld, 1))
+    spread.copy_(torch.randint(-128, 128, (few, k), generator=g, dtype=torch.int8))
+    a, b = (spread, _operand(many, k, g)[0]) if far == "a" else (_operand(many, k, g)[0], spread)
+    m, n = len(a), len(b)
+    plan = E.i8_gemm_plan(m, n, k)
+    assert plan["kernel"] == "large" and plan["cut"] == 1
+    sa, sb = torch.rand(m, generator=g).cuda(), torch.rand(n, generator=g).cuda()
+    out = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    E.op_i8_gemm(a, sa, b, sb, out)
+    assert torch.equal(out, _expected(a, sa, b, sb, None, None, "bf16"))
+
+
 @gpu
 def test_rows_far_apart():
     """Rows of operands 8 MB apart: offsets in a tile that pass 31 bits."""
