@@ -131,6 +131,94 @@ def test_binding_refuses():
             E.op_i8_gemm(**{**ok, **bad})
 
 
+class _Elsewhere(torch.Tensor):
+    """A tensor that says it is on another device."""
+
+    def get_device(self):
+        return 1
+
+
+def _elsewhere(t):
+    return t.as_subclass(_Elsewhere)
+
+
+def _quant_calls():
+    x, ones = torch.zeros((3, 40), dtype=torch.bfloat16), torch.ones(40)
+    codes, scales = E.i8_alloc(3, 40, device="cpu")
+    wide = torch.zeros((3, 80), dtype=torch.bfloat16)
+    ok = dict(x=x, codes=codes, scales=scales)
+    normed, gated = dict(norm_eps=1e-6, gain=ones), dict(up=x)
+    for kw in ({}, dict(norm_eps=1e-6), normed, gated, dict(x=wide[:, :40]), dict(up=wide[:, 40:]),
+               dict(codes=torch.zeros((3, 96), dtype=torch.int8)[:, 16:64]), dict(x=wide[:1, ::2][:, :1].expand(3, 1))):
+        yield "not on a GPU", ok | kw
+    for t in (x.half(), x[0], x[None], x.int()):
+        yield r"x is bfloat16 or float32 \[rows, width\]", ok | dict(x=t)
+    for t in (codes.float(), codes[0], codes.view(torch.uint8), codes[None]):
+        yield r"codes are int8 \[rows, K\]", ok | dict(codes=t)
+    yield "codes have contiguous rows", ok | dict(codes=torch.zeros((3, 96), dtype=torch.int8)[:, ::2])
+    yield "codes have contiguous rows", ok | dict(codes=torch.zeros((48, 3), dtype=torch.int8).t())
+    for t in (codes[:2], codes[:, :40], codes[:, :47]):
+        yield r"codes are \[3, 48\]", ok | dict(codes=t)
+    yield r"x is torch.bfloat16 \[3, 40\] where", ok | dict(x=_elsewhere(x))
+    yield "x has contiguous rows", ok | dict(x=wide[:, ::2])
+    yield "x has contiguous rows", ok | dict(x=torch.zeros((40, 3)).t())
+    for t in (x[:2], x[:, :39], x.float(), _elsewhere(x)):
+        yield r"up is torch.bfloat16 \[3, 40\] where", ok | dict(up=t)
+    yield "up has contiguous rows", ok | dict(up=wide[:, ::2])
+    for t in (scales[:2], scales.double(), torch.ones(6)[::2], _elsewhere(scales)):
+        yield "scales is 3 contiguous float32", ok | dict(scales=t)
+    for t in (ones[:39], ones.double(), torch.ones(80)[::2], _elsewhere(ones)):
+        yield "gain is 40 contiguous float32", ok | dict(norm_eps=1e-6, gain=t)
+    for kw in (normed | gated, dict(norm_eps=1e-6, up=x), dict(gain=ones), dict(gain=ones, up=x)):
+        yield "normed .* or gated", ok | kw
+
+
+def _gemm_calls():
+    (a, sa), (b, sb) = E.i8_alloc(3, 48, device="cpu"), E.i8_alloc(5, 48, device="cpu")
+    out, work = torch.zeros((3, 5)), torch.zeros(64, dtype=torch.uint8)
+    ok = dict(a=a, scale_a=sa, b=b, scale_b=sb, out=out)
+    for kw in ({}, dict(residual=out), dict(bias=torch.ones(5)), dict(workspace=work), dict(workspace=work, stream=0),
+               dict(out=torch.zeros((3, 9))[:, 2:7]), dict(residual=torch.zeros((3, 9))[:, 2:7])):
+        yield "not on a GPU", ok | kw
+    for name, t in (("a", a), ("b", b)):
+        for bad in (t.int(), t[0], t.view(torch.uint8)) + ((_elsewhere(t),) if name == "b" else ()):
+            yield rf"{name} are int8 \[rows, K\]", ok | {name: bad}
+        yield f"{name} have contiguous rows", ok | {name: torch.zeros((len(t), 96), dtype=torch.int8)[:, ::2]}
+        yield "a and b have rows of one width", ok | {name: t[:, :32]}
+    for t in (out.half(), out[0], out.double()):
+        yield r"out is bfloat16 or float32 \[rows, width\]", ok | dict(out=t)
+    for t in (out[:2], out[:, :4], torch.zeros((5, 3)), _elsewhere(out)):
+        yield r"out is torch.float32 \[3, 5\] where", ok | dict(out=t)
+    yield "out has contiguous rows", ok | dict(out=torch.zeros((5, 3)).t())
+    for t in (out[:2], out[:, :4], out.bfloat16(), _elsewhere(out)):
+        yield r"residual is torch.float32 \[3, 5\] where", ok | dict(residual=t)
+    yield "residual has contiguous rows", ok | dict(residual=torch.zeros((3, 10))[:, ::2])
+    for name, n, t in (("scale_a", 3, sa), ("scale_b", 5, sb), ("bias", 5, torch.ones(5))):
+        for bad in (t[1:], t.double(), torch.ones(2 * n)[::2], _elsewhere(t)):
+            yield f"{name} is {n} contiguous float32", ok | {name: bad}
+    yield "explicit stream needs a workspace", ok | dict(stream=0)
+    for t in (torch.zeros((8, 16))[:, ::2], _elsewhere(work)):
+        yield "workspace is contiguous and where", ok | dict(workspace=t)
+
+
+@pytest.mark.parametrize("calls,op", [(_quant_calls, "op_i8_quant"), (_gemm_calls, "op_i8_gemm")], ids=["quant", "gemm"])
+def test_binding_refuses_each_argument(calls, op):
+    """By the check that is meant: calls that are right get as far as the one that asks for a GPU."""
+    for message, kw in calls():
+        with pytest.raises(E.EbrlError, match=message):
+            getattr(E, op)(**kw)
+
+
+def test_workspaces_are_refused():
+    a, b = torch.zeros((3, 48), dtype=torch.int8), torch.zeros((5, 48), dtype=torch.int8)
+    assert E.i8_gemm_workspace(a, b).device == a.device
+    for args in ((a[0], b), (a, b[0]), (a[None], b)):
+        with pytest.raises(E.EbrlError, match=r"codes are \[rows, K\]"):
+            E.i8_gemm_workspace(*args)
+    with pytest.raises(E.EbrlError, match="EINVAL|INVALID|ebrl_op_i8_gemm_workspace"):
+        E.i8_gemm_workspace(a[:, :40], b[:, :40])
+
+
 # --------------------------------------------------------- rows to codes --
 
 def _values(op, x, up, gain, eps):

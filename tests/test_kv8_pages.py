@@ -131,6 +131,98 @@ def test_binding_refuses():
     refused(E.kv8_compact_workspace, codes[0], table)
 
 
+class _Elsewhere(torch.Tensor):
+    """A tensor that says it is on another device."""
+
+    def get_device(self):
+        return 1
+
+
+def _elsewhere(t):
+    return t.as_subclass(_Elsewhere)
+
+
+def _table_calls():
+    """(message, function, arguments): each call is refused by the check that the message is of."""
+    table, refs = torch.full((2, 3), -1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    one, two = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    fork, free = dict(src=one, dst=one, length=one), dict(seq=one)
+    pool = dict(block_table=table, refs=refs)
+    for f, kw in ((E.op_kv8_fork, fork), (E.op_kv8_free, free), (E.op_kv8_free, free | dict(keep=one))):
+        yield "not on a GPU", f, pool | kw
+        for t in (refs.long(), refs[::2], refs[None]):
+            yield "refs are contiguous int32", f, pool | kw | dict(refs=t)
+        for t in (table.long(), table[0], table[:, ::2], table.t(), _elsewhere(table)):
+            yield "block_table is contiguous int32", f, pool | kw | dict(block_table=t)
+        for name in kw:
+            if name in ("dst", "seq") and len(kw) > 1:      # (the one that says how many rows there are)
+                other = "src" if name == "dst" else "keep"
+                yield f"{other} is 2 contiguous int32", f, pool | kw | {name: two}
+            else:
+                yield f"{name} is 1 contiguous int32" if len(kw) > 1 else "not on a GPU", f, pool | kw | {name: two}
+            for t in (one.long(), _elsewhere(one)):
+                yield f"{name} is 1 contiguous int32", f, pool | kw | {name: t}
+        name = list(kw)[0]
+        spread = torch.zeros(6, dtype=torch.int32)[::3]
+        yield f"{name} is 2 contiguous int32", f, pool | {k: two for k in kw} | {name: spread}
+
+
+def _pool_calls():
+    codes, scales = E.kv8_alloc(4, 2, 64, device="cpu")
+    table, refs = torch.full((2, 3), -1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    one, two = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    work = torch.zeros(4096, dtype=torch.uint8)
+    raw = codes.view(torch.uint8)
+    many, many_scales = raw[None].repeat(3, 1, 1, 1, 1), scales[None].repeat(3, 1, 1, 1)
+    pool = dict(codes=codes, scales=scales, block_table=table, refs=refs)
+    reserve = dict(seq=one, pos0=one, count=one, max_count=4, lacking=one)
+    compact = dict(new_table=table, new_refs=refs, used=one)
+    for f, kw, ints in ((E.op_kv8_reserve, reserve, ["pos0", "count", "lacking"]), (E.op_kv8_compact, compact, ["used"])):
+        gap = raw.new_zeros((3, 6, 2, 2, 1024))[:, :4]
+        for more in ({}, dict(workspace=work), dict(workspace=work, stream=0), dict(codes=raw), dict(codes=many, scales=many_scales),
+                     dict(codes=gap, scales=many_scales)):
+            yield "not on a GPU", f, pool | kw | more
+        yield "refs are contiguous int32", f, pool | kw | dict(refs=refs.long())
+        yield "block_table is contiguous int32", f, pool | kw | dict(block_table=table[0])
+        for t in (codes.float(), codes[0], raw[:, :1], raw[..., :1000], raw[..., :0], many[None], many[:0]):
+            yield "codes are float8_e4m3fn or bytes", f, pool | kw | dict(codes=t)
+        for t in (raw[:3], raw.transpose(1, 2), raw[:, :, :1], _elsewhere(raw), many[:, :, :, :1], raw.new_zeros((4, 2, 2, 2048))[..., ::2]):
+            yield "codes of a layer are contiguous", f, pool | kw | dict(codes=t, scales=many_scales if t.dim() == 5 else scales)
+        for t in (scales.double(), scales[:3], scales[:, :1], scales[None], scales.new_ones((4, 2, 4))[..., ::2], _elsewhere(scales)):
+            yield "scales are float32", f, pool | kw | dict(scales=t)
+        yield "scales are float32", f, pool | kw | dict(codes=many, scales=many_scales[:2])
+        yield "scales are float32", f, pool | kw | dict(codes=many, scales=many_scales.transpose(2, 3))
+        for name in ints:
+            for t in (two, one.long(), _elsewhere(one)):
+                yield f"{name} is 1 contiguous int32", f, pool | kw | {name: t}
+        yield "explicit stream needs a workspace", f, pool | kw | dict(stream=0)
+        for t in (torch.zeros((64, 64))[:, ::2], _elsewhere(work)):
+            yield "workspace is contiguous and where", f, pool | kw | dict(workspace=t)
+    yield "pos0 is 2 contiguous int32", E.op_kv8_reserve, pool | reserve | dict(seq=two)
+    yield "seq is 1 contiguous int32", E.op_kv8_reserve, pool | reserve | dict(seq=one.long())
+    for n in (-1, 1 << 31):
+        yield f"max_count {n}", E.op_kv8_reserve, pool | reserve | dict(max_count=n)
+    for name, t in (("new_table", table[:1]), ("new_refs", refs[:3])):
+        yield "have the shapes of block_table and refs", E.op_kv8_compact, pool | compact | {name: t}
+    for name, t in (("new_table", table.long()), ("new_table", torch.zeros((3, 2), dtype=torch.int32).t()),
+                    ("new_table", _elsewhere(table)), ("new_refs", refs.long()), ("new_refs", _elsewhere(refs))):
+        yield f"{name} is [0-9]+ contiguous int32", E.op_kv8_compact, pool | compact | {name: t}
+    for sizes in ((-1, 3), (1, -1), (1 << 31, 3), (1, 1 << 31)):
+        yield "ebrl_op_kv8_reserve_workspace: ", E.kv8_reserve_workspace, dict(codes=codes, block_table=table, n=sizes[0],
+                                                                              max_count=sizes[1])
+    for f, kw in ((E.kv8_reserve_workspace, dict(n=1, max_count=1)), (E.kv8_compact_workspace, {})):
+        yield r"block_table is \[sequences, pages\]", f, dict(codes=codes, block_table=table[0]) | kw
+        yield "codes are float8_e4m3fn or bytes", f, dict(codes=codes[0], block_table=table) | kw
+
+
+@pytest.mark.parametrize("calls", [_table_calls, _pool_calls], ids=["tables", "pools"])
+def test_binding_refuses_each_argument(calls):
+    """By the check that is meant: calls that are right get as far as the one that asks for a GPU."""
+    for message, f, kw in calls():
+        with pytest.raises(E.EbrlError, match=message):
+            f(**kw)
+
+
 @pytest.mark.parametrize("n", [65537, (1 << 32) + 1])
 def test_more_rows_than_a_call_takes(n):
     """Refused for their number, also where its low 32 bits are a small one (tensors without memory)."""
