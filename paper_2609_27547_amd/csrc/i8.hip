@@ -16,7 +16,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // Vectors that lie in memory at the alignment of an element: global loads and stores
 // take any, and a row segment stays one instruction.  9216 rows of 4095 columns, fp32, normed
-// 48 us (4096: 49; by elements 76); bf16, gated 67 (44; 102).
+// 38 us (of 4096 39), bf16, gated 63 (42); read by elements they took 76 and 102.
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
@@ -207,7 +207,7 @@ EBRL_DEV float i8_most(float m, float v) { return __builtin_elementwise_maximum(
 // more in 64 bits, one code in 1e4, and so is a whole row where 32 bits do not do
 // (near the ends of their range, or not finite).  9216 rows of 11008 (bf16): 124 us, 4.1
 // TB/s, 195 with 64 bits throughout.  Two workgroups of twelve waves share a CU, whose
-// vector units are half busy: the rest is the wait for a row and the exchange.
+// vector units are busy 73 % of the cycles: the rest is the wait for a row and the exchange.
 // Eight waves with three places 149 (159 held to three workgroups a CU), six with four
 // 186; persistent workgroups with the next row in flight 152.
 template <typename T, int OP, int WAVES, int CHUNKS>
@@ -566,10 +566,11 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 // read them.  Workgroups are persistent; the next tile's first DMAs go out before
 // the epilogue, whose stores drain behind them.  `full` tiles are dealt evenly, those
 // of the last round cut in `split`.
-//  * What bounds it: power.  8192 x 8192 x 8192 takes 364 us, 3.02 POPS (the library's
-//    product of that size 522 to 540, 2.04 to 2.11); 9216 x 12288 x 4096 345 (420 to 431).
-//    The matrix units are busy 70 % of the cycles, at a clock that the card holds at 1.85
-//    GHz; a K tile takes 1.3 us with one on every CU, of which 1.1 are products.
+//  * What bounds it: power.  8192 x 8192 x 8192 takes 362 us, 3.04 POPS (the library's
+//    product of that size 511 to 540, 2.04 to 2.15); 9216 x 12288 x 4096 330 with two sets of
+//    operands in turn (411 to 431), 345 with three, which no cache holds.  There the matrix
+//    units are busy 73 % of the cycles, at a clock that the card holds at 1.75 GHz; a K tile
+//    takes 1.3 us with one on every CU, of which 1.1 are products.
 //  * The epilogue loads nothing that the compiler waits for, since its waits count the
 //    DMAs too, which it does not see: scales and bias come through LDS, the residual is
 //    asked for three row groups ahead, the next tile's DMAs go out behind its last
@@ -583,7 +584,7 @@ EBRL_DEV i32x4 i8_fragment(const char* lds) { return *reinterpret_cast<const i32
 //    none in the K loop, 364).  The multiplying group goes first (s_setprio: 5476 x 8192 x
 //    1024 51 -> 48, nothing at long K).
 //  * With a residual the tiles of a round meet in memory at the end: 9216 x 4096 x 11008,
-//    fp32, 345 us, of which 302 MB of residual and results are 63.  Half the XCDs
+//    fp32, 348 us, of which 302 MB of residual and results are 63.  Half the XCDs
 //    taking their part of the last round first, so that the rounds do not end together:
 //    425 us (the code of the parts twice in the loop, and spills); starts 1 to 20 us
 //    apart: no change.
@@ -970,9 +971,10 @@ __global__ __launch_bounds__(512, 2) void i8_big_kernel(const int8_t* __restrict
 // Small outputs (fewer 256 x 256 tiles than CUs): BM x BN tiles on four waves
 // (2 x 2), a ring of ST K tiles in LDS with ST - 1 of them in flight, one barrier a
 // K tile; scales and residual ahead of the first operands.  Bound by what a CU draws
-// through LDS, 70 to 90 GB/s: a K tile takes 0.2 (32 x 64), 0.3 (64 x 64) and 0.42 us (64
-// x 128) with one workgroup on a CU, 0.3, 0.39 and 0.7 with two.  800 x 1024 x 4096 12.9
-// us, 591 x 1003 x 1296 8.0.
+// into LDS, by the times of the sizes 70 to 90 GB/s (at 591 x 1003 x 1296 the matrix units
+// are busy 4 % of the cycles, the vector units 9, LDS reads 7): a K tile takes 0.2 (32 x 64),
+// 0.3 (64 x 64) and 0.42 us (64 x 128) with one workgroup on a CU, 0.3, 0.39 and 0.7 with
+// two.  800 x 1024 x 4096 12.9 us, 591 x 1003 x 1296 8.0.
 template <typename T, int BM, int BN, int ST>
 __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restrict__ A, uint32_t lda,
                                                          const int8_t* __restrict__ B, uint32_t ldb, int M, int N, int K,
@@ -1102,9 +1104,11 @@ __global__ __launch_bounds__(256, 2) void i8_ring_kernel(const int8_t* __restric
 // tiles are summed through LDS.  With several ranges of K (splits) the sums go to the
 // workspace and i8_join_kernel adds them up.  NT: each weight is read by one workgroup.
 //
-// Bound by memory where the slices fill the chip in one round (1 x 12288 x 4096 9.9 us,
-// 5.1 TB/s with launch and tail; 8 x 4096 x 11008 9.4, 4.8), by what a CU draws through
-// LDS, 57 to 70 GB/s, where activations are half of it and more (64 x 12288 x 4096 14 to 15).
+// Bound by memory where the slices fill the chip in one round (1 x 12288 x 4096 10.2 us,
+// 4.9 TB/s with launch and tail; 8 x 4096 x 11008 10.4, 8.9 in a row of them, 5.1), by what a CU
+// draws into LDS, by the times 57 to 70 GB/s, where activations are half of it and more (64 x
+// 12288 x 4096 14 to 15; at 37 x 22016 x 4096 the matrix units are busy 9 % of the cycles, the
+// vector units 12, LDS reads 6).
 // Slices of 16, 48 or 96 columns are those that make one round of 256 workgroups of 4096,
 // 12288 and 22016 outputs: 37 x 22016 x 4096 19.8 us with 96, 22.2 with 48, 25 with 64; 17 x
 // 4096 x 4096 6.2 with 16, 7.8 with 32.  Eight waves instead of four: never faster (1 x
@@ -1355,8 +1359,9 @@ constexpr int i8_decode_stages(int xr, int bn) {
 
 // The kernel and tile whose modelled time (us) is least.  The constants are a fit to
 // all candidates on 385 products (M 1 to 9216, N 300 to 22016, K 1024 to 11008, bf16
-// output, weights from HBM): the candidate it picks is on average 0.7 % and at worst 11 %
-// slower than the best one.  No choice changes a result.
+// output, weights from HBM).  On 385 others of that range the candidate it picks is within 1 %
+// of the best one on 287, on average 2.4 % and at worst 28 % slower (1 to 8 rows on 22016
+// outputs, where slices of 96 columns make one round).  No choice changes a result.
 static I8Plan i8_plan(int M, int N, int K) {
     constexpr int CUS = 256;
     const int nk = (K + 127) / 128;
@@ -1403,7 +1408,8 @@ static I8Plan i8_plan(int M, int N, int K) {
     // of K cost a launch more, and their sums' way through memory.  More than 512 rows
     // come from memory too, and a K tile takes a third longer: where one round of
     // workgroups does, for few outputs (66 such products that would be the ring's: 22 %
-    // less time on average, 1609 x 52 x 10944 19.3 -> 11.8 us; 20 % more at worst).
+    // less time on average, 1609 x 52 x 10944 19.3 -> 11.8 us; on 80 others the pick is 4 %
+    // slower than the best on average, 29 % at worst).
     {
         const int xr = M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : up(M, up(M, 64)) <= 48 ? 48 : 64;
         const int m_tiles = (int)up(M, xr);
@@ -1470,10 +1476,10 @@ template <typename T> static void i8_gemm_launch(const ebrl_i8_gemm_args& a, con
                                p.full, p.cut, epi);
         };
         // Results that the 256 MB cache will not hold beside the operands until they are read,
-        // in whole cache lines, are stored past it: 9216 x 12288 x 4096 343 -> 330 us (bf16), 383 ->
-        // 360 (fp32), with the rows' quantisation behind it 423 -> 412.  Smaller ones are read
-        // from it (5476 x 8192 x 1024 and its gated rows 78 us, 84 past it), as is a residual
-        // stream (9216 x 4096 x 4096 and its norm 194, 200).
+        // in whole cache lines, are stored past it: with two sets of operands in turn 9216 x
+        // 12288 x 4096 343 -> 330 us (bf16), 383 -> 360 (fp32), with the rows' quantisation
+        // behind it 423 -> 412.  Smaller ones are read from it (5476 x 8192 x 1024 and its gated
+        // rows 78 us, 84 past it), as is a residual stream (9216 x 4096 x 4096 and its norm 194, 200).
         const int64_t esz = sizeof(T);
         const bool stream = a.M * (a.N * esz) >= 128 << 20 && (uintptr_t)a.c % 128 == 0 && a.ldc * esz % 128 == 0;
         if (a.residual) big(i8_big_kernel<T, true, false>);

@@ -8,9 +8,9 @@
 // in the chunk.  Atomics add and subtract whole numbers only.
 //
 // Bound by launches and latencies where little is copied (8 branches of two prefixes:
-// 2.4 us a release, 3.7 a fork, 4.3 and 4.5 the two launches of a reservation), else by
+// 2.5 us a release, 3.6 a fork, 4.4 each of the two launches of a reservation), else by
 // memory: 256 branches of 1 MB pages 53 us, writes at 4.8 TB/s (their 16 source pages
-// stay in the caches: with the loads left out it takes as long); 900 moves of 576 KB 202
+// stay in the caches: with the loads left out it takes as long); 900 moves of 576 KB 205
 // us, 5.2 TB/s read and written, where a large copy makes 4.8.
 #include <hip/hip_runtime.h>
 
