@@ -50,11 +50,11 @@ typedef struct ebrl_kv8_pool {
 
 /* Row dst[i] takes the pages of row src[i]'s first len[i] tokens, the last of them
  * also where it is partly filled; its other entries become -1.  Pages that dst[i]
- * held before are released.  src, dst, len: device int32 [n].  A fork whose source
- * is a destination of the call is left out, and of several forks to one row all
- * but the first.  Codes and scales are not touched (codes, scales and their
- * strides may be 0).  n: at most 65536, here and below.  Returns EBRL_E_INVALID on
- * bad arguments. */
+ * held before are released (no call of ebrl_op_kv8_free is needed first).  src, dst,
+ * len: device int32 [n].  A fork whose source is a destination of the call is left
+ * out, and of several forks to one row all but the first.  Codes and scales are not
+ * touched (codes, scales and their strides may be 0).  n: at most 65536, here and
+ * below.  Returns EBRL_E_INVALID on bad arguments. */
 int ebrl_op_kv8_fork(const ebrl_kv8_pool* pool, const int32_t* src, const int32_t* dst, const int32_t* len, int32_t n,
                      void* stream);
 
@@ -78,9 +78,10 @@ int64_t ebrl_op_kv8_reserve_workspace(const ebrl_kv8_pool* pool, int32_t n, int3
  * entries that holds no page, or one that other entries hold too (refs above 1
  * before the call), gets a page of its own: the k-th that needs one gets the k-th
  * lowest free id.  A shared page is released for it, and if it holds tokens before
- * pos0[i], its codes and scales are copied in every layer.  count[i] is cut to
- * max_count and to the table's row; of several i for one row all but the first are
- * left out.  Pages that this call releases are free from the next one on.
+ * pos0[i], its codes and scales are copied in every layer.  A pos0[i] below 0 counts
+ * as 0, and count[i] is cut to max_count and to the table's row; of several i for one
+ * row all but the first are left out.  Pages that this call releases are free from
+ * the next one on.
  *
  * *lacking (device int32): 0, or how many pages were missing: then the call has
  * changed nothing, and a write that follows without a look at it writes nothing

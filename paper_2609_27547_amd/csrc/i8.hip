@@ -139,8 +139,8 @@ template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]
 // The codes of eight neighbours in each of CHUNKS places, `step` columns apart from j on (those
 // of columns past the last are codes of zeros); columns from `wide` on are left as they are.
 // Adding 1.5 * 2^28 and a half rounds y inv + 1/2 to 2^-24ths, with the whole number in the low
-// word's last byte.  The product is off by less than 2^-42, so that is the one nearest to y / s
-// unless the fraction is 0: then y / s may be a tie, or on either side of one, and
+// word's last byte.  The product is off by less than 2^-36 (of which a sum of 2^20 squares is
+// most), so that is the one nearest to y / s unless the fraction is 0: then y / s may be a tie, or on either side of one, and
 // `exactly(column)` gives its code by divisions, stored over the first (one in 2^24, but for data
 // of few bits).
 template <int CHUNKS, typename F>
