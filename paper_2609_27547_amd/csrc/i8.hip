@@ -37,9 +37,10 @@ constexpr int64_t I8_MAX_TILES = 1 << 23;
 // about 1e-4 of its size.  With 32-bit y that is one code in 1e5, with 64-bit ones
 // none.  The vector units do 64-bit adds and products at the rate of 32-bit ones.
 //
-// Bound by memory from some thousand rows on: 9216 fp32 rows of 4096, normed, 39 us (4.8
-// TB/s), as they are 32 (5.9), bf16 ones as they are 20 (5.7); bf16 ones, normed, by their
-// vector instructions, 32; a row alone 2.7 us, a launch and two memory latencies.
+// Bound by memory from some thousand rows on: 9216 fp32 rows of 4092, normed, 37 us (5.1
+// TB/s; of 4096, whose rows start on the same channels, 39), as they are 32 (5.9), bf16 ones as
+// they are 20 (5.7); bf16 ones, normed, by their vector instructions, 30 (of 4096 33); a row
+// alone 2.7 us, a launch and two memory latencies.
 
 // 1 / d and 1 / sqrt(d): two steps of Newton's, 2^-23, 2^-46, then all bits.
 EBRL_DEV double i8_rcp(double d) {
@@ -84,10 +85,9 @@ EBRL_DEV float i8_gate_fast(float g, float u) {
 }
 // y / s to the nearest whole number, ties to even.
 EBRL_DEV uint32_t i8_code(double y, double s) { return (uint32_t)(int)rint(y / s); }
-// Byte BYTE of four words.
-template <int BYTE> EBRL_DEV uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    constexpr uint32_t two = 0x0c0c0400 + BYTE * 0x0101;
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, two), __builtin_amdgcn_perm(b, a, two), 0x05040100);
+// The low bytes of four words.
+EBRL_DEV uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
 }
 // The scale that rows with |y| <= top need; infinity: none, the row is not finite.
 EBRL_DEV float i8_scale(double top, bool bad) {
@@ -138,24 +138,25 @@ template <typename T> EBRL_DEV void i8_load8(const T* p, int left, float (&v)[8]
 }
 // The codes of eight neighbours in each of CHUNKS places, `step` columns apart from j on (those
 // of columns past the last are codes of zeros); columns from `wide` on are left as they are.
-// Adding 1.5 * 2^28 and a half rounds y inv + 1/2 to 2^-24ths, with the whole number in the low
-// word's last byte.  The product is off by less than 2^-36 (of which a sum of 2^20 squares is
-// most), so that is the one nearest to y / s unless the fraction is 0: then y / s may be a tie, or on either side of one, and
-// `exactly(column)` gives its code by divisions, stored over the first (one in 2^24, but for data
-// of few bits).
+// Adding 1.5 * 2^20 and a half rounds y inv + 1/2 to 2^-32ths, with the whole number in the high
+// word's low byte and the fraction in the low word.  The product is off by less than 2^-36 (of
+// which a sum of 2^20 squares is most), so that is the one nearest to y / s unless the fraction
+// is 0: then y / s may be a tie, or on either side of one, and `exactly(column)` gives its code by
+// divisions, stored over the first (one in 2^32, but for data of few bits).
 template <int CHUNKS, typename F>
 EBRL_DEV void i8_store(int8_t* out, const double (&y)[CHUNKS][8], int j, int step, int wide, double inv, bool bad, F exactly) {
-    auto code = [&](int c, int e) { return (uint32_t)__builtin_bit_cast(uint64_t, fma(y[c][e], inv, 402653184.5)); };
+    auto code = [&](int c, int e) { return __builtin_bit_cast(uint2, fma(y[c][e], inv, 1572864.5)); };
     uint32_t least = ~0u;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         uint32_t k[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            k[e] = code(c, e);
-            least = min(least, k[e] << 8);
+            const uint2 w = code(c, e);
+            k[e] = w.y;
+            least = min(least, w.x);
         }
-        const uint32_t lo = i8_pack<3>(k[0], k[1], k[2], k[3]), hi = i8_pack<3>(k[4], k[5], k[6], k[7]);
+        const uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
         if (j + c * step < wide) *reinterpret_cast<uint2*>(out + j + c * step) = bad ? make_uint2(0, 0) : make_uint2(lo, hi);
     }
     if (least == 0 && !bad) {
@@ -163,7 +164,7 @@ EBRL_DEV void i8_store(int8_t* out, const double (&y)[CHUNKS][8], int j, int ste
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) these |= (code(c, e) << 8 == 0 ? 1u : 0u) << (8 * c + e);
+            for (int e = 0; e < 8; ++e) these |= (code(c, e).x == 0 ? 1u : 0u) << (8 * c + e);
         for (; these; these &= these - 1) {
             const int i = __builtin_ctz(these), at = j + (i >> 3) * step + (i & 7);
             out[at] = (int8_t)exactly(at);
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void i8_quant_kernel
                     border[e] = fmaf(fabsf(z[c][e]), eb, fabsf(fmaf(z[c][e], invf, -(t - 12582912.0f))));
                     near = fmaxf(near, border[e]);
                 }
-                uint32_t lo = i8_pack<0>(k[0], k[1], k[2], k[3]), hi = i8_pack<0>(k[4], k[5], k[6], k[7]);
+                uint32_t lo = i8_pack(k[0], k[1], k[2], k[3]), hi = i8_pack(k[4], k[5], k[6], k[7]);
                 if (near >= 0.5f) {
                     unsigned these = 0;
 #pragma unroll
